@@ -47,7 +47,8 @@
  *   - One host thread at a time per cache.
  *   - Element types: A2T_F32 (float) or A2T_BF16 (bfloat16, raw 16-bit).
  *     Q, K, V and O all use the cache's dtype; arithmetic is fp32 with
- *     fp64-accurate rotary angles.
+ *     fp64-accurate rotary angles.  A2T_MX4: Q, K, V and O are bfloat16 and
+ *     the cache holds the rows in 4 bits (below).
  *   - Rotary encoding: rotate-half, x'[i] = x[i] cos a - x[i+D/2] sin a,
  *     x'[i+D/2] = x[i+D/2] cos a + x[i] sin a, a = pos * theta^(-2i/D), i < D/2.
  *     Query head h reads KV head h / (n_q_heads / n_kv_heads).
@@ -65,6 +66,22 @@
  *   advances the ring head past the rows it passes over and moves only their
  *   retained rows into the kept region; a2t_read_layout / a2t_read_kv return
  *   the rows in cache order.
+ *
+ * Rows held in 4 bits (A2T_MX4)
+ *   A head's row of K (rotated) or V is held as D / 32 blocks of 32 elements: a
+ *   scale 2^e per block and 4-bit elements 0, 0.5, 1, 1.5, 2, 3, 4, 6 with a
+ *   sign, in units of 2^e.  With a the block's largest magnitude, e is
+ *   floor(log2 a) - 2, and one more where a >= 1.75 2^floor(log2 a), kept within
+ *   [-124, 125]; an element becomes the nearest of those values (ties to the
+ *   one in an even place of that list), at most 6.  So an element is off by at
+ *   most 1/5 of its block's largest magnitude (1/4 where e is held at 125), a
+ *   head's row takes D / 2 + D / 32 bytes (68 of 256 at head dim 128), and a
+ *   row is encoded once, as it is appended.  A block with an infinity or a NaN
+ *   is NaN throughout.  K is rotated with the rotary table's cosines (fp64
+ *   angles, rounded to fp32) and rounded to fp32 once before it is encoded.
+ *   Attention is that of the values held: exact products of them with queries
+ *   that carry 8 significant bits, fp32 sums, probabilities rounded to bf16.
+ *   Values of non-finite rows reach only the queries that see them.
  */
 #ifndef A2T_H
 #define A2T_H
@@ -93,7 +110,8 @@ typedef enum a2t_status {
                                for device work */
 } a2t_status;
 
-typedef enum a2t_dtype { A2T_F32 = 0, A2T_BF16 = 1 } a2t_dtype;
+/* A2T_MX4: a cache of bfloat16 input and output whose rows are held in 4 bits. */
+typedef enum a2t_dtype { A2T_F32 = 0, A2T_BF16 = 1, A2T_MX4 = 2 } a2t_dtype;
 
 /* Row classes (Sec. 3.3).  ACOUSTIC covers every structural state the paper
  * evicts besides the ASR delimiters: unit marker, audio tokens, native
@@ -138,6 +156,10 @@ typedef struct a2t_config {
      * aligned), each L*S*Hkv*(unit_rows + kept_rows)*D elements of the cache
      * dtype: the ring of every (layer, stream, KV head) first, then the kept
      * regions ([L][S][Hkv][unit_rows][D] followed by [L][S][Hkv][kept_rows][D]).
+     * A2T_MX4: L*S*Hkv*(unit_rows + kept_rows) rows of D/2 + D/32 bytes: the codes
+     * of all rows in that order (D/2 bytes a row, element i in bits 4 (i % 2) ..
+     * + 3 of byte i / 2), then their scales (D/32 bytes a row, e + 127, 255 for
+     * NaN); no initial contents are needed.
      * Both NULL: the library allocates and frees them.  Both set: the caller
      * keeps them alive until a2t_cache_destroy returns; the library never frees
      * them.  Only one set: A2T_ERR_INVALID.  Ignored for host-only caches. */
@@ -220,15 +242,15 @@ int a2t_append(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* st
  * stream's keys over several workgroups, each split's output rows of a bf16
  * cache are held in fp16 until they are combined (normalised by the split's
  * own sum, so each value lies within the range of the V entries): bf16 V
- * entries must stay within fp16's range (|v| <= 65504).  fp32 caches keep
- * fp32 split outputs.
+ * entries must stay within fp16's range (|v| <= 65504; of an A2T_MX4 cache
+ * |v| < 57344, so that the values held do).  fp32 caches keep fp32 split outputs.
  * The layer must have appended the current step.  Errors: INVALID, STATE. */
 int a2t_chunk_attn(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* stream_ids,
                    const int32_t* n_q, const void* q, void* o);
 
 /* a2t_append on one layer followed by a2t_chunk_attn on that layer, in one
  * launch where the kernels allow it (fp32 caches; bf16 caches except for steps
- * of many query rows): the workgroups whose key tiles hold the step's new rows
+ * of many query rows; A2T_MX4 caches encode the rows in a launch of its own): the workgroups whose key tiles hold the step's new rows
  * rotate and store them while staging them for attention.  Arguments as in the two calls (layer 0..L-1 only; n_q
  * host [n_streams] with 1 <= n_q <= n_rows; q and o packed [sum n_q][Hq][D]).
  * Results and cache contents are the same as the two calls. */
@@ -335,7 +357,7 @@ int a2t_evict_rule(a2t_cache* c, int32_t n_streams, const int32_t* stream_ids,
  * ------------------------------------------------------------------------- */
 
 /* Hand the host's per-stream state to the device (synchronises).  Errors:
- * INVALID (fp32 cache), STATE (already begun, or a host step still open),
+ * INVALID (fp32 or A2T_MX4 cache), STATE (already begun, or a host step still open),
  * NODEV (host-only cache). */
 int a2t_dev_begin(a2t_cache* c);
 
@@ -415,8 +437,27 @@ int a2t_read_last_evict(a2t_cache* c, int32_t stream, int32_t* n_pre, uint8_t* m
                         int32_t* new_slot);
 
 /* Copy one layer's resident K (rotated) and V of a stream to host in cache
- * order (synchronises).  k, v: host [resident][Hkv][D] in the cache dtype. */
+ * order (synchronises).  k, v: host [resident][Hkv][D] in the cache dtype
+ * (A2T_MX4: the values held, as bfloat16, which is exact; NaN as 0x7fc0).
+ * Either may be NULL.  OOM: no host memory for the codes of an A2T_MX4 cache. */
 int a2t_read_kv(a2t_cache* c, int32_t layer, int32_t stream, void* k, void* v);
+
+/* The resident rows of streams, in cache order, to device memory: what a
+ * session's context is handed on, stored or inspected by.  Asynchronous on the
+ * cache's stream; allocates nothing.
+ *   layer       0..L-1, or A2T_ALL_LAYERS.
+ *   stream_ids  host [n_streams], distinct.
+ *   k, v        device, packed in stream order: [sum R][Hkv][D] for one layer,
+ *               [L][sum R][Hkv][D] for A2T_ALL_LAYERS, R the streams' resident
+ *               rows (a2t_resident; a stream without rows takes no place).  K
+ *               rotated, in the cache dtype (A2T_MX4: bfloat16, as a2t_read_kv).
+ *               16-byte aligned; one of them may be NULL.
+ * An open step's rows are resident once the layers read have appended them.
+ * Errors: INVALID (layer, ids, both pointers NULL, alignment), STATE (a layer
+ * read has not appended the open step, or device-planned steps hold the
+ * state), NODEV. */
+int a2t_read_rows(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* stream_ids,
+                  void* k, void* v);
 
 /* Wait for all work enqueued by this cache.  Reports device faults. */
 int a2t_sync(a2t_cache* c);
@@ -425,7 +466,7 @@ int a2t_sync(a2t_cache* c);
  * kernel_filter: NULL disables timing; "" times every kernel; otherwise only
  * kernels whose name contains the string ("step_meta", "append",
  * "attn_tile", "attn_block", "attn_f32", "attn_f32x2" (attn_f32 with two query
- * blocks per workgroup), "attn_valu", "attn_merge", "evict").  While enabled, each
+ * blocks per workgroup), "attn_mx4", "attn_valu", "attn_merge", "evict", "read_rows").  While enabled, each
  * matching launch carries a start/stop event pair recorded at the dispatch's
  * own begin and end.  a2t_kernel_time waits for the
  * stream, then reports for the kernels whose name contains `kernel` the

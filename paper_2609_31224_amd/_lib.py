@@ -4,7 +4,7 @@ Every step of the KV path runs in the library's HIP kernels.  If libA2T.so is
 not built this module raises ImportError; there is no fallback.
 
 Device buffers are torch tensors on the GPU (contiguous, the cache dtype:
-torch.float32 or torch.bfloat16) or raw integer device addresses.  Host arrays
+torch.float32, or torch.bfloat16 for A2T_BF16 and A2T_MX4) or raw integer device addresses.  Host arrays
 are anything numpy can turn into a contiguous array of the right type.
 """
 from __future__ import annotations
@@ -29,6 +29,7 @@ A2T_ERR_HIP = -6
 A2T_ERR_NODEV = -7
 A2T_F32 = 0
 A2T_BF16 = 1
+A2T_MX4 = 2
 A2T_ALL_LAYERS = -1
 A2T_FLAG_HOST_ONLY = 1
 A2T_FLAG_NO_WORKSPACE = 2
@@ -41,7 +42,7 @@ EXPORTED = (
     "a2t_evict", "a2t_evict_rule", "a2t_dev_begin", "a2t_dev_end", "a2t_dev_open",
     "a2t_dev_append_attn", "a2t_dev_evict", "a2t_dev_evict_rule",
     "a2t_stream_info_get", "a2t_resident",
-    "a2t_read_layout", "a2t_read_last_evict", "a2t_read_kv", "a2t_sync",
+    "a2t_read_layout", "a2t_read_last_evict", "a2t_read_kv", "a2t_read_rows", "a2t_sync",
     "a2t_profile_enable", "a2t_kernel_time", "a2t_profile_reserve", "a2t_status_str",
     "a2t_abi_version", "a2t_distill_create", "a2t_distill_destroy", "a2t_distill_loss",
     "a2t_distill_profile_enable", "a2t_distill_profile_reserve", "a2t_distill_kernel_time",
@@ -107,6 +108,7 @@ def _load():
         "a2t_read_layout": (C.c_int, [VP, I32, P(I32), P(C.c_uint8), P(I32)]),
         "a2t_read_last_evict": (C.c_int, [VP, I32, P(I32), P(C.c_uint8), P(I32)]),
         "a2t_read_kv": (C.c_int, [VP, I32, I32, VP, VP]),
+        "a2t_read_rows": (C.c_int, [VP, I32, I32, P(I32), VP, VP]),
         "a2t_sync": (C.c_int, [VP]),
         "a2t_profile_enable": (C.c_int, [VP, C.c_char_p]),
         "a2t_kernel_time": (C.c_int, [VP, C.c_char_p, P(C.c_int64), P(C.c_double)]),
@@ -208,8 +210,8 @@ def a2t_cache_create(n_layers: int, n_streams: int, n_q_heads: int, n_kv_heads: 
                      attn_scale: float = 0.0, device: int = 0, stream=None,
                      k_pool=None, v_pool=None) -> Cache:
     """``k_pool``/``v_pool``: optional caller-owned device pools (torch tensors or
-    addresses) of L*S*Hkv*(unit_rows+kept_rows)*D elements each; the caller keeps
-    them alive until a2t_cache_destroy."""
+    addresses) of L*S*Hkv*(unit_rows+kept_rows)*D elements each (A2T_MX4: that many
+    rows of D/2 + D/32 bytes); the caller keeps them alive until a2t_cache_destroy."""
     cfg = a2t_config(n_layers, n_streams, n_q_heads, n_kv_heads, head_dim, dtype, unit_rows,
                      kept_rows, max_step_rows, flags, rope_theta, attn_scale, device, 0,
                      _dev(k_pool, "k_pool"), _dev(v_pool, "v_pool"))
@@ -388,7 +390,8 @@ def a2t_read_last_evict(c: Cache, stream: int):
 
 def a2t_read_kv(c: Cache, layer: int, stream: int):
     """Resident K (rotated) and V of one layer in cache order.  float32 arrays
-    for fp32 caches; for bf16 caches the raw 16-bit patterns (uint16)."""
+    for fp32 caches; for bf16 and A2T_MX4 caches the raw 16-bit patterns of the
+    bf16 values (uint16)."""
     n = a2t_stream_info_get(c, stream)["resident"]
     shape = (n, c.config.n_kv_heads, c.config.head_dim)
     dt = np.float32 if c.config.dtype == A2T_F32 else np.uint16
@@ -396,6 +399,17 @@ def a2t_read_kv(c: Cache, layer: int, stream: int):
     v = np.zeros(shape, dt)
     _check(_lib.a2t_read_kv(c.ptr, layer, stream, k.ctypes.data, v.ctypes.data), "a2t_read_kv")
     return k, v
+
+
+def a2t_read_rows(c: Cache, layer: int, stream_ids: Sequence[int], k=None, v=None) -> None:
+    """Resident rows of the streams, in cache order, into GPU tensors [rows][Hkv][D] (one
+    layer) or [L][rows][Hkv][D] (A2T_ALL_LAYERS) of the cache's input type, rows being the
+    sum of the streams' a2t_resident; either may be None.  Asynchronous on the cache's stream."""
+    ids = _i32(stream_ids)
+    rc = _lib.a2t_read_rows(c.ptr, layer, len(ids), _p(ids, C.c_int32),
+                            _dev(k, "k", c.torch_dtype if not isinstance(k, int) else None),
+                            _dev(v, "v", c.torch_dtype if not isinstance(v, int) else None))
+    _check(rc, "a2t_read_rows")
 
 
 def a2t_sync(c: Cache) -> None:

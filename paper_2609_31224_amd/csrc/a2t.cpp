@@ -9,6 +9,7 @@
 // compaction indices and row moves itself.
 #include "../../include/a2t.h"
 #include "a2t_internal.h"
+#include "mx4.h"
 
 #include <hip/hip_runtime.h>
 
@@ -507,6 +508,13 @@ bool f32_on_valu(const a2t_cache* c, int n, const int* tiles) {
 }
 constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
+// An attn_mx4 launch: query blocks per workgroup, and what its workgroups cost.
+int mx4_query_blocks(int query_rows) {
+    const int blocks = (query_rows + 15) / 16, groups = (blocks + 3) / 4;
+    return (blocks + groups - 1) / groups;
+}
+constexpr SplitCosts kMx4Costs{8, 4, 1 << 20, 4};
+
 // Where a launch's split partials go: the cache's workspace (default) or the
 // library's fixed device array (the no-allocation entry point, which plans
 // without the workspace limit and never times its launches).
@@ -555,6 +563,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     // stream it is still bound by streaming the resident K/V, and its staged
     // tile pipeline keeps more bytes in flight than the VALU kernel.
     bool f32 = c->cfg.dtype == A2T_F32, valu = !f32 && c->force_valu;
+    const bool mx4 = c->cfg.dtype == A2T_MX4;
     const int64_t rf = partial_row_floats(c->cfg.head_dim, f32 || valu);
     int query_blocks = 1;
     int max_rows = 0, tiles[kMaxDesc], nsplit[kMaxDesc];
@@ -568,15 +577,16 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     const bool block = !in_row0 && many_rows(c, n, ids, n_q);
     const bool one_row = f32 && !in_row0 && !wsc && G == 1 && max_rows == 1 && f32_on_valu(c, n, tiles);
     if (one_row) f32 = false, valu = true;
-    if (f32 || block || one_row) {
+    if (f32 || block || one_row || mx4) {
         SplitStream ss[kMaxDesc];
         if (f32) query_blocks = f32_query_blocks(c, n, tiles, n_q);
+        if (mx4) query_blocks = mx4_query_blocks(G * max_rows);
         for (int i = 0; i < n; ++i) {
             const int rows = G * n_q[i];
-            ss[i] = {tiles[i], c->cfg.n_kv_heads * (f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
+            ss[i] = {tiles[i], c->cfg.n_kv_heads * (mx4 ? mx4_groups(rows, query_blocks) : f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
                      floats[i]};   // one row: one workgroup
         }
-        c->planner.plan(n, ss, f32 ? f32_costs(c->cfg.head_dim, query_blocks) : block ? kBlockCosts : kValuCosts, c->target_wgs, c->force_splits,
+        c->planner.plan(n, ss, mx4 ? kMx4Costs : f32 ? f32_costs(c->cfg.head_dim, query_blocks) : block ? kBlockCosts : kValuCosts, c->target_wgs, c->force_splits,
                         wsc ? wsc->floats : c->dev.ws_floats, nsplit);
     } else {
         plan_splits(c, n, tiles, floats, nsplit, wsc ? INT64_MAX : c->dev.ws_floats);
@@ -654,6 +664,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     b.max_rows = max_rows;
     hipError_t e;
     auto launch = [&](const DevState& st, const KTimer& kt) {
+        if (mx4) return launch_attn_mx4(st, b, query_blocks, q, o, c->stream, kt);
         if (f32) return launch_attn_f32(st, b, query_blocks, q, o, k_in, v_in, c->stream, kt);
         if (valu) return launch_attn_valu(st, b, q, o, c->stream, kt);
         if (block) return launch_attn_block(st, b, q, o, c->stream, kt);
@@ -671,7 +682,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
         return e == hipSuccess ? A2T_OK : hip_fail(c);
     }
     {
-        ProfScope ps(c, f32 ? (query_blocks == 2 ? "attn_f32x2" : "attn_f32") : valu ? "attn_valu" : block ? "attn_block" : "attn_tile");
+        ProfScope ps(c, mx4 ? "attn_mx4" : f32 ? (query_blocks == 2 ? "attn_f32x2" : "attn_f32") : valu ? "attn_valu" : block ? "attn_block" : "attn_tile");
         e = launch(c->dev, ps.kt());
     }
     if (e != hipSuccess) return hip_fail(c);
@@ -764,7 +775,7 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
     const int G = k.n_q_heads / k.n_kv_heads;
     if (G != 1 && G != 2 && G != 4 && G != 8) return A2T_ERR_INVALID;
     if (k.head_dim != 64 && k.head_dim != 128) return A2T_ERR_INVALID;
-    if (k.dtype != A2T_F32 && k.dtype != A2T_BF16) return A2T_ERR_INVALID;
+    if (k.dtype != A2T_F32 && k.dtype != A2T_BF16 && k.dtype != A2T_MX4) return A2T_ERR_INVALID;
     if (k.unit_rows < 1 || k.kept_rows < 0) return A2T_ERR_INVALID;
     if (k.max_step_rows < 1 || k.max_step_rows > 1024) return A2T_ERR_INVALID;
     if (k.rope_theta < 0 || k.attn_scale < 0) return A2T_ERR_INVALID;
@@ -803,7 +814,7 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
         c->target_wgs = std::max(1, env_int("A2T_TARGET_WGS", cus));
     }
     c->force_splits = std::max(0, env_int("A2T_SPLITS", 0));
-    c->force_valu = env_flag("A2T_FORCE_VALU");
+    c->force_valu = k.dtype == A2T_BF16 && env_flag("A2T_FORCE_VALU");
     // the split planner's scratch, so that no attention call allocates
     for (auto* v : {&c->plan_tiles, &c->plan_splits, &c->plan_tmp, &c->plan_order}) v->reserve(kMaxDesc);
     c->plan_heap.reserve((size_t)c->target_wgs);
@@ -840,8 +851,10 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
         return A2T_ERR_NODEV;
     }
     DeviceGuard dg(k.device);
-    const int64_t elt = k.dtype == A2T_F32 ? 4 : 2;
-    const int64_t lsh = (int64_t)k.n_layers * k.n_streams * k.n_kv_heads * k.head_dim * elt;
+    const bool mx4 = k.dtype == A2T_MX4;
+    const int64_t heads = (int64_t)k.n_layers * k.n_streams * k.n_kv_heads;
+    // bytes of one row of every (layer, stream, head), without the scales of rows held in 4 bits
+    const int64_t lsh = mx4 ? heads * (k.head_dim / 2) : heads * k.head_dim * (k.dtype == A2T_F32 ? 4 : 2);
     const int64_t S = k.n_streams;
     const int64_t tot = (int64_t)k.unit_rows + k.kept_rows;
     // workspace for key-split partials (none with A2T_FLAG_NO_WORKSPACE: such a
@@ -854,10 +867,12 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
         if (hipMalloc(p, std::max<int64_t>(bytes, 256)) != hipSuccess) ok = false;
     };
     // K and V pools: [L][S][Hkv][unit_rows][D] ring, then [L][S][Hkv][kept_rows][D] kept
+    // (rows held in 4 bits: the codes in that order, then the scales in the same)
+    const int64_t pool_bytes = mx4 ? mx4_pool_bytes(heads * tot, k.head_dim) : lsh * tot;
     c->own_pools = (k.k_pool == nullptr);
     if (c->own_pools) {
-        alloc(&d.k_unit, lsh * tot);
-        alloc(&d.v_unit, lsh * tot);
+        alloc(&d.k_unit, pool_bytes);
+        alloc(&d.v_unit, pool_bytes);
     } else {
         d.k_unit = k.k_pool;
         d.v_unit = k.v_pool;
@@ -1080,8 +1095,8 @@ static int append_impl(a2t_cache* c, int32_t layer, int32_t n_streams, const int
             hipError_t e;
             {
                 ProfScope ps(c, "append");
-                e = launch_append(c->dev, ab, layer == A2T_ALL_LAYERS ? k.n_layers : 1, kin, vin,
-                                  c->stream, ps.kt());
+                e = (k.dtype == A2T_MX4 ? launch_append_mx4 : launch_append)(
+                    c->dev, ab, layer == A2T_ALL_LAYERS ? k.n_layers : 1, kin, vin, c->stream, ps.kt());
             }
             if (e != hipSuccess) return hip_fail(c);
         }
@@ -1110,8 +1125,9 @@ int append_attn_impl(a2t_cache* c, int32_t layer, int32_t n_streams, const int32
                      const int32_t* pos, const int32_t* unit_id, const int32_t* n_q, const void* q,
                      void* o, const WsChoice* wsc) {
     // steps of many query rows append first and then run attn_block: each of its
-    // query blocks would otherwise rotate the step's keys again
-    bool fused = c->cfg.dtype == A2T_F32 || !c->force_valu;
+    // query blocks would otherwise rotate the step's keys again; rows held in 4 bits are
+    // encoded by a launch of its own
+    bool fused = c->cfg.dtype == A2T_F32 || (c->cfg.dtype == A2T_BF16 && !c->force_valu);
     for (int i0 = 0; i0 < n_streams && fused; i0 += kMaxDesc)
         fused = !many_rows(c, std::min(kMaxDesc, n_streams - i0), ids + i0, n_q + i0, layer == 0 ? n_rows + i0 : nullptr);
     int rc = append_impl(c, layer, n_streams, ids, n_rows, kin, vin, seg, pos, unit_id, !fused);
@@ -1329,13 +1345,22 @@ int evict_impl(a2t_cache* c, int32_t n_streams, const int32_t* ids, const int32_
     if (!c->host_only) {
         DeviceGuard dg(c->cfg.device);
         EvictBatch eb{};
+        const bool mx4 = c->cfg.dtype == A2T_MX4;
+        bool keeps = false;   // some stream of the batch retains rows
         auto flush = [&]() -> int {
             if (eb.count == 0) return A2T_OK;
             hipError_t e;
             {
                 ProfScope ps(c, "evict");
-                e = launch_evict(c->dev, eb, c->stream, ps.kt());
+                DevState st = c->dev;
+                if (mx4) st.L = 0;   // metadata, mask and new slots only
+                e = launch_evict(st, eb, c->stream, ps.kt());
             }
+            if (mx4 && e == hipSuccess && keeps) {
+                ProfScope ps(c, "evict");
+                e = launch_move_mx4(c->dev, eb, c->stream, ps.kt());
+            }
+            keeps = false;
             eb.count = 0;
             return e == hipSuccess ? A2T_OK : hip_fail(c);
         };
@@ -1343,6 +1368,7 @@ int evict_impl(a2t_cache* c, int32_t n_streams, const int32_t* ids, const int32_
             const EvictPlan& p = plans[i];
             if (p.evicted == 0) continue;
             const StreamState& s = c->ss[ids[i]];
+            keeps |= p.n_keep > 0;
             eb.d[eb.count++] = EvictDesc{ids[i], s.kept, s.head, p.R_pre, p.span, p.u_last, p.n_keep, p.sink};
             if (eb.count == kMaxDesc && (rc = flush())) return rc;
         }
@@ -1475,6 +1501,94 @@ int a2t_read_last_evict(a2t_cache* c, int32_t stream, int32_t* n_pre, uint8_t* m
     return A2T_OK;
 }
 
+int a2t_read_rows(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* ids, void* kout, void* vout) {
+    if (!c) return A2T_ERR_INVALID;
+    if (c->poisoned) return A2T_ERR_HIP;
+    if (c->dev_mode) return A2T_ERR_STATE;
+    const a2t_config& k = c->cfg;
+    if (layer < A2T_ALL_LAYERS || layer >= k.n_layers) return A2T_ERR_INVALID;
+    int rc = check_streams(c, n_streams, ids);
+    if (rc) return rc;
+    if ((!kout && !vout) || unaligned16(kout) || unaligned16(vout)) return A2T_ERR_INVALID;
+    int64_t total = 0;
+    for (int i = 0; i < n_streams; ++i) {
+        const StreamState& s = c->ss[ids[i]];
+        // an open step's rows count as resident: they have to be there in every layer read
+        if (layer == A2T_ALL_LAYERS ? !s.step_complete() : !s.appended[layer]) return A2T_ERR_STATE;
+        total += s.resident();
+    }
+    if (c->host_only) return A2T_ERR_NODEV;
+    DeviceGuard dg(k.device);
+    const int n_layers = layer == A2T_ALL_LAYERS ? k.n_layers : 1;
+    int64_t row0 = 0;
+    for (int i0 = 0; i0 < n_streams; i0 += kMaxDesc) {
+        const int n = std::min(kMaxDesc, n_streams - i0);
+        ReadBatch rb{};
+        rb.layer0 = layer == A2T_ALL_LAYERS ? 0 : layer;
+        rb.total_rows = total;
+        for (int i = 0; i < n; ++i) {
+            const StreamState& s = c->ss[ids[i0 + i]];
+            if (s.resident() == 0) continue;
+            rb.d[rb.count++] = ReadDesc{ids[i0 + i], s.kept, s.head, s.resident(), row0};
+            rb.max_R = std::max(rb.max_R, s.resident());
+            row0 += s.resident();
+        }
+        if (rb.count == 0) continue;
+        hipError_t e;
+        {
+            ProfScope ps(c, "read_rows");
+            e = launch_read_rows(c->dev, rb, n_layers, kout, vout, c->stream, ps.kt());
+        }
+        if (e != hipSuccess) return hip_fail(c);
+    }
+    return A2T_OK;
+}
+
+// a2t_read_kv of rows held in 4 bits: the codes and scales of a run of rows at a time come
+// to the host and are decoded there (every value is a bf16 number).
+static int read_kv_mx4(a2t_cache* c, int32_t layer, int32_t stream, void* kout, void* vout) {
+    const StreamState& s = c->ss[stream];
+    const DevState& st = c->dev;
+    const int D = st.D, cb = D / 2, nb = D / kMxBlock, T = s.kept, U = s.ring;
+    constexpr int kRows = 4096;   // rows of a run
+    uint8_t* const codes = new (std::nothrow) uint8_t[(size_t)kRows * (cb + nb)];
+    if (!codes) return A2T_ERR_OOM;
+    uint8_t* const scales = codes + (size_t)kRows * cb;
+    static const float level[8] = {0.f, 0.5f, 1.f, 1.5f, 2.f, 3.f, 4.f, 6.f};
+    bool ok = true;
+    for (int which = 0; which < 2; ++which) {
+        uint16_t* dst = static_cast<uint16_t*>(which ? vout : kout);
+        if (!dst) continue;
+        const Mx4Pool p = mx4_pool(st, which ? st.v_unit : st.k_unit);
+        for (int g = 0; g < st.Hkv && ok; ++g) {
+            for (int j = 0; j < T + U && ok;) {
+                // the run of rows from j on: to the end of the kept region, the ring's last slot
+                // or the newest row
+                const int slot = j < T ? j : (s.head + (j - T)) % st.unit_rows;
+                const int n = std::min(kRows, j < T ? T - j : std::min(T + U - j, st.unit_rows - slot));
+                const int64_t row = (j < T ? mx4_kept_row(st, layer, stream, g) : mx4_ring_row(st, layer, stream, g)) + slot;
+                ok = hipMemcpy(codes, p.codes + row * cb, (size_t)n * cb, hipMemcpyDeviceToHost) == hipSuccess &&
+                     hipMemcpy(scales, p.scales + row * nb, (size_t)n * nb, hipMemcpyDeviceToHost) == hipSuccess;
+                for (int r = 0; r < n && ok; ++r)
+                    for (int x = 0; x < D; ++x) {
+                        const int code = codes[(size_t)r * cb + x / 2] >> 4 * (x & 1), byte = scales[(size_t)r * nb + x / kMxBlock];
+                        uint16_t bits = 0x7fc0;
+                        if (byte != kMxNaN) {
+                            const float v = std::ldexp(level[code & 7], byte - 127);
+                            uint32_t u;
+                            std::memcpy(&u, &v, 4);
+                            bits = (uint16_t)(u >> 16 | (code & 8 ? 0x8000u : 0u));
+                        }
+                        dst[((size_t)(j + r) * st.Hkv + g) * D + x] = bits;
+                    }
+                j += n;
+            }
+        }
+    }
+    delete[] codes;
+    return ok ? A2T_OK : hip_fail(c);
+}
+
 int a2t_read_kv(a2t_cache* c, int32_t layer, int32_t stream, void* kout, void* vout) {
     if (!c || stream < 0 || stream >= c->cfg.n_streams || layer < 0 || layer >= c->cfg.n_layers)
         return A2T_ERR_INVALID;
@@ -1485,6 +1599,7 @@ int a2t_read_kv(a2t_cache* c, int32_t layer, int32_t stream, void* kout, void* v
     DeviceGuard dg(c->cfg.device);
     const StreamState& s = c->ss[stream];
     const a2t_config& k = c->cfg;
+    if (k.dtype == A2T_MX4) return read_kv_mx4(c, layer, stream, kout, vout);
     const size_t elt = k.dtype == A2T_F32 ? 4 : 2;
     const size_t row = (size_t)k.head_dim * elt;       // one head of one row
     const size_t dpitch = row * k.n_kv_heads;          // host row pitch

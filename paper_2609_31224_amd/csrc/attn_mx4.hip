@@ -1,0 +1,482 @@
+// Causal attention of a step's rows over rows held in 4 bits (A2T_MX4 caches; chunk and decode;
+// gfx950).  The layout of a block is in mx4.h.
+//
+//   attn_mx4  one workgroup = (key split, QB blocks of 16 query rows, KV head, stream),
+//             8 waves: wave w takes every eighth 32-key block of the split; the eight
+//             states are combined in LDS at the end.
+//
+// Scores: v_mfma_scale_f32_16x16x128_f8f6f4 multiplies K as it is stored, scales included,
+// with Q in e4m3.  A rotated query element has 8 significant bits here, as it has in bf16: a
+// block of 32 is scaled by a power of two and written as hi + lo, both e4m3 (4 bits each, lo
+// with a scale of 2^-4).  At head dim 128 that is two products per 16 keys, at 64 one, whose
+// first 64 dims are K times hi and whose last 64 are K times lo.
+// Values: a lane's 16 bytes of V are a block, which the scaled conversion turns into bf16
+// (exactly); transposed LDS reads then give the operand of v_mfma_f32_16x16x32_bf16.
+// Nothing is shared between waves before the end, so there are no barriers in the loop; the
+// next block's codes are in flight while one is computed.
+#include "a2t_internal.h"
+#include "mx4_device.h"
+
+#include <hip/hip_ext.h>
+#include <math.h>
+
+#include <type_traits>
+
+namespace a2t {
+namespace {
+
+constexpr int kKeyBlock = 32;    // keys of a wave's block
+constexpr int kRows = 16;        // query rows of a product
+constexpr int kKeyWaves = 8;     // waves of a workgroup: they share its keys
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+// global memory (a pointer picked by branches would be loaded from as a flat address)
+__device__ __forceinline__ u32x4 gload16(const uint8_t* p) {
+    return *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(reinterpret_cast<uintptr_t>(p));
+}
+__device__ __forceinline__ int gload1(const uint8_t* p) {
+    return *reinterpret_cast<const __attribute__((address_space(1))) uint8_t*>(reinterpret_cast<uintptr_t>(p));
+}
+// LDS accesses of the wave before this one come before those after it, whatever the compiler
+// knows about their addresses in one lane (the hardware keeps a wave's LDS accesses in order)
+__device__ __forceinline__ void wave_lds_order() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+}
+// max / sum over the four lanes l % 16 + 16 i that hold one query column
+__device__ __forceinline__ float col_max(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float col_sum(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// Lane l of a wave is (column l % 16, group lg = l / 16).
+//   scores   S^T[16 keys x 16 queries]: A = K, lane: key l % 16, block lg of 32 dims; B = Q^T,
+//            lane: query l % 16, dims 16 lg .. + 15 of each half of the 128; scales: one byte
+//            of each operand's row and block lg.  The lane gets keys 4 lg + e of its query.
+//   values   O^T[16 dims x 16 queries]: the 32 keys are contracted in the order in which the
+//            scores of two products lie in a lane, keys 4 lg + e and 16 + 4 lg + e; the lane
+//            gets dims 4 lg + e of each 16.
+// V in LDS: a key's 16-byte chunk c is at c ^ f(key), so that neither the four keys x four
+// blocks of a store nor the eight keys x two chunks of half a transposed read share banks.
+template <int D>
+__device__ __forceinline__ int v_chunk(int key, int c) {
+    const int y = D == 128 ? key & 7 : (key >> 1) & 3;
+    return key * (D / 8) + (c ^ (2 * y | ((y >> 1) & 1)));
+}
+
+template <int D, int QB, int N>
+__global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevState st, AttnBatchT<N> b,
+                                                                                   WgStart<N> start, const uint16_t* q,
+                                                                                   uint16_t* o) {
+    constexpr int NB = D / kMxBlock;   // blocks of a row
+    constexpr int CB = D / 2;          // bytes of a row's codes
+    constexpr int DB = D / 16;         // 16-dim blocks of O
+    constexpr int VL = D / 64;         // 16-byte loads of V per lane and key block
+    constexpr int QP = D / 64;         // products per 16 keys: hi and lo, or both in one
+    constexpr int kStride = kKeyWaves * kKeyBlock;
+    // (its chunks are found by exclusive or on their addresses: whole rows are aligned)
+    __shared__ __align__(256) u32x4 s_mem[kKeyWaves * kKeyBlock * D / 8];   // V of each wave's block; at the end the states
+    __shared__ u32x4 s_q[QB][QP][2][64];                     // Q operands
+    __shared__ uint8_t s_qs[QB][64];                         // ... and their scales
+    __shared__ float2 s_ml[kKeyWaves][kRows];
+    f32x4(&s_part)[kKeyWaves][DB][64] = *reinterpret_cast<f32x4(*)[kKeyWaves][DB][64]>(s_mem);
+    static_assert(sizeof(f32x4) * kKeyWaves * DB * 64 <= sizeof(s_mem), "the states of one block of query rows fit");
+
+    int wg;
+    const AttnDesc d = b.d[stream_of(start, b.count, &wg)];
+    const int G = st.G, M = G * d.n_q, R = d.R;
+    const int blocks = (M + kRows - 1) / kRows, groups = (blocks + QB - 1) / QB;
+    auto uniform = [](int x) { return __builtin_amdgcn_readfirstlane(x); };   // divisions run on the vector ALU
+    // linear block (split, query group, KV head), heads fastest: the workgroups of a head
+    // share an XCD's L2 when the head count divides the 8 XCDs
+    const int y = uniform(wg / st.Hkv), g = wg - y * st.Hkv;
+    const int sp = uniform(y / groups), grp = groups - 1 - (y - sp * groups);
+    if (sp >= d.splits) return;
+    const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+    const int mw = grp * QB * kRows;   // the workgroup's first query row
+    const int vis0 = R - d.n_q;
+    int qi[QB];                        // step row of the lane's queries (past M: that of row M-1)
+#pragma unroll
+    for (int x = 0; x < QB; ++x) qi[x] = min(mw + x * kRows + l16, M - 1) / G;
+    const int last_i = uniform((min(M, mw + QB * kRows) - 1) / G);
+    const int k_end = vis0 + last_i + 1;
+    const int t0 = sp * d.tile_q + min(sp, d.tile_r), t1 = t0 + d.tile_q + (sp < d.tile_r ? 1 : 0);
+    // this wave's key blocks: k0, k0 + kStride, ..; n of them
+    const int k0 = t0 * kTileKeys + w * kKeyBlock;
+    const int n = max(0, (min(k_end, t1 * kTileKeys) - k0 + kStride - 1) / kStride);
+
+    const int kept = d.kept, head = d.head, ring_rows = st.unit_rows;
+    const Mx4Pool kp = mx4_pool(st, st.k_unit), vp = mx4_pool(st, st.v_unit);
+    const int64_t ring0 = mx4_ring_row(st, b.layer, d.s, g), kept0 = mx4_kept_row(st, b.layer, d.s, g);
+    auto ring_slot = [&](int j) {
+        const int slot = head + (j - kept);
+        return slot >= ring_rows ? slot - ring_rows : slot;
+    };
+    auto row_of = [&](int j) -> int64_t {
+        j = min(j, R - 1);   // keys past R read row R-1 and are masked
+        return j < kept ? kept0 + j : ring0 + ring_slot(j);
+    };
+    // first row of a key block that is one run of rows
+    auto run_of = [&](int kb, int64_t* row) {
+        if (kb + kKeyBlock > R) return false;
+        if (kb + kKeyBlock <= kept) {
+            *row = kept0 + kb;
+            return true;
+        }
+        const int slot = ring_slot(kb);
+        *row = ring0 + slot;
+        return kb >= kept && slot + kKeyBlock <= ring_rows;
+    };
+
+    f32x4 acc[QB][DB];
+    float mrun[QB], lrun[QB];
+#pragma unroll
+    for (int x = 0; x < QB; ++x) {
+        mrun[x] = -INFINITY;
+        lrun[x] = 0.f;
+#pragma unroll
+        for (int c = 0; c < DB; ++c) acc[x][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    u32x4 kc[2], vc[VL];
+    int ks[2], vs[VL];   // their scale bytes
+    auto load_k = [&](int kb) {
+        const int c = lg & (NB - 1);
+        int64_t row;
+        if (run_of(kb, &row)) {
+            const uint8_t *p = kp.codes + row * CB, *ps = kp.scales + row * NB;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                kc[t] = gload16(p + (uint32_t)((16 * t + l16) * CB + 16 * c));
+                ks[t] = gload1(ps + (uint32_t)((16 * t + l16) * NB + c));
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                row = row_of(kb + 16 * t + l16);
+                kc[t] = gload16(kp.codes + row * CB + 16 * c);
+                ks[t] = gload1(kp.scales + row * NB + c);
+            }
+        }
+    };
+    auto load_v = [&](int kb) {
+        int64_t row;
+        if (run_of(kb, &row)) {
+            const uint8_t *p = vp.codes + row * CB, *ps = vp.scales + row * NB;
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {
+                vc[j] = gload16(p + (uint32_t)(16 * (64 * j + lane)));
+                vs[j] = gload1(ps + (uint32_t)(64 * j + lane));
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {
+                const int c = (64 * j + lane) % NB;
+                row = row_of(kb + (64 * j + lane) / NB);
+                vc[j] = gload16(vp.codes + row * CB + 16 * c);
+                vs[j] = gload1(vp.scales + row * NB + c);
+            }
+        }
+    };
+    if (n > 0) {
+        load_k(k0);
+        load_v(k0);
+    }
+
+    // Q^T operands, rotated and scaled by scale * log2(e): a thread takes 8 dims of the lower
+    // half and their partners of the upper one, four threads a block.  Rows past M read row
+    // M - 1 and are never stored.
+    for (int x = threadIdx.x; x < QB * kRows * (D / 16); x += 64 * kKeyWaves) {
+        const int r = x / (D / 16), d0 = (x - r * (D / 16)) * 8;
+        const int m = min(mw + r, M - 1), i = m / G;
+        const uint16_t* qp = q + ((int64_t)(d.q_row0 + i) * st.Hq + g * G + (m - i * G)) * D + d0;
+        const float4* cp = reinterpret_cast<const float4*>(
+            st.rope + ((int64_t)d.s * st.max_step_rows + d.rope_row0 + i) * (D / 2) + d0);
+        const u32x4 a = *reinterpret_cast<const u32x4*>(qp), a2 = *reinterpret_cast<const u32x4*>(qp + D / 2);
+        float y[2][8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float4 cs = cp[e];
+            const float lo0 = __uint_as_float(a[e] << 16), lo1 = __uint_as_float(a[e] & 0xffff0000u);
+            const float hi0 = __uint_as_float(a2[e] << 16), hi1 = __uint_as_float(a2[e] & 0xffff0000u);
+            y[0][2 * e] = (lo0 * cs.x - hi0 * cs.y) * st.scale_log2e;
+            y[0][2 * e + 1] = (lo1 * cs.z - hi1 * cs.w) * st.scale_log2e;
+            y[1][2 * e] = (hi0 * cs.x + lo0 * cs.y) * st.scale_log2e;
+            y[1][2 * e + 1] = (hi1 * cs.z + lo1 * cs.w) * st.scale_log2e;
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t big = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(y[h][e]) & 0x7fffffffu);
+            big = max(big, (uint32_t)__shfl_xor((int)big, 1));
+            big = max(big, (uint32_t)__shfl_xor((int)big, 2));
+            // the largest magnitude becomes 128 to 256 units of 2^(scale - 127), of e4m3's 448
+            const int scale = big >= 0x7f800000u ? kMxNaN : max((int)(big >> 23) - 7, 5);
+            const float inv = __uint_as_float((uint32_t)(254 - min(scale, 253)) << 23);
+            uint2 hi{0u, 0u}, lo{0u, 0u};
+            if (scale != kMxNaN) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float* z = &y[h][4 * e];
+                    int c = 0, c2 = 0;
+                    c = __builtin_amdgcn_cvt_pk_fp8_f32(z[0] * inv, z[1] * inv, c, false);
+                    c = __builtin_amdgcn_cvt_pk_fp8_f32(z[2] * inv, z[3] * inv, c, true);
+                    const f32x2 b0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
+                    c2 = __builtin_amdgcn_cvt_pk_fp8_f32((z[0] * inv - b0[0]) * 16.f, (z[1] * inv - b0[1]) * 16.f, c2, false);
+                    c2 = __builtin_amdgcn_cvt_pk_fp8_f32((z[2] * inv - b1[0]) * 16.f, (z[3] * inv - b1[1]) * 16.f, c2, true);
+                    (e ? hi.y : hi.x) = (uint32_t)c;
+                    (e ? lo.y : lo.x) = (uint32_t)c2;
+                }
+            }
+            const int at = d0 + h * (D / 2), xb = r / kRows, l = (at % 64) / 16 * 16 + r % kRows;
+            if constexpr (D == 128) {
+                reinterpret_cast<uint2*>(&s_q[xb][0][at / 64][l])[at / 8 % 2] = hi;
+                reinterpret_cast<uint2*>(&s_q[xb][1][at / 64][l])[at / 8 % 2] = lo;
+            } else {
+                reinterpret_cast<uint2*>(&s_q[xb][0][0][l])[at / 8 % 2] = hi;
+                reinterpret_cast<uint2*>(&s_q[xb][0][1][l])[at / 8 % 2] = lo;
+            }
+            if (at % kMxBlock == 0) {
+                s_qs[xb][at / kMxBlock * 16 + r % kRows] = (uint8_t)scale;
+                if constexpr (D == 64)   // the product's last 64 dims
+                    s_qs[xb][(at / kMxBlock + 2) * 16 + r % kRows] = (uint8_t)(scale == kMxNaN ? kMxNaN : scale - 4);
+            }
+        }
+    }
+    __syncthreads();
+    int qs[QB];
+#pragma unroll
+    for (int x = 0; x < QB; ++x) qs[x] = s_qs[x][lane];
+    auto q_op = [&](int x, int p) {
+        const u32x4 a = s_q[x][p][0][lane], b2 = s_q[x][p][1][lane];
+        return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2[0], (int)b2[1], (int)b2[2], (int)b2[3]};
+    };
+
+    u32x4* const s_v = s_mem + w * (kKeyBlock * D / 8);
+    // transposed reads: 16 lanes read 8 bytes each of four keys' 32 bytes
+    const int vk = 4 * lg + (l16 >> 2);
+    const char* const vt = reinterpret_cast<const char*>(s_v) + v_chunk<D>(vk, (l16 & 3) >> 1) * 16 + (l16 & 1) * 8;
+    auto v_half = [&](int c, int half) {
+        // chunk 2 c of the lane's key: the swizzle and c touch the same bits of the address
+        const uint32_t at = (lds_addr(vt) ^ (uint32_t)(32 * c)) + half * 16 * D * 2;
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)at);
+    };
+
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+        const int kb = k0 + i * kStride;
+        // V: codes to bf16 rows in LDS
+        bool nan_v = false;
+#pragma unroll
+        for (int j = 0; j < VL; ++j) {
+            const int key = (64 * j + lane) / NB, c = (64 * j + lane) % NB;
+            nan_v |= vs[j] == kMxNaN;
+            const float s = __uint_as_float((uint32_t)vs[j] << 23);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                u32x4 x = mx4_to_bf16(vc[j][e], s);
+                s_v[v_chunk<D>(key, 4 * c + e)] = x;
+            }
+        }
+        const bool any_nan = __any(nan_v);
+        int nan_bytes[VL];
+        if (any_nan) {
+            // a block that is NaN counts for the queries that see its key, below; its place
+            // holds zeros, which change nothing for the others
+#pragma unroll
+            for (int j = 0; j < VL; ++j) {
+                nan_bytes[j] = vs[j];
+                const int key = (64 * j + lane) / NB, c = (64 * j + lane) % NB;
+                if (vs[j] == kMxNaN)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s_v[v_chunk<D>(key, 4 * c + e)] = u32x4{0u, 0u, 0u, 0u};
+            }
+        }
+        wave_lds_order();   // other lanes read these rows
+        if (i + 1 < n) load_v(kb + kStride);
+
+        // scores, relative to the running reference
+        f32x4 sc[QB][2];
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
+            const float mu = mrun[x] == -INFINITY ? 0.f : mrun[x];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) sc[x][t] = f32x4{-mu, -mu, -mu, -mu};
+#pragma unroll
+            for (int p = 0; p < QP; ++p) {
+                const i32x8 qv = q_op(x, p);
+                const int s = p == 0 || qs[x] == kMxNaN ? qs[x] : qs[x] - 4;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const i32x8 kv = {(int)kc[t][0], (int)kc[t][1], (int)kc[t][2], (int)kc[t][3], 0, 0, 0, 0};
+                    sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, sc[x][t], 4, 0, 0, ks[t], 0, s);
+                }
+            }
+        }
+        if (i + 1 < n) load_k(kb + kStride);
+
+        const bool masked = kb + kKeyBlock - 1 > vis0;
+        bf16x8 p[QB];
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
+            if (masked) {
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (kb + 16 * t + 4 * lg + e > vis0 + qi[x]) sc[x][t][e] = -INFINITY;
+            }
+            float top = fmaxf(fmaxf(sc[x][0][0], sc[x][0][1]), fmaxf(sc[x][0][2], sc[x][0][3]));
+            top = fmaxf(top, fmaxf(fmaxf(sc[x][1][0], sc[x][1][1]), fmaxf(sc[x][1][2], sc[x][1][3])));
+            top = col_max(top);
+            // the reference follows the row maximum lazily: set by the first visible key, then
+            // raised (and the running sums rescaled) only when a block exceeds it by more than 2^8
+            const bool fresh = mrun[x] == -INFINITY;
+            if (__any(top > (fresh ? -INFINITY : 8.f))) {
+                const float up = fresh ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
+                const float corr = __builtin_amdgcn_exp2f(fresh ? 0.f : -up);   // nothing is summed yet where fresh
+                mrun[x] = fresh ? (top == -INFINITY ? -INFINITY : top) : mrun[x] + up;
+                lrun[x] *= corr;
+#pragma unroll
+                for (int c = 0; c < DB; ++c) acc[x][c] *= corr;
+#pragma unroll
+                for (int t = 0; t < 2; ++t) sc[x][t] -= up;
+            }
+            float pr[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[x][e >> 2][e & 3]);
+            lrun[x] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
+            p[x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]),
+                                                    pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])});
+        }
+#pragma unroll
+        for (int c = 0; c < DB; ++c) {
+            const i16x4 a = v_half(c, 0), a2 = v_half(c, 1);
+            const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, a2, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int x = 0; x < QB; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[x], acc[x][c], 0, 0, 0);
+        }
+        wave_lds_order();   // the next block takes this one's place
+        if (any_nan) {
+#pragma unroll 1
+            for (int key = 0; key < kKeyBlock; ++key) {
+#pragma unroll
+                for (int c = 0; c < NB; ++c) {
+                    const int at = key * NB + c;
+                    int byte = 0;
+#pragma unroll
+                    for (int j = 0; j < VL; ++j)
+                        if (at / 64 == j) byte = __builtin_amdgcn_readlane(nan_bytes[j], at & 63);
+                    if (byte != kMxNaN) continue;
+#pragma unroll
+                    for (int x = 0; x < QB; ++x)
+                        if (kb + key <= vis0 + qi[x]) {
+                            const float z = __uint_as_float(0x7fc00000u);
+                            acc[x][2 * c] = acc[x][2 * c + 1] = f32x4{z, z, z, z};
+                        }
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int x = 0; x < QB; ++x) {
+        lrun[x] = col_sum(lrun[x]);
+        if (mrun[x] == -INFINITY && lrun[x] != 0.f) mrun[x] = 0.f;   // a NaN sum keeps its weight
+    }
+
+    // combine the waves' states, one block of query rows after the other: each wave sums an
+    // eighth of the dims
+    const bool whole = d.splits == 1;
+    float* po = st.ws + d.ws_off;
+#pragma unroll
+    for (int x = 0; x < QB; ++x) {
+        __syncthreads();   // V, or the states of the block before
+#pragma unroll
+        for (int c = 0; c < DB; ++c) s_part[w][c][lane] = acc[x][c];
+        if (lg == 0) s_ml[w][l16] = make_float2(mrun[x], lrun[x]);
+        __syncthreads();
+        const int mq = mw + x * kRows + l16;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < kKeyWaves; ++k) mx = fmaxf(mx, s_ml[k][l16].x);
+        auto weight = [&](int k) {
+            const float m = s_ml[k][l16].x;
+            return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
+        };
+        float wt[kKeyWaves], L = 0.f;
+#pragma unroll
+        for (int k = 0; k < kKeyWaves; ++k) {
+            wt[k] = weight(k);
+            L += wt[k] * s_ml[k][l16].y;
+        }
+        // split partials: O / sum in fp16 (attn_merge_kernel; a split that sees no key of a row
+        // is zeros with a maximum of -inf), else the bf16 output
+        const float inv = L == 0.f && !whole ? 0.f : 1.f / L;
+        const int64_t at = ((int64_t)sp * st.Hkv + g) * M + mq;
+        for (int c = w; c < DB && mq < M; c += kKeyWaves) {   // dims 16 c + 4 lg .. + 3
+            f32x4 O = s_part[0][c][lane] * wt[0];
+#pragma unroll
+            for (int k = 1; k < kKeyWaves; ++k) O += s_part[k][c][lane] * wt[k];
+            O *= inv;
+            if (whole) {
+                uint16_t* orow = o + ((int64_t)(d.q_row0 + qi[x]) * st.Hq + g * G + (mq - qi[x] * G)) * D;
+                *reinterpret_cast<uint2*>(orow + 16 * c + 4 * lg) = make_uint2(pack_bf16x2(O[0], O[1]), pack_bf16x2(O[2], O[3]));
+            } else {
+                uint16_t* orow = reinterpret_cast<uint16_t*>(po) + at * D;
+                *reinterpret_cast<uint2*>(orow + 16 * c + 4 * lg) = make_uint2(pack_f16x2(O[0], O[1]), pack_f16x2(O[2], O[3]));
+            }
+        }
+        if (!whole && w == 0 && lg == 0 && mq < M)
+            *reinterpret_cast<float2*>(po + (int64_t)d.splits * st.Hkv * M * (D / 2) + at * 2) = make_float2(mx, L);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, const void* q, void* o,
+                           hipStream_t stream, const KTimer& kt) {
+    const dim3 block(64 * kKeyWaves);
+    const uint16_t* qq = static_cast<const uint16_t*>(q);
+    uint16_t* oo = static_cast<uint16_t*>(o);
+    return by_size<AttnBatchT>(b, [&](const auto& bb) {
+        constexpr int N = sizeof(bb.d) / sizeof(bb.d[0]);
+        WgStart<N> start{};
+        const dim3 grid = place_workgroups(b.count, &start, [&](int i) {
+            return mx4_groups(st.G * b.d[i].n_q, query_blocks) * b.d[i].splits * st.Hkv;
+        });
+        auto go = [&](auto kernel) {
+            if (kt.start)
+                hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo);
+            else
+                hipLaunchKernelGGL(kernel, grid, block, 0, stream, st, bb, start, qq, oo);
+            return hipGetLastError();
+        };
+        auto sized = [&](auto dim) {
+            constexpr int D = decltype(dim)::value;
+            switch (query_blocks) {
+                case 1: return go(attn_mx4_kernel<D, 1, N>);
+                case 2: return go(attn_mx4_kernel<D, 2, N>);
+                case 3: return go(attn_mx4_kernel<D, 3, N>);
+                case 4: return go(attn_mx4_kernel<D, 4, N>);
+                default: return hipErrorInvalidValue;
+            }
+        };
+        if (st.D == 128) return sized(std::integral_constant<int, 128>{});
+        if (st.D == 64) return sized(std::integral_constant<int, 64>{});
+        return hipErrorInvalidValue;
+    });
+}
+
+}  // namespace a2t

@@ -1,0 +1,204 @@
+// Rows of A2T_MX4 caches as they are written, and rows of any cache read back (gfx950).
+//
+//   append_mx4  rotates a step's keys by their positions, encodes K and V and stores
+//               codes and scales in the ring.
+//   move_mx4    copies the rows that an eviction retains into the kept region.
+//   read_rows   resident rows in cache order: decoded (A2T_MX4) or copied.
+#include "a2t_internal.h"
+#include "a2t.h"
+#include "mx4_device.h"
+
+#include <hip/hip_ext.h>
+
+#include <type_traits>
+
+namespace a2t {
+namespace {
+
+constexpr int kRowThreads = 256;
+
+__device__ __forceinline__ void unpack8(const u32x4& r, float (&x)[8]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(r[e] << 16);
+        x[2 * e + 1] = __uint_as_float(r[e] & 0xffff0000u);
+    }
+}
+// Encodes a thread's 8 elements of a block that four neighbouring lanes share; *scale: its byte.
+__device__ __forceinline__ uint32_t encode8(const float (&x)[8], int* scale) {
+    uint32_t big = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(x[e]) & 0x7fffffffu);
+    big = max(big, (uint32_t)__shfl_xor((int)big, 1));
+    big = max(big, (uint32_t)__shfl_xor((int)big, 2));
+    *scale = mx4_scale(big);
+    const float s = __uint_as_float((uint32_t)*scale << 23);
+    uint32_t c = 0;   // round to nearest even, saturating
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], s, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], s, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], s, 2);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], s, 3);
+    return *scale == kMxNaN ? 0u : c;
+}
+
+// One thread per (row, KV head, 8 dims of the lower half and their rotate-half partners of
+// the upper one), K and V: every element is loaded once, and four lanes hold a block.
+//
+// The rotation is computed in 64 bits (products of a bf16 and an fp32 number are exact there)
+// and rounded to fp32 once, so that what a key is encoded as follows from the inputs and the
+// rotary table alone: two fp32 roundings would put one key in ~10^7 on the other side of a
+// border between two codes, depending on the compiler's choice of fused operations.
+template <class BT>
+__global__ __launch_bounds__(kRowThreads) void append_mx4_kernel(DevState st, BT b, const uint16_t* k, const uint16_t* v) {
+    const AppendDesc d = b.d[blockIdx.y];
+    const int D = st.D, half = D / 2, tph = D / 16, tpr = st.Hkv * tph;
+    const int x = blockIdx.x * kRowThreads + threadIdx.x;
+    const int r = x / tpr;
+    if (r >= d.n) return;   // whole groups of four lanes: tpr is a multiple of 4
+    const int c = x - r * tpr, g = c / tph, d0 = (c - g * tph) * 8;
+    int slot = d.slot0 + r;
+    if (slot >= st.unit_rows) slot -= st.unit_rows;
+    const int64_t in = (((int64_t)blockIdx.z * b.total_rows + d.in_row0 + r) * st.Hkv + g) * D + d0;
+    const u32x4 klo = *reinterpret_cast<const u32x4*>(k + in), khi = *reinterpret_cast<const u32x4*>(k + in + half);
+    const u32x4 vlo = *reinterpret_cast<const u32x4*>(v + in), vhi = *reinterpret_cast<const u32x4*>(v + in + half);
+    const float4* cs4 = reinterpret_cast<const float4*>(st.rope + ((int64_t)d.s * st.max_step_rows + r) * half + d0);
+    float4 cs[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) cs[e] = cs4[e];
+    float lo[8], hi[8], ylo[8], yhi[8];
+    unpack8(klo, lo);
+    unpack8(khi, hi);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        const double co = e & 1 ? cs[e / 2].z : cs[e / 2].x, si = e & 1 ? cs[e / 2].w : cs[e / 2].y;
+        ylo[e] = (float)((double)lo[e] * co - (double)hi[e] * si);
+        yhi[e] = (float)((double)hi[e] * co + (double)lo[e] * si);
+    }
+    const int64_t row = mx4_ring_row(st, b.layer0 + blockIdx.z, d.s, g) + slot;
+    auto store = [&](const Mx4Pool& p, const float(&y)[8], int at) {
+        int scale;
+        const uint32_t code = encode8(y, &scale);
+        *reinterpret_cast<uint32_t*>(p.codes + row * half + at / 2) = code;
+        if (at % kMxBlock == 0) p.scales[row * (D / kMxBlock) + at / kMxBlock] = (uint8_t)scale;
+    };
+    const Mx4Pool kp = mx4_pool(st, st.k_unit), vp = mx4_pool(st, st.v_unit);
+    store(kp, ylo, d0);
+    store(kp, yhi, d0 + half);
+    unpack8(vlo, lo);
+    unpack8(vhi, hi);
+    store(vp, lo, d0);
+    store(vp, hi, d0 + half);
+}
+
+// grid (rows, stream, layer): a wave takes every fourth row of the span that eviction has
+// passed over and copies it, where it is kept, to the slot that the eviction's index pass found for
+// it.  A chunk is a block's 16 bytes of codes, and its scale byte goes with it.
+template <class BT>
+__global__ __launch_bounds__(kRowThreads) void move_mx4_kernel(DevState st, BT b) {
+    const EvictDesc d = b.d[blockIdx.y];
+    const int lane = threadIdx.x & 63, nb = st.D / kMxBlock, chunks = 2 * st.Hkv * nb, layer = blockIdx.z;
+    const int64_t eb = (int64_t)d.s * ((int64_t)st.unit_rows + st.kept_rows);
+    const Mx4Pool kp = mx4_pool(st, st.k_unit), vp = mx4_pool(st, st.v_unit);
+    for (int x = blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6); x < d.span; x += gridDim.x * (kRowThreads / 64)) {
+        const int to = st.ev_slot[eb + d.kept + x];
+        if (to < 0) continue;
+        int from = d.head + x;
+        if (from >= st.unit_rows) from -= st.unit_rows;
+        for (int c = lane; c < chunks; c += 64) {
+            const bool is_v = c >= chunks / 2;
+            const int y = is_v ? c - chunks / 2 : c, g = y / nb, ch = y - g * nb;
+            const Mx4Pool& p = is_v ? vp : kp;
+            const int64_t src = (mx4_ring_row(st, layer, d.s, g) + from) * nb + ch;
+            const int64_t dst = (mx4_kept_row(st, layer, d.s, g) + to) * nb + ch;
+            reinterpret_cast<u32x4*>(p.codes)[dst] = reinterpret_cast<const u32x4*>(p.codes)[src];
+            p.scales[dst] = p.scales[src];
+        }
+    }
+}
+
+// grid (rows, stream, layer x {K, V}): one thread per 16 bytes of output.
+template <int DTYPE, class BT>
+__global__ __launch_bounds__(kRowThreads) void read_rows_kernel(DevState st, BT b, char* k, char* v) {
+    constexpr int EPT = DTYPE == A2T_F32 ? 4 : 8;   // elements of a thread
+    const ReadDesc d = b.d[blockIdx.y];
+    const int D = st.D, cph = D / EPT, cpr = st.Hkv * cph;
+    const int64_t x = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
+    const int j = (int)(x / cpr);
+    if (j >= d.R) return;
+    const int c = (int)(x - (int64_t)j * cpr), g = c / cph, d0 = (c - g * cph) * EPT;
+    const bool is_v = blockIdx.z & 1;
+    const int z = blockIdx.z >> 1, layer = b.layer0 + z;
+    char* const out = is_v ? v : k;
+    if (!out) return;
+    const bool in_kept = j < d.kept;
+    int at = in_kept ? j : d.head + (j - d.kept);
+    if (!in_kept && at >= st.unit_rows) at -= st.unit_rows;
+    u32x4 r;
+    if constexpr (DTYPE == A2T_MX4) {
+        const Mx4Pool p = mx4_pool(st, is_v ? st.v_unit : st.k_unit);
+        const int64_t row = (in_kept ? mx4_kept_row(st, layer, d.s, g) : mx4_ring_row(st, layer, d.s, g)) + at;
+        const uint32_t code = *reinterpret_cast<const uint32_t*>(p.codes + row * (D / 2) + d0 / 2);
+        const uint32_t byte = p.scales[row * (D / kMxBlock) + d0 / kMxBlock];
+        r = mx4_to_bf16(code, __uint_as_float(byte << 23));
+        if (byte == kMxNaN) r = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};   // one NaN, as on the host
+    } else {
+        const void* pool = is_v ? (in_kept ? st.v_kept : st.v_unit) : (in_kept ? st.k_kept : st.k_unit);
+        const int64_t e = pool_index(st, layer, d.s, g, in_kept ? st.kept_rows : st.unit_rows, at) + d0;
+        r = *reinterpret_cast<const u32x4*>(static_cast<const char*>(pool) + e * (16 / EPT));
+    }
+    const int64_t o = (((int64_t)z * b.total_rows + d.row0 + j) * st.Hkv + g) * D + d0;
+    *reinterpret_cast<u32x4*>(out + o * (16 / EPT)) = r;
+}
+
+}  // namespace
+
+hipError_t launch_append_mx4(const DevState& st, const AppendBatch& b, int n_layers, const void* k, const void* v,
+                             hipStream_t stream, const KTimer& kt) {
+    const int tpr = st.Hkv * st.D / 16;
+    const dim3 grid((b.max_n * tpr + kRowThreads - 1) / kRowThreads, b.count, n_layers);
+    const uint16_t *kk = static_cast<const uint16_t*>(k), *vv = static_cast<const uint16_t*>(v);
+    return by_size<AppendBatchT>(b, [&](const auto& bb) {
+        using B = std::decay_t<decltype(bb)>;
+        if (kt.start)
+            hipExtLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb, kk, vv);
+        else
+            hipLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, st, bb, kk, vv);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_move_mx4(const DevState& st, const EvictBatch& b, hipStream_t stream, const KTimer& kt) {
+    int span = 1;
+    for (int i = 0; i < b.count; ++i) span = b.d[i].span > span ? b.d[i].span : span;
+    const dim3 grid(span < 256 ? (span + 3) / 4 : 64, b.count, st.L);
+    return by_size<EvictBatchT>(b, [&](const auto& bb) {
+        using B = std::decay_t<decltype(bb)>;
+        if (kt.start)
+            hipExtLaunchKernelGGL((move_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb);
+        else
+            hipLaunchKernelGGL((move_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, st, bb);
+        return hipGetLastError();
+    });
+}
+
+hipError_t launch_read_rows(const DevState& st, const ReadBatch& b, int n_layers, void* k, void* v, hipStream_t stream,
+                            const KTimer& kt) {
+    const int cpr = st.Hkv * st.D / (st.dtype == A2T_F32 ? 4 : 8);
+    const dim3 grid((uint32_t)(((int64_t)b.max_R * cpr + kRowThreads - 1) / kRowThreads), b.count, 2 * n_layers);
+    char *kk = static_cast<char*>(k), *vv = static_cast<char*>(v);
+    return by_size<ReadBatchT>(b, [&](const auto& bb) {
+        using B = std::decay_t<decltype(bb)>;
+        auto go = [&](auto kernel) {
+            if (kt.start)
+                hipExtLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb, kk, vv);
+            else
+                hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, stream, st, bb, kk, vv);
+            return hipGetLastError();
+        };
+        if (st.dtype == A2T_F32) return go(read_rows_kernel<A2T_F32, B>);
+        if (st.dtype == A2T_BF16) return go(read_rows_kernel<A2T_BF16, B>);
+        return go(read_rows_kernel<A2T_MX4, B>);
+    });
+}
+
+}  // namespace a2t
