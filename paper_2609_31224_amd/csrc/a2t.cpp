@@ -509,8 +509,12 @@ bool f32_on_valu(const a2t_cache* c, int n, const int* tiles) {
 constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
 // An attn_mx4 launch: query blocks per workgroup, and what its workgroups cost.
+// Three is the most that a wave's registers hold without spilling (four: listening units of 16
+// sessions 419 us a step of four layers, three: 258, two: 254, one: 261; 1,024 rows onto 4,096
+// keys 254, 226, 247 and 268 us, two layers).
+constexpr int kMx4Blocks = 3;
 int mx4_query_blocks(int query_rows) {
-    const int blocks = (query_rows + 15) / 16, groups = (blocks + 3) / 4;
+    const int blocks = (query_rows + 15) / 16, groups = (blocks + kMx4Blocks - 1) / kMx4Blocks;
     return (blocks + groups - 1) / groups;
 }
 constexpr SplitCosts kMx4Costs{8, 4, 1 << 20, 4};

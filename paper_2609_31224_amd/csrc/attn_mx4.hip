@@ -46,18 +46,12 @@ __device__ __forceinline__ void wave_lds_order() {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
 }
-// max / sum over the four lanes l % 16 + 16 i that hold one query column
+// max over the four lanes l % 16 + 16 i that hold one query column
 __device__ __forceinline__ float col_max(float x) {
     const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
     const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
-__device__ __forceinline__ float col_sum(float x) {
-    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // Lane l of a wave is (column l % 16, group lg = l / 16).
@@ -139,59 +133,80 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
         return kb >= kept && slot + kKeyBlock <= ring_rows;
     };
 
-    f32x4 acc[QB][DB];
-    float mrun[QB], lrun[QB];
+    f32x4 acc[QB][DB], lsum[QB];   // lsum: the sum of probabilities, in every element
+    float mrun[QB];
 #pragma unroll
     for (int x = 0; x < QB; ++x) {
         mrun[x] = -INFINITY;
-        lrun[x] = 0.f;
+        lsum[x] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < DB; ++c) acc[x][c] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
     u32x4 kc[2], vc[VL];
     int ks[2], vs[VL];   // their scale bytes
-    auto load_k = [&](int kb) {
-        const int c = lg & (NB - 1);
+    // where a key block's rows are: a run from `row` on, or each row on its own
+    struct Place {
         int64_t row;
-        if (run_of(kb, &row)) {
-            const uint8_t *p = kp.codes + row * CB, *ps = kp.scales + row * NB;
+        bool run;
+    };
+    auto place_of = [&](int kb) {
+        Place p{0, false};
+        p.run = run_of(kb, &p.row);
+        return p;
+    };
+    // (addresses are picked by branches, the loads are not: a value loaded on one side of a
+    // branch would be waited for there)
+    auto load_k = [&](int kb, const Place& at, int ln) {
+        const int l16 = ln & 15, c = (ln >> 4) & (NB - 1);
+        const uint8_t *p[2], *ps[2];
+        if (at.run) {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                kc[t] = gload16(p + (uint32_t)((16 * t + l16) * CB + 16 * c));
-                ks[t] = gload1(ps + (uint32_t)((16 * t + l16) * NB + c));
+                p[t] = kp.codes + at.row * CB + (uint32_t)((16 * t + l16) * CB + 16 * c);
+                ps[t] = kp.scales + at.row * NB + (uint32_t)((16 * t + l16) * NB + c);
             }
         } else {
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                row = row_of(kb + 16 * t + l16);
-                kc[t] = gload16(kp.codes + row * CB + 16 * c);
-                ks[t] = gload1(kp.scales + row * NB + c);
+                const int64_t row = row_of(kb + 16 * t + l16);
+                p[t] = kp.codes + row * CB + 16 * c;
+                ps[t] = kp.scales + row * NB + c;
             }
         }
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+            kc[t] = gload16(p[t]);
+            ks[t] = gload1(ps[t]);
+        }
     };
-    auto load_v = [&](int kb) {
-        int64_t row;
-        if (run_of(kb, &row)) {
-            const uint8_t *p = vp.codes + row * CB, *ps = vp.scales + row * NB;
+    auto load_v = [&](int kb, const Place& at, int ln) {
+        const uint8_t *p[VL], *ps[VL];
+        if (at.run) {
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
-                vc[j] = gload16(p + (uint32_t)(16 * (64 * j + lane)));
-                vs[j] = gload1(ps + (uint32_t)(64 * j + lane));
+                p[j] = vp.codes + at.row * CB + (uint32_t)(16 * (64 * j + ln));
+                ps[j] = vp.scales + at.row * NB + (uint32_t)(64 * j + ln);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
-                const int c = (64 * j + lane) % NB;
-                row = row_of(kb + (64 * j + lane) / NB);
-                vc[j] = gload16(vp.codes + row * CB + 16 * c);
-                vs[j] = gload1(vp.scales + row * NB + c);
+                const int c = (64 * j + ln) % NB;
+                const int64_t row = row_of(kb + (64 * j + ln) / NB);
+                p[j] = vp.codes + row * CB + 16 * c;
+                ps[j] = vp.scales + row * NB + c;
             }
+        }
+#pragma unroll
+        for (int j = 0; j < VL; ++j) {
+            vc[j] = gload16(p[j]);
+            vs[j] = gload1(ps[j]);
         }
     };
     if (n > 0) {
-        load_k(k0);
-        load_v(k0);
+        const Place at = place_of(k0);
+        load_v(k0, at, lane);
+        load_k(k0, at, lane);
     }
 
     // Q^T operands, rotated and scaled by scale * log2(e): a thread takes 8 dims of the lower
@@ -259,36 +274,44 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
     int qs[QB];
 #pragma unroll
     for (int x = 0; x < QB; ++x) qs[x] = s_qs[x][lane];
-    auto q_op = [&](int x, int p) {
-        const u32x4 a = s_q[x][p][0][lane], b2 = s_q[x][p][1][lane];
+    auto q_op = [&](int x, int p, int ln) {
+        const u32x4 a = s_q[x][p][0][ln], b2 = s_q[x][p][1][ln];
         return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2[0], (int)b2[1], (int)b2[2], (int)b2[3]};
     };
 
-    u32x4* const s_v = s_mem + w * (kKeyBlock * D / 8);
-    // transposed reads: 16 lanes read 8 bytes each of four keys' 32 bytes
-    const int vk = 4 * lg + (l16 >> 2);
-    const char* const vt = reinterpret_cast<const char*>(s_v) + v_chunk<D>(vk, (l16 & 3) >> 1) * 16 + (l16 & 1) * 8;
-    auto v_half = [&](int c, int half) {
-        // chunk 2 c of the lane's key: the swizzle and c touch the same bits of the address
-        const uint32_t at = (lds_addr(vt) ^ (uint32_t)(32 * c)) + half * 16 * D * 2;
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(uintptr_t)at);
+    // this wave's V: where the lane's block e (of 8 dims) of its first row goes, and the lane's
+    // place in the transposed reads (16 lanes read 8 bytes each of four keys' 32 bytes).  The
+    // swizzle and e (the 16-dim block c) touch the same bits of the address.
+    const uint32_t s_v = lds_addr(s_mem) + w * (kKeyBlock * D * 2);
+    const uint32_t v_in0 = s_v + 16 * v_chunk<D>(lane / NB, 4 * (lane % NB));
+    const uint32_t v_out0 = s_v + 16 * v_chunk<D>(4 * lg + (l16 >> 2), (l16 & 3) >> 1) + 8 * (l16 & 1);
+    auto v_store = [&](uint32_t v_in, int j, int e, const u32x4& x) {   // row 64 j / NB + lane / NB
+        *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((uintptr_t)((v_in ^ (16u * e)) + j * (64 / NB) * D * 2)) = x;
     };
+    auto v_half = [&](uint32_t v_out, int c, int half) {
+        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) i16x4*)(uintptr_t)((v_out ^ (32u * c)) + half * 16 * D * 2));
+    };
+    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
         const int kb = k0 + i * kStride;
+        // the block after it (past the last one: row R - 1 once more, one cache line)
+        const int kb_next = i + 1 < n ? kb + kStride : R;
+        const Place next = place_of(kb_next);
+        // registers: no address of the lane is kept from one pass to the next
+        int ln = lane;
+        uint32_t v_in = v_in0, v_out = v_out0;
+        asm volatile("" : "+v"(ln), "+v"(v_in), "+v"(v_out));
         // V: codes to bf16 rows in LDS
         bool nan_v = false;
 #pragma unroll
         for (int j = 0; j < VL; ++j) {
-            const int key = (64 * j + lane) / NB, c = (64 * j + lane) % NB;
             nan_v |= vs[j] == kMxNaN;
             const float s = __uint_as_float((uint32_t)vs[j] << 23);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                u32x4 x = mx4_to_bf16(vc[j][e], s);
-                s_v[v_chunk<D>(key, 4 * c + e)] = x;
-            }
+            for (int e = 0; e < 4; ++e) v_store(v_in, j, e, mx4_to_bf16(vc[j][e], s));
         }
         const bool any_nan = __any(nan_v);
         int nan_bytes[VL];
@@ -298,25 +321,26 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
 #pragma unroll
             for (int j = 0; j < VL; ++j) {
                 nan_bytes[j] = vs[j];
-                const int key = (64 * j + lane) / NB, c = (64 * j + lane) % NB;
                 if (vs[j] == kMxNaN)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s_v[v_chunk<D>(key, 4 * c + e)] = u32x4{0u, 0u, 0u, 0u};
+                    for (int e = 0; e < 4; ++e) v_store(v_in, j, e, u32x4{0u, 0u, 0u, 0u});
             }
         }
         wave_lds_order();   // other lanes read these rows
-        if (i + 1 < n) load_v(kb + kStride);
+        load_v(kb_next, next, ln);
+        __builtin_amdgcn_sched_barrier(0);
 
         // scores, relative to the running reference
         f32x4 sc[QB][2];
 #pragma unroll
         for (int x = 0; x < QB; ++x) {
+            if (x == 2) __builtin_amdgcn_sched_barrier(0);   // registers: the Q operands of two blocks at a time
             const float mu = mrun[x] == -INFINITY ? 0.f : mrun[x];
 #pragma unroll
             for (int t = 0; t < 2; ++t) sc[x][t] = f32x4{-mu, -mu, -mu, -mu};
 #pragma unroll
             for (int p = 0; p < QP; ++p) {
-                const i32x8 qv = q_op(x, p);
+                const i32x8 qv = q_op(x, p, ln);
                 const int s = p == 0 || qs[x] == kMxNaN ? qs[x] : qs[x] - 4;
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
@@ -325,45 +349,57 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
                 }
             }
         }
-        if (i + 1 < n) load_k(kb + kStride);
+        __builtin_amdgcn_sched_barrier(0);   // into the registers that the products have read
+        load_k(kb_next, next, ln);
 
-        const bool masked = kb + kKeyBlock - 1 > vis0;
-        bf16x8 p[QB];
+        if (kb + kKeyBlock - 1 > vis0) {   // some row does not see every key
 #pragma unroll
-        for (int x = 0; x < QB; ++x) {
-            if (masked) {
+            for (int x = 0; x < QB; ++x)
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (kb + 16 * t + 4 * lg + e > vis0 + qi[x]) sc[x][t][e] = -INFINITY;
-            }
-            float top = fmaxf(fmaxf(sc[x][0][0], sc[x][0][1]), fmaxf(sc[x][0][2], sc[x][0][3]));
-            top = fmaxf(top, fmaxf(fmaxf(sc[x][1][0], sc[x][1][1]), fmaxf(sc[x][1][2], sc[x][1][3])));
-            top = col_max(top);
-            // the reference follows the row maximum lazily: set by the first visible key, then
-            // raised (and the running sums rescaled) only when a block exceeds it by more than 2^8
-            const bool fresh = mrun[x] == -INFINITY;
-            if (__any(top > (fresh ? -INFINITY : 8.f))) {
-                const float up = fresh ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
-                const float corr = __builtin_amdgcn_exp2f(fresh ? 0.f : -up);   // nothing is summed yet where fresh
-                mrun[x] = fresh ? (top == -INFINITY ? -INFINITY : top) : mrun[x] + up;
-                lrun[x] *= corr;
+        }
+        // the reference follows the row maximum lazily: set by the first block (a row that sees
+        // none of its keys sees none of the later ones), then raised, and the running sums
+        // rescaled, only when a block exceeds it by more than 2^8
+        float top[QB], most = -INFINITY;
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
+            top[x] = fmaxf(fmaxf(sc[x][0][0], sc[x][0][1]), sc[x][0][2]);
+            top[x] = fmaxf(fmaxf(top[x], sc[x][0][3]), sc[x][1][0]);
+            top[x] = fmaxf(fmaxf(top[x], sc[x][1][1]), sc[x][1][2]);
+            top[x] = fmaxf(top[x], sc[x][1][3]);
+            most = fmaxf(most, top[x]);
+        }
+        if (i == 0 || __any(most > 8.f)) {
+#pragma unroll
+            for (int x = 0; x < QB; ++x) {
+                const float t = col_max(top[x]);
+                const float up = i ? fmaxf(t, 0.f) : t == -INFINITY ? 0.f : t;
+                mrun[x] = i ? mrun[x] + up : t;
+                const float corr = __builtin_amdgcn_exp2f(i ? -up : 0.f);
+                lsum[x] *= corr;
 #pragma unroll
                 for (int c = 0; c < DB; ++c) acc[x][c] *= corr;
 #pragma unroll
-                for (int t = 0; t < 2; ++t) sc[x][t] -= up;
+                for (int t2 = 0; t2 < 2; ++t2) sc[x][t2] -= up;
             }
+        }
+        bf16x8 p[QB];
+#pragma unroll
+        for (int x = 0; x < QB; ++x) {
             float pr[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[x][e >> 2][e & 3]);
-            lrun[x] += ((pr[0] + pr[1]) + (pr[2] + pr[3])) + ((pr[4] + pr[5]) + (pr[6] + pr[7]));
             p[x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]),
                                                     pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])});
+            lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[x], lsum[x], 0, 0, 0);
         }
 #pragma unroll
         for (int c = 0; c < DB; ++c) {
-            const i16x4 a = v_half(c, 0), a2 = v_half(c, 1);
+            const i16x4 a = v_half(v_out, c, 0), a2 = v_half(v_out, c, 1);
             const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, a2, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int x = 0; x < QB; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[x], acc[x][c], 0, 0, 0);
@@ -390,12 +426,6 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
             }
         }
     }
-#pragma unroll
-    for (int x = 0; x < QB; ++x) {
-        lrun[x] = col_sum(lrun[x]);
-        if (mrun[x] == -INFINITY && lrun[x] != 0.f) mrun[x] = 0.f;   // a NaN sum keeps its weight
-    }
-
     // combine the waves' states, one block of query rows after the other: each wave sums an
     // eighth of the dims
     const bool whole = d.splits == 1;
@@ -405,7 +435,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
         __syncthreads();   // V, or the states of the block before
 #pragma unroll
         for (int c = 0; c < DB; ++c) s_part[w][c][lane] = acc[x][c];
-        if (lg == 0) s_ml[w][l16] = make_float2(mrun[x], lrun[x]);
+        if (lg == 0) s_ml[w][l16] = make_float2(mrun[x], lsum[x][0]);
         __syncthreads();
         const int mq = mw + x * kRows + l16;
         float mx = -INFINITY;
@@ -439,7 +469,8 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
             }
         }
         if (!whole && w == 0 && lg == 0 && mq < M)
-            *reinterpret_cast<float2*>(po + (int64_t)d.splits * st.Hkv * M * (D / 2) + at * 2) = make_float2(mx, L);
+            *reinterpret_cast<float2*>(po + (int64_t)d.splits * st.Hkv * M * (D / 2) + at * 2) =
+                make_float2(mx == -INFINITY && L != 0.f ? 0.f : mx, L);   // a NaN sum keeps its weight
     }
 }
 
@@ -469,7 +500,6 @@ hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blo
                 case 1: return go(attn_mx4_kernel<D, 1, N>);
                 case 2: return go(attn_mx4_kernel<D, 2, N>);
                 case 3: return go(attn_mx4_kernel<D, 3, N>);
-                case 4: return go(attn_mx4_kernel<D, 4, N>);
                 default: return hipErrorInvalidValue;
             }
         };

@@ -1,7 +1,7 @@
 """GPU parity of A2T_MX4 caches (rows held in 4 bits) against the float64 oracle: encoded rows
 and rows read back exactly, attention within a bound that the oracle derives from the
 roundings it is computed with.  Query rows around the 16-row blocks and the workgroups of one to
-four blocks, key counts around the 32-key blocks, both head dims, one to eight query heads
+three blocks, key counts around the 32-key blocks, both head dims, one to eight query heads
 per KV head, rings that wrap, kept regions, every eviction rule, key splits, batches.
 """
 import numpy as np
@@ -45,9 +45,9 @@ def test_one_row(gpu, d):
     (32, 8, 64, 22, 900, None, "fused", None),      # 88: two groups of three
     (32, 8, 128, 22, 900, None, "fused", 5),        # the last 5 of 22 rows query: two blocks
     (6, 3, 128, 40, 130, "5", "noalloc", None),     # 80: two groups of three
-    (8, 1, 64, 16, 130, "3", "noalloc", None),      # 128: two groups of four
+    (8, 1, 64, 16, 130, "3", "noalloc", None),      # 128: three groups of three
     (2, 2, 64, 90, 3, "128", "separate", None),     # more splits asked for than tiles
-    (8, 2, 128, 61, 0, "4", "all", None),           # 244: four groups of four
+    (8, 2, 128, 61, 0, "4", "all", None),           # 244: six groups of three
 ])
 def test_chunks(gpu, monkeypatch, hq, hkv, d, rows, prefix, splits, calls, query_rows):
     if splits:
