@@ -508,14 +508,34 @@ bool f32_on_valu(const a2t_cache* c, int n, const int* tiles) {
 }
 constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
-// An attn_mx4 launch: query blocks per workgroup, and what its workgroups cost.
-// Three is the most that a wave's registers hold without spilling (four: listening units of 16
-// sessions 419 us a step of four layers, three: 258, two: 254, one: 261; 1,024 rows onto 4,096
-// keys 254, 226, 247 and 268 us, two layers).
-constexpr int kMx4Blocks = 3;
-int mx4_query_blocks(int query_rows) {
-    const int blocks = (query_rows + 15) / 16, groups = (blocks + kMx4Blocks - 1) / kMx4Blocks;
-    return (blocks + groups - 1) / groups;
+// An attn_mx4 launch: blocks of 16 query rows and waves (key blocks at a time) per workgroup,
+// and what its workgroups cost.
+//
+// Three blocks are the most that a wave's registers hold without spilling (four: listening
+// units of 16 sessions 419 us a step of four layers, three: 258, two: 254, one: 261; 1,024 rows
+// onto 4,096 keys 254, 226, 247 and 268 us, two layers).
+//
+// Workgroups of four waves and two blocks where there are more than two for each CU anyway
+// and few keys: two of them share a CU, so that one's first loads and the combining of
+// its waves' states go with the other's products (777 rows of 32/4 heads of 64 onto none 12.3
+// against 21.6 us, 1,024 rows of 32/8 heads of 128 onto none 27.6 against 35.6; onto 4,096
+// keys 119 against 121, onto 16,384 364 against 352).
+constexpr int kMx4Blocks = 3, kMx4FewTiles = 64;
+struct Mx4Shape {
+    int query_blocks, key_waves;
+};
+Mx4Shape mx4_shape(const a2t_cache* c, int n, const int* tiles, const int32_t* n_q) {
+    const int Hkv = c->cfg.n_kv_heads, G = c->cfg.n_q_heads / Hkv;
+    int rows = 1, longest = 1;
+    int64_t pairs = 0;
+    for (int i = 0; i < n; ++i) {
+        rows = std::max(rows, G * n_q[i]);
+        longest = std::max(longest, tiles[i]);
+        pairs += (int64_t)Hkv * mx4_groups(G * n_q[i], 2);
+    }
+    if (rows > 16 && longest <= kMx4FewTiles && pairs > 2 * c->target_wgs) return {2, 4};
+    const int blocks = (rows + 15) / 16, groups = (blocks + kMx4Blocks - 1) / kMx4Blocks;
+    return {(blocks + groups - 1) / groups, 8};
 }
 constexpr SplitCosts kMx4Costs{8, 4, 1 << 20, 4};
 
@@ -570,6 +590,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     const bool mx4 = c->cfg.dtype == A2T_MX4;
     const int64_t rf = partial_row_floats(c->cfg.head_dim, f32 || valu);
     int query_blocks = 1;
+    Mx4Shape shape{1, 8};
     int max_rows = 0, tiles[kMaxDesc], nsplit[kMaxDesc];
     int64_t floats[kMaxDesc];
     for (int i = 0; i < n; ++i) {
@@ -584,7 +605,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     if (f32 || block || one_row || mx4) {
         SplitStream ss[kMaxDesc];
         if (f32) query_blocks = f32_query_blocks(c, n, tiles, n_q);
-        if (mx4) query_blocks = mx4_query_blocks(G * max_rows);
+        if (mx4) query_blocks = (shape = mx4_shape(c, n, tiles, n_q)).query_blocks;
         for (int i = 0; i < n; ++i) {
             const int rows = G * n_q[i];
             ss[i] = {tiles[i], c->cfg.n_kv_heads * (mx4 ? mx4_groups(rows, query_blocks) : f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
@@ -668,7 +689,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     b.max_rows = max_rows;
     hipError_t e;
     auto launch = [&](const DevState& st, const KTimer& kt) {
-        if (mx4) return launch_attn_mx4(st, b, query_blocks, q, o, c->stream, kt);
+        if (mx4) return launch_attn_mx4(st, b, query_blocks, shape.key_waves, q, o, c->stream, kt);
         if (f32) return launch_attn_f32(st, b, query_blocks, q, o, k_in, v_in, c->stream, kt);
         if (valu) return launch_attn_valu(st, b, q, o, c->stream, kt);
         if (block) return launch_attn_block(st, b, q, o, c->stream, kt);

@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kKeyBlock = 32;    // keys of a wave's block
 constexpr int kRows = 16;        // query rows of a product
-constexpr int kKeyWaves = 8;     // waves of a workgroup: they share its keys
+constexpr int kAhead = 3;        // V operands read ahead of the products
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
@@ -69,8 +69,8 @@ __device__ __forceinline__ int v_chunk(int key, int c) {
     return key * (D / 8) + (c ^ (2 * y | ((y >> 1) & 1)));
 }
 
-template <int D, int QB, int N>
-__global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevState st, AttnBatchT<N> b,
+template <int D, int QB, int KW, int N>
+__global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevState st, AttnBatchT<N> b,
                                                                                    WgStart<N> start, const uint16_t* q,
                                                                                    uint16_t* o) {
     constexpr int NB = D / kMxBlock;   // blocks of a row
@@ -78,14 +78,15 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
     constexpr int DB = D / 16;         // 16-dim blocks of O
     constexpr int VL = D / 64;         // 16-byte loads of V per lane and key block
     constexpr int QP = D / 64;         // products per 16 keys: hi and lo, or both in one
-    constexpr int kStride = kKeyWaves * kKeyBlock;
+    constexpr int kStride = KW * kKeyBlock;
+    constexpr bool kPipe = QB > 1;
     // (its chunks are found by exclusive or on their addresses: whole rows are aligned)
-    __shared__ __align__(256) u32x4 s_mem[kKeyWaves * kKeyBlock * D / 8];   // V of each wave's block; at the end the states
+    __shared__ __align__(256) u32x4 s_mem[(kPipe ? 2 : 1) * KW * kKeyBlock * D / 8];   // V of each wave's block; at the end the states
     __shared__ u32x4 s_q[QB][QP][2][64];                     // Q operands
     __shared__ uint8_t s_qs[QB][64];                         // ... and their scales
-    __shared__ float2 s_ml[kKeyWaves][kRows];
-    f32x4(&s_part)[kKeyWaves][DB][64] = *reinterpret_cast<f32x4(*)[kKeyWaves][DB][64]>(s_mem);
-    static_assert(sizeof(f32x4) * kKeyWaves * DB * 64 <= sizeof(s_mem), "the states of one block of query rows fit");
+    __shared__ float2 s_ml[KW][kRows];
+    f32x4(&s_part)[KW][DB][64] = *reinterpret_cast<f32x4(*)[KW][DB][64]>(s_mem);
+    static_assert(sizeof(f32x4) * KW * DB * 64 <= sizeof(s_mem), "the states of one block of query rows fit");
 
     int wg;
     const AttnDesc d = b.d[stream_of(start, b.count, &wg)];
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
     // Q^T operands, rotated and scaled by scale * log2(e): a thread takes 8 dims of the lower
     // half and their partners of the upper one, four threads a block.  Rows past M read row
     // M - 1 and are never stored.
-    for (int x = threadIdx.x; x < QB * kRows * (D / 16); x += 64 * kKeyWaves) {
+    for (int x = threadIdx.x; x < QB * kRows * (D / 16); x += 64 * KW) {
         const int r = x / (D / 16), d0 = (x - r * (D / 16)) * 8;
         const int m = min(mw + r, M - 1), i = m / G;
         const uint16_t* qp = q + ((int64_t)(d.q_row0 + i) * st.Hq + g * G + (m - i * G)) * D + d0;
@@ -274,84 +275,58 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
     int qs[QB];
 #pragma unroll
     for (int x = 0; x < QB; ++x) qs[x] = s_qs[x][lane];
-    auto q_op = [&](int x, int p, int ln) {
-        const u32x4 a = s_q[x][p][0][ln], b2 = s_q[x][p][1][ln];
-        return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2[0], (int)b2[1], (int)b2[2], (int)b2[3]};
-    };
-
     // this wave's V: where the lane's block e (of 8 dims) of its first row goes, and the lane's
     // place in the transposed reads (16 lanes read 8 bytes each of four keys' 32 bytes).  The
     // swizzle and e (the 16-dim block c) touch the same bits of the address.
+    constexpr int kBuf = KW * kKeyBlock * D * 2;   // bytes of a buffer
     const uint32_t s_v = lds_addr(s_mem) + w * (kKeyBlock * D * 2);
     const uint32_t v_in0 = s_v + 16 * v_chunk<D>(lane / NB, 4 * (lane % NB));
     const uint32_t v_out0 = s_v + 16 * v_chunk<D>(4 * lg + (l16 >> 2), (l16 & 3) >> 1) + 8 * (l16 & 1);
     auto v_store = [&](uint32_t v_in, int j, int e, const u32x4& x) {   // row 64 j / NB + lane / NB
         *reinterpret_cast<__attribute__((address_space(3))) u32x4*>((uintptr_t)((v_in ^ (16u * e)) + j * (64 / NB) * D * 2)) = x;
     };
-    auto v_half = [&](uint32_t v_out, int c, int half) {
-        return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (__attribute__((address_space(3))) i16x4*)(uintptr_t)((v_out ^ (32u * c)) + half * 16 * D * 2));
+    auto v_op = [&](uint32_t v_out, int c) {
+        i16x4 h[2];
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+            h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (__attribute__((address_space(3))) i16x4*)(uintptr_t)((v_out ^ (32u * c)) + half * 16 * D * 2));
+        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
+    // LDS reads and matrix products stay in the order written; other vector operations move freely
+    auto ordered = [] { __builtin_amdgcn_sched_barrier(0x6); };
+    // nothing moves past; between two of these a product is followed by m vector operations
+    auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
     const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
 
-#pragma unroll 1
-    for (int i = 0; i < n; ++i) {
-        const int kb = k0 + i * kStride;
-        // the block after it (past the last one: row R - 1 once more, one cache line)
-        const int kb_next = i + 1 < n ? kb + kStride : R;
-        const Place next = place_of(kb_next);
-        // registers: no address of the lane is kept from one pass to the next
-        int ln = lane;
-        uint32_t v_in = v_in0, v_out = v_out0;
-        asm volatile("" : "+v"(ln), "+v"(v_in), "+v"(v_out));
-        // V: codes to bf16 rows in LDS
-        bool nan_v = false;
+    f32x4 sc[QB][2];   // scores of a block, relative to the running reference
+    bf16x8 p[QB];      // its probabilities
+    i32x8 qv[2][QP];   // Q operands, read one block of rows ahead of the products
+    auto read_q = [&](int x, int ln) {
 #pragma unroll
-        for (int j = 0; j < VL; ++j) {
-            nan_v |= vs[j] == kMxNaN;
-            const float s = __uint_as_float((uint32_t)vs[j] << 23);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v_store(v_in, j, e, mx4_to_bf16(vc[j][e], s));
+        for (int k = 0; k < QP; ++k) {
+            const u32x4 a = s_q[x][k][0][ln], b2 = s_q[x][k][1][ln];
+            qv[x & 1][k] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2[0], (int)b2[1], (int)b2[2], (int)b2[3]};
         }
-        const bool any_nan = __any(nan_v);
-        int nan_bytes[VL];
-        if (any_nan) {
-            // a block that is NaN counts for the queries that see its key, below; its place
-            // holds zeros, which change nothing for the others
+    };
+    auto score = [&](int x) {
+        const float mu = mrun[x] == -INFINITY ? 0.f : mrun[x];
 #pragma unroll
-            for (int j = 0; j < VL; ++j) {
-                nan_bytes[j] = vs[j];
-                if (vs[j] == kMxNaN)
+        for (int t = 0; t < 2; ++t) sc[x][t] = f32x4{-mu, -mu, -mu, -mu};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) v_store(v_in, j, e, u32x4{0u, 0u, 0u, 0u});
+        for (int k = 0; k < QP; ++k) {
+            const int s = k == 0 || qs[x] == kMxNaN ? qs[x] : qs[x] - 4;
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const i32x8 kv = {(int)kc[t][0], (int)kc[t][1], (int)kc[t][2], (int)kc[t][3], 0, 0, 0, 0};
+                sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv[x & 1][k], sc[x][t], 4, 0, 0, ks[t], 0, s);
             }
         }
-        wave_lds_order();   // other lanes read these rows
-        load_v(kb_next, next, ln);
-        __builtin_amdgcn_sched_barrier(0);
-
-        // scores, relative to the running reference
-        f32x4 sc[QB][2];
-#pragma unroll
-        for (int x = 0; x < QB; ++x) {
-            if (x == 2) __builtin_amdgcn_sched_barrier(0);   // registers: the Q operands of two blocks at a time
-            const float mu = mrun[x] == -INFINITY ? 0.f : mrun[x];
-#pragma unroll
-            for (int t = 0; t < 2; ++t) sc[x][t] = f32x4{-mu, -mu, -mu, -mu};
-#pragma unroll
-            for (int p = 0; p < QP; ++p) {
-                const i32x8 qv = q_op(x, p, ln);
-                const int s = p == 0 || qs[x] == kMxNaN ? qs[x] : qs[x] - 4;
-#pragma unroll
-                for (int t = 0; t < 2; ++t) {
-                    const i32x8 kv = {(int)kc[t][0], (int)kc[t][1], (int)kc[t][2], (int)kc[t][3], 0, 0, 0, 0};
-                    sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv, sc[x][t], 4, 0, 0, ks[t], 0, s);
-                }
-            }
-        }
-        __builtin_amdgcn_sched_barrier(0);   // into the registers that the products have read
-        load_k(kb_next, next, ln);
-
+    };
+    // hides what a row does not see, and moves the reference, lazily: the first block sets it (a row that sees
+    // none of its keys sees none of the later ones), and it is raised, and the running sums
+    // rescaled, only when a block exceeds it by more than 2^8
+    auto settle = [&](int kb, bool first) {
         if (kb + kKeyBlock - 1 > vis0) {   // some row does not see every key
 #pragma unroll
             for (int x = 0; x < QB; ++x)
@@ -361,9 +336,6 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
                     for (int e = 0; e < 4; ++e)
                         if (kb + 16 * t + 4 * lg + e > vis0 + qi[x]) sc[x][t][e] = -INFINITY;
         }
-        // the reference follows the row maximum lazily: set by the first block (a row that sees
-        // none of its keys sees none of the later ones), then raised, and the running sums
-        // rescaled, only when a block exceeds it by more than 2^8
         float top[QB], most = -INFINITY;
 #pragma unroll
         for (int x = 0; x < QB; ++x) {
@@ -373,13 +345,13 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
             top[x] = fmaxf(top[x], sc[x][1][3]);
             most = fmaxf(most, top[x]);
         }
-        if (i == 0 || __any(most > 8.f)) {
+        if (first || __any(most > 8.f)) {
 #pragma unroll
             for (int x = 0; x < QB; ++x) {
                 const float t = col_max(top[x]);
-                const float up = i ? fmaxf(t, 0.f) : t == -INFINITY ? 0.f : t;
-                mrun[x] = i ? mrun[x] + up : t;
-                const float corr = __builtin_amdgcn_exp2f(i ? -up : 0.f);
+                const float up = !first ? fmaxf(t, 0.f) : t == -INFINITY ? 0.f : t;
+                mrun[x] = first ? t : mrun[x] + up;
+                const float corr = __builtin_amdgcn_exp2f(first ? 0.f : -up);
                 lsum[x] *= corr;
 #pragma unroll
                 for (int c = 0; c < DB; ++c) acc[x][c] *= corr;
@@ -387,43 +359,185 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
                 for (int t2 = 0; t2 < 2; ++t2) sc[x][t2] -= up;
             }
         }
-        bf16x8 p[QB];
+    };
+    auto weigh = [&](int x) {
+        float pr[8];
 #pragma unroll
-        for (int x = 0; x < QB; ++x) {
-            float pr[8];
+        for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[x][e >> 2][e & 3]);
+        p[x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]),
+                                                pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])});
+    };
+    auto sum = [&](int x) { lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[x], lsum[x], 0, 0, 0); };
+    // step m of 4 VL: a lane's 8 values of V to LDS as bf16
+    auto take_v = [&](uint32_t v_in, int m) {
+        v_store(v_in, m / 4, m % 4, mx4_to_bf16(vc[m / 4][m % 4], __uint_as_float((uint32_t)vs[m / 4] << 23)));
+    };
+    // A block of V that is NaN counts for the queries that see its key: their sums become NaN here;
+    // its place takes zeros, which change nothing for the others.
+    auto nan_v = [&](uint32_t v_in, int kb) {
+        bool any = false;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[x][e >> 2][e & 3]);
-            p[x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]),
-                                                    pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])});
-            lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[x], lsum[x], 0, 0, 0);
+        for (int j = 0; j < VL; ++j) any |= vs[j] == kMxNaN;
+        if (!__any(any)) return;
+#pragma unroll
+        for (int j = 0; j < VL; ++j)
+            if (vs[j] == kMxNaN)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v_store(v_in, j, e, u32x4{0u, 0u, 0u, 0u});
+#pragma unroll 1
+        for (int key = 0; key < kKeyBlock; ++key) {
+#pragma unroll
+            for (int c = 0; c < NB; ++c) {
+                const int at = key * NB + c;
+                int byte = 0;
+#pragma unroll
+                for (int j = 0; j < VL; ++j)
+                    if (at / 64 == j) byte = __builtin_amdgcn_readlane(vs[j], at & 63);
+                if (byte != kMxNaN) continue;
+#pragma unroll
+                for (int x = 0; x < QB; ++x)
+                    if (kb + key <= vis0 + qi[x]) {
+                        const float z = __uint_as_float(0x7fc00000u);
+                        acc[x][2 * c] = acc[x][2 * c + 1] = f32x4{z, z, z, z};
+                    }
+            }
         }
+    };
+    bf16x8 vv[kAhead + 1];   // V operands, read kAhead 16-dim blocks ahead of the products
+
+    if constexpr (!kPipe) {
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            const int kb = k0 + i * kStride;
+            // the block after it (past the last one: row R - 1 once more, one cache line)
+            const int kb_next = i + 1 < n ? kb + kStride : R;
+            const Place next = place_of(kb_next);
+            // registers: no address of the lane is kept from one pass to the next
+            int ln = lane;
+            uint32_t v_in = v_in0, v_out = v_out0;
+            asm volatile("" : "+v"(ln), "+v"(v_in), "+v"(v_out));
+            read_q(0, ln);
+            ordered();
+#pragma unroll
+            for (int m = 0; m < 4 * VL; ++m) take_v(v_in, m);
+            nan_v(v_in, kb);
+            wave_lds_order();   // other lanes read these rows
+            load_v(kb_next, next, ln);
+            ordered();
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int x = 0; x < QB; ++x) {
+                if (x + 1 < QB) read_q(x + 1, ln);
+                ordered();
+                score(x);
+                ordered();
+            }
+            __builtin_amdgcn_s_setprio(0);
+            load_k(kb_next, next, ln);   // into the registers that the products have read
+#pragma unroll
+            for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
+            ordered();
+            settle(kb, i == 0);
+#pragma unroll
+            for (int x = 0; x < QB; ++x) weigh(x), sum(x);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int c = 0; c < DB; ++c) {
+                if (c + kAhead < DB) vv[(c + kAhead) % (kAhead + 1)] = v_op(v_out, c + kAhead);
+                ordered();
+#pragma unroll
+                for (int x = 0; x < QB; ++x)
+                    acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[c % (kAhead + 1)], p[x], acc[x][c], 0, 0, 0);
+                ordered();
+            }
+            __builtin_amdgcn_s_setprio(0);
+            wave_lds_order();   // the next block takes this one's place
+        }
+    } else if (n > 0) {
+        auto values = [&](int c) {
+#pragma unroll
+            for (int x = 0; x < QB; ++x)
+                acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[c % (kAhead + 1)], p[x], acc[x][c], 0, 0, 0);
+        };
+        {
+            const int kb_next = n > 1 ? k0 + kStride : R;
+            const Place next = place_of(kb_next);
+#pragma unroll
+            for (int m = 0; m < 4 * VL; ++m) take_v(v_in0, m);
+            nan_v(v_in0, k0);
+            load_v(kb_next, next, lane);
+#pragma unroll
+            for (int x = 0; x < QB; ++x) read_q(x, lane), score(x);
+            fence();
+            load_k(kb_next, next, lane);
+            settle(k0, true);
+        }
+        // In each pass the probabilities and products of a block go with the next one's scores and V: the matrix
+        // units work on one while the vector units work on the other.
+#pragma unroll 1
+        for (int i = 0; i + 1 < n; ++i) {
+            const int kb = k0 + (i + 1) * kStride;   // the next block; K and V are in registers or on their way
+            const int kb_next = i + 2 < n ? kb + kStride : R;
+            const Place next = place_of(kb_next);
+            int ln = lane;
+            const uint32_t flip = i & 1 ? kBuf : 0;
+            uint32_t v_in = v_in0 + (kBuf - flip), v_out = v_out0 + flip;
+            asm volatile("" : "+v"(ln), "+v"(v_in), "+v"(v_out));
+            wave_lds_order();   // other lanes wrote this block's rows
+            read_q(0, ln);
+            fence();
+            weigh(0);
+#pragma unroll
+            for (int x = 0; x < QB; ++x) {
+                if (x + 1 < QB) read_q(x + 1, ln);
+                else {
+#pragma unroll
+                    for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
+                }
+                fence();
+                score(x);
+                sum(x);
+                if (x + 1 < QB) weigh(x + 1);
+#pragma unroll
+                for (int m = 0; m < 2 * QP + 1; ++m) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                }
+                fence();
+            }
+            load_k(kb_next, next, ln);   // into the registers that the products have read
+            fence();
+#pragma unroll
+            for (int c = 0; c < DB; ++c) {
+                if (c + kAhead < DB) vv[(c + kAhead) % (kAhead + 1)] = v_op(v_out, c + kAhead);
+                values(c);
+                take_v(v_in, c);
+                static_assert(DB == 4 * VL, "a step of V for each block of products");
+                if (c + kAhead < DB) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                for (int x = 0; x < QB; ++x) {
+                    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
+                }
+                fence();
+            }
+            nan_v(v_in, kb);
+            load_v(kb_next, next, ln);
+            settle(kb, false);
+        }
+        // the last block
+        const uint32_t v_out = v_out0 + (n & 1 ? 0 : kBuf);
+        wave_lds_order();
+#pragma unroll
+        for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
+#pragma unroll
+        for (int x = 0; x < QB; ++x) weigh(x), sum(x);
 #pragma unroll
         for (int c = 0; c < DB; ++c) {
-            const i16x4 a = v_half(v_out, c, 0), a2 = v_half(v_out, c, 1);
-            const bf16x8 vv = __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, a2, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-            for (int x = 0; x < QB; ++x) acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv, p[x], acc[x][c], 0, 0, 0);
-        }
-        wave_lds_order();   // the next block takes this one's place
-        if (any_nan) {
-#pragma unroll 1
-            for (int key = 0; key < kKeyBlock; ++key) {
-#pragma unroll
-                for (int c = 0; c < NB; ++c) {
-                    const int at = key * NB + c;
-                    int byte = 0;
-#pragma unroll
-                    for (int j = 0; j < VL; ++j)
-                        if (at / 64 == j) byte = __builtin_amdgcn_readlane(nan_bytes[j], at & 63);
-                    if (byte != kMxNaN) continue;
-#pragma unroll
-                    for (int x = 0; x < QB; ++x)
-                        if (kb + key <= vis0 + qi[x]) {
-                            const float z = __uint_as_float(0x7fc00000u);
-                            acc[x][2 * c] = acc[x][2 * c + 1] = f32x4{z, z, z, z};
-                        }
-                }
-            }
+            if (c + kAhead < DB) vv[(c + kAhead) % (kAhead + 1)] = v_op(v_out, c + kAhead);
+            ordered();
+            values(c);
+            ordered();
         }
     }
     // combine the waves' states, one block of query rows after the other: each wave sums an
@@ -440,14 +554,14 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
         const int mq = mw + x * kRows + l16;
         float mx = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < kKeyWaves; ++k) mx = fmaxf(mx, s_ml[k][l16].x);
+        for (int k = 0; k < KW; ++k) mx = fmaxf(mx, s_ml[k][l16].x);
         auto weight = [&](int k) {
             const float m = s_ml[k][l16].x;
             return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
         };
-        float wt[kKeyWaves], L = 0.f;
+        float wt[KW], L = 0.f;
 #pragma unroll
-        for (int k = 0; k < kKeyWaves; ++k) {
+        for (int k = 0; k < KW; ++k) {
             wt[k] = weight(k);
             L += wt[k] * s_ml[k][l16].y;
         }
@@ -455,10 +569,10 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
         // is zeros with a maximum of -inf), else the bf16 output
         const float inv = L == 0.f && !whole ? 0.f : 1.f / L;
         const int64_t at = ((int64_t)sp * st.Hkv + g) * M + mq;
-        for (int c = w; c < DB && mq < M; c += kKeyWaves) {   // dims 16 c + 4 lg .. + 3
+        for (int c = w; c < DB && mq < M; c += KW) {   // dims 16 c + 4 lg .. + 3
             f32x4 O = s_part[0][c][lane] * wt[0];
 #pragma unroll
-            for (int k = 1; k < kKeyWaves; ++k) O += s_part[k][c][lane] * wt[k];
+            for (int k = 1; k < KW; ++k) O += s_part[k][c][lane] * wt[k];
             O *= inv;
             if (whole) {
                 uint16_t* orow = o + ((int64_t)(d.q_row0 + qi[x]) * st.Hq + g * G + (mq - qi[x] * G)) * D;
@@ -476,9 +590,8 @@ __global__ __launch_bounds__(64 * kKeyWaves, QB == 1 ? 4 : 2) void attn_mx4_kern
 
 }  // namespace
 
-hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, const void* q, void* o,
+hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, int key_waves, const void* q, void* o,
                            hipStream_t stream, const KTimer& kt) {
-    const dim3 block(64 * kKeyWaves);
     const uint16_t* qq = static_cast<const uint16_t*>(q);
     uint16_t* oo = static_cast<uint16_t*>(o);
     return by_size<AttnBatchT>(b, [&](const auto& bb) {
@@ -488,6 +601,7 @@ hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blo
             return mx4_groups(st.G * b.d[i].n_q, query_blocks) * b.d[i].splits * st.Hkv;
         });
         auto go = [&](auto kernel) {
+            const dim3 block(64 * key_waves);
             if (kt.start)
                 hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo);
             else
@@ -496,10 +610,12 @@ hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blo
         };
         auto sized = [&](auto dim) {
             constexpr int D = decltype(dim)::value;
+            if (key_waves == 4 && query_blocks == 2) return go(attn_mx4_kernel<D, 2, 4, N>);
+            if (key_waves != 8) return hipErrorInvalidValue;
             switch (query_blocks) {
-                case 1: return go(attn_mx4_kernel<D, 1, N>);
-                case 2: return go(attn_mx4_kernel<D, 2, N>);
-                case 3: return go(attn_mx4_kernel<D, 3, N>);
+                case 1: return go(attn_mx4_kernel<D, 1, 8, N>);
+                case 2: return go(attn_mx4_kernel<D, 2, 8, N>);
+                case 3: return go(attn_mx4_kernel<D, 3, 8, N>);
                 default: return hipErrorInvalidValue;
             }
         };

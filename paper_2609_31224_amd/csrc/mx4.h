@@ -80,8 +80,9 @@ using ReadBatch = ReadBatchT<kMaxDesc>;
 
 // Launchers (attn_mx4.hip, mx4_rows.hip).  Each issues one kernel unless it says otherwise.
 // MFMA attention (chunk and decode, D 64 or 128; the step's rows already stored), query_blocks
-// (1 to 3) blocks of 16 query rows per workgroup.  Split partials as launch_attn_tile's.
-hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, const void* q, void* o,
+// (1 to 3) blocks of 16 query rows and key_waves (8; 4 with two blocks) waves per workgroup.
+// Split partials as launch_attn_tile's.
+hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, int key_waves, const void* q, void* o,
                            hipStream_t stream, const KTimer& kt);
 // Encodes and stores a step's rows (launch_append of other caches).
 hipError_t launch_append_mx4(const DevState& st, const AppendBatch& b, int n_layers, const void* k, const void* v,

@@ -236,3 +236,14 @@ def test_query_that_is_not_finite(gpu, d):
     bad = np.zeros((rows, 4), bool)
     bad[7, 1] = bad[8, 3] = True
     assert np.isnan(outs[1][bad]).all() and np.array_equal(outs[0][~bad], outs[1][~bad])
+
+
+@pytest.mark.parametrize("d,hq,hkv,rows,prefix", [(64, 8, 1, 23, 40), (128, 4, 2, 37, 70), (128, 16, 4, 9, 500), (64, 2, 2, 65, 0)])
+def test_small_workgroups(gpu, monkeypatch, d, hq, hkv, rows, prefix):
+    """Workgroups of four waves (launches with more than two of them per CU: here one CU is
+    counted), whole and with forced splits."""
+    monkeypatch.setenv("A2T_TARGET_WGS", "1")
+    for splits in ("0", "3"):
+        monkeypatch.setenv("A2T_SPLITS", splits)
+        spec = tiny_stream([SMALL, _unit(rows), [SEG_RESPONSE], _unit(rows + 2), SMALL], prefix=prefix)
+        _run([spec], hq, hkv, d, budgets=[prefix + rows], calls="fused", unit_rows=2 * rows + 60 + prefix)
