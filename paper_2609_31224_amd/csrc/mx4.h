@@ -72,7 +72,7 @@ struct ReadBatchT {
     int32_t count;
     int32_t layer0;       // first layer read
     int32_t max_R;
-    int32_t pad_;
+    int32_t rows;         // rows of a workgroup (set by the launcher)
     int64_t total_rows;   // rows per layer in the packed output
     ReadDesc d[N];
 };

@@ -16,6 +16,7 @@ namespace a2t {
 namespace {
 
 constexpr int kRowThreads = 256;
+constexpr int64_t kFullThreads = 256 * 1024;   // threads that fill the CUs
 
 __device__ __forceinline__ void unpack8(const u32x4& r, float (&x)[8]) {
 #pragma unroll
@@ -41,53 +42,66 @@ __device__ __forceinline__ uint32_t encode8(const float (&x)[8], int* scale) {
     return *scale == kMxNaN ? 0u : c;
 }
 
-// One thread per (row, KV head, 8 dims of the lower half and their rotate-half partners of
-// the upper one), K and V: every element is loaded once, and four lanes hold a block.
+// One thread per (row, 8 dims of the lower half and their rotate-half partners of the upper one,
+// `heads` KV heads one after the other), K and V: every element is loaded once, four lanes
+// hold a block, and the next head's loads are in flight while one is encoded.
 //
 // The rotation is computed in 64 bits (products of a bf16 and an fp32 number are exact there)
 // and rounded to fp32 once, so that what a key is encoded as follows from the inputs and the
 // rotary table alone: two fp32 roundings would put one key in ~10^7 on the other side of a
 // border between two codes, depending on the compiler's choice of fused operations.
 template <class BT>
-__global__ __launch_bounds__(kRowThreads) void append_mx4_kernel(DevState st, BT b, const uint16_t* k, const uint16_t* v) {
+__global__ __launch_bounds__(kRowThreads) void append_mx4_kernel(DevState st, BT b, const uint16_t* k, const uint16_t* v,
+                                                                 int heads) {
     const AppendDesc d = b.d[blockIdx.y];
-    const int D = st.D, half = D / 2, tph = D / 16, tpr = st.Hkv * tph;
-    const int x = blockIdx.x * kRowThreads + threadIdx.x;
-    const int r = x / tpr;
-    if (r >= d.n) return;   // whole groups of four lanes: tpr is a multiple of 4
-    const int c = x - r * tpr, g = c / tph, d0 = (c - g * tph) * 8;
+    const uint32_t D = st.D, half = D / 2, tph = D / 16, groups = ((uint32_t)st.Hkv + heads - 1) / heads;
+    const uint32_t x = blockIdx.x * kRowThreads + threadIdx.x;
+    const uint32_t y = x / tph, r = y / groups;
+    if (r >= (uint32_t)d.n) return;   // whole groups of four lanes: tph is a multiple of 4
+    const uint32_t d0 = (x - y * tph) * 8, g0 = (y - r * groups) * heads, g1 = min(g0 + heads, (uint32_t)st.Hkv);
     int slot = d.slot0 + r;
     if (slot >= st.unit_rows) slot -= st.unit_rows;
-    const int64_t in = (((int64_t)blockIdx.z * b.total_rows + d.in_row0 + r) * st.Hkv + g) * D + d0;
-    const u32x4 klo = *reinterpret_cast<const u32x4*>(k + in), khi = *reinterpret_cast<const u32x4*>(k + in + half);
-    const u32x4 vlo = *reinterpret_cast<const u32x4*>(v + in), vhi = *reinterpret_cast<const u32x4*>(v + in + half);
+    const int64_t in = (((int64_t)blockIdx.z * b.total_rows + d.in_row0 + r) * st.Hkv + g0) * D + d0;
+    const uint16_t *pk = k + in, *pv = v + in;
     const float4* cs4 = reinterpret_cast<const float4*>(st.rope + ((int64_t)d.s * st.max_step_rows + r) * half + d0);
+    u32x4 raw[4];
+    auto load = [&] {
+        raw[0] = *reinterpret_cast<const u32x4*>(pk);
+        raw[1] = *reinterpret_cast<const u32x4*>(pk + half);
+        raw[2] = *reinterpret_cast<const u32x4*>(pv);
+        raw[3] = *reinterpret_cast<const u32x4*>(pv + half);
+    };
+    load();
     float4 cs[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e) cs[e] = cs4[e];
-    float lo[8], hi[8], ylo[8], yhi[8];
-    unpack8(klo, lo);
-    unpack8(khi, hi);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const double co = e & 1 ? cs[e / 2].z : cs[e / 2].x, si = e & 1 ? cs[e / 2].w : cs[e / 2].y;
-        ylo[e] = (float)((double)lo[e] * co - (double)hi[e] * si);
-        yhi[e] = (float)((double)hi[e] * co + (double)lo[e] * si);
-    }
-    const int64_t row = mx4_ring_row(st, b.layer0 + blockIdx.z, d.s, g) + slot;
-    auto store = [&](const Mx4Pool& p, const float(&y)[8], int at) {
-        int scale;
-        const uint32_t code = encode8(y, &scale);
-        *reinterpret_cast<uint32_t*>(p.codes + row * half + at / 2) = code;
-        if (at % kMxBlock == 0) p.scales[row * (D / kMxBlock) + at / kMxBlock] = (uint8_t)scale;
-    };
     const Mx4Pool kp = mx4_pool(st, st.k_unit), vp = mx4_pool(st, st.v_unit);
-    store(kp, ylo, d0);
-    store(kp, yhi, d0 + half);
-    unpack8(vlo, lo);
-    unpack8(vhi, hi);
-    store(vp, lo, d0);
-    store(vp, hi, d0 + half);
+    int64_t row = mx4_ring_row(st, b.layer0 + blockIdx.z, d.s, g0) + slot;
+    for (uint32_t g = g0; g < g1; ++g, row += st.unit_rows) {
+        const u32x4 klo = raw[0], khi = raw[1], vlo = raw[2], vhi = raw[3];
+        if (g + 1 < g1) pk += D, pv += D, load();
+        auto store = [&](const Mx4Pool& p, const float(&y)[8], uint32_t at) {
+            int scale;
+            const uint32_t code = encode8(y, &scale);
+            *reinterpret_cast<uint32_t*>(p.codes + row * half + at / 2) = code;
+            if (at % kMxBlock == 0) p.scales[row * (D / kMxBlock) + at / kMxBlock] = (uint8_t)scale;
+        };
+        float lo[8], hi[8], ylo[8], yhi[8];
+        unpack8(klo, lo);
+        unpack8(khi, hi);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const double co = e & 1 ? cs[e / 2].z : cs[e / 2].x, si = e & 1 ? cs[e / 2].w : cs[e / 2].y;
+            ylo[e] = (float)((double)lo[e] * co - (double)hi[e] * si);
+            yhi[e] = (float)((double)hi[e] * co + (double)lo[e] * si);
+        }
+        store(kp, ylo, d0);
+        store(kp, yhi, d0 + half);
+        unpack8(vlo, lo);
+        unpack8(vhi, hi);
+        store(vp, lo, d0);
+        store(vp, hi, d0 + half);
+    }
 }
 
 // grid (rows, stream, layer): a wave takes every fourth row of the span that eviction has
@@ -116,53 +130,76 @@ __global__ __launch_bounds__(kRowThreads) void move_mx4_kernel(DevState st, BT b
     }
 }
 
-// grid (rows, stream, layer x {K, V}): one thread per 16 bytes of output.
+// grid (rows / b.rows, stream, layer x {K, V}): a workgroup writes b.rows consecutive rows, a
+// thread 16 bytes of every kRowThreads-th chunk of them, four loads ahead of their stores.
 template <int DTYPE, class BT>
 __global__ __launch_bounds__(kRowThreads) void read_rows_kernel(DevState st, BT b, char* k, char* v) {
-    constexpr int EPT = DTYPE == A2T_F32 ? 4 : 8;   // elements of a thread
+    constexpr int EPT = DTYPE == A2T_F32 ? 4 : 8, EB = 16 / EPT;   // elements of a chunk, bytes of one
+    constexpr int U = 4;
     const ReadDesc d = b.d[blockIdx.y];
-    const int D = st.D, cph = D / EPT, cpr = st.Hkv * cph;
-    const int64_t x = (int64_t)blockIdx.x * kRowThreads + threadIdx.x;
-    const int j = (int)(x / cpr);
-    if (j >= d.R) return;
-    const int c = (int)(x - (int64_t)j * cpr), g = c / cph, d0 = (c - g * cph) * EPT;
     const bool is_v = blockIdx.z & 1;
-    const int z = blockIdx.z >> 1, layer = b.layer0 + z;
     char* const out = is_v ? v : k;
-    if (!out) return;
-    const bool in_kept = j < d.kept;
-    int at = in_kept ? j : d.head + (j - d.kept);
-    if (!in_kept && at >= st.unit_rows) at -= st.unit_rows;
-    u32x4 r;
-    if constexpr (DTYPE == A2T_MX4) {
-        const Mx4Pool p = mx4_pool(st, is_v ? st.v_unit : st.k_unit);
-        const int64_t row = (in_kept ? mx4_kept_row(st, layer, d.s, g) : mx4_ring_row(st, layer, d.s, g)) + at;
-        const uint32_t code = *reinterpret_cast<const uint32_t*>(p.codes + row * (D / 2) + d0 / 2);
-        const uint32_t byte = p.scales[row * (D / kMxBlock) + d0 / kMxBlock];
-        r = mx4_to_bf16(code, __uint_as_float(byte << 23));
-        if (byte == kMxNaN) r = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};   // one NaN, as on the host
-    } else {
-        const void* pool = is_v ? (in_kept ? st.v_kept : st.v_unit) : (in_kept ? st.k_kept : st.k_unit);
-        const int64_t e = pool_index(st, layer, d.s, g, in_kept ? st.kept_rows : st.unit_rows, at) + d0;
-        r = *reinterpret_cast<const u32x4*>(static_cast<const char*>(pool) + e * (16 / EPT));
+    const int j0 = blockIdx.x * b.rows, rows = min(b.rows, d.R - j0);
+    if (rows <= 0 || !out) return;
+    const uint32_t D = st.D, cph = D / EPT, cpr = st.Hkv * cph;
+    const int z = blockIdx.z >> 1, layer = b.layer0 + z;
+    const uint32_t dr = kRowThreads / cpr, dc = kRowThreads - dr * cpr;   // from a thread's chunk to its next
+    uint32_t r = threadIdx.x / cpr, c = threadIdx.x - r * cpr;
+    char* const to = out + ((int64_t)z * b.total_rows + d.row0 + j0) * cpr * 16;
+    const Mx4Pool p = mx4_pool(st, is_v ? st.v_unit : st.k_unit);
+    const void* const pool_ring = is_v ? st.v_unit : st.k_unit;
+    const void* const pool_kept = is_v ? st.v_kept : st.k_kept;
+    while (r < (uint32_t)rows) {
+        u32x4 x[U];
+        uint32_t code[U], byte[U], at_r[U], at_c[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            at_r[u] = r, at_c[u] = c;
+            const int j = j0 + (int)min(r, (uint32_t)rows - 1);
+            const uint32_t g = c / cph, d0 = (c - g * cph) * EPT;
+            const bool in_kept = j < d.kept;
+            int at = in_kept ? j : d.head + (j - d.kept);
+            if (!in_kept && at >= st.unit_rows) at -= st.unit_rows;
+            if constexpr (DTYPE == A2T_MX4) {
+                const int64_t row = (in_kept ? mx4_kept_row(st, layer, d.s, g) : mx4_ring_row(st, layer, d.s, g)) + at;
+                code[u] = *reinterpret_cast<const uint32_t*>(p.codes + row * (D / 2) + d0 / 2);
+                byte[u] = p.scales[row * (D / kMxBlock) + d0 / kMxBlock];
+            } else {
+                const int64_t e = pool_index(st, layer, d.s, g, in_kept ? st.kept_rows : st.unit_rows, at) + d0;
+                x[u] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(in_kept ? pool_kept : pool_ring) + e * EB);
+            }
+            r += dr, c += dc;
+            if (c >= cpr) c -= cpr, ++r;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if constexpr (DTYPE == A2T_MX4) {
+                x[u] = mx4_to_bf16(code[u], __uint_as_float(byte[u] << 23));
+                if (byte[u] == kMxNaN) x[u] = u32x4{0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u, 0x7fc07fc0u};   // one NaN, as on the host
+            }
+            if (at_r[u] < (uint32_t)rows)
+                __builtin_nontemporal_store(x[u], reinterpret_cast<u32x4*>(to + ((uint64_t)at_r[u] * cpr + at_c[u]) * 16));
+        }
     }
-    const int64_t o = (((int64_t)z * b.total_rows + d.row0 + j) * st.Hkv + g) * D + d0;
-    *reinterpret_cast<u32x4*>(out + o * (16 / EPT)) = r;
 }
 
 }  // namespace
 
 hipError_t launch_append_mx4(const DevState& st, const AppendBatch& b, int n_layers, const void* k, const void* v,
                              hipStream_t stream, const KTimer& kt) {
-    const int tpr = st.Hkv * st.D / 16;
-    const dim3 grid((b.max_n * tpr + kRowThreads - 1) / kRowThreads, b.count, n_layers);
+    // heads of a thread: more while the threads still fill the CUs
+    const int64_t threads = (int64_t)b.max_n * b.count * n_layers * st.Hkv * (st.D / 16);
+    int heads = 1;
+    while (heads < st.Hkv && threads / (2 * heads) >= kFullThreads) heads *= 2;
+    const int64_t per_stream = (int64_t)b.max_n * ((st.Hkv + heads - 1) / heads) * (st.D / 16);
+    const dim3 grid((uint32_t)((per_stream + kRowThreads - 1) / kRowThreads), b.count, n_layers);
     const uint16_t *kk = static_cast<const uint16_t*>(k), *vv = static_cast<const uint16_t*>(v);
     return by_size<AppendBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         if (kt.start)
-            hipExtLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb, kk, vv);
+            hipExtLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb, kk, vv, heads);
         else
-            hipLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, st, bb, kk, vv);
+            hipLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, st, bb, kk, vv, heads);
         return hipGetLastError();
     });
 }
@@ -184,9 +221,12 @@ hipError_t launch_move_mx4(const DevState& st, const EvictBatch& b, hipStream_t 
 hipError_t launch_read_rows(const DevState& st, const ReadBatch& b, int n_layers, void* k, void* v, hipStream_t stream,
                             const KTimer& kt) {
     const int cpr = st.Hkv * st.D / (st.dtype == A2T_F32 ? 4 : 8);
-    const dim3 grid((uint32_t)(((int64_t)b.max_R * cpr + kRowThreads - 1) / kRowThreads), b.count, 2 * n_layers);
+    ReadBatch rb = b;
+    // rows of a workgroup: eight chunks a thread, a row at least
+    rb.rows = cpr > kRowThreads * 8 ? 1 : kRowThreads * 8 / cpr;
+    const dim3 grid((b.max_R + rb.rows - 1) / rb.rows, b.count, 2 * n_layers);
     char *kk = static_cast<char*>(k), *vv = static_cast<char*>(v);
-    return by_size<ReadBatchT>(b, [&](const auto& bb) {
+    return by_size<ReadBatchT>(rb, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         auto go = [&](auto kernel) {
             if (kt.start)
