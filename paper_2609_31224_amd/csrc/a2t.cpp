@@ -1549,7 +1549,6 @@ int a2t_read_rows(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t*
     for (int i0 = 0; i0 < n_streams; i0 += kMaxDesc) {
         const int n = std::min(kMaxDesc, n_streams - i0);
         ReadBatch rb{};
-        rb.layer0 = layer == A2T_ALL_LAYERS ? 0 : layer;
         rb.total_rows = total;
         for (int i = 0; i < n; ++i) {
             const StreamState& s = c->ss[ids[i0 + i]];
@@ -1559,12 +1558,15 @@ int a2t_read_rows(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t*
             row0 += s.resident();
         }
         if (rb.count == 0) continue;
-        hipError_t e;
-        {
+        constexpr int kMostLayers = 16384;   // of a launch (its grid has a plane for K and V of each)
+        for (int l0 = 0; l0 < n_layers; l0 += kMostLayers) {
+            const size_t at = (size_t)l0 * total * k.n_kv_heads * k.head_dim * (k.dtype == A2T_F32 ? 4 : 2);
             ProfScope ps(c, "read_rows");
-            e = launch_read_rows(c->dev, rb, n_layers, kout, vout, c->stream, ps.kt());
+            rb.layer0 = layer == A2T_ALL_LAYERS ? l0 : layer;
+            if (launch_read_rows(c->dev, rb, std::min(kMostLayers, n_layers - l0), kout ? static_cast<char*>(kout) + at : nullptr,
+                                 vout ? static_cast<char*>(vout) + at : nullptr, c->stream, ps.kt()) != hipSuccess)
+                return hip_fail(c);
         }
-        if (e != hipSuccess) return hip_fail(c);
     }
     return A2T_OK;
 }

@@ -27,7 +27,7 @@ namespace {
 
 constexpr int kKeyBlock = 32;    // keys of a wave's block
 constexpr int kRows = 16;        // query rows of a product
-constexpr int kAhead = 3;        // V operands read ahead of the products
+constexpr int kAhead = 4;        // V operands read ahead of the products
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));

@@ -104,16 +104,16 @@ __global__ __launch_bounds__(kRowThreads) void append_mx4_kernel(DevState st, BT
     }
 }
 
-// grid (rows, stream, layer): a wave takes every fourth row of the span that eviction has
+// grid (layer, stream, rows): a wave takes every fourth row of the span that eviction has
 // passed over and copies it, where it is kept, to the slot that the eviction's index pass found for
 // it.  A chunk is a block's 16 bytes of codes, and its scale byte goes with it.
 template <class BT>
 __global__ __launch_bounds__(kRowThreads) void move_mx4_kernel(DevState st, BT b) {
     const EvictDesc d = b.d[blockIdx.y];
-    const int lane = threadIdx.x & 63, nb = st.D / kMxBlock, chunks = 2 * st.Hkv * nb, layer = blockIdx.z;
+    const int lane = threadIdx.x & 63, nb = st.D / kMxBlock, chunks = 2 * st.Hkv * nb, layer = blockIdx.x;
     const int64_t eb = (int64_t)d.s * ((int64_t)st.unit_rows + st.kept_rows);
     const Mx4Pool kp = mx4_pool(st, st.k_unit), vp = mx4_pool(st, st.v_unit);
-    for (int x = blockIdx.x * (kRowThreads / 64) + (threadIdx.x >> 6); x < d.span; x += gridDim.x * (kRowThreads / 64)) {
+    for (int x = blockIdx.z * (kRowThreads / 64) + (threadIdx.x >> 6); x < d.span; x += gridDim.z * (kRowThreads / 64)) {
         const int to = st.ev_slot[eb + d.kept + x];
         if (to < 0) continue;
         int from = d.head + x;
@@ -207,7 +207,7 @@ hipError_t launch_append_mx4(const DevState& st, const AppendBatch& b, int n_lay
 hipError_t launch_move_mx4(const DevState& st, const EvictBatch& b, hipStream_t stream, const KTimer& kt) {
     int span = 1;
     for (int i = 0; i < b.count; ++i) span = b.d[i].span > span ? b.d[i].span : span;
-    const dim3 grid(span < 256 ? (span + 3) / 4 : 64, b.count, st.L);
+    const dim3 grid(st.L, b.count, span < 256 ? (span + 3) / 4 : 64);
     return by_size<EvictBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         if (kt.start)

@@ -247,3 +247,334 @@ def test_small_workgroups(gpu, monkeypatch, d, hq, hkv, rows, prefix):
         monkeypatch.setenv("A2T_SPLITS", splits)
         spec = tiny_stream([SMALL, _unit(rows), [SEG_RESPONSE], _unit(rows + 2), SMALL], prefix=prefix)
         _run([spec], hq, hkv, d, budgets=[prefix + rows], calls="fused", unit_rows=2 * rows + 60 + prefix)
+
+
+# ------------------------------------------------------------------ the calls around them
+def _fill(a2t, c, ids, n, k, v, start=0, unit=0, layer=None):
+    seg = np.full(int(np.sum(n)), SEG_ACOUSTIC, np.uint8)
+    pos = np.concatenate([np.arange(start, start + m) for m in n])
+    a2t.a2t_append(c, a2t.A2T_ALL_LAYERS if layer is None else layer, ids, n, k, v, seg, pos, [unit] * len(ids))
+
+
+def _randn(*shape, seed=0, dtype=None):
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    return torch.randn(shape, generator=g, device="cuda").to(dtype or torch.bfloat16)
+
+
+def test_device_refusals(gpu):
+    """What a device cache refuses changes nothing."""
+    import paper_2609_31224_amd as a2t
+    c = a2t.a2t_cache_create(2, 2, 4, 2, 64, a2t.A2T_MX4, 64, 8, 16)
+    k, v, q = _randn(3, 2, 64), _randn(3, 2, 64), _randn(3, 4, 64)
+
+    def status(fn, *a):
+        try:
+            fn(*a)
+            return 0
+        except a2t.A2TError as e:
+            return e.status
+    assert status(a2t.a2t_dev_begin, c) == a2t.A2T_ERR_INVALID
+    meta = (np.full(3, SEG_ACOUSTIC, np.uint8), np.arange(3), [0])
+    a2t.a2t_append(c, 0, [1], [3], k, v, *meta)
+    before = [a2t.a2t_stream_info_get(c, s) for s in range(2)]
+    o = _randn(3, 4, 64, seed=5)
+    was = o.clone()
+    assert status(a2t.a2t_chunk_attn, c, 1, [1], [3], q, o) == a2t.A2T_ERR_STATE       # layer not appended
+    assert status(a2t.a2t_chunk_attn, c, 0, [0], [1], q, o) == a2t.A2T_ERR_STATE       # no open step
+    assert status(a2t.a2t_chunk_attn, c, 0, [1], [4], q, o) == a2t.A2T_ERR_STATE       # more queries than rows
+    assert status(a2t.a2t_decode_attn, c, 0, [1, 1], q, o) == a2t.A2T_ERR_INVALID
+    assert status(a2t.a2t_chunk_attn, c, 0, [1], [3], q.data_ptr() + 2, o.data_ptr()) == a2t.A2T_ERR_INVALID
+    assert status(a2t.a2t_append, c, 1, [1], [3], k.data_ptr() + 8, v.data_ptr(), None, None, None) == a2t.A2T_ERR_INVALID
+    assert status(a2t.a2t_read_rows, c, 1, [1], k, v) == a2t.A2T_ERR_STATE
+    assert status(a2t.a2t_read_rows, c, 0, [1], None, None) == a2t.A2T_ERR_INVALID
+    assert status(a2t.a2t_evict, c, [1], [0], 0) == a2t.A2T_ERR_STATE
+    with pytest.raises(ValueError):
+        a2t.a2t_read_rows(c, 0, [1], k.float(), None)      # bfloat16 in and out
+    with pytest.raises(ValueError):
+        a2t.a2t_chunk_attn(c, 0, [1], [3], q.float(), o.float())
+    a2t.a2t_sync(c)
+    assert [a2t.a2t_stream_info_get(c, s) for s in range(2)] == before
+    assert (o == was).all()
+    a2t.a2t_cache_destroy(c)
+
+
+@pytest.mark.parametrize("dtype", ["mx4", "bf16", "f32"])
+@pytest.mark.parametrize("hkv,d", [(3, 64), (2, 128), (40, 128)])
+def test_read_rows(gpu, dtype, hkv, d):
+    """Rows in cache order of streams with a kept region, a wrapped ring, one row and none, for every cache type: what
+    a2t_read_kv reads, no more rows than those, either output alone, one layer or all."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    t = torch.float32 if dtype == "f32" else torch.bfloat16
+    L, S = 2, 4
+    c = a2t.a2t_cache_create(L, S, hkv, hkv, d, {"mx4": a2t.A2T_MX4, "bf16": a2t.A2T_BF16, "f32": a2t.A2T_F32}[dtype], 70, 60, 40)
+    pos = 0
+    for unit in range(6):      # streams 0 and 1: some rows kept, the ring has wrapped
+        n = [17, 12]
+        seg = np.where(np.arange(29) % 3 == 0, SEG_TEXT, SEG_ACOUSTIC).astype(np.uint8)
+        a2t.a2t_append(c, a2t.A2T_ALL_LAYERS, [0, 1], n, _randn(L, 29, hkv, d, seed=unit, dtype=t), _randn(L, 29, hkv, d, seed=50 + unit, dtype=t),
+                       seg, np.concatenate([np.arange(pos, pos + 17), np.arange(pos, pos + 12)]), [unit, unit])
+        a2t.a2t_evict(c, [0, 1], [30, 35], 1)
+        pos += 17
+    _fill(a2t, c, [2], [1], _randn(L, 1, hkv, d, seed=9, dtype=t), _randn(L, 1, hkv, d, seed=10, dtype=t))
+    info = [a2t.a2t_stream_info_get(c, s) for s in range(S)]
+    assert info[0]["kept"] and info[1]["kept"] and info[0]["ring_head"] and info[3]["resident"] == 0
+    assert info[0]["ring_head"] + info[0]["ring"] > 70 or info[1]["ring_head"] + info[1]["ring"] > 70
+    ids = [1, 3, 2, 0]
+    rows = [info[s]["resident"] for s in ids]
+    total = sum(rows)
+    want = [[np.concatenate([a2t.a2t_read_kv(c, layer, s)[w] for s in ids]) for layer in range(L)] for w in range(2)]
+    mark = 7.0
+
+    def call(layer, which):
+        shape = (L, total, hkv, d) if layer == a2t.A2T_ALL_LAYERS else (total, hkv, d)
+        size = int(np.prod(shape))
+        out = [torch.full((size + 64,), mark, dtype=t, device="cuda") for _ in range(2)]
+        a2t.a2t_read_rows(c, layer, ids, *[x[:size] if w in which else None for w, x in enumerate(out)])
+        a2t.a2t_sync(c)
+        for w, x in enumerate(out):
+            x, behind = x[:size].view(shape), x[size:]
+            assert (behind == mark).all()
+            if w not in which:
+                assert (x == mark).all()
+                continue
+            got = x.cpu().numpy() if dtype == "f32" else x.view(torch.int16).cpu().numpy().view(np.uint16)
+            for i, l in enumerate(range(L) if layer == a2t.A2T_ALL_LAYERS else [layer]):
+                assert np.array_equal(got[i] if layer == a2t.A2T_ALL_LAYERS else got, want[w][l]), (layer, w, l)
+    for layer in (a2t.A2T_ALL_LAYERS, 0, 1):
+        for which in ((0, 1), (0,), (1,)):
+            call(layer, which)
+    a2t.a2t_read_rows(c, 0, [3], _randn(1, hkv, d, dtype=t), None)      # no rows at all
+    a2t.a2t_sync(c)
+    a2t.a2t_cache_destroy(c)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_callers_pools(gpu, d):
+    """Pools of the documented size, with what is in them before: rows come out the same, nothing is
+    written behind them, and the codes and scales are where the header says."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    L, S, hkv, unit_rows, kept_rows, n = 2, 3, 2, 20, 6, 9
+    rows = L * S * hkv * (unit_rows + kept_rows)
+    size = rows * (d // 2 + d // 32)
+    pools = [torch.full((size + 256,), 0xa5, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    assert all(p.data_ptr() % 256 == 0 for p in pools)
+    c = a2t.a2t_cache_create(L, S, hkv, hkv, d, a2t.A2T_MX4, unit_rows, kept_rows, n, k_pool=pools[0], v_pool=pools[1])
+    k, v = _randn(L, 2 * n, hkv, d, seed=1), _randn(L, 2 * n, hkv, d, seed=2)
+    _fill(a2t, c, [0, 2], [n, n], k, v)
+    a2t.a2t_sync(c)
+    for p in pools:
+        assert (p[size:] == 0xa5).all()
+    codes = pools[1][:rows * d // 2].cpu().numpy()[:L * S * hkv * unit_rows * d // 2].reshape(L, S, hkv, unit_rows, d // 2)
+    scales = pools[1][rows * d // 2:size].cpu().numpy()[:L * S * hkv * unit_rows * d // 32].reshape(L, S, hkv, unit_rows, d // 32)
+    assert (codes[:, 1] == 0xa5).all() and (codes[:, :, :, n:] == 0xa5).all() and (scales[:, :, :, n:] == 0xa5).all()
+    codes, scales = codes[:, [0, 2], :, :n], scales[:, [0, 2], :, :n]
+    nib = np.stack([codes & 15, codes >> 4], -1).reshape(L, 2, hkv, n, d)
+    val = mx4.LEVELS[nib & 7] * np.where(nib & 8, -1, 1) * np.repeat(2.0 ** (scales.astype(int) - 127), 32, -1)
+    want = mx4.hold(v.float().cpu().numpy()).reshape(L, 2, n, hkv, d).transpose(0, 1, 3, 2, 4)
+    assert np.array_equal(val, want)
+    a2t.a2t_cache_destroy(c)
+
+
+@pytest.mark.parametrize("hq,hkv,d,rows", [(32, 8, 128, 22), (4, 1, 64, 1), (8, 2, 128, 40)])
+def test_no_allocation_calls(gpu, hq, hkv, d, rows):
+    """a2t_append_attn_noalloc on a cache without a workspace against a2t_append_attn: the same rows, outputs
+    within the rounding of the partials (fp16: half a step of 2^-11 of values below 6 each, twice over) and of
+    the output."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    mk = lambda flags: a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, 4100 + rows, 0, 1024, flags=flags)  # noqa: E731
+    ca, cb = mk(0), mk(a2t.A2T_FLAG_NO_WORKSPACE)
+    for i in range(4):
+        k, v = _randn(1, 1000, hkv, d, seed=i), _randn(1, 1000, hkv, d, seed=20 + i)
+        for c in (ca, cb):
+            _fill(a2t, c, [0], [1000], k, v, start=1000 * i, unit=i)
+    k, v, q = _randn(rows, hkv, d, seed=7), _randn(rows, hkv, d, seed=8), _randn(rows, hq, d, seed=9)
+    seg, pos = np.full(rows, SEG_ACOUSTIC, np.uint8), np.arange(4000, 4000 + rows)
+    oa, ob = torch.zeros_like(q), torch.zeros_like(q)
+    a2t.a2t_append_attn(ca, 0, [0], [rows], k, v, seg, pos, [9], [rows], q, oa)
+    a2t.a2t_append_attn_noalloc(cb, 0, [0], [rows], k, v, seg, pos, [9], [rows], q, ob)
+    a2t.a2t_sync(ca)
+    a2t.a2t_sync(cb)
+    assert (oa.float() - ob.float()).abs().max() <= 2 * 6 * 2.0 ** -11 + 2 * 2.0 ** -8 * oa.float().abs().max()
+    for x, y in zip(a2t.a2t_read_kv(ca, 0, 0), a2t.a2t_read_kv(cb, 0, 0)):
+        assert np.array_equal(x, y)
+    for c in (ca, cb):
+        a2t.a2t_cache_destroy(c)
+
+
+def test_other_streams(gpu):
+    """A cache on a stream of its own, moved to another one, with the default stream busy."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    spec = tiny_stream([SMALL, _unit(20), [SEG_RESPONSE], _unit(33)], prefix=100)
+    busy = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    s = Sessions([spec], 8, 2, 128, budgets=[60], calls="fused", stream=side)
+    try:
+        for t, st in enumerate(spec.steps):
+            for _ in range(4):
+                busy = busy @ busy * 1e-3
+            torch.cuda.synchronize()      # the test's own uploads are on the default stream
+            a2t.a2t_sync(s.cache)
+            a2t.a2t_set_stream(s.cache, other if t % 2 else side)
+            s._dev = lambda x, up=s.__class__._dev: (up(s, x), torch.cuda.current_stream().synchronize())[0]
+            s.step([(0, st)], t)
+    finally:
+        s.close()
+
+
+@pytest.mark.parametrize("streams,resident,rows,hq,hkv,d", [(1, 3000, 1, 32, 8, 128), (3, 500, 22, 8, 2, 64), (2, 0, 130, 8, 1, 128)])
+def test_captured_calls(gpu, streams, resident, rows, hq, hkv, d):
+    """Attention and a2t_read_rows of an open step captured in a graph: every replay, with eager calls, a changed query
+    and synchronisations between, gives the eager result."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    side = torch.cuda.Stream()
+    c = a2t.a2t_cache_create(1, streams, hq, hkv, d, a2t.A2T_MX4, resident + rows, 0, 1024, stream=side)
+    at = 0
+    while at < resident:
+        n = min(1024, resident - at)
+        k, v = _randn(1, n * streams, hkv, d, seed=at), _randn(1, n * streams, hkv, d, seed=at + 1)
+        torch.cuda.synchronize()
+        _fill(a2t, c, range(streams), [n] * streams, k, v, start=at, unit=at)
+        at += n
+    k, v = _randn(1, rows * streams, hkv, d, seed=91), _randn(1, rows * streams, hkv, d, seed=92)
+    torch.cuda.synchronize()
+    _fill(a2t, c, range(streams), [rows] * streams, k, v, start=resident, unit=resident + 1)
+    q = _randn(rows * streams, hq, d, seed=93)
+    o = torch.zeros_like(q)
+    back = torch.zeros((streams * (resident + rows), hkv, d), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+
+    def calls():
+        if rows == 1:
+            a2t.a2t_decode_attn(c, 0, range(streams), q, o)
+        else:
+            a2t.a2t_chunk_attn(c, 0, range(streams), [rows] * streams, q, o)
+        a2t.a2t_read_rows(c, 0, range(streams), None, back)
+    calls()
+    a2t.a2t_sync(c)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls()
+    for i in range(5):
+        q.copy_(_randn(rows * streams, hq, d, seed=200 + i))
+        o.fill_(3.0)
+        back.fill_(3.0)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.clone(), back.clone()
+        o.fill_(4.0)
+        back.fill_(4.0)
+        torch.cuda.synchronize()
+        calls()
+        a2t.a2t_sync(c)
+        assert torch.equal(got[0], o) and torch.equal(got[1], back), i
+        assert torch.isfinite(o.float()).all()
+    a2t.a2t_cache_destroy(c)
+
+
+def test_results_do_not_vary(gpu):
+    """The same call twice gives the same bits, whatever ran before it."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    c = a2t.a2t_cache_create(1, 3, 32, 8, 128, a2t.A2T_MX4, 3000, 0, 1024)
+    for i in range(2):
+        _fill(a2t, c, [0, 1, 2], [1000, 700, 13], _randn(1, 1713, 8, 128, seed=i), _randn(1, 1713, 8, 128, seed=5 + i), start=1000 * i, unit=i)
+    q = _randn(1713, 32, 128, seed=3)
+    first = None
+    for _ in range(3):
+        o = torch.zeros_like(q)
+        a2t.a2t_chunk_attn(c, 0, [0, 1, 2], [1000, 700, 13], q, o)
+        d = torch.zeros((3, 32, 128), dtype=q.dtype, device="cuda")
+        a2t.a2t_decode_attn(c, 0, [2, 0, 1], q[:3].contiguous(), d)
+        a2t.a2t_sync(c)
+        first = first or (o, d)
+        assert torch.equal(first[0], o) and torch.equal(first[1], d)
+    a2t.a2t_cache_destroy(c)
+
+
+@pytest.mark.parametrize("kept", [False, True])
+def test_offsets_past_32_bits(gpu, kept):
+    """Rows of the last head of a pool whose codes pass 4 GiB, in the ring or in the kept region: written, moved, read
+    and attended where they belong."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    hq, hkv, d, unit_rows, kept_rows = 2, 1, 128, 1 << 20, 1 << 16
+    S = 66      # 66 x 1,114,112 rows of 64 bytes: 4.7 GB of codes a pool
+    c = a2t.a2t_cache_create(1, S, hq, hkv, d, a2t.A2T_MX4, unit_rows, kept_rows, 300)
+    n, s = 300, S - 1
+    k, v, q = _randn(1, n, hkv, d, seed=1), _randn(1, n, hkv, d, seed=2), _randn(1, hq, d, seed=3)
+    seg = np.where(np.arange(n) % 2, SEG_TEXT, SEG_ACOUSTIC).astype(np.uint8)
+    a2t.a2t_append(c, a2t.A2T_ALL_LAYERS, [s], [n], k, v, seg, np.arange(n), [0])
+    live = np.arange(n)
+    if kept:
+        assert a2t.a2t_evict(c, [s], [0], 0)[0][0] == n // 2
+        live = live[seg == SEG_TEXT]
+    k1, v1 = _randn(1, 1, hkv, d, seed=4), _randn(1, 1, hkv, d, seed=5)
+    a2t.a2t_append(c, a2t.A2T_ALL_LAYERS, [s], [1], k1, v1, [SEG_ACOUSTIC], [n], [1])
+    o = torch.zeros_like(q)
+    a2t.a2t_decode_attn(c, 0, [s], q, o)
+    kr, vr = (bf16_bits_to_f32(x) for x in a2t.a2t_read_kv(c, 0, s))
+    back = torch.zeros((len(live) + 1, hkv, d), dtype=torch.bfloat16, device="cuda")
+    a2t.a2t_read_rows(c, 0, [s], None, back)
+    a2t.a2t_sync(c)
+    both = torch.cat([v[0, live], v1[0]]).float().cpu().numpy()
+    assert np.array_equal(vr, mx4.hold(both)) and np.array_equal(back.float().cpu().numpy(), vr)
+    keys = torch.cat([k[0, live], k1[0]]).float().cpu().numpy()
+    pos = np.append(live, n)
+    assert np.array_equal(kr, mx4.hold(mx4.rotate_to_f32(keys, pos, 1e6)))
+    cache = mx4.OracleMx4Cache(hq, hkv, d)
+    cache.append(np.full(len(pos), SEG_ACOUSTIC), pos, 0, {0: keys}, {0: both})
+    want, bound = cache.attention_bound(0, q.float().cpu().numpy(), 1)
+    assert (np.abs(o.float().cpu().numpy() - want) <= bound).all()
+    a2t.a2t_cache_destroy(c)
+
+
+@pytest.mark.parametrize("small", [False, True])
+@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 4, 1), (128, 2, 2)])
+def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv, small):
+    """The same behind several key blocks a wave, with workgroups of eight and of four waves; and values of a resident
+    row, which every query sees."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_SPLITS", "1")
+    if small:
+        monkeypatch.setenv("A2T_TARGET_WGS", "1")
+    old, rows, bad = 900, 70, 33
+    g = torch.Generator(device="cuda").manual_seed(6)
+    k0, v0 = (torch.randn((old, hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
+    k, v, q = (torch.randn((rows, h, d), generator=g, device="cuda").bfloat16() for h in (hkv, hkv, hq))
+
+    def run(new=False, resident=None):
+        vv, vr = v.clone(), v0.clone()
+        if new:
+            vv[bad, :, 37] = float("nan")
+        if resident is not None:
+            vr[resident, 0, 2] = float("-inf")
+        c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, old + rows, 0, old)
+        o = torch.zeros_like(q)
+        a2t.a2t_append(c, 0, [0], [old], k0, vr, np.full(old, SEG_ACOUSTIC, np.uint8), np.arange(old), [0])
+        a2t.a2t_append_attn(c, 0, [0], [rows], k, vv, np.full(rows, SEG_ACOUSTIC, np.uint8), np.arange(old, old + rows), [1],
+                            [rows], q, o)
+        a2t.a2t_sync(c)
+        a2t.a2t_cache_destroy(c)
+        return o.float().cpu().numpy()
+
+    clean = run()
+    assert np.isfinite(clean).all()
+    got = run(new=True)
+    assert np.array_equal(got[:bad], clean[:bad])
+    assert np.isnan(got[bad:, :, 32:64]).all()
+    keep = np.r_[0:32, 64:d]
+    assert np.array_equal(got[bad:][..., keep], clean[bad:][..., keep])
+    for row in (0, 300, 899):      # the first KV head's query heads, 32 dims
+        got = run(resident=row)
+        mine = hq // hkv
+        assert np.isnan(got[:, :mine, :32]).all()
+        assert np.array_equal(got[:, :mine, 32:], clean[:, :mine, 32:]) and np.array_equal(got[:, mine:], clean[:, mine:])
