@@ -483,6 +483,10 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
             const uint32_t flip = i & 1 ? kBuf : 0;
             uint32_t v_in = v_in0 + (kBuf - flip), v_out = v_out0 + flip;
             asm volatile("" : "+v"(ln), "+v"(v_in), "+v"(v_out));
+            // the two waves of a SIMD (w and w + 4) take turns in coming first: with the older one always
+            // first it ended its keys a quarter earlier and left the other one alone
+            if ((i ^ (w >> 2)) & 1) __builtin_amdgcn_s_setprio(2);
+            else __builtin_amdgcn_s_setprio(0);
             wave_lds_order();   // other lanes wrote this block's rows
             read_q(0, ln);
             fence();
@@ -525,6 +529,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
             load_v(kb_next, next, ln);
             settle(kb, false);
         }
+        __builtin_amdgcn_s_setprio(0);
         // the last block
         const uint32_t v_out = v_out0 + (n & 1 ? 0 : kBuf);
         wave_lds_order();
