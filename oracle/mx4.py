@@ -75,13 +75,13 @@ class OracleMx4Cache(OracleCache):
 
     def attention_bound(self, layer, q, n_q):
         """(o, bound): attention as OracleCache.attention's, and what a computation may be off by
-        that holds rotated queries and probabilities to 8 significant bits (an error of up to
-        2^-8 of each, independent from element to element), partial outputs to 11 and the
-        output to 8.
+        that holds rotated queries as two e2m3 numbers (an error of up to 1/128 unit, the largest
+        magnitude of a block of 32 being at least 3.875 units; independent from element to
+        element), probabilities to 8 significant bits, partial outputs to 11 and the output to 8.
 
-        A score's error is a sum of D independent ones, uniform in +- 2^-8 |q_i k_i|: six of its
-        standard deviations are taken as its bound.  An error d_j of the scores moves the
-        output by p_j d_j (v_j - o) to first order."""
+        A score's error is a sum of D independent ones, uniform in +- a_b |k_i| / (128 * 3.875), a_b the
+        largest magnitude of the query's block: six of its standard deviations are taken as its
+        bound.  An error d_j of the scores moves the output by p_j d_j (v_j - o) to first order."""
         q_pos = self.pos[self.resident - n_q:]
         q_rot = rope.rotate(np.asarray(q, np.float64), q_pos, self.theta)
         k, v = self.k[layer], self.v[layer]
@@ -94,7 +94,8 @@ class OracleMx4Cache(OracleCache):
             s = np.where(mask, self.scale * (q_rot[:, h] @ kk.T), -np.inf)
             p = np.exp(s - s.max(1, keepdims=True))
             p /= p.sum(1, keepdims=True)
-            d = 6 * self.scale * 2.0 ** -8 / np.sqrt(3) * np.sqrt(np.square(q_rot[:, h]) @ np.square(kk).T)
+            most = np.repeat(np.abs(q_rot[:, h]).reshape(n_q, -1, BLOCK).max(-1), BLOCK, -1)
+            d = 6 * self.scale / (128 * 3.875 * np.sqrt(3)) * np.sqrt(np.square(most) @ np.square(kk).T)
             for i in range(n_q):
                 w = p[i] * d[i]
                 bound[i, h] = np.abs(vv - o[i, h]).T @ w + 2.0 ** -8 * (np.abs(vv).T @ p[i])

@@ -6,10 +6,13 @@
 //             states are combined in LDS at the end.
 //
 // Scores: v_mfma_scale_f32_16x16x128_f8f6f4 multiplies K as it is stored, scales included,
-// with Q in e4m3.  A rotated query element has 8 significant bits here, as it has in bf16: a
-// block of 32 is scaled by a power of two and written as hi + lo, both e4m3 (4 bits each, lo
-// with a scale of 2^-4).  At head dim 128 that is two products per 16 keys, at 64 one, whose
-// first 64 dims are K times hi and whose last 64 are K times lo.
+// with Q in e2m3 (6 bits): a block of 32 rotated elements is scaled by a power of two and
+// written as hi + lo, both e2m3, lo with a scale of 2^-4.  hi is off by up to 1/4 unit where the largest
+// element has 3.875 to 7.75 of them, and hi + lo by up to 1/128 (elements above 4 units; 1/256 below): 2^-8.9
+// of the block's largest element, where bf16 is off by up to 2^-8 of each.  (Both in e4m3, 2^-8 of each
+// too: products at half the rate, 1,024 rows onto 16,384 keys 342 us instead of 317.)  At head dim 128 that
+// is two products per 16 keys, at 64 one, whose first 64 dims are K times hi and whose last 64 are K
+// times lo.
 // Values: a lane's 16 bytes of V are a block, which the scaled conversion turns into bf16
 // (exactly); transposed LDS reads then give the operand of v_mfma_f32_16x16x32_bf16.
 // Nothing is shared between waves before the end, so there are no barriers in the loop; the
@@ -31,7 +34,9 @@ constexpr int kAhead = 4;        // V operands read ahead of the products
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x32 __attribute__((ext_vector_type(32)));
 
 // global memory (a pointer picked by branches would be loaded from as a flat address)
 __device__ __forceinline__ u32x4 gload16(const uint8_t* p) {
@@ -56,8 +61,8 @@ __device__ __forceinline__ float col_max(float x) {
 
 // Lane l of a wave is (column l % 16, group lg = l / 16).
 //   scores   S^T[16 keys x 16 queries]: A = K, lane: key l % 16, block lg of 32 dims; B = Q^T,
-//            lane: query l % 16, dims 16 lg .. + 15 of each half of the 128; scales: one byte
-//            of each operand's row and block lg.  The lane gets keys 4 lg + e of its query.
+//            lane: query l % 16, block lg; scales: one byte of each operand's row and block
+//            lg.  The lane gets keys 4 lg + e of its query.
 //   values   O^T[16 dims x 16 queries]: the 32 keys are contracted in the order in which the
 //            scores of two products lie in a lane, keys 4 lg + e and 16 + 4 lg + e; the lane
 //            gets dims 4 lg + e of each 16.
@@ -82,8 +87,9 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
     constexpr bool kPipe = QB > 1;
     // (its chunks are found by exclusive or on their addresses: whole rows are aligned)
     __shared__ __align__(256) u32x4 s_mem[(kPipe ? 2 : 1) * KW * kKeyBlock * D / 8];   // V of each wave's block; at the end the states
-    __shared__ u32x4 s_q[QB][QP][2][64];                     // Q operands
-    __shared__ uint8_t s_qs[QB][64];                         // ... and their scales
+    __shared__ u32x4 s_q[QB][QP][64];           // Q operands, their first 16 bytes
+    __shared__ uint2 s_q2[QB][QP][64];          // ... the other 8
+    __shared__ uint8_t s_qs[QB][64];            // ... and their scales
     __shared__ float2 s_ml[KW][kRows];
     f32x4(&s_part)[KW][DB][64] = *reinterpret_cast<f32x4(*)[KW][DB][64]>(s_mem);
     static_assert(sizeof(f32x4) * KW * DB * 64 <= sizeof(s_mem), "the states of one block of query rows fit");
@@ -204,77 +210,112 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
             vs[j] = gload1(ps[j]);
         }
     };
-    if (n > 0) {
+    auto load_first = [&] {
+        if (n == 0) return;
         const Place at = place_of(k0);
         load_v(k0, at, lane);
         load_k(k0, at, lane);
-    }
+    };
 
-    // Q^T operands, rotated and scaled by scale * log2(e): a thread takes 8 dims of the lower
-    // half and their partners of the upper one, four threads a block.  Rows past M read row
+    // Q^T operands.  First the rows, rotated and scaled by scale * log2(e), to LDS: a thread
+    // takes 8 dims of the lower half and their partners of the upper one.  Rows past M read row
     // M - 1 and are never stored.
-    for (int x = threadIdx.x; x < QB * kRows * (D / 16); x += 64 * KW) {
+    constexpr int kPad = kMxBlock + 4;   // a block's floats in LDS: 16 lanes' reads do not share banks
+    constexpr int kItems = QB * kRows * (D / 16), kTurns = (kItems + 64 * KW - 1) / (64 * KW);
+    float* const s_rows = reinterpret_cast<float*>(s_mem);
+    static_assert(sizeof(float) * QB * kRows * NB * kPad <= sizeof(s_mem), "the rotated rows fit");
+#pragma unroll
+    for (int turn = 0; turn < kTurns; ++turn) {
+        const int x = turn * 64 * KW + (int)threadIdx.x;
         const int r = x / (D / 16), d0 = (x - r * (D / 16)) * 8;
         const int m = min(mw + r, M - 1), i = m / G;
         const uint16_t* qp = q + ((int64_t)(d.q_row0 + i) * st.Hq + g * G + (m - i * G)) * D + d0;
         const float4* cp = reinterpret_cast<const float4*>(
             st.rope + ((int64_t)d.s * st.max_step_rows + d.rope_row0 + i) * (D / 2) + d0);
         const u32x4 a = *reinterpret_cast<const u32x4*>(qp), a2 = *reinterpret_cast<const u32x4*>(qp + D / 2);
-        float y[2][8];
+        float4 cs[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) cs[e] = cp[e];
+        if (turn == 0) {
+            __builtin_amdgcn_sched_barrier(0);
+            load_first();   // K and V behind them: loads return in order
+        }
+        f32x4 lo[2], hi[2];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float4 cs = cp[e];
             const float lo0 = __uint_as_float(a[e] << 16), lo1 = __uint_as_float(a[e] & 0xffff0000u);
             const float hi0 = __uint_as_float(a2[e] << 16), hi1 = __uint_as_float(a2[e] & 0xffff0000u);
-            y[0][2 * e] = (lo0 * cs.x - hi0 * cs.y) * st.scale_log2e;
-            y[0][2 * e + 1] = (lo1 * cs.z - hi1 * cs.w) * st.scale_log2e;
-            y[1][2 * e] = (hi0 * cs.x + lo0 * cs.y) * st.scale_log2e;
-            y[1][2 * e + 1] = (hi1 * cs.z + lo1 * cs.w) * st.scale_log2e;
+            lo[e / 2][2 * (e & 1)] = (lo0 * cs[e].x - hi0 * cs[e].y) * st.scale_log2e;
+            lo[e / 2][2 * (e & 1) + 1] = (lo1 * cs[e].z - hi1 * cs[e].w) * st.scale_log2e;
+            hi[e / 2][2 * (e & 1)] = (hi0 * cs[e].x + lo0 * cs[e].y) * st.scale_log2e;
+            hi[e / 2][2 * (e & 1) + 1] = (hi1 * cs[e].z + lo1 * cs[e].w) * st.scale_log2e;
         }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            uint32_t big = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) big = max(big, __float_as_uint(y[h][e]) & 0x7fffffffu);
-            big = max(big, (uint32_t)__shfl_xor((int)big, 1));
-            big = max(big, (uint32_t)__shfl_xor((int)big, 2));
-            // the largest magnitude becomes 128 to 256 units of 2^(scale - 127), of e4m3's 448
-            const int scale = big >= 0x7f800000u ? kMxNaN : max((int)(big >> 23) - 7, 5);
-            const float inv = __uint_as_float((uint32_t)(254 - min(scale, 253)) << 23);
-            uint2 hi{0u, 0u}, lo{0u, 0u};
-            if (scale != kMxNaN) {
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float* z = &y[h][4 * e];
-                    int c = 0, c2 = 0;
-                    c = __builtin_amdgcn_cvt_pk_fp8_f32(z[0] * inv, z[1] * inv, c, false);
-                    c = __builtin_amdgcn_cvt_pk_fp8_f32(z[2] * inv, z[3] * inv, c, true);
-                    const f32x2 b0 = __builtin_amdgcn_cvt_pk_f32_fp8(c, false), b1 = __builtin_amdgcn_cvt_pk_f32_fp8(c, true);
-                    c2 = __builtin_amdgcn_cvt_pk_fp8_f32((z[0] * inv - b0[0]) * 16.f, (z[1] * inv - b0[1]) * 16.f, c2, false);
-                    c2 = __builtin_amdgcn_cvt_pk_fp8_f32((z[2] * inv - b1[0]) * 16.f, (z[3] * inv - b1[1]) * 16.f, c2, true);
-                    (e ? hi.y : hi.x) = (uint32_t)c;
-                    (e ? lo.y : lo.x) = (uint32_t)c2;
-                }
-            }
-            const int at = d0 + h * (D / 2), xb = r / kRows, l = (at % 64) / 16 * 16 + r % kRows;
-            if constexpr (D == 128) {
-                reinterpret_cast<uint2*>(&s_q[xb][0][at / 64][l])[at / 8 % 2] = hi;
-                reinterpret_cast<uint2*>(&s_q[xb][1][at / 64][l])[at / 8 % 2] = lo;
-            } else {
-                reinterpret_cast<uint2*>(&s_q[xb][0][0][l])[at / 8 % 2] = hi;
-                reinterpret_cast<uint2*>(&s_q[xb][0][1][l])[at / 8 % 2] = lo;
-            }
-            if (at % kMxBlock == 0) {
-                s_qs[xb][at / kMxBlock * 16 + r % kRows] = (uint8_t)scale;
-                if constexpr (D == 64)   // the product's last 64 dims
-                    s_qs[xb][(at / kMxBlock + 2) * 16 + r % kRows] = (uint8_t)(scale == kMxNaN ? kMxNaN : scale - 4);
-            }
+        if (kItems % (64 * KW) == 0 || x < kItems) {
+            f32x4* const l = reinterpret_cast<f32x4*>(s_rows + (r * NB + d0 / kMxBlock) * kPad + d0 % kMxBlock);
+            f32x4* const h = reinterpret_cast<f32x4*>(s_rows + (r * NB + (d0 + D / 2) / kMxBlock) * kPad + (d0 + D / 2) % kMxBlock);
+            l[0] = lo[0], l[1] = lo[1];
+            h[0] = hi[0], h[1] = hi[1];
         }
     }
     __syncthreads();
-    int qs[QB];
+    // Then the operands, a lane a block: with one block of rows every wave makes them for
+    // itself, else wave x makes those of the 16 rows x.
+    i32x8 qv[2][QP];   // Q operands (of one block of rows; else read one block ahead of the products)
+    int qs[QB];        // ... and their scales
+    if (QB == 1 || w < QB) {
+        const int x0 = QB == 1 ? 0 : w;
+        const f32x4* row = reinterpret_cast<const f32x4*>(s_rows + ((x0 * kRows + l16) * NB + (lg & (NB - 1))) * kPad);
+        f32x16 even, odd;   // the conversion interleaves its two operands
+        uint32_t big = 0;
 #pragma unroll
-    for (int x = 0; x < QB; ++x) qs[x] = s_qs[x][lane];
+        for (int k = 0; k < 8; ++k) {
+            const f32x4 x = row[k];
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                even[2 * k + e] = x[2 * e];
+                odd[2 * k + e] = x[2 * e + 1];
+                big = max(big, max(__float_as_uint(x[2 * e]) & 0x7fffffffu, __float_as_uint(x[2 * e + 1]) & 0x7fffffffu));
+            }
+        }
+        // the largest magnitude becomes 3.875 to 7.75 units of 2^(scale - 127), of e2m3's 7.5
+        const int scale = big >= 0x7f800000u ? kMxNaN : max((int)((big + 0x80000u) >> 23) - 2, 5);
+        u32x6 hi{0u, 0u, 0u, 0u, 0u, 0u}, lo = hi;
+        if (scale != kMxNaN) {
+            const float unit = __uint_as_float((uint32_t)scale << 23);
+            hi = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
+            const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(hi, unit);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                even[e] -= back[2 * e];
+                odd[e] -= back[2 * e + 1];
+            }
+            lo = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit * 0.0625f);
+        }
+        auto put = [&](int k, const u32x6& x) {
+            if constexpr (QB == 1) {
+                qv[0][k] = i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+            } else {
+                s_q[w][k][lane] = u32x4{x[0], x[1], x[2], x[3]};
+                s_q2[w][k][lane] = make_uint2(x[4], x[5]);
+            }
+        };
+        int mine = scale;
+        if constexpr (D == 128) {
+            put(0, hi);
+            put(1, lo);
+        } else {   // the product's last 64 dims are lo
+            put(0, lg < NB ? hi : lo);
+            mine = lg < NB || scale == kMxNaN ? scale : scale - 4;
+        }
+        if (QB == 1) qs[0] = mine;
+        else s_qs[w][lane] = (uint8_t)mine;
+    }
+    __syncthreads();   // V takes the rows' place
+    if constexpr (QB > 1) {
+#pragma unroll
+        for (int x = 0; x < QB; ++x) qs[x] = s_qs[x][lane];
+    }
+
     // this wave's V: where the lane's block e (of 8 dims) of its first row goes, and the lane's
     // place in the transposed reads (16 lanes read 8 bytes each of four keys' 32 bytes).  The
     // swizzle and e (the 16-dim block c) touch the same bits of the address.
@@ -301,12 +342,13 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
 
     f32x4 sc[QB][2];   // scores of a block, relative to the running reference
     bf16x8 p[QB];      // its probabilities
-    i32x8 qv[2][QP];   // Q operands, read one block of rows ahead of the products
     auto read_q = [&](int x, int ln) {
+        if constexpr (QB == 1) return;
 #pragma unroll
         for (int k = 0; k < QP; ++k) {
-            const u32x4 a = s_q[x][k][0][ln], b2 = s_q[x][k][1][ln];
-            qv[x & 1][k] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2[0], (int)b2[1], (int)b2[2], (int)b2[3]};
+            const u32x4 a = s_q[x][k][ln];
+            const uint2 b2 = s_q2[x][k][ln];
+            qv[x & 1][k] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2.x, (int)b2.y, 0, 0};
         }
     };
     auto score = [&](int x) {
@@ -319,7 +361,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const i32x8 kv = {(int)kc[t][0], (int)kc[t][1], (int)kc[t][2], (int)kc[t][3], 0, 0, 0, 0};
-                sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv[x & 1][k], sc[x][t], 4, 0, 0, ks[t], 0, s);
+                sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv[x & 1][k], sc[x][t], 4, 2, 0, ks[t], 0, s);
             }
         }
     };
