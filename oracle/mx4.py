@@ -73,15 +73,18 @@ class OracleMx4Cache(OracleCache):
             self.k[l][-n:] = hold(rotate_to_f32(k[l], pos, self.theta))
             self.v[l][-n:] = hold(v[l])
 
-    def attention_bound(self, layer, q, n_q):
+    def attention_bound(self, layer, q, n_q, least=1e-6):
         """(o, bound): attention as OracleCache.attention's, and what a computation may be off by
         that holds rotated queries as two e2m3 numbers (an error of up to 1/128 unit, the largest
         magnitude of a block of 32 being at least 3.875 units; independent from element to
-        element), probabilities to 8 significant bits, partial outputs to 11 and the output to 8.
+        element), probabilities to 11 significant bits or 2^-25 of the largest, partial outputs to 11
+        and the output to 8; `least`: and that partial outputs are fp16.
 
         A score's error is a sum of D independent ones, uniform in +- a_b |k_i| / (128 * 3.875), a_b the
         largest magnitude of the query's block: six of its standard deviations are taken as its
-        bound.  An error d_j of the scores moves the output by p_j d_j (v_j - o) to first order."""
+        bound.  An error d_j of the scores moves the output by p_j d_j (v_j - o) to first order,
+        an error e_j of a probability by e_j (v_j - o); fp32 sums and exponentials take as much as
+        2^-13 of the sum of magnitudes."""
         q_pos = self.pos[self.resident - n_q:]
         q_rot = rope.rotate(np.asarray(q, np.float64), q_pos, self.theta)
         k, v = self.k[layer], self.v[layer]
@@ -98,5 +101,6 @@ class OracleMx4Cache(OracleCache):
             d = 6 * self.scale / (128 * 3.875 * np.sqrt(3)) * np.sqrt(np.square(most) @ np.square(kk).T)
             for i in range(n_q):
                 w = p[i] * d[i]
-                bound[i, h] = np.abs(vv - o[i, h]).T @ w + 2.0 ** -8 * (np.abs(vv).T @ p[i])
-        return o, bound + (2.0 ** -8 + 2.0 ** -11) * np.abs(o) + 1e-6
+                e = np.where(mask[i], np.maximum(2.0 ** -11 * p[i], 2.0 ** -25 * p[i].max()), 0.0)
+                bound[i, h] = np.abs(vv - o[i, h]).T @ (w + e) + 2.0 ** -13 * (np.abs(vv).T @ p[i])
+        return o, bound + (2.0 ** -8 + 2.0 ** -11) * np.abs(o) + least

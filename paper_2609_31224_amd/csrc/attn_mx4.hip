@@ -10,11 +10,15 @@
 // written as hi + lo, both e2m3, lo with a scale of 2^-4.  hi is off by up to 1/4 unit where the largest
 // element has 3.875 to 7.75 of them, and hi + lo by up to 1/128 (elements above 4 units; 1/256 below): 2^-8.9
 // of the block's largest element, where bf16 is off by up to 2^-8 of each.  (Both in e4m3, 2^-8 of each
-// too: products at half the rate, 1,024 rows onto 16,384 keys 342 us instead of 317.)  At head dim 128 that
+// too: products at half the rate, 1,024 rows onto 16,384 keys 337 us instead of 318.)  At head dim 128 that
 // is two products per 16 keys, at 64 one, whose first 64 dims are K times hi and whose last 64 are K
 // times lo.
-// Values: a lane's 16 bytes of V are a block, which the scaled conversion turns into bf16
-// (exactly); transposed LDS reads then give the operand of v_mfma_f32_16x16x32_bf16.
+// Values: a lane's 16 bytes of V are a block, which the scaled conversion turns into fp16
+// (exactly); transposed LDS reads then give the operand of v_mfma_f32_16x16x32_f16.  The few blocks
+// that fp16 does not hold are added in fp32.  Probabilities are fp16, relative to a reference that
+// a wave's largest one reaches or exceeds: off by up to 2^-11 of each, or 2^-25 of the largest.  (In bf16, at the
+// same time, they were off by as much as the output's own rounding: an error against 64 bits of 0.0026
+// instead of 0.0020 relative, the bf16 output alone 0.0017; 64 sessions on 4,096 keys.)
 // Nothing is shared between waves before the end, so there are no barriers in the loop; the
 // next block's codes are in flight while one is computed.
 #include "a2t_internal.h"
@@ -332,16 +336,16 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
         for (int half = 0; half < 2; ++half)
             h[half] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                 (__attribute__((address_space(3))) i16x4*)(uintptr_t)((v_out ^ (32u * c)) + half * 16 * D * 2));
-        return __builtin_bit_cast(bf16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
+        return __builtin_bit_cast(f16x8, __builtin_shufflevector(h[0], h[1], 0, 1, 2, 3, 4, 5, 6, 7));
     };
     // LDS reads and matrix products stay in the order written; other vector operations move freely
     auto ordered = [] { __builtin_amdgcn_sched_barrier(0x6); };
     // nothing moves past; between two of these a product is followed by m vector operations
     auto fence = [] { __builtin_amdgcn_sched_barrier(0); };
-    const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+    const f16x8 ones = __builtin_bit_cast(f16x8, u32x4{0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u});
 
     f32x4 sc[QB][2];   // scores of a block, relative to the running reference
-    bf16x8 p[QB];      // its probabilities
+    f16x8 p[QB];       // its probabilities
     auto read_q = [&](int x, int ln) {
         if constexpr (QB == 1) return;
 #pragma unroll
@@ -406,46 +410,63 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
         float pr[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) pr[e] = __builtin_amdgcn_exp2f(sc[x][e >> 2][e & 3]);
-        p[x] = __builtin_bit_cast(bf16x8, u32x4{pack_bf16x2(pr[0], pr[1]), pack_bf16x2(pr[2], pr[3]),
-                                                pack_bf16x2(pr[4], pr[5]), pack_bf16x2(pr[6], pr[7])});
+        p[x] = __builtin_bit_cast(f16x8, u32x4{mx4_pack_f16x2(pr[0], pr[1]), mx4_pack_f16x2(pr[2], pr[3]),
+                                               mx4_pack_f16x2(pr[4], pr[5]), mx4_pack_f16x2(pr[6], pr[7])});
     };
-    auto sum = [&](int x) { lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, p[x], lsum[x], 0, 0, 0); };
-    // step m of 4 VL: a lane's 8 values of V to LDS as bf16
+    auto sum = [&](int x) { lsum[x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(ones, p[x], lsum[x], 0, 0, 0); };
+    // step m of 4 VL: a lane's 8 values of V to LDS as fp16
     auto take_v = [&](uint32_t v_in, int m) {
-        v_store(v_in, m / 4, m % 4, mx4_to_bf16(vc[m / 4][m % 4], __uint_as_float((uint32_t)vs[m / 4] << 23)));
+        v_store(v_in, m / 4, m % 4, mx4_to_f16(vc[m / 4][m % 4], __uint_as_float((uint32_t)vs[m / 4] << 23)));
     };
-    // A block of V that is NaN counts for the queries that see its key: their sums become NaN here;
-    // its place takes zeros, which change nothing for the others.
-    auto nan_v = [&](uint32_t v_in, int kb) {
+    // Blocks of V that fp16 does not hold (outside its range, or NaN) become zeros in LDS; odd says that
+    // there are some.  add_odd gives the queries that see their keys these products in fp32, once the block's
+    // scores are settled.  (Blocks of zeros have the lowest scale and are in order.)
+    bool odd = false;
+    auto odd_v = [&](uint32_t v_in) {
+        auto out = [&](int j) { return (uint32_t)(vs[j] - kMxF16Low) > (uint32_t)(kMxF16High - kMxF16Low); };
         bool any = false;
 #pragma unroll
-        for (int j = 0; j < VL; ++j) any |= vs[j] == kMxNaN;
-        if (!__any(any)) return;
+        for (int j = 0; j < VL; ++j) any |= out(j);
+        odd = __any(any);
+        if (!odd) return;
+        any = false;
 #pragma unroll
         for (int j = 0; j < VL; ++j)
-            if (vs[j] == kMxNaN)
+            if (out(j)) {
+                any |= vs[j] == kMxNaN || (vc[j][0] | vc[j][1] | vc[j][2] | vc[j][3]) != 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v_store(v_in, j, e, u32x4{0u, 0u, 0u, 0u});
+            }
+        odd = __any(any);
+    };
+    auto add_odd = [&](int kb) {
 #pragma unroll 1
         for (int key = 0; key < kKeyBlock; ++key) {
+            const int64_t row = row_of(kb + key);
+            float pr[QB];   // the lane's queries': of lane (key % 16) / 4, scores key / 16, key % 4
+#pragma unroll
+            for (int x = 0; x < QB; ++x) {
+                float s = sc[x][0][0];
+#pragma unroll
+                for (int e = 1; e < 8; ++e) s = 4 * (key >> 4) + (key & 3) == e ? sc[x][e >> 2][e & 3] : s;
+                pr[x] = __builtin_amdgcn_exp2f(__shfl(s, 16 * ((key & 15) >> 2) + l16));
+            }
 #pragma unroll
             for (int c = 0; c < NB; ++c) {
-                const int at = key * NB + c;
-                int byte = 0;
+                const int byte = gload1(vp.scales + row * NB + c);
+                if ((uint32_t)(byte - kMxF16Low) <= (uint32_t)(kMxF16High - kMxF16Low)) continue;
 #pragma unroll
-                for (int j = 0; j < VL; ++j)
-                    if (at / 64 == j) byte = __builtin_amdgcn_readlane(vs[j], at & 63);
-                if (byte != kMxNaN) continue;
+                for (int h = 0; h < 2; ++h) {   // dims 32 c + 16 h + 4 lg ..
+                    const uint8_t* at = vp.codes + row * CB + 16 * c + 8 * h + 2 * lg;
+                    const f32x4 v = mx4_to_f32(gload1(at) | gload1(at + 1) << 8, byte);
 #pragma unroll
-                for (int x = 0; x < QB; ++x)
-                    if (kb + key <= vis0 + qi[x]) {
-                        const float z = __uint_as_float(0x7fc00000u);
-                        acc[x][2 * c] = acc[x][2 * c + 1] = f32x4{z, z, z, z};
-                    }
+                    for (int x = 0; x < QB; ++x)
+                        if (kb + key <= vis0 + qi[x]) acc[x][2 * c + h] += v * pr[x];
+                }
             }
         }
     };
-    bf16x8 vv[kAhead + 1];   // V operands, read kAhead 16-dim blocks ahead of the products
+    f16x8 vv[kAhead + 1];   // V operands, read kAhead 16-dim blocks ahead of the products
 
     if constexpr (!kPipe) {
 #pragma unroll 1
@@ -462,7 +483,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
             ordered();
 #pragma unroll
             for (int m = 0; m < 4 * VL; ++m) take_v(v_in, m);
-            nan_v(v_in, kb);
+            odd_v(v_in);
             wave_lds_order();   // other lanes read these rows
             load_v(kb_next, next, ln);
             ordered();
@@ -480,6 +501,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
             for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
             ordered();
             settle(kb, i == 0);
+            if (odd) add_odd(kb);
 #pragma unroll
             for (int x = 0; x < QB; ++x) weigh(x), sum(x);
             __builtin_amdgcn_s_setprio(1);
@@ -489,7 +511,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
                 ordered();
 #pragma unroll
                 for (int x = 0; x < QB; ++x)
-                    acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[c % (kAhead + 1)], p[x], acc[x][c], 0, 0, 0);
+                    acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv[c % (kAhead + 1)], p[x], acc[x][c], 0, 0, 0);
                 ordered();
             }
             __builtin_amdgcn_s_setprio(0);
@@ -499,20 +521,21 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
         auto values = [&](int c) {
 #pragma unroll
             for (int x = 0; x < QB; ++x)
-                acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vv[c % (kAhead + 1)], p[x], acc[x][c], 0, 0, 0);
+                acc[x][c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vv[c % (kAhead + 1)], p[x], acc[x][c], 0, 0, 0);
         };
         {
             const int kb_next = n > 1 ? k0 + kStride : R;
             const Place next = place_of(kb_next);
 #pragma unroll
             for (int m = 0; m < 4 * VL; ++m) take_v(v_in0, m);
-            nan_v(v_in0, k0);
+            odd_v(v_in0);
             load_v(kb_next, next, lane);
 #pragma unroll
             for (int x = 0; x < QB; ++x) read_q(x, lane), score(x);
             fence();
             load_k(kb_next, next, lane);
             settle(k0, true);
+            if (odd) add_odd(k0);
         }
         // In each pass the probabilities and products of a block go with the next one's scores and V: the matrix
         // units work on one while the vector units work on the other.
@@ -567,9 +590,10 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
                 }
                 fence();
             }
-            nan_v(v_in, kb);
+            odd_v(v_in);
             load_v(kb_next, next, ln);
             settle(kb, false);
+            if (odd) add_odd(kb);
         }
         __builtin_amdgcn_s_setprio(0);
         // the last block

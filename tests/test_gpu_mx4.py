@@ -578,3 +578,37 @@ def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv
         mine = hq // hkv
         assert np.isnan(got[:, :mine, :32]).all()
         assert np.array_equal(got[:, :mine, 32:], clean[:, :mine, 32:]) and np.array_equal(got[:, mine:], clean[:, mine:])
+
+
+@pytest.mark.parametrize("small", [False, True])
+@pytest.mark.parametrize("d,hq,hkv,rows", [(64, 4, 2, 5), (128, 2, 2, 10), (64, 4, 1, 70), (128, 4, 1, 70), (128, 2, 2, 20)])
+@pytest.mark.parametrize("exps", [[-40], [-26, -25, -24, -23, -22, -12, -11], [10, 11, 12, 13, 14, 0], [-110, -60, -20, 0, 0, 0, 20, 100],
+                                  [0, 0, 0, 0, 0, 120]])
+def test_scales_of_values_apart(gpu, monkeypatch, d, hq, hkv, rows, small, exps):
+    """Blocks of V whose scales fp16 holds beside some it does not, blocks of zeros, and rows
+    of the step that only some of its rows see; every output element within its own bound."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_SPLITS", "1")
+    if small:
+        monkeypatch.setenv("A2T_TARGET_WGS", "1")
+    old = 333
+    rng = np.random.default_rng(9)
+    n = old + rows
+    scale = np.repeat(2.0 ** rng.choice(exps, (n, hkv, d // 32)), 32, -1) * np.repeat(rng.random((n, hkv, d // 32)) < 0.9, 32, -1)
+    k, v, q = (bf16_round(rng.standard_normal((m, h, d))) for m, h in ((n, hkv), (n, hkv), (rows, hq)))
+    v = bf16_round(v * scale)
+    kd, vd, qd = (torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda().bfloat16() for x in (k, v, q))
+    seg = np.full(n, SEG_ACOUSTIC, np.uint8)
+    c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, n, 0, old)
+    ref = mx4.OracleMx4Cache(hq, hkv, d, [0], theta=1e6)
+    o = torch.full_like(qd, float("nan"))
+    a2t.a2t_append(c, 0, [0], [old], kd[:old], vd[:old], seg[:old], np.arange(old), [0])
+    a2t.a2t_append_attn(c, 0, [0], [rows], kd[old:], vd[old:], seg[old:], np.arange(old, n), [1], [rows], qd, o)
+    a2t.a2t_sync(c)
+    a2t.a2t_cache_destroy(c)
+    for part, unit in ((slice(0, old), 0), (slice(old, n), 1)):
+        ref.append(seg[part], np.arange(n)[part], unit, {0: k[part]}, {0: v[part]})
+    want, bound = ref.attention_bound(0, q, rows, least=0.0)
+    off = np.abs(o.float().cpu().numpy().astype(np.float64) - want) - bound
+    assert np.isfinite(off).all() and (off <= 0).all(), (float(off.max()), np.unravel_index(off.argmax(), off.shape))
