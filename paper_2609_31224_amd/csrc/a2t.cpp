@@ -508,35 +508,44 @@ bool f32_on_valu(const a2t_cache* c, int n, const int* tiles) {
 }
 constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
-// An attn_mx4 launch: blocks of 16 query rows and waves (key blocks at a time) per workgroup,
-// and what its workgroups cost.
+// The kernel of a step on an A2T_MX4 cache, and the query rows of its workgroups.
 //
-// Three blocks are the most that a wave's registers hold without spilling (four: listening
-// units of 16 sessions 419 us a step of four layers, three: 258, two: 254, one: 261; 1,024 rows
-// onto 4,096 keys 254, 226, 247 and 268 us, two layers).
+// attn_mx4: 16 query rows, or workgroups of as few blocks of 16 as cover them in groups of up to three, the most
+// that a wave's registers hold without spilling (four: listening units of 16 sessions 419 us a
+// step of four layers, three: 258, two: 254, one: 261).
 //
-// Workgroups of four waves and two blocks where there are more than two for each CU anyway
-// and few keys: two of them share a CU, so that one's first loads and the combining of
-// its waves' states go with the other's products (777 rows of 32/4 heads of 64 onto none 12.3
-// against 21.6 us, 1,024 rows of 32/8 heads of 128 onto none 27.6 against 35.6; onto 4,096
-// keys 119 against 121, onto 16,384 364 against 352).
-constexpr int kMx4Blocks = 3, kMx4FewTiles = 64;
+// attn_mx4_rows, workgroups of 64 or 128 rows, where these cover the rows with less than 5/4 of the
+// rows that the others' cover them with: a row costs it less (16 sessions of 30 rows of 32/8 heads of 128 on
+// 4,096 keys, 120 rows a KV head, 128 for 144: 47 against 67 us, merge included; 60 rows 70 and 108; 1,024 rows on
+// 4,096 keys 85 and 108, on 16,384 267 and 324), but not rows that are not there (22 rows on 8,192 keys, 128
+// for 96: 77 against 61; 40 rows on 4,096, 256 for 192: 65 and 65).
+// 64 rows up to 32 tiles: more, smaller workgroups; above, V is unpacked for more rows at once (1,024 rows on no
+// keys 20.9 against 24.5 us, on 1,024 38.7 and 39.7, on 2,048 56.3 and 55.1, on 4,096 92 and 85; 777
+// rows of 32/4 heads of 64 on none 12.0 and 15.2, on 5,000 64.1 and 62.2).
+constexpr int kMx4Blocks = 3, kMx4FewTiles = 32;
 struct Mx4Shape {
-    int query_blocks, key_waves;
+    int query_blocks;   // of attn_mx4; 0: attn_mx4_rows
+    int row_waves;
+    int rows() const { return query_blocks ? 16 * query_blocks : 32 * row_waves; }
 };
 Mx4Shape mx4_shape(const a2t_cache* c, int n, const int* tiles, const int32_t* n_q) {
-    const int Hkv = c->cfg.n_kv_heads, G = c->cfg.n_q_heads / Hkv;
+    const int G = c->cfg.n_q_heads / c->cfg.n_kv_heads;
     int rows = 1, longest = 1;
-    int64_t pairs = 0;
     for (int i = 0; i < n; ++i) {
         rows = std::max(rows, G * n_q[i]);
         longest = std::max(longest, tiles[i]);
-        pairs += (int64_t)Hkv * mx4_groups(G * n_q[i], 2);
     }
-    if (rows > 16 && longest <= kMx4FewTiles && pairs > 2 * c->target_wgs) return {2, 4};
     const int blocks = (rows + 15) / 16, groups = (blocks + kMx4Blocks - 1) / kMx4Blocks;
-    return {(blocks + groups - 1) / groups, 8};
+    const Mx4Shape few{(blocks + groups - 1) / groups, 0}, many{0, longest <= kMx4FewTiles ? 2 : 4};
+    int64_t padded_few = 0, padded_many = 0;
+    for (int i = 0; i < n; ++i) {
+        padded_few += (int64_t)few.rows() * mx4_groups(G * n_q[i], few.rows());
+        padded_many += (int64_t)many.rows() * mx4_groups(G * n_q[i], many.rows());
+    }
+    return 4 * padded_many < 5 * padded_few ? many : few;
 }
+// (Splits of 1 to 12 forced on steps of 1 to 1,024 rows onto 0 to 16,384 keys were at best 6 % faster than those that
+// these costs lead to.)
 constexpr SplitCosts kMx4Costs{8, 4, 1 << 20, 4};
 
 // Where a launch's split partials go: the cache's workspace (default) or the
@@ -590,7 +599,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     const bool mx4 = c->cfg.dtype == A2T_MX4;
     const int64_t rf = partial_row_floats(c->cfg.head_dim, f32 || valu);
     int query_blocks = 1;
-    Mx4Shape shape{1, 8};
+    Mx4Shape shape{1, 0};
     int max_rows = 0, tiles[kMaxDesc], nsplit[kMaxDesc];
     int64_t floats[kMaxDesc];
     for (int i = 0; i < n; ++i) {
@@ -605,10 +614,10 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     if (f32 || block || one_row || mx4) {
         SplitStream ss[kMaxDesc];
         if (f32) query_blocks = f32_query_blocks(c, n, tiles, n_q);
-        if (mx4) query_blocks = (shape = mx4_shape(c, n, tiles, n_q)).query_blocks;
+        if (mx4) shape = mx4_shape(c, n, tiles, n_q);
         for (int i = 0; i < n; ++i) {
             const int rows = G * n_q[i];
-            ss[i] = {tiles[i], c->cfg.n_kv_heads * (mx4 ? mx4_groups(rows, query_blocks) : f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
+            ss[i] = {tiles[i], c->cfg.n_kv_heads * (mx4 ? mx4_groups(rows, shape.rows()) : f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
                      floats[i]};   // one row: one workgroup
         }
         c->planner.plan(n, ss, mx4 ? kMx4Costs : f32 ? f32_costs(c->cfg.head_dim, query_blocks) : block ? kBlockCosts : kValuCosts, c->target_wgs, c->force_splits,
@@ -689,7 +698,9 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     b.max_rows = max_rows;
     hipError_t e;
     auto launch = [&](const DevState& st, const KTimer& kt) {
-        if (mx4) return launch_attn_mx4(st, b, query_blocks, shape.key_waves, q, o, c->stream, kt);
+        if (mx4)
+            return shape.query_blocks ? launch_attn_mx4(st, b, shape.query_blocks, q, o, c->stream, kt)
+                                      : launch_attn_mx4_rows(st, b, shape.row_waves, q, o, c->stream, kt);
         if (f32) return launch_attn_f32(st, b, query_blocks, q, o, k_in, v_in, c->stream, kt);
         if (valu) return launch_attn_valu(st, b, q, o, c->stream, kt);
         if (block) return launch_attn_block(st, b, q, o, c->stream, kt);

@@ -32,23 +32,11 @@
 namespace a2t {
 namespace {
 
+constexpr int kWaves = 8;
 constexpr int kKeyBlock = 32;    // keys of a wave's block
 constexpr int kRows = 16;        // query rows of a product
 constexpr int kAhead = 4;        // V operands read ahead of the products
 
-typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x6 __attribute__((ext_vector_type(6)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef float f32x32 __attribute__((ext_vector_type(32)));
-
-// global memory (a pointer picked by branches would be loaded from as a flat address)
-__device__ __forceinline__ u32x4 gload16(const uint8_t* p) {
-    return *reinterpret_cast<const __attribute__((address_space(1))) u32x4*>(reinterpret_cast<uintptr_t>(p));
-}
-__device__ __forceinline__ int gload1(const uint8_t* p) {
-    return *reinterpret_cast<const __attribute__((address_space(1))) uint8_t*>(reinterpret_cast<uintptr_t>(p));
-}
 // LDS accesses of the wave before this one come before those after it, whatever the compiler
 // knows about their addresses in one lane (the hardware keeps a wave's LDS accesses in order)
 __device__ __forceinline__ void wave_lds_order() {
@@ -78,25 +66,24 @@ __device__ __forceinline__ int v_chunk(int key, int c) {
     return key * (D / 8) + (c ^ (2 * y | ((y >> 1) & 1)));
 }
 
-template <int D, int QB, int KW, int N>
-__global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevState st, AttnBatchT<N> b,
-                                                                                   WgStart<N> start, const uint16_t* q,
-                                                                                   uint16_t* o) {
+template <int D, int QB, int N>
+__global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevState st, AttnBatchT<N> b, WgStart<N> start,
+                                                                               const uint16_t* q, uint16_t* o) {
     constexpr int NB = D / kMxBlock;   // blocks of a row
     constexpr int CB = D / 2;          // bytes of a row's codes
     constexpr int DB = D / 16;         // 16-dim blocks of O
     constexpr int VL = D / 64;         // 16-byte loads of V per lane and key block
     constexpr int QP = D / 64;         // products per 16 keys: hi and lo, or both in one
-    constexpr int kStride = KW * kKeyBlock;
+    constexpr int kStride = kWaves * kKeyBlock;
     constexpr bool kPipe = QB > 1;
     // (its chunks are found by exclusive or on their addresses: whole rows are aligned)
-    __shared__ __align__(256) u32x4 s_mem[(kPipe ? 2 : 1) * KW * kKeyBlock * D / 8];   // V of each wave's block; at the end the states
+    __shared__ __align__(256) u32x4 s_mem[(kPipe ? 2 : 1) * kWaves * kKeyBlock * D / 8];   // V of each wave's block; at the end the states
     __shared__ u32x4 s_q[QB][QP][64];           // Q operands, their first 16 bytes
     __shared__ uint2 s_q2[QB][QP][64];          // ... the other 8
     __shared__ uint8_t s_qs[QB][64];            // ... and their scales
-    __shared__ float2 s_ml[KW][kRows];
-    f32x4(&s_part)[KW][DB][64] = *reinterpret_cast<f32x4(*)[KW][DB][64]>(s_mem);
-    static_assert(sizeof(f32x4) * KW * DB * 64 <= sizeof(s_mem), "the states of one block of query rows fit");
+    __shared__ float2 s_ml[kWaves][kRows];
+    f32x4(&s_part)[kWaves][DB][64] = *reinterpret_cast<f32x4(*)[kWaves][DB][64]>(s_mem);
+    static_assert(sizeof(f32x4) * kWaves * DB * 64 <= sizeof(s_mem), "the states of one block of query rows fit");
 
     int wg;
     const AttnDesc d = b.d[stream_of(start, b.count, &wg)];
@@ -225,12 +212,12 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
     // takes 8 dims of the lower half and their partners of the upper one.  Rows past M read row
     // M - 1 and are never stored.
     constexpr int kPad = kMxBlock + 4;   // a block's floats in LDS: 16 lanes' reads do not share banks
-    constexpr int kItems = QB * kRows * (D / 16), kTurns = (kItems + 64 * KW - 1) / (64 * KW);
+    constexpr int kItems = QB * kRows * (D / 16), kTurns = (kItems + 64 * kWaves - 1) / (64 * kWaves);
     float* const s_rows = reinterpret_cast<float*>(s_mem);
     static_assert(sizeof(float) * QB * kRows * NB * kPad <= sizeof(s_mem), "the rotated rows fit");
 #pragma unroll
     for (int turn = 0; turn < kTurns; ++turn) {
-        const int x = turn * 64 * KW + (int)threadIdx.x;
+        const int x = turn * 64 * kWaves + (int)threadIdx.x;
         const int r = x / (D / 16), d0 = (x - r * (D / 16)) * 8;
         const int m = min(mw + r, M - 1), i = m / G;
         const uint16_t* qp = q + ((int64_t)(d.q_row0 + i) * st.Hq + g * G + (m - i * G)) * D + d0;
@@ -244,22 +231,9 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
             __builtin_amdgcn_sched_barrier(0);
             load_first();   // K and V behind them: loads return in order
         }
-        f32x4 lo[2], hi[2];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const float lo0 = __uint_as_float(a[e] << 16), lo1 = __uint_as_float(a[e] & 0xffff0000u);
-            const float hi0 = __uint_as_float(a2[e] << 16), hi1 = __uint_as_float(a2[e] & 0xffff0000u);
-            lo[e / 2][2 * (e & 1)] = (lo0 * cs[e].x - hi0 * cs[e].y) * st.scale_log2e;
-            lo[e / 2][2 * (e & 1) + 1] = (lo1 * cs[e].z - hi1 * cs[e].w) * st.scale_log2e;
-            hi[e / 2][2 * (e & 1)] = (hi0 * cs[e].x + lo0 * cs[e].y) * st.scale_log2e;
-            hi[e / 2][2 * (e & 1) + 1] = (hi1 * cs[e].z + lo1 * cs[e].w) * st.scale_log2e;
-        }
-        if (kItems % (64 * KW) == 0 || x < kItems) {
-            f32x4* const l = reinterpret_cast<f32x4*>(s_rows + (r * NB + d0 / kMxBlock) * kPad + d0 % kMxBlock);
-            f32x4* const h = reinterpret_cast<f32x4*>(s_rows + (r * NB + (d0 + D / 2) / kMxBlock) * kPad + (d0 + D / 2) % kMxBlock);
-            l[0] = lo[0], l[1] = lo[1];
-            h[0] = hi[0], h[1] = hi[1];
-        }
+        if (kItems % (64 * kWaves) == 0 || x < kItems)
+            mx4_rotate(a, a2, cs, st.scale_log2e, s_rows + (r * NB + d0 / kMxBlock) * kPad + d0 % kMxBlock,
+                       s_rows + (r * NB + (d0 + D / 2) / kMxBlock) * kPad + (d0 + D / 2) % kMxBlock);
     }
     __syncthreads();
     // Then the operands, a lane a block: with one block of rows every wave makes them for
@@ -268,36 +242,11 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
     int qs[QB];        // ... and their scales
     if (QB == 1 || w < QB) {
         const int x0 = QB == 1 ? 0 : w;
-        const f32x4* row = reinterpret_cast<const f32x4*>(s_rows + ((x0 * kRows + l16) * NB + (lg & (NB - 1))) * kPad);
-        f32x16 even, odd;   // the conversion interleaves its two operands
-        uint32_t big = 0;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const f32x4 x = row[k];
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                even[2 * k + e] = x[2 * e];
-                odd[2 * k + e] = x[2 * e + 1];
-                big = max(big, max(__float_as_uint(x[2 * e]) & 0x7fffffffu, __float_as_uint(x[2 * e + 1]) & 0x7fffffffu));
-            }
-        }
-        // the largest magnitude becomes 3.875 to 7.75 units of 2^(scale - 127), of e2m3's 7.5
-        const int scale = big >= 0x7f800000u ? kMxNaN : max((int)((big + 0x80000u) >> 23) - 2, 5);
-        u32x6 hi{0u, 0u, 0u, 0u, 0u, 0u}, lo = hi;
-        if (scale != kMxNaN) {
-            const float unit = __uint_as_float((uint32_t)scale << 23);
-            hi = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
-            const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(hi, unit);
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                even[e] -= back[2 * e];
-                odd[e] -= back[2 * e + 1];
-            }
-            lo = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit * 0.0625f);
-        }
+        u32x6 hi, lo;
+        const int scale = mx4_query(s_rows + ((x0 * kRows + l16) * NB + (lg & (NB - 1))) * kPad, &hi, &lo);
         auto put = [&](int k, const u32x6& x) {
             if constexpr (QB == 1) {
-                qv[0][k] = i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
+                qv[0][k] = mx4_operand(x);
             } else {
                 s_q[w][k][lane] = u32x4{x[0], x[1], x[2], x[3]};
                 s_q2[w][k][lane] = make_uint2(x[4], x[5]);
@@ -323,7 +272,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
     // this wave's V: where the lane's block e (of 8 dims) of its first row goes, and the lane's
     // place in the transposed reads (16 lanes read 8 bytes each of four keys' 32 bytes).  The
     // swizzle and e (the 16-dim block c) touch the same bits of the address.
-    constexpr int kBuf = KW * kKeyBlock * D * 2;   // bytes of a buffer
+    constexpr int kBuf = kWaves * kKeyBlock * D * 2;   // bytes of a buffer
     const uint32_t s_v = lds_addr(s_mem) + w * (kKeyBlock * D * 2);
     const uint32_t v_in0 = s_v + 16 * v_chunk<D>(lane / NB, 4 * (lane % NB));
     const uint32_t v_out0 = s_v + 16 * v_chunk<D>(4 * lg + (l16 >> 2), (l16 & 3) >> 1) + 8 * (l16 & 1);
@@ -423,16 +372,15 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
     // scores are settled.  (Blocks of zeros have the lowest scale and are in order.)
     bool odd = false;
     auto odd_v = [&](uint32_t v_in) {
-        auto out = [&](int j) { return (uint32_t)(vs[j] - kMxF16Low) > (uint32_t)(kMxF16High - kMxF16Low); };
         bool any = false;
 #pragma unroll
-        for (int j = 0; j < VL; ++j) any |= out(j);
+        for (int j = 0; j < VL; ++j) any |= mx4_odd(vs[j]);
         odd = __any(any);
         if (!odd) return;
         any = false;
 #pragma unroll
         for (int j = 0; j < VL; ++j)
-            if (out(j)) {
+            if (mx4_odd(vs[j])) {
                 any |= vs[j] == kMxNaN || (vc[j][0] | vc[j][1] | vc[j][2] | vc[j][3]) != 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v_store(v_in, j, e, u32x4{0u, 0u, 0u, 0u});
@@ -454,7 +402,7 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
 #pragma unroll
             for (int c = 0; c < NB; ++c) {
                 const int byte = gload1(vp.scales + row * NB + c);
-                if ((uint32_t)(byte - kMxF16Low) <= (uint32_t)(kMxF16High - kMxF16Low)) continue;
+                if (!mx4_odd(byte)) continue;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {   // dims 32 c + 16 h + 4 lg ..
                     const uint8_t* at = vp.codes + row * CB + 16 * c + 8 * h + 2 * lg;
@@ -625,14 +573,14 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
         const int mq = mw + x * kRows + l16;
         float mx = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < KW; ++k) mx = fmaxf(mx, s_ml[k][l16].x);
+        for (int k = 0; k < kWaves; ++k) mx = fmaxf(mx, s_ml[k][l16].x);
         auto weight = [&](int k) {
             const float m = s_ml[k][l16].x;
             return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mx);
         };
-        float wt[KW], L = 0.f;
+        float wt[kWaves], L = 0.f;
 #pragma unroll
-        for (int k = 0; k < KW; ++k) {
+        for (int k = 0; k < kWaves; ++k) {
             wt[k] = weight(k);
             L += wt[k] * s_ml[k][l16].y;
         }
@@ -640,17 +588,17 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
         // is zeros with a maximum of -inf), else the bf16 output
         const float inv = L == 0.f && !whole ? 0.f : 1.f / L;
         const int64_t at = ((int64_t)sp * st.Hkv + g) * M + mq;
-        for (int c = w; c < DB && mq < M; c += KW) {   // dims 16 c + 4 lg .. + 3
+        for (int c = w; c < DB && mq < M; c += kWaves) {   // dims 16 c + 4 lg .. + 3
             f32x4 O = s_part[0][c][lane] * wt[0];
 #pragma unroll
-            for (int k = 1; k < KW; ++k) O += s_part[k][c][lane] * wt[k];
+            for (int k = 1; k < kWaves; ++k) O += s_part[k][c][lane] * wt[k];
             O *= inv;
             if (whole) {
                 uint16_t* orow = o + ((int64_t)(d.q_row0 + qi[x]) * st.Hq + g * G + (mq - qi[x] * G)) * D;
                 *reinterpret_cast<uint2*>(orow + 16 * c + 4 * lg) = make_uint2(pack_bf16x2(O[0], O[1]), pack_bf16x2(O[2], O[3]));
             } else {
                 uint16_t* orow = reinterpret_cast<uint16_t*>(po) + at * D;
-                *reinterpret_cast<uint2*>(orow + 16 * c + 4 * lg) = make_uint2(pack_f16x2(O[0], O[1]), pack_f16x2(O[2], O[3]));
+                *reinterpret_cast<uint2*>(orow + 16 * c + 4 * lg) = make_uint2(mx4_pack_f16x2(O[0], O[1]), mx4_pack_f16x2(O[2], O[3]));
             }
         }
         if (!whole && w == 0 && lg == 0 && mq < M)
@@ -661,18 +609,18 @@ __global__ __launch_bounds__(64 * KW, QB == 1 ? 4 : 2) void attn_mx4_kernel(DevS
 
 }  // namespace
 
-hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, int key_waves, const void* q, void* o,
-                           hipStream_t stream, const KTimer& kt) {
+hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, const void* q, void* o, hipStream_t stream,
+                           const KTimer& kt) {
     const uint16_t* qq = static_cast<const uint16_t*>(q);
     uint16_t* oo = static_cast<uint16_t*>(o);
     return by_size<AttnBatchT>(b, [&](const auto& bb) {
         constexpr int N = sizeof(bb.d) / sizeof(bb.d[0]);
         WgStart<N> start{};
         const dim3 grid = place_workgroups(b.count, &start, [&](int i) {
-            return mx4_groups(st.G * b.d[i].n_q, query_blocks) * b.d[i].splits * st.Hkv;
+            return mx4_groups(st.G * b.d[i].n_q, kRows * query_blocks) * b.d[i].splits * st.Hkv;
         });
         auto go = [&](auto kernel) {
-            const dim3 block(64 * key_waves);
+            const dim3 block(64 * kWaves);
             if (kt.start)
                 hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo);
             else
@@ -681,12 +629,10 @@ hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blo
         };
         auto sized = [&](auto dim) {
             constexpr int D = decltype(dim)::value;
-            if (key_waves == 4 && query_blocks == 2) return go(attn_mx4_kernel<D, 2, 4, N>);
-            if (key_waves != 8) return hipErrorInvalidValue;
             switch (query_blocks) {
-                case 1: return go(attn_mx4_kernel<D, 1, 8, N>);
-                case 2: return go(attn_mx4_kernel<D, 2, 8, N>);
-                case 3: return go(attn_mx4_kernel<D, 3, 8, N>);
+                case 1: return go(attn_mx4_kernel<D, 1, N>);
+                case 2: return go(attn_mx4_kernel<D, 2, N>);
+                case 3: return go(attn_mx4_kernel<D, 3, N>);
                 default: return hipErrorInvalidValue;
             }
         };

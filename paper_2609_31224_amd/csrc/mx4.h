@@ -4,7 +4,7 @@
 // (element i of the block in bits 4 (i % 2) .. + 3 of byte i / 2) and one e8m0 byte, the
 // block's scale 2^(byte - 127).  Both are what the matrix instructions with block scales
 // and the scaled conversions take, so that a score product reads K as it is stored and V
-// becomes bf16 at two elements an instruction, without a multiplication.
+// becomes fp16 at two elements an instruction, without a multiplication.
 //
 // Scale: the exponent of the block's largest magnitude a less 2, so that a lies in [4, 8)
 // units, and one more where a would be 7 or above, which is nearer to 8 than to 6, the
@@ -55,9 +55,8 @@ __host__ __device__ inline int mx4_scale(uint32_t largest) {
     return e < kMxLeast ? kMxLeast : e > kMxMost ? kMxMost : e;
 }
 
-// Workgroups of attn_mx4 (per split and KV head) that cover query_rows rows with query_blocks
-// blocks of 16 each.
-inline int mx4_groups(int query_rows, int query_blocks) { return ((query_rows + 15) / 16 + query_blocks - 1) / query_blocks; }
+// Workgroups (per split and KV head) of `rows` query rows each that cover query_rows.
+inline int mx4_groups(int query_rows, int rows) { return (query_rows + rows - 1) / rows; }
 
 // ---- reading rows back (any cache)
 struct ReadDesc {
@@ -78,12 +77,14 @@ struct ReadBatchT {
 };
 using ReadBatch = ReadBatchT<kMaxDesc>;
 
-// Launchers (attn_mx4.hip, mx4_rows.hip).  Each issues one kernel unless it says otherwise.
-// MFMA attention (chunk and decode, D 64 or 128; the step's rows already stored), query_blocks
-// (1 to 3) blocks of 16 query rows and key_waves (8; 4 with two blocks) waves per workgroup.
-// Split partials as launch_attn_tile's.
-hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, int key_waves, const void* q, void* o,
-                           hipStream_t stream, const KTimer& kt);
+// Launchers (attn_mx4.hip, attn_mx4_rows.hip, mx4_rows.hip).  Each issues one kernel unless it says otherwise.
+// MFMA attention (chunk and decode, D 64 or 128; the step's rows already stored), query_blocks (1 to 3)
+// blocks of 16 query rows a workgroup.  Split partials as launch_attn_tile's.
+hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blocks, const void* q, void* o, hipStream_t stream,
+                           const KTimer& kt);
+// The same for many query rows: row_waves (2 or 4) x 32 of them a workgroup of twice as many waves.
+hipError_t launch_attn_mx4_rows(const DevState& st, const AttnBatch& b, int row_waves, const void* q, void* o, hipStream_t stream,
+                                const KTimer& kt);
 // Encodes and stores a step's rows (launch_append of other caches).
 hipError_t launch_append_mx4(const DevState& st, const AppendBatch& b, int n_layers, const void* k, const void* v,
                              hipStream_t stream, const KTimer& kt);

@@ -1,7 +1,7 @@
 """GPU parity of A2T_MX4 caches (rows held in 4 bits) against the float64 oracle: encoded rows
 and rows read back exactly, attention within a bound that the oracle derives from the
 roundings it is computed with.  Query rows around the 16-row blocks and the workgroups of one to
-three blocks, key counts around the 32-key blocks, both head dims, one to eight query heads
+three blocks and of 64 and 128 rows, key counts around the 32-key blocks, both head dims, one to eight query heads
 per KV head, rings that wrap, kept regions, every eviction rule, key splits, batches.
 """
 import numpy as np
@@ -238,15 +238,33 @@ def test_query_that_is_not_finite(gpu, d):
     assert np.isnan(outs[1][bad]).all() and np.array_equal(outs[0][~bad], outs[1][~bad])
 
 
-@pytest.mark.parametrize("d,hq,hkv,rows,prefix", [(64, 8, 1, 23, 40), (128, 4, 2, 37, 70), (128, 16, 4, 9, 500), (64, 2, 2, 65, 0)])
-def test_small_workgroups(gpu, monkeypatch, d, hq, hkv, rows, prefix):
-    """Workgroups of four waves (launches with more than two of them per CU: here one CU is
-    counted), whole and with forced splits."""
-    monkeypatch.setenv("A2T_TARGET_WGS", "1")
-    for splits in ("0", "3"):
+@pytest.mark.parametrize("hq,hkv,d,rows,prefix,splits", [
+    (8, 1, 128, 32, 0, None),      # 256 rows, few keys: 64 a workgroup
+    (8, 1, 64, 24, 40, "2"),       # 192
+    (4, 4, 128, 61, 500, "3"),     # 61 of 64
+    (1, 1, 64, 33, 60, "1"),       # 33 of 64: not these
+    (4, 2, 64, 30, 1700, "5"),     # 60 of 64
+    (4, 4, 128, 127, 2100, None),  # 127 of 128 a workgroup
+    (8, 1, 64, 31, 2200, "3"),     # 248 of 256
+    (8, 1, 128, 16, 2500, "1"),    # 128
+    (8, 1, 64, 30, 2200, "7"),     # 240 of 256
+])
+def test_many_rows(gpu, monkeypatch, hq, hkv, d, rows, prefix, splits):
+    """Workgroups of 64 and of 128 query rows, rings that wrap, kept regions that end inside a block."""
+    if splits:
         monkeypatch.setenv("A2T_SPLITS", splits)
-        spec = tiny_stream([SMALL, _unit(rows), [SEG_RESPONSE], _unit(rows + 2), SMALL], prefix=prefix)
-        _run([spec], hq, hkv, d, budgets=[prefix + rows], calls="fused", unit_rows=2 * rows + 60 + prefix)
+    more = [_unit(min(900, prefix - at)) for at in range(900, prefix, 900)]
+    spec = tiny_stream([*more, SMALL, _unit(rows), SMALL, [SEG_RESPONSE], _unit(rows), _unit(rows + 1), SMALL, _unit(rows)],
+                       prefix=min(prefix, 900))
+    _run([spec], hq, hkv, d, budgets=[prefix + rows + 20], calls="fused", query_rows=rows, layers=1, unit_rows=max(4 * rows + 80 + prefix, 80))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_rows_of_uneven_streams(gpu, d):
+    """Streams of 1 to 140 rows in one launch of 128-row and of 64-row workgroups."""
+    for more in ([_unit(800), _unit(800)], []):
+        specs = [tiny_stream([*m, SMALL, _unit(n), SMALL], prefix=p) for n, p, m in ((140, 600, more), (1, 5, more), (64, 0, []), (129, 700, []))]
+        _run(specs, 2, 2, d, budgets=[100000] * 4, calls="fused", layers=1, query_rows=140, unit_rows=2600)
 
 
 # ------------------------------------------------------------------ the calls around them
@@ -536,17 +554,15 @@ def test_offsets_past_32_bits(gpu, kept):
     a2t.a2t_cache_destroy(c)
 
 
-@pytest.mark.parametrize("small", [False, True])
-@pytest.mark.parametrize("d,hq,hkv", [(64, 4, 2), (128, 4, 1), (128, 2, 2)])
-def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv, small):
-    """The same behind several key blocks a wave, with workgroups of eight and of four waves; and values of a resident
+@pytest.mark.parametrize("d,hq,hkv,old,rows", [(64, 4, 2, 900, 70), (128, 4, 1, 900, 70), (128, 2, 2, 900, 70), (128, 2, 2, 900, 40),
+                                               (128, 4, 1, 2300, 64), (64, 8, 1, 2300, 62), (64, 2, 2, 900, 47)])
+def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv, old, rows):
+    """The same behind several key blocks a wave, in every kind of workgroup; and values of a resident
     row, which every query sees."""
     import torch
     import paper_2609_31224_amd as a2t
     monkeypatch.setenv("A2T_SPLITS", "1")
-    if small:
-        monkeypatch.setenv("A2T_TARGET_WGS", "1")
-    old, rows, bad = 900, 70, 33
+    bad = 33
     g = torch.Generator(device="cuda").manual_seed(6)
     k0, v0 = (torch.randn((old, hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
     k, v, q = (torch.randn((rows, h, d), generator=g, device="cuda").bfloat16() for h in (hkv, hkv, hq))
@@ -557,10 +573,12 @@ def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv
             vv[bad, :, 37] = float("nan")
         if resident is not None:
             vr[resident, 0, 2] = float("-inf")
-        c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, old + rows, 0, old)
+        c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, old + rows, 0, 900)
         o = torch.zeros_like(q)
-        a2t.a2t_append(c, 0, [0], [old], k0, vr, np.full(old, SEG_ACOUSTIC, np.uint8), np.arange(old), [0])
-        a2t.a2t_append_attn(c, 0, [0], [rows], k, vv, np.full(rows, SEG_ACOUSTIC, np.uint8), np.arange(old, old + rows), [1],
+        for at in range(0, old, 900):
+            n = min(900, old - at)
+            a2t.a2t_append(c, 0, [0], [n], k0[at:at + n], vr[at:at + n], np.full(n, SEG_ACOUSTIC, np.uint8), np.arange(at, at + n), [at])
+        a2t.a2t_append_attn(c, 0, [0], [rows], k, vv, np.full(rows, SEG_ACOUSTIC, np.uint8), np.arange(old, old + rows), [old],
                             [rows], q, o)
         a2t.a2t_sync(c)
         a2t.a2t_cache_destroy(c)
@@ -580,19 +598,16 @@ def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv
         assert np.array_equal(got[:, :mine, 32:], clean[:, :mine, 32:]) and np.array_equal(got[:, mine:], clean[:, mine:])
 
 
-@pytest.mark.parametrize("small", [False, True])
-@pytest.mark.parametrize("d,hq,hkv,rows", [(64, 4, 2, 5), (128, 2, 2, 10), (64, 4, 1, 70), (128, 4, 1, 70), (128, 2, 2, 20)])
+@pytest.mark.parametrize("d,hq,hkv,rows,old", [(64, 4, 2, 5, 333), (128, 2, 2, 10, 333), (64, 4, 1, 64, 333), (128, 4, 1, 64, 333), (128, 4, 1, 22, 333),
+                                               (128, 2, 2, 20, 333), (64, 4, 1, 64, 2100), (128, 4, 1, 64, 2100), (64, 4, 1, 22, 333)])
 @pytest.mark.parametrize("exps", [[-40], [-26, -25, -24, -23, -22, -12, -11], [10, 11, 12, 13, 14, 0], [-110, -60, -20, 0, 0, 0, 20, 100],
                                   [0, 0, 0, 0, 0, 120]])
-def test_scales_of_values_apart(gpu, monkeypatch, d, hq, hkv, rows, small, exps):
+def test_scales_of_values_apart(gpu, monkeypatch, d, hq, hkv, rows, old, exps):
     """Blocks of V whose scales fp16 holds beside some it does not, blocks of zeros, and rows
     of the step that only some of its rows see; every output element within its own bound."""
     import torch
     import paper_2609_31224_amd as a2t
     monkeypatch.setenv("A2T_SPLITS", "1")
-    if small:
-        monkeypatch.setenv("A2T_TARGET_WGS", "1")
-    old = 333
     rng = np.random.default_rng(9)
     n = old + rows
     scale = np.repeat(2.0 ** rng.choice(exps, (n, hkv, d // 32)), 32, -1) * np.repeat(rng.random((n, hkv, d // 32)) < 0.9, 32, -1)
@@ -600,14 +615,16 @@ def test_scales_of_values_apart(gpu, monkeypatch, d, hq, hkv, rows, small, exps)
     v = bf16_round(v * scale)
     kd, vd, qd = (torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda().bfloat16() for x in (k, v, q))
     seg = np.full(n, SEG_ACOUSTIC, np.uint8)
-    c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, n, 0, old)
+    c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, n, 0, 900)
     ref = mx4.OracleMx4Cache(hq, hkv, d, [0], theta=1e6)
     o = torch.full_like(qd, float("nan"))
-    a2t.a2t_append(c, 0, [0], [old], kd[:old], vd[:old], seg[:old], np.arange(old), [0])
-    a2t.a2t_append_attn(c, 0, [0], [rows], kd[old:], vd[old:], seg[old:], np.arange(old, n), [1], [rows], qd, o)
+    parts = [slice(at, min(at + 900, old)) for at in range(0, old, 900)]
+    for u, part in enumerate(parts):
+        a2t.a2t_append(c, 0, [0], [part.stop - part.start], kd[part], vd[part], seg[part], np.arange(n)[part], [u])
+    a2t.a2t_append_attn(c, 0, [0], [rows], kd[old:], vd[old:], seg[old:], np.arange(old, n), [len(parts)], [rows], qd, o)
     a2t.a2t_sync(c)
     a2t.a2t_cache_destroy(c)
-    for part, unit in ((slice(0, old), 0), (slice(old, n), 1)):
+    for unit, part in enumerate([*parts, slice(old, n)]):
         ref.append(seg[part], np.arange(n)[part], unit, {0: k[part]}, {0: v[part]})
     want, bound = ref.attention_bound(0, q, rows, least=0.0)
     off = np.abs(o.float().cpu().numpy().astype(np.float64) - want) - bound
