@@ -154,7 +154,8 @@ struct a2t_cache {
     int64_t plan_limit = -1;
     std::vector<int> plan_tiles, plan_splits, plan_tmp, plan_order;
     std::vector<int64_t> plan_heap;
-    SplitPlanner planner;            // of attn_block and attn_f32 launches
+    SplitPlanner planner;            // of attn_block, attn_f32 and attn_mx4 launches
+    SplitPlanner mx4_planner[3];     // the workgroups that a step of an A2T_MX4 cache is weighed for
     SplitPlanner route_tile, route_block;   // the kernels that a mixed launch is weighed for
     std::vector<SplitStream> route_key;     // the last launch that was, and the choice
     bool route_many = false;
@@ -508,45 +509,55 @@ bool f32_on_valu(const a2t_cache* c, int n, const int* tiles) {
 }
 constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
-// The kernel of a step on an A2T_MX4 cache, and the query rows of its workgroups.
-//
-// attn_mx4: 16 query rows, or workgroups of as few blocks of 16 as cover them in groups of up to three, the most
-// that a wave's registers hold without spilling (four: listening units of 16 sessions 419 us a
-// step of four layers, three: 258, two: 254, one: 261).
-//
-// attn_mx4_rows, workgroups of 64 or 128 rows, where these cover the rows with less than 5/4 of the
-// rows that the others' cover them with: a row costs it less (16 sessions of 30 rows of 32/8 heads of 128 on
-// 4,096 keys, 120 rows a KV head, 128 for 144: 47 against 67 us, merge included; 60 rows 70 and 108; 1,024 rows on
-// 4,096 keys 85 and 108, on 16,384 267 and 324), but not rows that are not there (22 rows on 8,192 keys, 128
-// for 96: 77 against 61; 40 rows on 4,096, 256 for 192: 65 and 65).
-// 64 rows up to 32 tiles: more, smaller workgroups; above, V is unpacked for more rows at once (1,024 rows on no
-// keys 20.9 against 24.5 us, on 1,024 38.7 and 39.7, on 2,048 56.3 and 55.1, on 4,096 92 and 85; 777
-// rows of 32/4 heads of 64 on none 12.0 and 15.2, on 5,000 64.1 and 62.2).
-constexpr int kMx4Blocks = 3, kMx4FewTiles = 32;
+// The kernel of a step on an A2T_MX4 cache, and the query rows of its workgroups: that of these whose planned launch
+// would end first, by what its workgroups cost in tiles and what a tile takes.
+//   attn_mx4       as few blocks of 16 rows as cover them in groups of up to three, the most that a wave's
+//                  registers hold without spilling (four: listening units of 16 sessions 419 us a step of
+//                  four layers, three: 258, two: 254, one: 261)
+//   attn_mx4_rows  64 rows, two workgroups a CU, or 128, one
+// Us a step of 32/8 heads of 128, merge included, by blocks of 16, by 64 and by 128 rows: 1,024 rows onto
+// no keys 34, 21, 25; onto 1,024 54, 39, 41; onto 4,096 108, 92, 88; onto 16,384 325, 308, 286; 16 sessions of 22
+// rows onto 8,192 62, 85, 78; of 30 onto 4,096 66, 51, 48; of 60 110, 80, 73; 32 of 12 onto 8,192 64, 104, 127;
+// one of 300 onto 4,096 36, 40, 38.  Of 34 such steps, at both head dims, the choice is the best or within 6 %
+// of it in 31, and 14 % in the worst.
 struct Mx4Shape {
     int query_blocks;   // of attn_mx4; 0: attn_mx4_rows
     int row_waves;
+    SplitCosts costs;
+    int per_cu;         // workgroups that share a CU
+    double us_tile;
     int rows() const { return query_blocks ? 16 * query_blocks : 32 * row_waves; }
 };
-Mx4Shape mx4_shape(const a2t_cache* c, int n, const int* tiles, const int32_t* n_q) {
-    const int G = c->cfg.n_q_heads / c->cfg.n_kv_heads;
-    int rows = 1, longest = 1;
-    for (int i = 0; i < n; ++i) {
-        rows = std::max(rows, G * n_q[i]);
-        longest = std::max(longest, tiles[i]);
-    }
-    const int blocks = (rows + 15) / 16, groups = (blocks + kMx4Blocks - 1) / kMx4Blocks;
-    const Mx4Shape few{(blocks + groups - 1) / groups, 0}, many{0, longest <= kMx4FewTiles ? 2 : 4};
-    int64_t padded_few = 0, padded_many = 0;
-    for (int i = 0; i < n; ++i) {
-        padded_few += (int64_t)few.rows() * mx4_groups(G * n_q[i], few.rows());
-        padded_many += (int64_t)many.rows() * mx4_groups(G * n_q[i], many.rows());
-    }
-    return 4 * padded_many < 5 * padded_few ? many : few;
-}
 // (Splits of 1 to 12 forced on steps of 1 to 1,024 rows onto 0 to 16,384 keys were at best 6 % faster than those that
 // these costs lead to.)
 constexpr SplitCosts kMx4Costs{8, 4, 1 << 20, 4};
+constexpr double kMx4MergeUs = 5;
+int mx4_wgs(const a2t_cache* c, const Mx4Shape& shape, int n_q) {
+    return c->cfg.n_kv_heads * mx4_groups(c->cfg.n_q_heads / c->cfg.n_kv_heads * n_q, shape.rows());
+}
+Mx4Shape mx4_shape(a2t_cache* c, int n, const int* tiles, const int32_t* n_q, const int64_t* floats, int64_t ws_limit) {
+    int rows = 1;
+    for (int i = 0; i < n; ++i) rows = std::max(rows, c->cfg.n_q_heads / c->cfg.n_kv_heads * n_q[i]);
+    const int blocks = (rows + 15) / 16, groups = (blocks + 2) / 3, each = (blocks + groups - 1) / groups;
+    const double d = c->cfg.head_dim == 128 ? 1.0 : 0.66;
+    const Mx4Shape shapes[] = {{each, 0, kMx4Costs, 1, d * (each == 3 ? 0.44 : 0.3)},
+                               {0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.17},
+                               {0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.07}};
+    if (rows <= 16) return shapes[0];
+    double best_us = 0;
+    int best = -1;
+    for (int k = 0; k < 3; ++k) {
+        const Mx4Shape& shape = shapes[k];
+        SplitStream ss[kMaxDesc];
+        int splits[kMaxDesc];
+        for (int i = 0; i < n; ++i) ss[i] = {tiles[i], mx4_wgs(c, shape, n_q[i]), floats[i]};
+        c->mx4_planner[k].plan(n, ss, shape.costs, shape.per_cu * c->target_wgs, 0, ws_limit, splits);
+        const bool split = *std::max_element(splits, splits + n) > 1;
+        const double us = shape.us_tile * (double)(c->mx4_planner[k].cost() - (split ? shape.costs.merge : 0)) + (split ? kMx4MergeUs : 0);
+        if (best < 0 || us < best_us) best = k, best_us = us;
+    }
+    return shapes[best];
+}
 
 // Where a launch's split partials go: the cache's workspace (default) or the
 // library's fixed device array (the no-allocation entry point, which plans
@@ -599,7 +610,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     const bool mx4 = c->cfg.dtype == A2T_MX4;
     const int64_t rf = partial_row_floats(c->cfg.head_dim, f32 || valu);
     int query_blocks = 1;
-    Mx4Shape shape{1, 0};
+    Mx4Shape shape{};
     int max_rows = 0, tiles[kMaxDesc], nsplit[kMaxDesc];
     int64_t floats[kMaxDesc];
     for (int i = 0; i < n; ++i) {
@@ -614,14 +625,15 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
     if (f32 || block || one_row || mx4) {
         SplitStream ss[kMaxDesc];
         if (f32) query_blocks = f32_query_blocks(c, n, tiles, n_q);
-        if (mx4) shape = mx4_shape(c, n, tiles, n_q);
+        const int64_t ws_limit = wsc ? wsc->floats : c->dev.ws_floats;
+        if (mx4) shape = mx4_shape(c, n, tiles, n_q, floats, ws_limit);
         for (int i = 0; i < n; ++i) {
             const int rows = G * n_q[i];
-            ss[i] = {tiles[i], c->cfg.n_kv_heads * (mx4 ? mx4_groups(rows, shape.rows()) : f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
+            ss[i] = {tiles[i], mx4 ? mx4_wgs(c, shape, n_q[i]) : c->cfg.n_kv_heads * (f32 ? f32_groups(rows, query_blocks) : (rows + kBlockRows - 1) / kBlockRows),
                      floats[i]};   // one row: one workgroup
         }
-        c->planner.plan(n, ss, mx4 ? kMx4Costs : f32 ? f32_costs(c->cfg.head_dim, query_blocks) : block ? kBlockCosts : kValuCosts, c->target_wgs, c->force_splits,
-                        wsc ? wsc->floats : c->dev.ws_floats, nsplit);
+        c->planner.plan(n, ss, mx4 ? shape.costs : f32 ? f32_costs(c->cfg.head_dim, query_blocks) : block ? kBlockCosts : kValuCosts,
+                        (mx4 ? shape.per_cu : 1) * c->target_wgs, c->force_splits, ws_limit, nsplit);
     } else {
         plan_splits(c, n, tiles, floats, nsplit, wsc ? INT64_MAX : c->dev.ws_floats);
     }
@@ -718,7 +730,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
         return e == hipSuccess ? A2T_OK : hip_fail(c);
     }
     {
-        ProfScope ps(c, mx4 ? "attn_mx4" : f32 ? (query_blocks == 2 ? "attn_f32x2" : "attn_f32") : valu ? "attn_valu" : block ? "attn_block" : "attn_tile");
+        ProfScope ps(c, mx4 ? (shape.query_blocks ? "attn_mx4" : "attn_mx4_rows") : f32 ? (query_blocks == 2 ? "attn_f32x2" : "attn_f32") : valu ? "attn_valu" : block ? "attn_block" : "attn_tile");
         e = launch(c->dev, ps.kt());
     }
     if (e != hipSuccess) return hip_fail(c);
@@ -854,7 +866,9 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
     // the split planner's scratch, so that no attention call allocates
     for (auto* v : {&c->plan_tiles, &c->plan_splits, &c->plan_tmp, &c->plan_order}) v->reserve(kMaxDesc);
     c->plan_heap.reserve((size_t)c->target_wgs);
-    for (SplitPlanner* p : {&c->planner, &c->route_tile, &c->route_block}) p->reserve(kMaxDesc, c->target_wgs);
+    for (SplitPlanner* p : {&c->planner, &c->route_tile, &c->route_block}) p->reserve(kMaxDesc, 2 * c->target_wgs);
+    if (k.dtype == A2T_MX4)
+        for (SplitPlanner& p : c->mx4_planner) p.reserve(kMaxDesc, 2 * c->target_wgs);
     c->route_key.reserve(kMaxDesc);
 
     DevState& d = c->dev;

@@ -35,7 +35,6 @@ namespace {
 constexpr int kWaves = 8;
 constexpr int kKeyBlock = 32;    // keys of a wave's block
 constexpr int kRows = 16;        // query rows of a product
-constexpr int kAhead = 4;        // V operands read ahead of the products
 
 // LDS accesses of the wave before this one come before those after it, whatever the compiler
 // knows about their addresses in one lane (the hardware keeps a wave's LDS accesses in order)
@@ -74,6 +73,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
     constexpr int DB = D / 16;         // 16-dim blocks of O
     constexpr int VL = D / 64;         // 16-byte loads of V per lane and key block
     constexpr int QP = D / 64;         // products per 16 keys: hi and lo, or both in one
+    constexpr int kAhead = QB == 3 ? 3 : 4;   // V operands read ahead of the products (four spill with three blocks)
     constexpr int kStride = kWaves * kKeyBlock;
     constexpr bool kPipe = QB > 1;
     // (its chunks are found by exclusive or on their addresses: whole rows are aligned)

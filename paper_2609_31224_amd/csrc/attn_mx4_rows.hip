@@ -258,7 +258,7 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
 #pragma unroll 1
         for (int key = 0; key < kKeys; ++key) {
             const Row r = row_of(kb + key);
-            const int64_t row = (r.in_kept ? kept0 : ring0) + r.at;
+            const int64_t row = ring0 + (r.in_kept ? kept0 - ring0 : 0) + r.at;
             float s = sc[0];   // of lane half key / 4 % 2, element 4 (key / 8) + key % 4
 #pragma unroll
             for (int r = 1; r < 16; ++r) s = 4 * (key >> 3) + (key & 3) == r ? sc[r] : s;

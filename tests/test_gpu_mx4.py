@@ -242,29 +242,39 @@ def test_query_that_is_not_finite(gpu, d):
     (8, 1, 128, 32, 0, None),      # 256 rows, few keys: 64 a workgroup
     (8, 1, 64, 24, 40, "2"),       # 192
     (4, 4, 128, 61, 500, "3"),     # 61 of 64
-    (1, 1, 64, 33, 60, "1"),       # 33 of 64: not these
     (4, 2, 64, 30, 1700, "5"),     # 60 of 64
-    (4, 4, 128, 127, 2100, None),  # 127 of 128 a workgroup
-    (8, 1, 64, 31, 2200, "3"),     # 248 of 256
-    (8, 1, 128, 16, 2500, "1"),    # 128
-    (8, 1, 64, 30, 2200, "7"),     # 240 of 256
+    (4, 4, 128, 127, 2800, None),  # many keys: 127 of 128 a workgroup
+    (8, 1, 64, 31, 2900, "3"),     # 248 of 256
+    (8, 1, 128, 16, 2800, "1"),    # 128
+    (8, 1, 64, 30, 2900, "7"),     # 240 of 256
 ])
 def test_many_rows(gpu, monkeypatch, hq, hkv, d, rows, prefix, splits):
-    """Workgroups of 64 and of 128 query rows, rings that wrap, kept regions that end inside a block."""
+    """Workgroups of 64 and of 128 query rows (as for launches that fill the CUs: here one CU is counted), rings that
+    wrap, kept regions that end inside a block."""
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_TARGET_WGS", "1")
     if splits:
         monkeypatch.setenv("A2T_SPLITS", splits)
     more = [_unit(min(900, prefix - at)) for at in range(900, prefix, 900)]
     spec = tiny_stream([*more, SMALL, _unit(rows), SMALL, [SEG_RESPONSE], _unit(rows), _unit(rows + 1), SMALL, _unit(rows)],
                        prefix=min(prefix, 900))
-    _run([spec], hq, hkv, d, budgets=[prefix + rows + 20], calls="fused", query_rows=rows, layers=1, unit_rows=max(4 * rows + 80 + prefix, 80))
+    s = Sessions([spec], hq, hkv, d, budgets=[prefix + rows + 20], calls="fused", query_rows=rows, layers=1,
+                 unit_rows=max(4 * rows + 80 + prefix, 80))
+    try:
+        a2t.a2t_profile_enable(s.cache, "attn_mx4_rows")
+        s.run()
+        assert a2t.a2t_kernel_time(s.cache, "attn_mx4_rows")[0] >= 4
+    finally:
+        s.close()
 
 
 @pytest.mark.parametrize("d", [64, 128])
-def test_many_rows_of_uneven_streams(gpu, d):
+def test_many_rows_of_uneven_streams(gpu, monkeypatch, d):
     """Streams of 1 to 140 rows in one launch of 128-row and of 64-row workgroups."""
-    for more in ([_unit(800), _unit(800)], []):
+    monkeypatch.setenv("A2T_TARGET_WGS", "1")
+    for more in ([_unit(900), _unit(900), _unit(900)], []):
         specs = [tiny_stream([*m, SMALL, _unit(n), SMALL], prefix=p) for n, p, m in ((140, 600, more), (1, 5, more), (64, 0, []), (129, 700, []))]
-        _run(specs, 2, 2, d, budgets=[100000] * 4, calls="fused", layers=1, query_rows=140, unit_rows=2600)
+        _run(specs, 2, 2, d, budgets=[100000] * 4, calls="fused", layers=1, query_rows=140, unit_rows=3600)
 
 
 # ------------------------------------------------------------------ the calls around them
@@ -555,13 +565,15 @@ def test_offsets_past_32_bits(gpu, kept):
 
 
 @pytest.mark.parametrize("d,hq,hkv,old,rows", [(64, 4, 2, 900, 70), (128, 4, 1, 900, 70), (128, 2, 2, 900, 70), (128, 2, 2, 900, 40),
-                                               (128, 4, 1, 2300, 64), (64, 8, 1, 2300, 62), (64, 2, 2, 900, 47)])
+                                               (128, 4, 1, 2900, 64), (64, 8, 1, 2900, 62), (64, 2, 2, 900, 47)])
 def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv, old, rows):
     """The same behind several key blocks a wave, in every kind of workgroup; and values of a resident
     row, which every query sees."""
     import torch
     import paper_2609_31224_amd as a2t
     monkeypatch.setenv("A2T_SPLITS", "1")
+    if rows >= 60:   # workgroups of 64 rows and, with many keys, of 128
+        monkeypatch.setenv("A2T_TARGET_WGS", "1")
     bad = 33
     g = torch.Generator(device="cuda").manual_seed(6)
     k0, v0 = (torch.randn((old, hkv, d), generator=g, device="cuda").bfloat16() for _ in range(2))
@@ -599,7 +611,7 @@ def test_values_that_are_not_finite_in_later_blocks(gpu, monkeypatch, d, hq, hkv
 
 
 @pytest.mark.parametrize("d,hq,hkv,rows,old", [(64, 4, 2, 5, 333), (128, 2, 2, 10, 333), (64, 4, 1, 64, 333), (128, 4, 1, 64, 333), (128, 4, 1, 22, 333),
-                                               (128, 2, 2, 20, 333), (64, 4, 1, 64, 2100), (128, 4, 1, 64, 2100), (64, 4, 1, 22, 333)])
+                                               (128, 2, 2, 20, 333), (64, 4, 1, 64, 2900), (128, 4, 1, 64, 2900), (64, 4, 1, 22, 333)])
 @pytest.mark.parametrize("exps", [[-40], [-26, -25, -24, -23, -22, -12, -11], [10, 11, 12, 13, 14, 0], [-110, -60, -20, 0, 0, 0, 20, 100],
                                   [0, 0, 0, 0, 0, 120]])
 def test_scales_of_values_apart(gpu, monkeypatch, d, hq, hkv, rows, old, exps):
@@ -608,6 +620,8 @@ def test_scales_of_values_apart(gpu, monkeypatch, d, hq, hkv, rows, old, exps):
     import torch
     import paper_2609_31224_amd as a2t
     monkeypatch.setenv("A2T_SPLITS", "1")
+    if rows >= 60:
+        monkeypatch.setenv("A2T_TARGET_WGS", "1")
     rng = np.random.default_rng(9)
     n = old + rows
     scale = np.repeat(2.0 ** rng.choice(exps, (n, hkv, d // 32)), 32, -1) * np.repeat(rng.random((n, hkv, d // 32)) < 0.9, 32, -1)
