@@ -9,8 +9,8 @@
 // 16x16x32 adds 14 and takes 17), so that larger ones leave them more.  V is unpacked once a workgroup and stage,
 // each wave its share, not once a wave.  Queries stay in registers.
 // Bounds: vector operations (~105 a wave and block of 32 x 32, exponentials and their roundings half of them)
-// and power: the clock falls to 1.85 GHz under 1,024 rows onto 16,384 keys (984 cycles a block and
-// SIMD, 385 of them products).  That launch takes 267 us, attn_mx4's waves of 48 rows 324.
+// and power: the clock falls to 1.9 GHz under 1,024 rows onto 16,384 keys (~1,000 cycles a block and
+// SIMD, 385 of them products).  That launch takes 270 to 286 us, card by card, attn_mx4's waves of 48 rows 325.
 #include "a2t_internal.h"
 #include "mx4_device.h"
 
@@ -258,7 +258,8 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
 #pragma unroll 1
         for (int key = 0; key < kKeys; ++key) {
             const Row r = row_of(kb + key);
-            const int64_t row = ring0 + (r.in_kept ? kept0 - ring0 : 0) + r.at;
+            const uint8_t* const codes = pick(r, v_kept, v_ring, CB) - 16 * (lane % NB);
+            const uint8_t* const scales = pick(r, vs_kept, vs_ring, NB) - lane % NB;
             float s = sc[0];   // of lane half key / 4 % 2, element 4 (key / 8) + key % 4
 #pragma unroll
             for (int r = 1; r < 16; ++r) s = 4 * (key >> 3) + (key & 3) == r ? sc[r] : s;
@@ -266,11 +267,11 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
             if (kb + key > see_to) continue;
 #pragma unroll
             for (int c = 0; c < NB; ++c) {
-                const int byte = gload1(vp.scales + row * NB + c);
+                const int byte = gload1(scales + c);
                 if (!mx4_odd(byte)) continue;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {   // dims 32 c + 8 i + 4 h ..
-                    const uint8_t* at = vp.codes + row * CB + 16 * c + 4 * i + 2 * h;
+                    const uint8_t* at = codes + 16 * c + 4 * i + 2 * h;
                     const f32x4 v = mx4_to_f32(gload1(at) | gload1(at + 1) << 8, byte);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[c][4 * i + e] += v[e] * pr;
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
 #pragma unroll 1
         for (; stage_key(i) < end_w; ++i) {
             uint32_t v_out = v_out0 + (i & 1) * kBuf;
-#pragma unroll 1
+#pragma unroll
             for (int blk = 0; blk < SB; ++blk, v_out += kKeys * D * 2) {
                 const int kb = stage_key(i) + blk * kKeys;
                 // the block after the next (past the last one: row R - 1)
@@ -326,8 +327,8 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
                 asm volatile("" : "+v"(p[0]), "+v"(p[1]), "+v"(lsum[0]), "+v"(lsum[1]));   // before the scores: in their registers
                 if (blk == 0 && i + 1 < passes) take_v(odd, (i & 1) ^ 1);
                 score();
+                load_k(after);   // the one needed first
                 if (blk == 0) load_v(stage_key(i + 2));
-                load_k(after);
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
