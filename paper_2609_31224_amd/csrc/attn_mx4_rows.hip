@@ -8,9 +8,9 @@
 // ~20 cycles whatever its size (32x32x16 f16 adds 17 to 19 to a run of vector operations and takes 33 by itself,
 // 16x16x32 adds 14 and takes 17), so that larger ones leave them more.  V is unpacked once a workgroup and stage,
 // each wave its share, not once a wave.  Queries stay in registers.
-// Bounds: vector operations (~105 a wave and block of 32 x 32, exponentials and their roundings half of them)
-// and power: the clock falls to 1.9 GHz under 1,024 rows onto 16,384 keys (~1,000 cycles a block and
-// SIMD, 385 of them products).  That launch takes 270 to 286 us, card by card, attn_mx4's waves of 48 rows 325.
+// Bounds: vector operations (~105 a wave and block of 32 x 32, exponentials and their roundings half of them),
+// products and what neither hides: 52 % and 35 % of the cycles of 1,024 rows onto 16,384 keys, at a clock that
+// power holds at 1.85 to 2.0 GHz.  That launch takes 270 to 286 us, card by card, attn_mx4's waves of 48 rows 325.
 #include "a2t_internal.h"
 #include "mx4_device.h"
 

@@ -96,7 +96,9 @@ __device__ __forceinline__ int mx4_query(const float* block, u32x6* hi, u32x6* l
     *hi = *lo = u32x6{0u, 0u, 0u, 0u, 0u, 0u};
     if (big >= 0x7f800000u) return kMxNaN;
     const int scale = max((int)((big + 0x80000u) >> 23) - 2, 5);
-    const float unit = __uint_as_float((uint32_t)scale << 23);
+    // (The conversions take several passes, and a result may not lie in their operands' registers, which the
+    // compiler does not know: operands are kept until after them.)
+    float unit = __uint_as_float((uint32_t)scale << 23);
     *hi = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
     const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(*hi, unit);
 #pragma unroll
@@ -104,8 +106,7 @@ __device__ __forceinline__ int mx4_query(const float* block, u32x6* hi, u32x6* l
         even[e] -= back[2 * e];
         odd[e] -= back[2 * e + 1];
     }
-    // (the conversions take several passes: a result may not lie in their operands' registers, which the
-    // compiler does not know: the operands of the last one are kept until after it)
+    asm volatile("" : "+v"(unit), "+v"(*hi), "+v"(even), "+v"(odd));
     float unit_lo = unit * 0.0625f;
     *lo = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit_lo);
     asm volatile("" : "+v"(*lo), "+v"(unit_lo), "+v"(even), "+v"(odd));
