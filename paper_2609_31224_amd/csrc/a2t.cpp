@@ -155,7 +155,7 @@ struct a2t_cache {
     std::vector<int> plan_tiles, plan_splits, plan_tmp, plan_order;
     std::vector<int64_t> plan_heap;
     SplitPlanner planner;            // of attn_block, attn_f32 and attn_mx4 launches
-    SplitPlanner mx4_planner[3];     // the workgroups that a step of an A2T_MX4 cache is weighed for
+    SplitPlanner mx4_planner[4];     // the workgroups that a step of an A2T_MX4 cache is weighed for
     SplitPlanner route_tile, route_block;   // the kernels that a mixed launch is weighed for
     std::vector<SplitStream> route_key;     // the last launch that was, and the choice
     bool route_many = false;
@@ -510,22 +510,21 @@ bool f32_on_valu(const a2t_cache* c, int n, const int* tiles) {
 constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
 // The kernel of a step on an A2T_MX4 cache, and the query rows of its workgroups: that of these whose planned launch
-// would end first, by what its workgroups cost in tiles and what a tile takes.
-//   attn_mx4       as few blocks of 16 rows as cover them in groups of up to three, the most that a wave's
-//                  registers hold without spilling (four: listening units of 16 sessions 419 us a step of
-//                  four layers, three: 258, two: 254, one: 261)
+// would end first, by what its workgroups cost in tiles, what a tile and the rest of a launch take.
+//   attn_mx4       one, two or three blocks of 16 rows, one workgroup a CU (four blocks spill: listening units
+//                  of 16 sessions 419 us a step of four layers, three: 258, two: 254, one: 261)
 //   attn_mx4_rows  64 rows, two workgroups a CU, or 128, one
-// Us a step of 32/8 heads of 128, merge included, by blocks of 16, by 64 and by 128 rows: 1,024 rows onto
-// no keys 34, 21, 25; onto 1,024 54, 39, 41; onto 4,096 108, 92, 88; onto 16,384 325, 308, 286; 16 sessions of 22
-// rows onto 8,192 62, 85, 78; of 30 onto 4,096 66, 51, 48; of 60 110, 80, 73; 32 of 12 onto 8,192 64, 104, 127;
-// one of 300 onto 4,096 36, 40, 38.  Of 34 such steps, at both head dims, the choice is the best or within 6 %
-// of it in 31, and 14 % in the worst.
+// Us a layer of 32/8 heads of 128, merge included, layers whose rows no cache holds in turn, by 48, 32, 64 and 128 rows:
+// 1,024 rows onto no keys 34, 36, 24, 25; onto 1,024 50, 54, 40, 38; onto 4,096 98, 108, 88, 80; onto 16,384 295, 325,
+// 295, 251; 16 sessions of 22 rows onto 8,192 64, 87, 84, 77; of 30 onto 4,096 66, 54, 55, 49; of 60 109, 103, 85, 76;
+// one of 22 onto 4,096 15.6, 14.3, 16.3, 16.8; 777 rows of 32/4 heads of 64 onto none 22, 24, 12, 15.  The times
+// below are fitted to 48 such steps, at both head dims: the choice is the best of the four or within 3 % of it.
 struct Mx4Shape {
     int query_blocks;   // of attn_mx4; 0: attn_mx4_rows
     int row_waves;
     SplitCosts costs;
     int per_cu;         // workgroups that share a CU
-    double us_tile;
+    double us_tile, us_launch;
     int rows() const { return query_blocks ? 16 * query_blocks : 32 * row_waves; }
 };
 // (Splits of 1 to 12 forced on steps of 1 to 1,024 rows onto 0 to 16,384 keys were at best 6 % faster than those that
@@ -538,22 +537,23 @@ int mx4_wgs(const a2t_cache* c, const Mx4Shape& shape, int n_q) {
 Mx4Shape mx4_shape(a2t_cache* c, int n, const int* tiles, const int32_t* n_q, const int64_t* floats, int64_t ws_limit) {
     int rows = 1;
     for (int i = 0; i < n; ++i) rows = std::max(rows, c->cfg.n_q_heads / c->cfg.n_kv_heads * n_q[i]);
-    const int blocks = (rows + 15) / 16, groups = (blocks + 2) / 3, each = (blocks + groups - 1) / groups;
     const double d = c->cfg.head_dim == 128 ? 1.0 : 0.66;
-    const Mx4Shape shapes[] = {{each, 0, kMx4Costs, 1, d * (each == 3 ? 0.44 : 0.3)},
-                               {0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.17},
-                               {0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.07}};
-    if (rows <= 16) return shapes[0];
+    const Mx4Shape shapes[] = {{3, 0, kMx4Costs, 1, d * 0.44, 3},
+                               {2, 0, kMx4Costs, 1, d * 0.38, 2},
+                               {0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.25, 4},
+                               {0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.05, 4}};
+    if (rows <= 16) return {1, 0, kMx4Costs, 1, 0, 0};
     double best_us = 0;
     int best = -1;
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 4; ++k) {
         const Mx4Shape& shape = shapes[k];
         SplitStream ss[kMaxDesc];
         int splits[kMaxDesc];
         for (int i = 0; i < n; ++i) ss[i] = {tiles[i], mx4_wgs(c, shape, n_q[i]), floats[i]};
         c->mx4_planner[k].plan(n, ss, shape.costs, shape.per_cu * c->target_wgs, 0, ws_limit, splits);
         const bool split = *std::max_element(splits, splits + n) > 1;
-        const double us = shape.us_tile * (double)(c->mx4_planner[k].cost() - (split ? shape.costs.merge : 0)) + (split ? kMx4MergeUs : 0);
+        const double us = shape.us_launch + shape.us_tile * (double)(c->mx4_planner[k].cost() - (split ? shape.costs.merge : 0)) +
+                          (split ? kMx4MergeUs : 0);
         if (best < 0 || us < best_us) best = k, best_us = us;
     }
     return shapes[best];
