@@ -80,7 +80,7 @@
  *   is NaN throughout.  K is rotated with the rotary table's cosines (fp64
  *   angles, rounded to fp32) and rounded to fp32 once before it is encoded.
  *   Attention is that of the values held: their products with rotated queries,
- *   which are rounded by at most 2^-8.9 of the largest element of their block of
+ *   which are rounded by at most 2^-13.9 of the largest element of their block of
  *   32, fp32 sums, probabilities rounded to fp16.
  *   Values of non-finite rows reach only the queries that see them.
  */

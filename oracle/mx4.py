@@ -75,14 +75,16 @@ class OracleMx4Cache(OracleCache):
 
     def attention_bound(self, layer, q, n_q, least=1e-6):
         """(o, bound): attention as OracleCache.attention's, and what a computation may be off by
-        that holds rotated queries as two e2m3 numbers (an error of up to 1/128 unit, the largest
+        that holds rotated queries as three e2m3 numbers (an error of up to 1/4096 unit, the largest
         magnitude of a block of 32 being at least 3.875 units; independent from element to
         element), probabilities to 11 significant bits or 2^-25 of the largest, partial outputs to 11
         and the output to 8; `least`: and that partial outputs are fp16.
 
-        A score's error is a sum of D independent ones, uniform in +- a_b |k_i| / (128 * 3.875), a_b the
+        A score's error is a sum of D independent ones, uniform in +- a_b |k_i| / (4096 * 3.875), a_b the
         largest magnitude of the query's block: six of its standard deviations are taken as its
-        bound.  An error d_j of the scores moves the output by p_j d_j (v_j - o) to first order,
+        bound.  Besides, fp32 roundings of the rotation (four of 2^-24 of |x_i| + |x_{i+D/2}|), of the score's
+        sum and of its difference to the reference (twelve of 2^-24 of the sum of magnitudes): 2^-20 of
+        sum |k_i| (|x_i| + |x_{i+D/2}|).  An error d_j of the scores moves the output by p_j d_j (v_j - o) to first order,
         an error e_j of a probability by e_j (v_j - o); fp32 sums and exponentials take as much as
         2^-13 of the sum of magnitudes."""
         q_pos = self.pos[self.resident - n_q:]
@@ -92,13 +94,16 @@ class OracleMx4Cache(OracleCache):
         bound = np.zeros_like(o)
         G = self.Hq // self.Hkv
         mask = self.pos[None, :] <= q_pos[:, None]
+        both = np.abs(np.asarray(q, np.float64))
+        both = both + np.roll(both, both.shape[-1] // 2, -1)
         for h in range(self.Hq):
             kk, vv = k[:, h // G], v[:, h // G]
             s = np.where(mask, self.scale * (q_rot[:, h] @ kk.T), -np.inf)
             p = np.exp(s - s.max(1, keepdims=True))
             p /= p.sum(1, keepdims=True)
             most = np.repeat(np.abs(q_rot[:, h]).reshape(n_q, -1, BLOCK).max(-1), BLOCK, -1)
-            d = 6 * self.scale / (128 * 3.875 * np.sqrt(3)) * np.sqrt(np.square(most) @ np.square(kk).T)
+            d = 6 * self.scale / (4096 * 3.875 * np.sqrt(3)) * np.sqrt(np.square(most) @ np.square(kk).T)
+            d += 2.0 ** -20 * self.scale * (both[:, h] @ np.abs(kk).T)
             for i in range(n_q):
                 w = p[i] * d[i]
                 e = np.where(mask[i], np.maximum(2.0 ** -11 * p[i], 2.0 ** -25 * p[i].max()), 0.0)

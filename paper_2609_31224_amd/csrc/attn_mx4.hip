@@ -6,13 +6,16 @@
 //             states are combined in LDS at the end.
 //
 // Scores: v_mfma_scale_f32_16x16x128_f8f6f4 multiplies K as it is stored, scales included,
-// with Q in e2m3 (6 bits): a block of 32 rotated elements is scaled by a power of two and
-// written as hi + lo, both e2m3, lo with a scale of 2^-4.  hi is off by up to 1/4 unit where the largest
-// element has 3.875 to 7.75 of them, and hi + lo by up to 1/128 (elements above 4 units; 1/256 below): 2^-8.9
-// of the block's largest element, where bf16 is off by up to 2^-8 of each.  (Both in e4m3, 2^-8 of each
-// too: products at half the rate, 1,024 rows onto 16,384 keys 337 us instead of 318.)  At head dim 128 that
-// is two products per 16 keys, at 64 one, whose first 64 dims are K times hi and whose last 64 are K
-// times lo.
+// with Q in e2m3 (6 bits): a block of 32 rotated elements is scaled by a power of two and written as three
+// e2m3 numbers an element, the later ones with scales 2^-4 and 2^-9 of the first one's.  The first is off by up to
+// 1/4 unit where the largest element has 3.875 to 7.75 of them, two by up to 1/128, three by 1/4096: 2^-13.9 of
+// the block's largest element.  The error is the same for the block's small elements, and their keys may be the
+// large ones: with four channels of Q 50 times and four others of K 20 times the rest, outputs are off by 0.0178 of
+// their size with two numbers, 0.0003 with three and 0.0026 with Q in bf16.  The third costs 10 % of the time of
+// long chunks and of units, none of decode on many keys (1,024 rows onto 16,384 keys 283 -> 311 us, 16 sessions of 22 rows onto
+// 8,192 63 -> 70).  (Two numbers in e4m3 take the products' time of four in e2m3.)  At head dim 128 that is
+// three products per 16 keys, at 64 two: K times the first part with K times the second in one's 128 dims, and K
+// times the third in half of the other's.
 // Values: a lane's 16 bytes of V are a block, which the scaled conversion turns into fp16
 // (exactly); transposed LDS reads then give the operand of v_mfma_f32_16x16x32_f16.  The few blocks
 // that fp16 does not hold are added in fp32.  Probabilities are fp16, relative to a reference that
@@ -78,8 +81,9 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
     constexpr int CB = D / 2;          // bytes of a row's codes
     constexpr int DB = D / 16;         // 16-dim blocks of O
     constexpr int VL = D / 64;         // 16-byte loads of V per lane and key block
-    constexpr int QP = D / 64;         // products per 16 keys: hi and lo, or both in one
-    constexpr int kAhead = QB == 3 ? 3 : 4;   // V operands read ahead of the products (four spill with three blocks)
+    constexpr int QP = D == 128 ? 3 : 2;   // products per 16 keys: one for each part of Q, or the first two in one
+    constexpr int kInRegs = QB == 1 && D == 128 ? 2 : QP;   // products whose Q operand stays in registers, of one block of rows
+    constexpr int kAhead = QB == 3 ? 2 : 4;   // V operands read ahead of the products (three spill with three blocks)
     constexpr int kStride = kWaves * kKeyBlock;
     constexpr bool kPipe = QB > 1;
     // (its chunks are found by exclusive or on their addresses: whole rows are aligned)
@@ -104,9 +108,9 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
     const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
     const int mw = grp * QB * kRows;   // the workgroup's first query row
     const int vis0 = R - d.n_q;
-    int qi[QB];                        // step row of the lane's queries (past M: that of row M-1)
-#pragma unroll
-    for (int x = 0; x < QB; ++x) qi[x] = min(mw + x * kRows + l16, M - 1) / G;
+    const int g_shift = __builtin_ctz(G);   // (G is 1, 2, 4 or 8)
+    // step row of lane ln's query of block x (past M: that of row M - 1)
+    auto step_row = [&](int x, int ln) { return min(mw + x * kRows + (ln & 15), M - 1) >> g_shift; };
     const int last_i = uniform((min(M, mw + QB * kRows) - 1) / G);
     const int k_end = vis0 + last_i + 1;
     const int t0 = sp * d.tile_q + min(sp, d.tile_r), t1 = t0 + d.tile_q + (sp < d.tile_r ? 1 : 0);
@@ -244,36 +248,33 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
     __syncthreads();
     // Then the operands, a lane a block: with one block of rows every wave makes them for
     // itself, else wave x makes those of the 16 rows x.
-    i32x8 qv[2][QP];   // Q operands (of one block of rows; else read one block ahead of the products)
-    int qs[QB];        // ... and their scales
+    i32x8 qv[QP];   // Q operands: of one block of rows, the last read for each block; else read as the block before is done with them
+    int qs;            // ... and their first part's scales, read with them
     if (QB == 1 || w < QB) {
         const int x0 = QB == 1 ? 0 : w;
-        u32x6 hi, lo;
-        const int scale = mx4_query(s_rows + ((x0 * kRows + l16) * NB + (lg & (NB - 1))) * kPad, &hi, &lo);
+        u32x6 part[kMxQueryParts];
+        const int scale = mx4_query(s_rows + ((x0 * kRows + l16) * NB + (lg & (NB - 1))) * kPad, part);
         auto put = [&](int k, const u32x6& x) {
-            if constexpr (QB == 1) {
-                qv[0][k] = mx4_operand(x);
-            } else {
-                s_q[w][k][lane] = u32x4{x[0], x[1], x[2], x[3]};
-                s_q2[w][k][lane] = make_uint2(x[4], x[5]);
+            if (QB == 1 && k < kInRegs) {
+                qv[k] = mx4_operand(x);
+            } else if (QB > 1 || w == 0) {
+                s_q[QB == 1 ? 0 : w][k][lane] = u32x4{x[0], x[1], x[2], x[3]};
+                s_q2[QB == 1 ? 0 : w][k][lane] = make_uint2(x[4], x[5]);
             }
         };
         int mine = scale;
         if constexpr (D == 128) {
-            put(0, hi);
-            put(1, lo);
-        } else {   // the product's last 64 dims are lo
-            put(0, lg < NB ? hi : lo);
-            mine = lg < NB || scale == kMxNaN ? scale : scale - 4;
+#pragma unroll
+            for (int k = 0; k < QP; ++k) put(k, part[k]);
+        } else {   // the last 64 dims of the products are the second part, and nothing
+            put(0, lg < NB ? part[0] : part[1]);
+            put(1, lg < NB ? part[2] : u32x6{0u, 0u, 0u, 0u, 0u, 0u});
+            mine = lg < NB ? scale : mx4_query_scale(scale, 1);
         }
-        if (QB == 1) qs[0] = mine;
+        if (QB == 1) qs = mine;
         else s_qs[w][lane] = (uint8_t)mine;
     }
     __syncthreads();   // V takes the rows' place
-    if constexpr (QB > 1) {
-#pragma unroll
-        for (int x = 0; x < QB; ++x) qs[x] = s_qs[x][lane];
-    }
 
     // this wave's V: where the lane's block e (of 8 dims) of its first row goes, and the lane's
     // place in the transposed reads (16 lanes read 8 bytes each of four keys' 32 bytes).  The
@@ -301,41 +302,47 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
 
     f32x4 sc[QB][2];   // scores of a block, relative to the running reference
     f16x8 p[QB];       // its probabilities
-    auto read_q = [&](int x, int ln) {
-        if constexpr (QB == 1) return;
-#pragma unroll
-        for (int k = 0; k < QP; ++k) {
-            const u32x4 a = s_q[x][k][ln];
-            const uint2 b2 = s_q2[x][k][ln];
-            qv[x & 1][k] = i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2.x, (int)b2.y, 0, 0};
-        }
+    auto read_part = [&](int x, int k, int ln) {
+        const u32x4 a = s_q[x][k][ln];
+        const uint2 b2 = s_q2[x][k][ln];
+        return i32x8{(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)b2.x, (int)b2.y, 0, 0};
     };
-    auto score = [&](int x) {
+    // those of block x that are not there yet
+    auto read_q = [&](int x, int ln) {
+#pragma unroll
+        for (int k = QB == 1 ? kInRegs : 0; k < QP; ++k) qv[k] = read_part(x, k, ln);
+        if (QB > 1) qs = s_qs[x][ln];
+    };
+    auto score = [&](int x, int ln) {   // and the operands of the next block
         const float mu = mrun[x] == -INFINITY ? 0.f : mrun[x];
 #pragma unroll
         for (int t = 0; t < 2; ++t) sc[x][t] = f32x4{-mu, -mu, -mu, -mu};
 #pragma unroll
         for (int k = 0; k < QP; ++k) {
-            const int s = k == 0 || qs[x] == kMxNaN ? qs[x] : qs[x] - 4;
+            const int s = mx4_query_scale(qs, D == 128 ? k : 2 * k);
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
                 const i32x8 kv = {(int)kc[t][0], (int)kc[t][1], (int)kc[t][2], (int)kc[t][3], 0, 0, 0, 0};
-                sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv[x & 1][k], sc[x][t], 4, 2, 0, ks[t], 0, s);
+                sc[x][t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(kv, qv[k], sc[x][t], 4, 2, 0, ks[t], 0, s);
             }
+            if (x + 1 < QB) qv[k] = read_part(x + 1, k, ln);
+            if (x + 1 < QB && k == QP - 1) qs = s_qs[x + 1][ln];
         }
     };
     // hides what a row does not see, and moves the reference, lazily: the first block sets it (a row that sees
     // none of its keys sees none of the later ones), and it is raised, and the running sums
     // rescaled, only when a block exceeds it by more than 2^8
-    auto settle = [&](int kb, bool first) {
+    auto settle = [&](int kb, bool first, int ln) {
         if (kb + kKeyBlock - 1 > vis0) {   // some row does not see every key
 #pragma unroll
-            for (int x = 0; x < QB; ++x)
+            for (int x = 0; x < QB; ++x) {
+                const int see = vis0 + step_row(x, ln) - kb - 4 * (ln >> 4);
 #pragma unroll
                 for (int t = 0; t < 2; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (kb + 16 * t + 4 * lg + e > vis0 + qi[x]) sc[x][t][e] = -INFINITY;
+                        if (16 * t + e > see) sc[x][t][e] = -INFINITY;
+            }
         }
         float top[QB], most = -INFINITY;
 #pragma unroll
@@ -415,7 +422,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
                     const f32x4 v = mx4_to_f32(gload1(at) | gload1(at + 1) << 8, byte);
 #pragma unroll
                     for (int x = 0; x < QB; ++x)
-                        if (kb + key <= vis0 + qi[x]) acc[x][2 * c + h] += v * pr[x];
+                        if (kb + key <= vis0 + step_row(x, lane)) acc[x][2 * c + h] += v * pr[x];
                 }
             }
         }
@@ -442,19 +449,14 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             load_v(kb_next, next, ln);
             ordered();
             __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-            for (int x = 0; x < QB; ++x) {
-                if (x + 1 < QB) read_q(x + 1, ln);
-                ordered();
-                score(x);
-                ordered();
-            }
+            score(0, ln);
+            ordered();
             __builtin_amdgcn_s_setprio(0);
             load_k(kb_next, next, ln);   // into the registers that the products have read
 #pragma unroll
             for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
             ordered();
-            settle(kb, i == 0);
+            settle(kb, i == 0, ln);
             if (odd) add_odd(kb);
 #pragma unroll
             for (int x = 0; x < QB; ++x) weigh(x), sum(x);
@@ -484,11 +486,12 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             for (int m = 0; m < 4 * VL; ++m) take_v(v_in0, m);
             odd_v(v_in0);
             load_v(kb_next, next, lane);
+            read_q(0, lane);
 #pragma unroll
-            for (int x = 0; x < QB; ++x) read_q(x, lane), score(x);
+            for (int x = 0; x < QB; ++x) score(x, lane);
             fence();
             load_k(kb_next, next, lane);
-            settle(k0, true);
+            settle(k0, true, lane);
             if (odd) add_odd(k0);
         }
         // In each pass the probabilities and products of a block go with the next one's scores and V: the matrix
@@ -512,19 +515,20 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             weigh(0);
 #pragma unroll
             for (int x = 0; x < QB; ++x) {
-                if (x + 1 < QB) read_q(x + 1, ln);
-                else {
+                if (x + 1 == QB) {
 #pragma unroll
                     for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
                 }
                 fence();
-                score(x);
+                score(x, ln);
                 sum(x);
                 if (x + 1 < QB) weigh(x + 1);
 #pragma unroll
                 for (int m = 0; m < 2 * QP + 1; ++m) {
                     __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
                     __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                    if (x + 1 < QB && m % 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    if (x + 1 < QB && m == 2 * QP - 1) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
                 }
                 fence();
             }
@@ -546,7 +550,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             }
             odd_v(v_in);
             load_v(kb_next, next, ln);
-            settle(kb, false);
+            settle(kb, false, ln);
             if (odd) add_odd(kb);
         }
         __builtin_amdgcn_s_setprio(0);
@@ -600,7 +604,8 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             for (int k = 1; k < kWaves; ++k) O += s_part[k][c][lane] * wt[k];
             O *= inv;
             if (whole) {
-                uint16_t* orow = o + ((int64_t)(d.q_row0 + qi[x]) * st.Hq + g * G + (mq - qi[x] * G)) * D;
+                const int i = mq >> g_shift;
+                uint16_t* orow = o + ((int64_t)(d.q_row0 + i) * st.Hq + g * G + (mq - i * G)) * D;
                 *reinterpret_cast<uint2*>(orow + 16 * c + 4 * lg) = make_uint2(pack_bf16x2(O[0], O[1]), pack_bf16x2(O[2], O[3]));
             } else {
                 uint16_t* orow = reinterpret_cast<uint16_t*>(po) + at * D;

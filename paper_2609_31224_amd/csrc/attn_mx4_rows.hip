@@ -7,10 +7,11 @@
 // The products are attn_mx4's (attn_mx4.hip), 32 by 32: a product holds up the vector units for
 // ~20 cycles whatever its size (32x32x16 f16 adds 17 to 19 to a run of vector operations and takes 33 by itself,
 // 16x16x32 adds 14 and takes 17), so that larger ones leave them more.  V is unpacked once a workgroup and stage,
-// each wave its share, not once a wave.  Queries stay in registers.
+// each wave its share, not once a wave.  Two of a query's three parts stay in registers; the third is read from LDS for
+// each block.
 // Bounds: vector operations (~105 a wave and block of 32 x 32, exponentials and their roundings half of them),
 // products and what neither hides: 52 % and 35 % of the cycles of 1,024 rows onto 16,384 keys, at a clock that
-// power holds at 1.85 to 2.0 GHz.  That launch takes 270 to 286 us, card by card, attn_mx4's waves of 48 rows 325.
+// power holds at 1.85 to 2.0 GHz, with two parts a query.  That launch takes 311 us with three, 283 with two.
 #include "a2t_internal.h"
 #include "mx4_device.h"
 
@@ -55,6 +56,8 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
     static_assert(RW * NB * 4096 <= kMem, "a group's states fit");
     // (V's chunks are found by exclusive or on their addresses: whole rows are aligned)
     __shared__ __align__(256) uint8_t s_mem[kMem];   // rotated rows; V of two stages a group; at the end states
+    __shared__ u32x4 s_q[RW][KS][64];     // third parts of the Q operands, their first 16 bytes
+    __shared__ uint2 s_q2[RW][KS][64];    // ... and the other 8
     __shared__ float2 s_ml[RW][kRows];
     __shared__ int s_odd[2][kWaves], s_any;   // a stage's share, any stage has blocks that fp16 does not hold
 
@@ -162,15 +165,26 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
     }
     __syncthreads();
     // Then the wave's operands, a lane a block of each 64 dims.
-    i32x8 qh[KS], ql[KS];   // hi and lo
-    int qs[KS];             // hi's scales; lo's are 2^-4 of them
+    // first and second part; the third is in LDS, where the wave reads it for each block (registers)
+    i32x8 qh[KS], ql[KS];
+    int qs[KS];             // the first part's scales
+    u32x6 q3[KS];
 #pragma unroll
     for (int t = 0; t < KS; ++t) {
-        u32x6 hi, lo;
-        qs[t] = mx4_query(s_rows + ((rw * kRows + l32) * NB + 2 * t + h) * kPad, &hi, &lo);
-        qh[t] = mx4_operand(hi), ql[t] = mx4_operand(lo);
+        u32x6 part[kMxQueryParts];
+        qs[t] = mx4_query(s_rows + ((rw * kRows + l32) * NB + 2 * t + h) * kPad, part);
+        qh[t] = mx4_operand(part[0]), ql[t] = mx4_operand(part[1]);
+        q3[t] = part[2];
     }
     __syncthreads();   // V takes the rows' place
+    if (kg == 0) {   // (both groups of waves have the same rows)
+#pragma unroll
+        for (int t = 0; t < KS; ++t) {
+            s_q[rw][t][lane] = u32x4{q3[t][0], q3[t][1], q3[t][2], q3[t][3]};
+            s_q2[rw][t][lane] = make_uint2(q3[t][4], q3[t][5]);
+        }
+    }
+    __syncthreads();
 
     // V in LDS: where the lane's block e (of 8 dims) of its first row goes, and the lane's
     // place in the transposed reads (16 lanes read 8 bytes each of four keys' 32 bytes).  The
@@ -214,9 +228,12 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
         auto dims = [&](auto x) {
             constexpr int t = decltype(x)::value;
             const i32x8 kv = {(int)kc[t][0], (int)kc[t][1], (int)kc[t][2], (int)kc[t][3], 0, 0, 0, 0};
-            const int lo = qs[t] == kMxNaN ? qs[t] : qs[t] - 4;
+            const u32x4 a = s_q[rw][t][lane];
+            const uint2 a2 = s_q2[rw][t][lane];
+            const i32x8 q3 = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], (int)a2.x, (int)a2.y, 0, 0};
             sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, qh[t], sc, 4, 2, 2 * t, k_scale, 0, qs[t]);
-            sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, ql[t], sc, 4, 2, 2 * t, k_scale, 0, lo);
+            sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, ql[t], sc, 4, 2, 2 * t, k_scale, 0, mx4_query_scale(qs[t], 1));
+            sc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(kv, q3, sc, 4, 2, 2 * t, k_scale, 0, mx4_query_scale(qs[t], 2));
         };
         dims(std::integral_constant<int, 0>());
         if constexpr (KS == 2) dims(std::integral_constant<int, 1>());

@@ -76,42 +76,50 @@ __device__ __forceinline__ void mx4_rotate(const u32x4& a, const u32x4& a2, cons
         reinterpret_cast<f32x4*>(hi)[e] = yh[e];
     }
 }
-// A block of a rotated query, in LDS, as two e2m3 numbers an element: the largest magnitude becomes 3.875 to 7.75
-// units (of e2m3's 7.5) of 2^(scale - 127), the scale byte that is returned; hi is off by up to 1/4
-// unit and lo, in units of 1/16, holds the rest to 1/128.
-__device__ __forceinline__ int mx4_query(const float* block, u32x6* hi, u32x6* lo) {
+// A block of a rotated query, in LDS, as three e2m3 numbers an element: the largest magnitude becomes 3.875 to 7.75
+// units (of e2m3's 7.5) of 2^(scale - 127), the scale byte that is returned; x[0] is off by up to 1/4
+// unit, x[1], in units of 2^-kMxQueryStep[1], holds the rest to 1/128, and x[2] that one to 1/4096.
+constexpr int kMxQueryParts = 3;
+constexpr int kMxQueryStep[kMxQueryParts] = {0, 4, 9};
+constexpr int kMxQueryLeast = 14;   // least scale byte (none goes below 0 where steps are taken off twice)
+__device__ __forceinline__ int mx4_query(const float* block, u32x6 (&x)[kMxQueryParts]) {
     const f32x4* row = reinterpret_cast<const f32x4*>(block);
     f32x16 even, odd;   // the conversion interleaves its two operands
     uint32_t big = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-        const f32x4 x = row[k];
+        const f32x4 y = row[k];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-            even[2 * k + e] = x[2 * e];
-            odd[2 * k + e] = x[2 * e + 1];
-            big = max(big, max(__float_as_uint(x[2 * e]) & 0x7fffffffu, __float_as_uint(x[2 * e + 1]) & 0x7fffffffu));
+            even[2 * k + e] = y[2 * e];
+            odd[2 * k + e] = y[2 * e + 1];
+            big = max(big, max(__float_as_uint(y[2 * e]) & 0x7fffffffu, __float_as_uint(y[2 * e + 1]) & 0x7fffffffu));
         }
     }
-    *hi = *lo = u32x6{0u, 0u, 0u, 0u, 0u, 0u};
+#pragma unroll
+    for (int p = 0; p < kMxQueryParts; ++p) x[p] = u32x6{0u, 0u, 0u, 0u, 0u, 0u};
     if (big >= 0x7f800000u) return kMxNaN;
-    const int scale = max((int)((big + 0x80000u) >> 23) - 2, 5);
+    const int scale = max((int)((big + 0x80000u) >> 23) - 2, kMxQueryLeast);
     // (The conversions take several passes, and a result may not lie in their operands' registers, which the
     // compiler does not know: operands are kept until after them.)
-    float unit = __uint_as_float((uint32_t)scale << 23);
-    *hi = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
-    const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(*hi, unit);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-        even[e] -= back[2 * e];
-        odd[e] -= back[2 * e + 1];
+    for (int p = 0; p < kMxQueryParts; ++p) {
+        float unit = __uint_as_float((uint32_t)(scale - kMxQueryStep[p]) << 23);
+        x[p] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
+        if (p + 1 < kMxQueryParts) {
+            const f32x32 back = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(x[p], unit);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                even[e] -= back[2 * e];
+                odd[e] -= back[2 * e + 1];
+            }
+        }
+        asm volatile("" : "+v"(unit), "+v"(x[p]), "+v"(even), "+v"(odd));
     }
-    asm volatile("" : "+v"(unit), "+v"(*hi), "+v"(even), "+v"(odd));
-    float unit_lo = unit * 0.0625f;
-    *lo = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit_lo);
-    asm volatile("" : "+v"(*lo), "+v"(unit_lo), "+v"(even), "+v"(odd));
     return scale;
 }
+// The scale of part p of a block with scale byte `scale`.
+__device__ __forceinline__ int mx4_query_scale(int scale, int p) { return scale == kMxNaN ? scale : scale - kMxQueryStep[p]; }
 __device__ __forceinline__ i32x8 mx4_operand(const u32x6& x) {
     return i32x8{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)x[4], (int)x[5], 0, 0};
 }
