@@ -198,7 +198,9 @@ typedef struct a2t_stream_info {
  *   A2T_TARGET_WGS  attention workgroups one launch spreads over (default:
  *                   the device's CU count, one 8-wave workgroup per CU)
  *   A2T_SPLITS      force this many key splits per stream (0 = planned)
- *   A2T_FORCE_VALU  nonzero: the VALU attention kernel for bf16 caches */
+ *   A2T_FORCE_VALU  nonzero: the VALU attention kernel for bf16 caches
+ *   A2T_MX4_ROWS    16, 32, 48, 64 or 128: query rows of an attention workgroup of
+ *                   A2T_MX4 caches (anything else = planned) */
 int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out);
 
 /* Wait for the stream, then free everything the cache owns.  NULL is a no-op. */
@@ -467,7 +469,9 @@ int a2t_sync(a2t_cache* c);
  * kernel_filter: NULL disables timing; "" times every kernel; otherwise only
  * kernels whose name contains the string ("step_meta", "append",
  * "attn_tile", "attn_block", "attn_f32", "attn_f32x2" (attn_f32 with two query
- * blocks per workgroup), "attn_mx4", "attn_mx4_rows", "attn_valu", "attn_merge", "evict", "read_rows").  While enabled, each
+ * blocks per workgroup), "attn_mx4", "attn_mx4x2", "attn_mx4x3" (16, 32, 48 query
+ * rows per workgroup), "attn_mx4_rows64", "attn_mx4_rows128", "attn_valu",
+ * "attn_merge", "evict", "read_rows").  While enabled, each
  * matching launch carries a start/stop event pair recorded at the dispatch's
  * own begin and end.  a2t_kernel_time waits for the
  * stream, then reports for the kernels whose name contains `kernel` the

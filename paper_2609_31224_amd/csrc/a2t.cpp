@@ -148,6 +148,7 @@ struct a2t_cache {
     // attention tuning
     int target_wgs = 1024;
     int force_splits = 0;
+    int force_mx4_rows = 0;          // query rows of an A2T_MX4 launch's workgroups (0: planned)
     // the last split plan (every layer of a step plans the same resident counts)
     int plan_n = 0;
     int plan_force = -1;
@@ -520,6 +521,7 @@ constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 // one of 22 onto 4,096 15.6, 14.3, 16.3, 16.8; 777 rows of 32/4 heads of 64 onto none 22, 24, 12, 15.  The times
 // below are fitted to 48 such steps, at both head dims: the choice is the best of the four or within 3 % of it.
 struct Mx4Shape {
+    const char* name;   // of its launches in the timings
     int query_blocks;   // of attn_mx4; 0: attn_mx4_rows
     int row_waves;
     SplitCosts costs;
@@ -538,21 +540,24 @@ Mx4Shape mx4_shape(a2t_cache* c, int n, const int* tiles, const int32_t* n_q, co
     int rows = 1;
     for (int i = 0; i < n; ++i) rows = std::max(rows, c->cfg.n_q_heads / c->cfg.n_kv_heads * n_q[i]);
     const double d = c->cfg.head_dim == 128 ? 1.0 : 0.66;
-    const Mx4Shape shapes[] = {{3, 0, kMx4Costs, 1, d * 0.44, 3},
-                               {2, 0, kMx4Costs, 1, d * 0.38, 2},
-                               {0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.25, 4},
-                               {0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.05, 4}};
-    if (rows <= 16) return {1, 0, kMx4Costs, 1, 0, 0};
+    const Mx4Shape shapes[] = {{"attn_mx4", 1, 0, kMx4Costs, 1, 0, 0},   // up to 16 rows
+                               {"attn_mx4x3", 3, 0, kMx4Costs, 1, d * 0.44, 3},
+                               {"attn_mx4x2", 2, 0, kMx4Costs, 1, d * 0.38, 2},
+                               {"attn_mx4_rows64", 0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.25, 4},
+                               {"attn_mx4_rows128", 0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.05, 4}};
+    for (const Mx4Shape& shape : shapes)
+        if (shape.rows() == c->force_mx4_rows) return shape;
+    if (rows <= 16) return shapes[0];
     double best_us = 0;
     int best = -1;
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 1; k < 5; ++k) {
         const Mx4Shape& shape = shapes[k];
         SplitStream ss[kMaxDesc];
         int splits[kMaxDesc];
         for (int i = 0; i < n; ++i) ss[i] = {tiles[i], mx4_wgs(c, shape, n_q[i]), floats[i]};
-        c->mx4_planner[k].plan(n, ss, shape.costs, shape.per_cu * c->target_wgs, 0, ws_limit, splits);
+        c->mx4_planner[k - 1].plan(n, ss, shape.costs, shape.per_cu * c->target_wgs, 0, ws_limit, splits);
         const bool split = *std::max_element(splits, splits + n) > 1;
-        const double us = shape.us_launch + shape.us_tile * (double)(c->mx4_planner[k].cost() - (split ? shape.costs.merge : 0)) +
+        const double us = shape.us_launch + shape.us_tile * (double)(c->mx4_planner[k - 1].cost() - (split ? shape.costs.merge : 0)) +
                           (split ? kMx4MergeUs : 0);
         if (best < 0 || us < best_us) best = k, best_us = us;
     }
@@ -730,7 +735,7 @@ int attn_launch(a2t_cache* c, int layer, int n, const int32_t* ids, const int32_
         return e == hipSuccess ? A2T_OK : hip_fail(c);
     }
     {
-        ProfScope ps(c, mx4 ? (shape.query_blocks ? "attn_mx4" : "attn_mx4_rows") : f32 ? (query_blocks == 2 ? "attn_f32x2" : "attn_f32") : valu ? "attn_valu" : block ? "attn_block" : "attn_tile");
+        ProfScope ps(c, mx4 ? shape.name : f32 ? (query_blocks == 2 ? "attn_f32x2" : "attn_f32") : valu ? "attn_valu" : block ? "attn_block" : "attn_tile");
         e = launch(c->dev, ps.kt());
     }
     if (e != hipSuccess) return hip_fail(c);
@@ -862,6 +867,7 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
         c->target_wgs = std::max(1, env_int("A2T_TARGET_WGS", cus));
     }
     c->force_splits = std::max(0, env_int("A2T_SPLITS", 0));
+    c->force_mx4_rows = env_int("A2T_MX4_ROWS", 0);
     c->force_valu = k.dtype == A2T_BF16 && env_flag("A2T_FORCE_VALU");
     // the split planner's scratch, so that no attention call allocates
     for (auto* v : {&c->plan_tiles, &c->plan_splits, &c->plan_tmp, &c->plan_order}) v->reserve(kMaxDesc);
