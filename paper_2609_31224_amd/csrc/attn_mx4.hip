@@ -329,10 +329,11 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             if (x + 1 < QB && k == QP - 1) qs = s_qs[x + 1][ln];
         }
     };
-    // hides what a row does not see, and moves the reference, lazily: the first block sets it (a row that sees
-    // none of its keys sees none of the later ones), and it is raised, and the running sums
-    // rescaled, only when a block exceeds it by more than 2^8
-    auto settle = [&](int kb, bool first, int ln) {
+    // hides what a row does not see, and moves the reference, lazily: the first block with a score sets it, and it is
+    // raised, and the running sums rescaled, only when a block exceeds it by more than 2^8.  (A row without
+    // one yet, which sees none of the wave's keys or whose scores are all -infinity in fp32, has the wave look at every block.)
+    bool unset = true;
+    auto settle = [&](int kb, int ln) {
         if (kb + kKeyBlock - 1 > vis0) {   // some row does not see every key
 #pragma unroll
             for (int x = 0; x < QB; ++x) {
@@ -353,19 +354,24 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             top[x] = fmaxf(top[x], sc[x][1][3]);
             most = fmaxf(most, top[x]);
         }
-        if (first || __any(most > 8.f)) {
+        if (unset || __any(most > 8.f)) {
 #pragma unroll
             for (int x = 0; x < QB; ++x) {
                 const float t = col_max(top[x]);
-                const float up = !first ? fmaxf(t, 0.f) : t == -INFINITY ? 0.f : t;
-                mrun[x] = first ? t : mrun[x] + up;
-                const float corr = __builtin_amdgcn_exp2f(first ? 0.f : -up);
+                const bool fresh = mrun[x] == -INFINITY;
+                const float up = !fresh ? fmaxf(t, 0.f) : t == -INFINITY ? 0.f : t;
+                mrun[x] = fresh ? t : mrun[x] + up;
+                const float corr = __builtin_amdgcn_exp2f(fresh ? 0.f : -up);
                 lsum[x] *= corr;
 #pragma unroll
                 for (int c = 0; c < DB; ++c) acc[x][c] *= corr;
 #pragma unroll
                 for (int t2 = 0; t2 < 2; ++t2) sc[x][t2] -= up;
             }
+            bool none = false;
+#pragma unroll
+            for (int x = 0; x < QB; ++x) none |= mrun[x] == -INFINITY;
+            unset = __any(none);
         }
     };
     auto weigh = [&](int x) {
@@ -456,7 +462,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
 #pragma unroll
             for (int c = 0; c < kAhead; ++c) vv[c] = v_op(v_out, c);
             ordered();
-            settle(kb, i == 0, ln);
+            settle(kb, ln);
             if (odd) add_odd(kb);
 #pragma unroll
             for (int x = 0; x < QB; ++x) weigh(x), sum(x);
@@ -491,7 +497,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             for (int x = 0; x < QB; ++x) score(x, lane);
             fence();
             load_k(kb_next, next, lane);
-            settle(k0, true, lane);
+            settle(k0, lane);
             if (odd) add_odd(k0);
         }
         // In each pass the probabilities and products of a block go with the next one's scores and V: the matrix
@@ -550,7 +556,7 @@ __global__ __launch_bounds__(64 * kWaves, QB == 1 ? 4 : 2) void attn_mx4_kernel(
             }
             odd_v(v_in);
             load_v(kb_next, next, ln);
-            settle(kb, false, ln);
+            settle(kb, ln);
             if (odd) add_odd(kb);
         }
         __builtin_amdgcn_s_setprio(0);

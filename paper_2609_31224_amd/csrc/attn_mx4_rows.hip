@@ -219,7 +219,9 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
     };
 
     f32x16 acc[NB], sc;
-    float mrun = -INFINITY, ref = 0.f, lsum[2] = {0.f, 0.f};   // ref: mrun, or 0 before a key was seen
+    // ref: mrun, or what every score in fp32 reaches before there was one (a score of -infinity has no weight)
+    constexpr float kLowest = -3.40282347e38f;
+    float mrun = -INFINITY, ref = kLowest, lsum[2] = {0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < NB; ++c) acc[c] = f32x16{};
     auto score = [&] {
@@ -239,9 +241,8 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
         if constexpr (KS == 2) dims(std::integral_constant<int, 1>());
         asm volatile("" : "+v"(sc));   // (the compiler would put them off to where they are read)
     };
-    // hides what a row does not see, and moves the reference, lazily: the first block sets it (a row that sees
-    // none of its keys sees none of the later ones), and it is raised, and the running sums
-    // rescaled, only when a block exceeds it by more than 2^8
+    // hides what a row does not see, and moves the reference, lazily: the first block with a score sets it, and it is
+    // raised, and the running sums rescaled, only when a block exceeds it by more than 2^8
     auto settle = [&](int kb, bool first) {
         if (kb + kKeys > see_all) {   // some row does not see every key, or the split ends
             const int see = see_to - kb - 4 * h;
@@ -257,16 +258,16 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
             half_top[x] = fmaxf(fmaxf(half_top[x], sc[8 * x + 5]), sc[8 * x + 6]);
         }
         const float top = fmaxf(fmaxf(fmaxf(half_top[0], sc[7]), half_top[1]), sc[15]);
-        if (first || __any(top > ref + 8.f)) {
+        if (first || __any(top >= ref + 8.f)) {   // (the lowest plus 8 is the lowest)
             const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
             const float t = fmaxf(mrun, fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1])));
             const float corr = first ? 0.f : __builtin_amdgcn_exp2f(ref - t);
-            if (first || t > ref) {
+            if (first || t >= ref) {
                 mrun = t;
                 lsum[0] *= corr, lsum[1] *= corr;
 #pragma unroll
                 for (int c = 0; c < NB; ++c) acc[c] *= corr;
-                ref = t == -INFINITY ? 0.f : t;
+                ref = fmaxf(t, kLowest);
             }
         }
     };
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(64 * RW * kGroups, 2) void attn_mx4_rows_kernel(Dev
     // does not hold are left out; where there were some the workgroup begins again with it.  (Both in one loop:
     // the compiler copies all sums from block to block, 421 us instead of 320.)
     auto run = [&](auto odd) {
-        mrun = -INFINITY, ref = lsum[0] = lsum[1] = 0.f;
+        mrun = -INFINITY, ref = kLowest, lsum[0] = lsum[1] = 0.f;
 #pragma unroll
         for (int c = 0; c < NB; ++c) acc[c] = f32x16{};
         take_v(odd, 0);
