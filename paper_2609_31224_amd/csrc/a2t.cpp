@@ -512,14 +512,18 @@ constexpr SplitCosts kValuCosts{4, 2, 1 << 20, 2};
 
 // The kernel of a step on an A2T_MX4 cache, and the query rows of its workgroups: that of these whose planned launch
 // would end first, by what its workgroups cost in tiles, what a tile and the rest of a launch take.
-//   attn_mx4       one, two or three blocks of 16 rows, one workgroup a CU (four blocks spill: listening units
-//                  of 16 sessions 419 us a step of four layers, three: 258, two: 254, one: 261)
+//   attn_mx4       one, two or three blocks of 16 rows; two and three: one workgroup a CU (four would not fit the registers)
 //   attn_mx4_rows  64 rows, two workgroups a CU, or 128, one
+// Up to 16 query rows run with one block.  Two of its workgroups share a CU, but its plans count one: counted as two, 77
+// decode steps (1 to 96 sessions of 1,024 to 16,384 keys, 1 to 8 KV heads) take 7 % more on average (32 sessions of 1,024 keys
+// of 8 heads of 128 11.8 -> 17.7 us, 64 uneven ones of 512 to 4,096 36.2 -> 42.1; 48 of 4,096 52.2 -> 48.6), as one
+// already brings the keys in at memory's rate and every split costs a merge.
 // Us a layer of 32/8 heads of 128, merge included, layers whose rows no cache holds in turn, by 48, 32, 64 and 128 rows:
-// 1,024 rows onto no keys 34, 36, 24, 25; onto 1,024 50, 54, 40, 38; onto 4,096 98, 108, 88, 80; onto 16,384 295, 325,
-// 295, 251; 16 sessions of 22 rows onto 8,192 64, 87, 84, 77; of 30 onto 4,096 66, 54, 55, 49; of 60 109, 103, 85, 76;
-// one of 22 onto 4,096 15.6, 14.3, 16.3, 16.8; 777 rows of 32/4 heads of 64 onto none 22, 24, 12, 15.  The times
-// below are fitted to 48 such steps, at both head dims: the choice is the best of the four or within 3 % of it.
+// 1,024 rows onto no keys 35, 37, 24, 26; onto 1,024 54, 58, 39, 41; onto 4,096 111, 120, 93, 87; onto 16,384 338, 361,
+// 305, 274; 16 sessions of 22 rows onto 8,192 65, 90, 87, 77; of 25 onto 4,096 70, 58, 53, 49; of 60 114, 110, 87, 77;
+// one of 22 onto 4,096 15.9, 14.1, 16.9, 17.8; 777 rows of 32/4 heads of 64 onto none 23, 25, 13, 16.  The times
+// below are fitted to 50 such steps, at both head dims; on these and 34 drawn ones the choice takes 0.9 % more than the
+// best of the four on average, at most 4 % more beyond the 3 % by which equal launches differ.
 struct Mx4Shape {
     const char* name;   // of its launches in the timings
     int query_blocks;   // of attn_mx4; 0: attn_mx4_rows
@@ -532,19 +536,19 @@ struct Mx4Shape {
 // (Splits of 1 to 12 forced on steps of 1 to 1,024 rows onto 0 to 16,384 keys were at best 6 % faster than those that
 // these costs lead to.)
 constexpr SplitCosts kMx4Costs{8, 4, 1 << 20, 4};
-constexpr double kMx4MergeUs = 5;
+constexpr double kMx4MergeUs = 5.5;
 int mx4_wgs(const a2t_cache* c, const Mx4Shape& shape, int n_q) {
     return c->cfg.n_kv_heads * mx4_groups(c->cfg.n_q_heads / c->cfg.n_kv_heads * n_q, shape.rows());
 }
 Mx4Shape mx4_shape(a2t_cache* c, int n, const int* tiles, const int32_t* n_q, const int64_t* floats, int64_t ws_limit) {
     int rows = 1;
     for (int i = 0; i < n; ++i) rows = std::max(rows, c->cfg.n_q_heads / c->cfg.n_kv_heads * n_q[i]);
-    const double d = c->cfg.head_dim == 128 ? 1.0 : 0.66;
+    const double d = c->cfg.head_dim == 128 ? 1.0 : 0.64;
     const Mx4Shape shapes[] = {{"attn_mx4", 1, 0, kMx4Costs, 1, 0, 0},   // up to 16 rows
-                               {"attn_mx4x3", 3, 0, kMx4Costs, 1, d * 0.44, 3},
-                               {"attn_mx4x2", 2, 0, kMx4Costs, 1, d * 0.38, 2},
-                               {"attn_mx4_rows64", 0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.25, 4},
-                               {"attn_mx4_rows128", 0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.05, 4}};
+                               {"attn_mx4x3", 3, 0, kMx4Costs, 1, d * 0.48, 4.5},
+                               {"attn_mx4x2", 2, 0, kMx4Costs, 1, d * 0.39, 2},
+                               {"attn_mx4_rows64", 0, 2, {2, 4, 1 << 20, 4}, 2, d * 1.23, 4.5},
+                               {"attn_mx4_rows128", 0, 4, {6, 4, 1 << 20, 4}, 1, d * 1.09, 5}};
     for (const Mx4Shape& shape : shapes)
         if (shape.rows() == c->force_mx4_rows) return shape;
     if (rows <= 16) return shapes[0];

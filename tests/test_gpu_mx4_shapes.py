@@ -94,3 +94,24 @@ def test_scales_of_values_apart(gpu, monkeypatch, rows, d, hq, hkv, new, exps):
     want, bound = ref.attention_bound(0, q, new, least=0.0)
     off = np.abs(o.float().cpu().numpy().astype(np.float64) - want) - bound
     assert np.isfinite(off).all() and (off <= 0).all(), (float(off.max()), np.unravel_index(off.argmax(), off.shape))
+
+
+@pytest.mark.parametrize("streams,rows,resident,kind", [(3, 1, 100, 16), (1, 22, 4096, 32), (16, 22, 4096, 48), (1, 1024, 0, 64), (1, 1024, 4096, 128)])
+def test_planned_kinds(gpu, streams, rows, resident, kind):
+    """Every kind is what some launch on the whole GPU is planned with."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    hq, hkv, d = 32, 8, 128
+    c = a2t.a2t_cache_create(1, streams, hq, hkv, d, a2t.A2T_MX4, resident + rows, 0, 1024)
+    a2t.a2t_profile_enable(c, "attn_mx4")
+    for at in [*range(0, resident, 1024), resident]:
+        n = min(1024, resident - at) if at < resident else rows
+        k = torch.zeros((1, n * streams, hkv, d), dtype=torch.bfloat16, device="cuda")
+        a2t.a2t_append(c, a2t.A2T_ALL_LAYERS, range(streams), [n] * streams, k, k, np.full(n * streams, SEG_ACOUSTIC, np.uint8),
+                       np.tile(np.arange(at, at + n), streams), [at] * streams)
+    q = torch.zeros((streams * rows, hq, d), dtype=torch.bfloat16, device="cuda")
+    o = torch.full_like(q, float("nan"))
+    a2t.a2t_chunk_attn(c, 0, range(streams), [rows] * streams, q, o)
+    assert launches(a2t, c) == {kind: 1}
+    assert (o == 0).all()
+    a2t.a2t_cache_destroy(c)
