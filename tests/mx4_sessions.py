@@ -65,6 +65,7 @@ class Sessions:
             rows = slice(first[j], first[j + 1])
             self.oracles[i].append(st.seg, st.pos, st.unit, {l: k[l][rows] for l in range(self.L)}, {l: v[l][rows] for l in range(self.L)})
         kd, vd = self._dev(k), self._dev(v)
+        torch.cuda.current_stream().synchronize()
         asks = np.concatenate([np.arange(first[j + 1] - nq[j], first[j + 1]) for j in range(len(act))])
         if self.calls == "all":
             a2t.a2t_append(c, a2t.A2T_ALL_LAYERS, ids, n, kd, vd, seg, pos, unit)
@@ -72,6 +73,7 @@ class Sessions:
             meta = (seg, pos, unit) if l == 0 else (None, None, None)
             qd = self._dev(q[l][asks])
             o = torch.full_like(qd, float("nan"))
+            torch.cuda.current_stream().synchronize()   # the cache may be on another stream than the uploads and fills
             if self.calls in ("fused", "noalloc") and not decode:
                 call = a2t.a2t_append_attn if self.calls == "fused" else a2t.a2t_append_attn_noalloc
                 call(c, l, ids, n, kd[l], vd[l], *meta, nq, qd, o)
@@ -120,6 +122,7 @@ class Sessions:
         a2t, c = self.a2t, self.cache
         total = sum(self.oracles[i].resident for i in ids)
         kr, vr = (torch.full((self.L, total, self.hkv, self.d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        torch.cuda.current_stream().synchronize()
         a2t.a2t_read_rows(c, a2t.A2T_ALL_LAYERS, ids, kr, vr)
         a2t.a2t_sync(c)
         kr, vr = (x.view(torch.int16).cpu().numpy().view(np.uint16) for x in (kr, vr))

@@ -1,0 +1,62 @@
+"""A2T_MX4 caches on a stream of their own while the default stream is busy: every call's work is on the
+cache's stream, waits for nothing on the other one and gives the result that it gives alone."""
+import numpy as np
+import pytest
+
+from synth.streams import SEG_ACOUSTIC, SEG_TEXT
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("d,hq,hkv,rows", [(128, 8, 2, 22), (64, 4, 4, 1), (128, 16, 2, 100)])
+def test_calls_beside_a_busy_default_stream(gpu, d, hq, hkv, rows):
+    import torch
+    import paper_2609_31224_amd as a2t
+    L, S, old = 2, 3, 700
+    n = old + 2 * rows
+    g = torch.Generator(device="cuda").manual_seed(8)
+    rand = lambda *shape: torch.randn(shape, generator=g, device="cuda").bfloat16()   # noqa: E731
+    first = [rand(L, S * old, hkv, d) for _ in range(2)]
+    steps = [[rand(L, S * rows, hkv, d), rand(L, S * rows, hkv, d), rand(L, S * rows, hq, d)] for _ in range(2)]
+    busy = torch.randn(8192, 8192, device="cuda")
+    into = torch.empty_like(busy)
+    torch.mm(busy, busy, out=into)      # the library of products sets itself up
+    segs = {m: np.where(np.arange(S * m) % 3, SEG_ACOUSTIC, SEG_TEXT).astype(np.uint8) for m in (old, rows)}
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def go(load):
+        """The calls of a session, moved to another stream halfway; [outputs], and whether the load outlasted them."""
+        outs = [torch.full((L, S * rows, hq, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in steps]
+        back = [torch.full((L, S * n, hkv, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        c = a2t.a2t_cache_create(L, S, hq, hkv, d, a2t.A2T_MX4, n, n, max(old, 100), stream=streams[0])
+        done = torch.cuda.Event()
+        torch.cuda.synchronize()        # nothing of the test's own is in flight
+        for _ in range(load):
+            torch.mm(busy, busy, out=into)
+        done.record()
+        a2t.a2t_append(c, a2t.A2T_ALL_LAYERS, range(S), [old] * S, *first, segs[old], np.tile(np.arange(old), S), [0] * S)
+        a2t.a2t_evict(c, range(S), [500] * S, 0)
+        for t, ((k, v, q), o) in enumerate(zip(steps, outs)):
+            pos = np.tile(np.arange(old + t * rows, old + (t + 1) * rows), S)
+            for l in range(L):
+                meta = (segs[rows], pos, [t + 1] * S) if l == 0 else (None, None, None)
+                a2t.a2t_append_attn(c, l, range(S), [rows] * S, k[l], v[l], *meta, [rows] * S, q[l], o[l])
+            if t == 0:
+                a2t.a2t_evict(c, range(S), [200] * S, 1)
+                a2t.a2t_sync(c)
+                a2t.a2t_set_stream(c, streams[1])
+        held = sum(a2t.a2t_resident(c, s)[0] for s in range(S))
+        flat = [x.view(-1)[:L * held * hkv * d] for x in back]
+        a2t.a2t_read_rows(c, a2t.A2T_ALL_LAYERS, range(S), *flat)
+        a2t.a2t_sync(c)
+        outlasted = not done.query()
+        torch.cuda.synchronize()
+        a2t.a2t_cache_destroy(c)
+        assert all(torch.isfinite(x.float()).all() for x in (*outs, *flat))
+        return [*outs, *flat], outlasted
+
+    want, _ = go(0)
+    got, outlasted = go(24)
+    assert outlasted, "the products ended before the calls did"
+    for x, y in zip(want, got):
+        assert torch.equal(x, y)
