@@ -36,8 +36,9 @@
  *     otherwise.
  *   - All compute is enqueued on the cache's HIP stream (a2t_set_stream).
  *     Nothing in a2t_append / a2t_append_attn / a2t_chunk_attn /
- *     a2t_decode_attn / a2t_evict / a2t_evict_rule allocates memory (every
- *     buffer is sized at creation); the a2t_read_* calls synchronise.  The
+ *     a2t_decode_attn / a2t_evict / a2t_evict_rule / a2t_read_rows allocates
+ *     memory (every buffer is sized at creation); the other a2t_read_* calls
+ *     synchronise.  The
  *     calls that open a step (layer 0 or A2T_ALL_LAYERS) stage its metadata
  *     in one of 16 pinned slots: with 16 earlier steps still queued on the
  *     device, opening one more waits until the oldest has run (back-pressure,
@@ -81,7 +82,8 @@
  *   angles, rounded to fp32) and rounded to fp32 once before it is encoded.
  *   Attention is that of the values held: their products with rotated queries,
  *   which are rounded by at most 2^-13.9 of the largest element of their block of
- *   32, fp32 sums, probabilities rounded to fp16.
+ *   32 (or of 2^-111, where that is more), fp32 sums, which are divided by the
+ *   probabilities' sum at the end, probabilities rounded to fp16.
  *   Values of non-finite rows reach only the queries that see them.
  */
 #ifndef A2T_H
@@ -105,7 +107,8 @@ typedef enum a2t_status {
                                or metadata that contradicts the registered step */
     A2T_ERR_CAPACITY = -3,  /* a region of the cache would overflow */
     A2T_ERR_STATE = -4,     /* call out of order (layer not appended, step open, ...) */
-    A2T_ERR_OOM = -5,       /* device or pinned-host allocation failed (create only) */
+    A2T_ERR_OOM = -5,       /* device or host allocation failed (create, a2t_read_kv of
+                               an A2T_MX4 cache) */
     A2T_ERR_HIP = -6,       /* HIP runtime error or device fault; the cache is poisoned */
     A2T_ERR_NODEV = -7      /* no usable gfx950 device, or a host-only cache was asked
                                for device work */
@@ -246,16 +249,19 @@ int a2t_append(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* st
  * cache are held in fp16 until they are combined (normalised by the split's
  * own sum, so each value lies within the range of the V entries): bf16 V
  * entries must stay within fp16's range (|v| <= 65504; of an A2T_MX4 cache
- * |v| < 57344, so that the values held do).  fp32 caches keep fp32 split outputs.
+ * |v| < 57344, so that the values held do), and outputs below 2^-14 are off by
+ * up to 2^-25.  fp32 caches keep fp32 split outputs.
  * The layer must have appended the current step.  Errors: INVALID, STATE. */
 int a2t_chunk_attn(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* stream_ids,
                    const int32_t* n_q, const void* q, void* o);
 
 /* a2t_append on one layer followed by a2t_chunk_attn on that layer, in one
  * launch where the kernels allow it (fp32 caches; bf16 caches except for steps
- * of many query rows; A2T_MX4 caches encode the rows in a launch of its own): the workgroups whose key tiles hold the step's new rows
- * rotate and store them while staging them for attention.  Arguments as in the two calls (layer 0..L-1 only; n_q
- * host [n_streams] with 1 <= n_q <= n_rows; q and o packed [sum n_q][Hq][D]).
+ * of many query rows; A2T_MX4 caches encode the rows in a launch of its own):
+ * the workgroups whose key tiles hold the step's new rows rotate and store them
+ * while staging them for attention.  Arguments as in the two calls (layer
+ * 0..L-1 only; n_q host [n_streams] with 1 <= n_q <= n_rows; q and o packed
+ * [sum n_q][Hq][D]).
  * Results and cache contents are the same as the two calls. */
 int a2t_append_attn(a2t_cache* c, int32_t layer, int32_t n_streams, const int32_t* stream_ids,
                     const int32_t* n_rows, const void* k, const void* v, const uint8_t* seg,
