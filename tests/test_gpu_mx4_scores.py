@@ -48,3 +48,46 @@ def test_keys_of_no_weight_come_first(gpu, monkeypatch, rows, d, offset, splits)
     got = o.float().cpu().numpy().astype(np.float64)
     print(f"worst error {(np.abs(got - want) / bound).max():.3f} of its bound, bound {bound.max():.3f}", flush=True)
     assert (np.abs(got - want) <= bound).all()
+
+
+@pytest.mark.parametrize("below", [12.5, 15.5, 18.5])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rows", list(NAMES))
+def test_many_small_probabilities(gpu, monkeypatch, rows, d, below):
+    """Every wave has one key of large score, whose value is 0, and many others at 2^-below of its probability: as
+    fp16 numbers these are normal or subnormal, and products and sums both have to count them."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    force(monkeypatch, rows, 1)
+    rng = np.random.default_rng(6)
+    hq, hkv, old, new = 4, 1, 4000, 33
+    n = old + new
+    k, q, v = np.zeros((n, hkv, d)), np.zeros((new, hq, d)), 8 + rng.random((n, hkv, d))
+    peaks = np.arange(0, 256, 32)
+    k[peaks, :, d - 1] = 4.0
+    v[peaks] = 0.0
+    q[..., d - 1] = below * np.log(2) * np.sqrt(d) / 4     # theta = 1e12 leaves the last dim as it is
+    k, q, v = bf16_round(k), bf16_round(q), bf16_round(v)
+    kd, vd, qd = (torch.from_numpy(np.ascontiguousarray(x, np.float32)).cuda().bfloat16() for x in (k, v, q))
+    seg = np.full(n, SEG_ACOUSTIC, np.uint8)
+    c = a2t.a2t_cache_create(1, 1, hq, hkv, d, a2t.A2T_MX4, n, 0, 1024, rope_theta=1e12)
+    ref = mx4.OracleMx4Cache(hq, hkv, d, [0], theta=1e12)
+    o = torch.full_like(qd, float("nan"))
+    for unit, at in enumerate((0, 1000, 2000, 3000, old)):
+        part = slice(at, min(at + 1000, old) if at < old else n)
+        m = part.stop - part.start
+        ref.append(seg[part], np.arange(n)[part], unit, {0: k[part]}, {0: v[part]})
+        if at < old:
+            a2t.a2t_append(c, 0, [0], [m], kd[part], vd[part], seg[part], np.arange(n)[part], [unit])
+        else:
+            a2t.a2t_append_attn(c, 0, [0], [m], kd[part], vd[part], seg[part], np.arange(n)[part], [unit], [m], qd, o)
+    a2t.a2t_sync(c)
+    a2t.a2t_cache_destroy(c)
+    want, bound = ref.attention_bound(0, q, new, least=0.0)
+    got = o.float().cpu().numpy().astype(np.float64)
+    print(f"worst error {(np.abs(got - want) / bound).max():.3f} of its bound, outputs {want.mean():.4f}, bound {bound.max():.5f}", flush=True)
+    assert (np.abs(got - want) <= bound).all()
+    # the small ones missing from the products, or (where they are a share of the sum worth it) from the sum, would
+    # not be within the bound: without them in the sum outputs grow by that share of themselves
+    share = want / 8.5
+    assert (bound < want / 2).all() and ((bound < want * share).all() or below > 16)
