@@ -404,11 +404,17 @@ def a2t_read_kv(c: Cache, layer: int, stream: int):
 def a2t_read_rows(c: Cache, layer: int, stream_ids: Sequence[int], k=None, v=None) -> None:
     """Resident rows of the streams, in cache order, into GPU tensors [rows][Hkv][D] (one
     layer) or [L][rows][Hkv][D] (A2T_ALL_LAYERS) of the cache's input type, rows being the
-    sum of the streams' a2t_resident; either may be None.  Asynchronous on the cache's stream."""
+    sum of the streams' a2t_resident; either may be None.  Tensors too small for them are a
+    ValueError.  Asynchronous on the cache's stream."""
     ids = _i32(stream_ids)
-    rc = _lib.a2t_read_rows(c.ptr, layer, len(ids), _p(ids, C.c_int32),
-                            _dev(k, "k", c.torch_dtype if not isinstance(k, int) else None),
-                            _dev(v, "v", c.torch_dtype if not isinstance(v, int) else None))
+    k_ptr = _dev(k, "k", c.torch_dtype if not isinstance(k, int) else None)
+    v_ptr = _dev(v, "v", c.torch_dtype if not isinstance(v, int) else None)
+    rows = sum(a2t_resident(c, int(s))[0] for s in ids if 0 <= s < c.config.n_streams)
+    need = rows * c.config.n_kv_heads * c.config.head_dim * (c.config.n_layers if layer == A2T_ALL_LAYERS else 1)
+    for what, x in (("k", k), ("v", v)):
+        if x is not None and not isinstance(x, int) and x.numel() < need:
+            raise ValueError(f"{what}: {x.numel()} elements, the resident rows have {need}")
+    rc = _lib.a2t_read_rows(c.ptr, layer, len(ids), _p(ids, C.c_int32), k_ptr, v_ptr)
     _check(rc, "a2t_read_rows")
 
 
