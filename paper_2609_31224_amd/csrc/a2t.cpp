@@ -868,7 +868,8 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
         if (c->host_only ||
             hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, k.device) != hipSuccess || cus <= 0)
             cus = 256;
-        c->target_wgs = std::max(1, env_int("A2T_TARGET_WGS", cus));
+        // (more than any launch has, and planners' scratch is sized by it)
+        c->target_wgs = std::clamp(env_int("A2T_TARGET_WGS", cus), 1, 1 << 20);
     }
     c->force_splits = std::max(0, env_int("A2T_SPLITS", 0));
     c->force_mx4_rows = env_int("A2T_MX4_ROWS", 0);
