@@ -20,16 +20,16 @@
 // (exactly); transposed LDS reads then give the operand of v_mfma_f32_16x16x32_f16.  The few blocks
 // that fp16 does not hold are added in fp32.  Probabilities are fp16, relative to a reference that
 // a wave's largest one reaches or exceeds: off by up to 2^-11 of each, or 2^-25 of the largest.  (In bf16, at the
-// same time, they were off by as much as the output's own rounding: an error against 64 bits of 0.0026
-// instead of 0.0020 relative, the bf16 output alone 0.0017; 64 sessions on 4,096 keys.)
+// same time, they were off by as much as the output's own rounding: with two parts a query an error against 64 bits of
+// 0.0026 instead of 0.0020 relative, 64 sessions on 4,096 keys.  With three it is 0.0017, that of the bf16 output alone.)
 // Nothing is shared between waves before the end, so there are no barriers in the loop; the
 // next block's codes are in flight while one is computed.
 //
 // One block of rows (decode): bound by memory where there are many sessions (64 of 4,096 keys, 48 us a
 // layer, 5.9 TB/s) or keys (one of 131,072: 26 us, 5.5 TB/s), by the launch and the way of the first loads for
-// one session of 4,096 (7 us, and 4 of the merge).  Two and three blocks: bound by vector operations and products
+// one session of 4,096 (7.5 us, and 4 of the merge).  Two and three blocks: bound by vector operations and products
 // together, which overlap little (a product takes the vector units' time, attn_mx4_rows.hip): 16 sessions of 22 rows
-// onto 8,192 keys 61 us, of which products are busy 33 %, vector operations 58 %.
+// onto 8,192 keys 65 to 71 us, of which products are busy 33 %, vector operations 56 %.
 #include "a2t_internal.h"
 #include "mx4_device.h"
 

@@ -10,8 +10,9 @@
 // each wave its share, not once a wave.  Two of a query's three parts stay in registers; the third is read from LDS for
 // each block.
 // Bounds: vector operations (~105 a wave and block of 32 x 32, exponentials and their roundings half of them),
-// products and what neither hides: 52 % and 35 % of the cycles of 1,024 rows onto 16,384 keys, at a clock that
-// power holds at 1.85 to 2.0 GHz, with two parts a query.  That launch takes 311 us with three, 283 with two.
+// products and what neither hides: 54 % and 42 % of the cycles of 1,024 rows onto 16,384 keys, at a clock that
+// power holds at 1.85 to 2.0 GHz.  That launch takes 274 to 317 us, card by card, attn_mx4's waves of 48 rows 338 where it
+// takes 274 (with two parts a query 251 to 283).
 #include "a2t_internal.h"
 #include "mx4_device.h"
 
