@@ -329,7 +329,7 @@ class Library:
                                                 case["hkv"], k.data_ptr(), k.stride(0), ko.data_ptr(), ko.stride(0), int(case["grad"])))]
         elif case["op"] == "attn":
             n = len(x["q"])
-            self.handle = a2t.a2t_prompt_create(n, case["hq"], case["hkv"], case["d"], dtype, stream=stream)
+            self.handle = a2t.a2t_prompt_create(n, case["hq"], case["hkv"], case["d"], dtype, flags=a2t.A2T_PROMPT_UNTIL if case["budget"] else 0, stream=stream)
             self.destroy = a2t.a2t_prompt_destroy
             o = torch.empty((n, case["hq"], case["d"]), dtype=x["q"].dtype, device=DEV)
             lse = torch.empty((case["hq"], n), dtype=torch.float32, device=DEV)
