@@ -138,6 +138,10 @@ typedef enum a2t_seg {
                                   the attention calls then run one split per stream,
                                   except a2t_append_attn_noalloc, which splits into the
                                   library's fixed array */
+#define A2T_FLAG_ROTATED 4u    /* keys and queries come rotated (a2t_rope_apply, whose pairs,
+                                  rotated share of a head and scaling the cache's own encoding
+                                  does not have): the cache stores and uses them as they are;
+                                  rope_theta is unused */
 
 typedef struct a2t_config {
     int32_t n_layers;       /* L >= 1 */
@@ -560,6 +564,178 @@ int a2t_distill_profile_enable(a2t_distill* d, int32_t enable);
  * a2t_profile_reserve).  Errors: INVALID, OOM. */
 int a2t_distill_profile_reserve(a2t_distill* d, int32_t n_launches);
 int a2t_distill_kernel_time(a2t_distill* d, int64_t* launches, double* total_ms);
+
+/* ---------------------------------------------------------------------------
+ * Training on whole sessions: what comes before and after the adaptation
+ * objective.  Rows of all sequences lie packed one after the other; rows of q,
+ * k and v are [heads][D] with a row stride in elements (a multiple of 8, at
+ * least heads * D), so that they may be parts of one projection's output.
+ * Device pointers are 16-byte aligned.  Every call enqueues kernels on the
+ * handle's stream and neither allocates, synchronises nor copies: host arrays
+ * travel in the launches, so that a call can be captured in a HIP graph and
+ * replayed on new contents of the same buffers.  A handle's workspace belongs
+ * to one call at a time: calls on one handle (and graphs captured from it) run
+ * one after the other, on one stream or ordered by the caller; work that
+ * overlaps takes handles of its own.  Rows behind the last sequence are
+ * neither read nor written.  One host thread at a time per handle.
+ * ------------------------------------------------------------------------- */
+
+/* ---- Rotary encoding of packed rows of queries and keys.  Row t turns the
+ * pairs (x, y) of its first r = rotary_dim channels of every head by
+ * a = pos[t] f_i, i < r / 2:
+ *   x' = m (x cos a - y sin a),  y' = m (y cos a + x sin a);
+ * the other channels are copied.  With theta the base and s the factor,
+ *   A2T_ROPE_PLAIN   f_i = theta^(-2i/r), m = 1
+ *   A2T_ROPE_LINEAR  f_i = theta^(-2i/r) / s  (positions interpolated)
+ *   A2T_ROPE_NTK     f_i = (theta s^(r/(r-2)))^(-2i/r)
+ *   A2T_ROPE_YARN    between the plain and the interpolated one: channels that
+ *                    turn more than turns_fast times within trained_rows keep
+ *                    theirs, those that turn less than turns_slow times are
+ *                    interpolated, with a ramp between: with
+ *                    c(n) = r ln(trained_rows / (2 pi n)) / (2 ln theta),
+ *                    lo = max(floor c(turns_fast), 0),
+ *                    hi = min(ceil c(turns_slow), r - 1) and
+ *                    w = (i - lo) / max(hi - lo, 0.001) within [0, 1],
+ *                    f_i = theta^(-2i/r) (1 - w + w / s), m = 0.1 ln s + 1.
+ * Angles are evaluated in fp64 for any int32 position; arithmetic is fp32 and
+ * outputs are rounded once. */
+#define A2T_ROPE_HALF 0    /* pairs (i, i + r/2), as the caches rotate */
+#define A2T_ROPE_PAIRS 1   /* pairs (2i, 2i + 1) */
+typedef enum a2t_rope_scaling { A2T_ROPE_PLAIN = 0, A2T_ROPE_LINEAR = 1, A2T_ROPE_NTK = 2, A2T_ROPE_YARN = 3 } a2t_rope_scaling;
+
+typedef struct a2t_rope_config {
+    int32_t head_dim;       /* D: 64 or 128 */
+    int32_t dtype;          /* A2T_F32 or A2T_BF16 */
+    int32_t rotary_dim;     /* r: a multiple of 16, at most D; 0 selects D */
+    int32_t layout;         /* A2T_ROPE_HALF or A2T_ROPE_PAIRS */
+    int32_t scaling;        /* a2t_rope_scaling */
+    int32_t trained_rows;   /* YARN: >= 1 */
+    double theta;           /* > 1; 0 selects 1e6 */
+    double factor;          /* s >= 1 (unused by PLAIN) */
+    double turns_fast;      /* YARN: >= turns_slow */
+    double turns_slow;      /* YARN: > 0 */
+    int32_t device;
+    int32_t reserved;
+} a2t_rope_config;
+
+typedef struct a2t_rope a2t_rope;
+
+/* Errors: INVALID, OOM, NODEV.  A handle holds no device memory. */
+int a2t_rope_create(const a2t_rope_config* cfg, void* hip_stream, a2t_rope** out);
+int a2t_rope_destroy(a2t_rope* r);
+int a2t_rope_set_stream(a2t_rope* r, void* hip_stream);
+
+/* Rotates n_rows rows (1 .. 2^26) of queries and keys in one launch; either may be NULL.
+ *   pos          device int32 [n_rows]
+ *   q, k         rows of q_heads, k_heads heads (4,096 together at most)
+ *   q_out, k_out outputs: the input itself (in place, at the same stride), or memory
+ *                that overlaps no input
+ *   grad         nonzero: the gradient of the inputs from that of the outputs
+ *                (angles -a)
+ * Errors: INVALID (sizes, strides, alignment, an output that partly overlaps
+ * its input), HIP. */
+int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, int32_t q_heads, const void* q,
+                   int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t k_heads, const void* k,
+                   int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t grad);
+
+/* ---- Causal attention over packed sequences, with its gradient: the training
+ * counterpart of a2t_chunk_attn, without a cache.  Queries and keys come
+ * rotated.  Query head h reads KV head h / (n_q_heads / n_kv_heads).
+ *   O_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i),
+ * over the rows j of i's sequence with j <= i and, where `until` is given,
+ * i < until[j].  until (device int32, one per packed row, places within the
+ * row's own sequence) says when a row has left the cache: trained with the
+ * until that a2t_evict's decisions give (a row evicted after the step that
+ * ends before place e has until = e; a row that stays, any number that is not
+ * below the sequence's rows), a session sees what it will see when it is
+ * served.  Any values are allowed; a row that sees nothing has O = 0,
+ * lse = -infinity and no gradient.  Rows of keys that leave in the order they
+ * came (as every eviction rule's do) cost what is visible; others are correct,
+ * but may cost more.
+ * Scores, softmax and sums are fp32; bf16 probabilities and score gradients
+ * are rounded to bf16 for the products that they enter.  Results do not depend
+ * on the order in which workgroups run.  Inputs are finite: a non-finite value
+ * of a row of v or of a gradient may reach every row of its sequence, and none
+ * of another's. */
+typedef struct a2t_prompt a2t_prompt;
+
+#define A2T_PROMPT_UNTIL 1u   /* calls may pass `until`: the handle holds copies of K and V */
+
+/* A handle for calls of up to max_rows packed rows (max_rows * n_q_heads <= 2^30).
+ * n_q_heads a multiple of n_kv_heads, at most 128 times as many; head_dim 64 or
+ * 128; dtype A2T_F32 or A2T_BF16; attn_scale 0 selects 1/sqrt(head_dim),
+ * otherwise within [1e-6, 1e6].  Allocates 4 n_q_heads bytes a row and, with
+ * A2T_PROMPT_UNTIL, K's and V's bytes and 20 more.  Errors: INVALID, OOM, NODEV. */
+int a2t_prompt_create(int32_t max_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                      double attn_scale, uint32_t flags, int32_t device, void* hip_stream, a2t_prompt** out);
+/* Waits for the stream, then frees the handle. */
+int a2t_prompt_destroy(a2t_prompt* p);
+int a2t_prompt_set_stream(a2t_prompt* p, void* hip_stream);
+
+/* Forward pass.
+ *   seq_rows  host [n_seqs], rows of each sequence (>= 0), at least one and at
+ *             most max_rows in all
+ *   q, k, v   device rows, strides in elements (at most 2^31)
+ *   until     device int32 [rows] or NULL
+ *   o         device [rows][Hq][D] out
+ *   lse       device float [Hq][rows] out (natural logarithm), or NULL
+ * Errors: INVALID (sizes, strides, alignment, `until` without A2T_PROMPT_UNTIL), HIP. */
+int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows, const void* q, int64_t q_stride,
+                    const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* until,
+                    void* o, float* lse);
+
+/* Gradients from that of o.  Inputs as in the forward pass, o and lse as it
+ * left them, d_o device [rows][Hq][D]; dq, dk, dv device out, rows at the
+ * strides of q, k and v (they may be parts of one tensor; they overlap no
+ * input).  Errors: as above. */
+int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows, const void* q, int64_t q_stride,
+                         const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* until,
+                         const void* o, const float* lse, const void* d_o, void* dq, void* dk, void* dv);
+
+/* ---- Preference loss of paired answers (transcripts, responses) on given
+ * logits, beside the adaptation objective: answers 2p (chosen) and 2p + 1
+ * (rejected) of pair p lie packed in that order.  With
+ *   ratio_a = sum over the answer's rows of ln p_policy(target) - ln p_reference(target),
+ *   h_p = beta (ratio_2p - ratio_2p+1),
+ *   L = mean_p -(1 - smoothing) ln sigma(h_p) - smoothing ln sigma(-h_p).
+ * A row whose target is outside [0, vocab) takes no part: ratio 0, zero gradient. */
+#define A2T_PREFER_MAX_PAIRS 256
+
+typedef struct a2t_prefer a2t_prefer;
+
+/* Scratch for up to max_rows rows (<= 2^22) of `vocab` logits (<= 2^30); dtype A2T_F32 or
+ * A2T_BF16 for logits and gradient.  Errors: INVALID, OOM, NODEV. */
+int a2t_prefer_create(int32_t max_rows, int32_t vocab, int32_t dtype, int32_t device, void* hip_stream,
+                      a2t_prefer** out);
+int a2t_prefer_destroy(a2t_prefer* p);
+int a2t_prefer_set_stream(a2t_prefer* p, void* hip_stream);
+
+/* ln p(target) of each row under softmax of its logits (0 where the target is
+ * outside the vocabulary): the score of an answer's tokens, or what a
+ * reference model is kept by.
+ *   logits  device [n_rows][stride], stride in elements, a multiple of 8
+ *   target  device int32 [n_rows]
+ *   logp    device float [n_rows] out.  Errors: INVALID, HIP. */
+int a2t_prefer_logp(a2t_prefer* p, int32_t n_rows, const void* logits, int64_t stride, const int32_t* target,
+                    float* logp);
+
+/* Loss and gradient.
+ *   n_pairs      1 .. A2T_PREFER_MAX_PAIRS
+ *   answer_rows  host [2 n_pairs], rows of each answer (>= 0; at least one row in all)
+ *   policy       device [rows][policy_stride] logits (stride a multiple of 8)
+ *   reference    device [rows][reference_stride] logits, or NULL with
+ *   ref_logp     device float [rows], ln p_reference(target) (exactly one of the two)
+ *   target       device int32 [rows]
+ *   beta > 0; smoothing within [0, 1]
+ *   losses       device float[3] out: L, the mean of h, the share of pairs with h > 0
+ *   ratios       device float [2 n_pairs] out, or NULL
+ *   grad         device [rows][policy_stride] out, dL / d policy logits (zero in the
+ *                stride's padding), or NULL; may be `policy` itself
+ * Errors: INVALID, HIP. */
+int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* answer_rows, const void* policy,
+                    int64_t policy_stride, const void* reference, int64_t reference_stride,
+                    const float* ref_logp, const int32_t* target, float beta, float smoothing, float* losses,
+                    float* ratios, void* grad);
 
 #ifdef __cplusplus
 }

@@ -33,6 +33,7 @@ A2T_MX4 = 2
 A2T_ALL_LAYERS = -1
 A2T_FLAG_HOST_ONLY = 1
 A2T_FLAG_NO_WORKSPACE = 2
+A2T_FLAG_ROTATED = 4
 A2T_RULE_UNIT, A2T_RULE_ROW, A2T_RULE_SINK_RECENT = 0, 1, 2
 SEG_PREFIX, SEG_ACOUSTIC, SEG_DELIM, SEG_TEXT, SEG_RESPONSE = 0, 1, 2, 3, 4
 
@@ -46,8 +47,16 @@ EXPORTED = (
     "a2t_profile_enable", "a2t_kernel_time", "a2t_profile_reserve", "a2t_status_str",
     "a2t_abi_version", "a2t_distill_create", "a2t_distill_destroy", "a2t_distill_loss",
     "a2t_distill_profile_enable", "a2t_distill_profile_reserve", "a2t_distill_kernel_time",
+    "a2t_rope_create", "a2t_rope_destroy", "a2t_rope_set_stream", "a2t_rope_apply",
+    "a2t_prompt_create", "a2t_prompt_destroy", "a2t_prompt_set_stream", "a2t_prompt_attn",
+    "a2t_prompt_attn_grad", "a2t_prefer_create", "a2t_prefer_destroy", "a2t_prefer_set_stream",
+    "a2t_prefer_logp", "a2t_prefer_loss",
 )
 A2T_ROW_NONE, A2T_ROW_ASR, A2T_ROW_NATIVE = 0, 1, 2
+A2T_ROPE_HALF, A2T_ROPE_PAIRS = 0, 1
+A2T_ROPE_PLAIN, A2T_ROPE_LINEAR, A2T_ROPE_NTK, A2T_ROPE_YARN = 0, 1, 2, 3
+A2T_PROMPT_UNTIL = 1
+A2T_PREFER_MAX_PAIRS = 256
 
 
 class a2t_config(C.Structure):
@@ -70,6 +79,15 @@ class a2t_stream_info(C.Structure):
     ]
 
 
+class a2t_rope_config(C.Structure):
+    _fields_ = [
+        ("head_dim", C.c_int32), ("dtype", C.c_int32), ("rotary_dim", C.c_int32),
+        ("layout", C.c_int32), ("scaling", C.c_int32), ("trained_rows", C.c_int32),
+        ("theta", C.c_double), ("factor", C.c_double), ("turns_fast", C.c_double),
+        ("turns_slow", C.c_double), ("device", C.c_int32), ("reserved", C.c_int32),
+    ]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is not built; run `python paper_2609_31224_amd/build.py`")
@@ -82,7 +100,7 @@ def _load():
     except ImportError:
         pass
     lib = C.CDLL(LIB_PATH)
-    P, I32, VP = C.POINTER, C.c_int32, C.c_void_p
+    P, I32, I64, VP = C.POINTER, C.c_int32, C.c_int64, C.c_void_p
     sig = {
         "a2t_cache_create": (C.c_int, [P(a2t_config), VP, P(VP)]),
         "a2t_cache_destroy": (C.c_int, [VP]),
@@ -122,6 +140,22 @@ def _load():
         "a2t_distill_profile_enable": (C.c_int, [VP, I32]),
         "a2t_distill_profile_reserve": (C.c_int, [VP, I32]),
         "a2t_distill_kernel_time": (C.c_int, [VP, P(C.c_int64), P(C.c_double)]),
+        "a2t_rope_create": (C.c_int, [P(a2t_rope_config), VP, P(VP)]),
+        "a2t_rope_destroy": (C.c_int, [VP]),
+        "a2t_rope_set_stream": (C.c_int, [VP, VP]),
+        "a2t_rope_apply": (C.c_int, [VP, I32, VP, I32, VP, I64, VP, I64, I32, VP, I64, VP, I64, I32]),
+        "a2t_prompt_create": (C.c_int, [I32, I32, I32, I32, I32, C.c_double, C.c_uint32, I32, VP, P(VP)]),
+        "a2t_prompt_destroy": (C.c_int, [VP]),
+        "a2t_prompt_set_stream": (C.c_int, [VP, VP]),
+        "a2t_prompt_attn": (C.c_int, [VP, I32, P(I32), VP, I64, VP, I64, VP, I64, VP, VP, VP]),
+        "a2t_prompt_attn_grad": (C.c_int, [VP, I32, P(I32), VP, I64, VP, I64, VP, I64, VP, VP, VP, VP,
+                                           VP, VP, VP]),
+        "a2t_prefer_create": (C.c_int, [I32, I32, I32, I32, VP, P(VP)]),
+        "a2t_prefer_destroy": (C.c_int, [VP]),
+        "a2t_prefer_set_stream": (C.c_int, [VP, VP]),
+        "a2t_prefer_logp": (C.c_int, [VP, I32, VP, I64, VP, VP]),
+        "a2t_prefer_loss": (C.c_int, [VP, I32, P(I32), VP, I64, VP, I64, VP, VP, C.c_float, C.c_float,
+                                      VP, VP, VP]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -487,3 +521,240 @@ def a2t_distill_loss(d: Distill, student, teacher, kind, target, dec_group, turn
                                _p(tu, C.c_int8), float(temperature),
                                _dev(losses, "losses", torch.float32), _dev(grad, "grad", dt))
     _check(rc, "a2t_distill_loss")
+
+
+# ---- training on whole sessions: rotary encoding, packed attention, preference loss
+def _torch_dtype(dtype: int):
+    import torch
+    return torch.float32 if dtype == A2T_F32 else torch.bfloat16
+
+
+def _rows(x, what: str, dtype, heads: Optional[int], dim: int, n: Optional[int] = None):
+    """(address, row stride) of a GPU tensor [rows][heads][dim] whose rows are dense; the rows may
+    be parts of wider ones.  Sizes that do not fit are a ValueError."""
+    import torch
+    if not isinstance(x, torch.Tensor):
+        raise TypeError(f"{what}: expected a GPU torch tensor")
+    if not x.is_cuda:
+        raise ValueError(f"{what}: tensor must live on the GPU")
+    if x.dtype != dtype:
+        raise ValueError(f"{what}: dtype {x.dtype}, the handle uses {dtype}")
+    if x.dim() != 3 or x.shape[2] != dim or (heads is not None and x.shape[1] != heads) or (n is not None and x.shape[0] != n):
+        want = f"[{'rows' if n is None else n}][{'heads' if heads is None else heads}][{dim}]"
+        raise ValueError(f"{what}: shape {tuple(x.shape)}, expected {want}")
+    if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != dim):
+        raise ValueError(f"{what}: a row's heads must be dense")
+    stride = x.stride(0) if x.shape[0] > 1 else max(x.stride(0), (x.shape[1] * dim + 7) // 8 * 8)
+    return x.data_ptr(), int(stride)
+
+
+def _flat(x, what: str, dtype, numel: int):
+    """Address of a contiguous GPU tensor with `numel` elements."""
+    if x is None:
+        return None
+    if isinstance(x, int):
+        raise TypeError(f"{what}: expected a GPU torch tensor")
+    ptr = _dev(x, what, dtype)
+    if x.numel() != numel:
+        raise ValueError(f"{what}: {x.numel()} elements, expected {numel}")
+    return ptr
+
+
+@dataclass
+class Rope:
+    """Handle returned by a2t_rope_create."""
+    ptr: C.c_void_p
+    head_dim: int
+    dtype: int
+
+
+def a2t_rope_create(head_dim: int, dtype: int, rotary_dim: int = 0, layout: int = A2T_ROPE_HALF, theta: float = 0.0,
+                    scaling: int = A2T_ROPE_PLAIN, factor: float = 1.0, trained_rows: int = 0, turns_fast: float = 32.0,
+                    turns_slow: float = 1.0, device: int = 0, stream=None) -> Rope:
+    cfg = a2t_rope_config(head_dim, dtype, rotary_dim, layout, scaling, trained_rows, theta, factor, turns_fast,
+                          turns_slow, device, 0)
+    out = C.c_void_p()
+    _check(_lib.a2t_rope_create(C.byref(cfg), _stream_handle(stream), C.byref(out)), "a2t_rope_create")
+    return Rope(out, head_dim, dtype)
+
+
+def a2t_rope_destroy(r: Rope) -> None:
+    if r.ptr:
+        _check(_lib.a2t_rope_destroy(r.ptr), "a2t_rope_destroy")
+        r.ptr = C.c_void_p()
+
+
+def a2t_rope_set_stream(r: Rope, stream) -> None:
+    _check(_lib.a2t_rope_set_stream(r.ptr, _stream_handle(stream)), "a2t_rope_set_stream")
+
+
+def a2t_rope_apply(r: Rope, pos, q=None, k=None, q_out=None, k_out=None, grad: bool = False) -> None:
+    """q, k: GPU tensors [rows][heads][D] (either may be None), rotated into q_out, k_out (the input
+    itself rotates in place); pos: GPU int32 [rows].  grad=True turns gradients of the outputs back."""
+    import torch
+    dt, n = _torch_dtype(r.dtype), int(pos.shape[0])
+    args = []
+    for what, x, out in (("q", q, q_out), ("k", k, k_out)):
+        if x is None:
+            if out is not None:
+                raise ValueError(f"{what}_out without {what}")
+            args += [0, None, 0, None, 0]
+            continue
+        heads = int(x.shape[1]) if x.dim() == 3 else None
+        args += [heads or 0, *_rows(x, what, dt, None, r.head_dim, n), *_rows(out, what + "_out", dt, heads, r.head_dim, n)]
+    _check(_lib.a2t_rope_apply(r.ptr, n, _flat(pos, "pos", torch.int32, n), *args, int(bool(grad))), "a2t_rope_apply")
+
+
+@dataclass
+class Prompt:
+    """Handle returned by a2t_prompt_create."""
+    ptr: C.c_void_p
+    max_rows: int
+    n_q_heads: int
+    n_kv_heads: int
+    head_dim: int
+    dtype: int
+
+
+def a2t_prompt_create(max_rows: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, attn_scale: float = 0.0,
+                      flags: int = 0, device: int = 0, stream=None) -> Prompt:
+    out = C.c_void_p()
+    _check(_lib.a2t_prompt_create(max_rows, n_q_heads, n_kv_heads, head_dim, dtype, attn_scale, flags, device,
+                                  _stream_handle(stream), C.byref(out)), "a2t_prompt_create")
+    return Prompt(out, max_rows, n_q_heads, n_kv_heads, head_dim, dtype)
+
+
+def a2t_prompt_destroy(p: Prompt) -> None:
+    if p.ptr:
+        _check(_lib.a2t_prompt_destroy(p.ptr), "a2t_prompt_destroy")
+        p.ptr = C.c_void_p()
+
+
+def a2t_prompt_set_stream(p: Prompt, stream) -> None:
+    _check(_lib.a2t_prompt_set_stream(p.ptr, _stream_handle(stream)), "a2t_prompt_set_stream")
+
+
+def _prompt_rows(p: Prompt, seq_rows, q, k, v, until):
+    import torch
+    rows = _i32(seq_rows)
+    n = int(rows.sum(dtype=np.int64))
+    dt = _torch_dtype(p.dtype)
+    given = []
+    for what, x, heads in (("q", q, p.n_q_heads), ("k", k, p.n_kv_heads), ("v", v, p.n_kv_heads)):
+        given.append(_rows(x, what, dt, heads, p.head_dim))
+        if x.shape[0] < n:
+            raise ValueError(f"{what}: {x.shape[0]} rows, the sequences have {n}")
+    if until is not None and _dev(until, "until", torch.int32) is not None and until.numel() < n:
+        raise ValueError(f"until: {until.numel()} entries, the sequences have {n} rows")
+    return rows, n, dt, given, None if until is None else until.data_ptr()
+
+
+def _packed(x, what: str, dt, p: Prompt, n: int):
+    ptr = _dev(x, what, dt)
+    if ptr is None or isinstance(x, int):
+        raise TypeError(f"{what}: expected a GPU torch tensor")
+    if x.dim() != 3 or x.shape[0] < n or tuple(x.shape[1:]) != (p.n_q_heads, p.head_dim):
+        raise ValueError(f"{what}: shape {tuple(x.shape)}, expected [{n}][{p.n_q_heads}][{p.head_dim}]")
+    return ptr
+
+
+def a2t_prompt_attn(p: Prompt, seq_rows: Sequence[int], q, k, v, o, lse=None, until=None) -> None:
+    """q, k, v: GPU tensors [rows][heads][D], rows dense; o: GPU [rows][Hq][D]; lse: GPU float32
+    [Hq][rows], rows the sum of seq_rows, or None; until: GPU int32 [rows] or None."""
+    import torch
+    rows, n, dt, given, ut = _prompt_rows(p, seq_rows, q, k, v, until)
+    _check(_lib.a2t_prompt_attn(p.ptr, len(rows), _p(rows, C.c_int32), *given[0], *given[1], *given[2], ut,
+                                _packed(o, "o", dt, p, n), _flat(lse, "lse", torch.float32, n * p.n_q_heads)),
+           "a2t_prompt_attn")
+
+
+def a2t_prompt_attn_grad(p: Prompt, seq_rows: Sequence[int], q, k, v, o, lse, d_o, dq, dk, dv, until=None) -> None:
+    """Gradients dq, dk, dv from d_o: GPU tensors shaped and strided like q, k, v."""
+    import torch
+    rows, n, dt, given, ut = _prompt_rows(p, seq_rows, q, k, v, until)
+    outs = []
+    for what, x, like, (_, stride), heads in (("dq", dq, q, given[0], p.n_q_heads), ("dk", dk, k, given[1], p.n_kv_heads),
+                                              ("dv", dv, v, given[2], p.n_kv_heads)):
+        ptr, own = _rows(x, what, dt, heads, p.head_dim)
+        if x.shape[0] < n or (own != stride and n > 1):
+            raise ValueError(f"{what}: {x.shape[0]} rows with stride {own}, expected {n} with stride {stride}")
+        outs.append(ptr)
+    if lse is None:
+        raise ValueError("lse: the forward pass's")
+    _check(_lib.a2t_prompt_attn_grad(p.ptr, len(rows), _p(rows, C.c_int32), *given[0], *given[1], *given[2], ut,
+                                     _packed(o, "o", dt, p, n), _flat(lse, "lse", torch.float32, n * p.n_q_heads),
+                                     _packed(d_o, "d_o", dt, p, n), *outs), "a2t_prompt_attn_grad")
+
+
+@dataclass
+class Prefer:
+    """Handle returned by a2t_prefer_create."""
+    ptr: C.c_void_p
+    max_rows: int
+    vocab: int
+    dtype: int
+
+
+def a2t_prefer_create(max_rows: int, vocab: int, dtype: int, device: int = 0, stream=None) -> Prefer:
+    out = C.c_void_p()
+    _check(_lib.a2t_prefer_create(max_rows, vocab, dtype, device, _stream_handle(stream), C.byref(out)), "a2t_prefer_create")
+    return Prefer(out, max_rows, vocab, dtype)
+
+
+def a2t_prefer_destroy(p: Prefer) -> None:
+    if p.ptr:
+        _check(_lib.a2t_prefer_destroy(p.ptr), "a2t_prefer_destroy")
+        p.ptr = C.c_void_p()
+
+
+def a2t_prefer_set_stream(p: Prefer, stream) -> None:
+    _check(_lib.a2t_prefer_set_stream(p.ptr, _stream_handle(stream)), "a2t_prefer_set_stream")
+
+
+def _logits(p: Prefer, x, what: str, n: int):
+    """(address, row stride) of a GPU tensor [rows][>= vocab] of logits, rows dense."""
+    import torch
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise ValueError(f"{what}: expected a GPU torch tensor")
+    if x.dtype != _torch_dtype(p.dtype):
+        raise ValueError(f"{what}: dtype {x.dtype}, the handle uses {_torch_dtype(p.dtype)}")
+    if x.dim() != 2 or x.shape[0] < n or x.shape[1] < p.vocab or x.stride(1) != 1:
+        raise ValueError(f"{what}: shape {tuple(x.shape)}, expected [{n}][{p.vocab} or more] with dense rows")
+    if x.stride(0) < x.shape[1] and x.shape[0] > 1:
+        raise ValueError(f"{what}: rows overlap")
+    # the last row is read (and the gradient's written) in whole chunks of 8 elements up to its stride
+    room = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
+    if room < (n - 1) * x.stride(0) + (x.stride(0) if what == "grad" else (p.vocab + 7) // 8 * 8):
+        raise ValueError(f"{what}: the last row ends before its stride does")
+    return x.data_ptr(), int(x.stride(0))
+
+
+def a2t_prefer_logp(p: Prefer, logits, target, logp) -> None:
+    """logits: GPU [rows][stride]; target: GPU int32 [rows]; logp: GPU float32 [rows] out."""
+    import torch
+    n = int(target.shape[0])
+    _check(_lib.a2t_prefer_logp(p.ptr, n, *_logits(p, logits, "logits", n), _flat(target, "target", torch.int32, n),
+                                _flat(logp, "logp", torch.float32, n)), "a2t_prefer_logp")
+
+
+def a2t_prefer_loss(p: Prefer, answer_rows: Sequence[int], policy, target, losses, reference=None, ref_logp=None,
+                    beta: float = 0.1, smoothing: float = 0.0, ratios=None, grad=None) -> None:
+    """answer_rows: host, rows of the chosen and the rejected answer of each pair in turn; policy,
+    reference: GPU [rows][stride] logits; losses: GPU float32 [3]; ratios: GPU float32, one per answer;
+    grad: GPU tensor like policy (or policy itself)."""
+    import torch
+    rows = _i32(answer_rows)
+    if rows.ndim != 1 or len(rows) % 2:
+        raise ValueError("answer_rows: two answers a pair")
+    n = int(rows.sum(dtype=np.int64))
+    ptr, stride = _logits(p, policy, "policy", n)
+    ref = (None, 0) if reference is None else _logits(p, reference, "reference", n)
+    g = None
+    if grad is not None:
+        g, own = _logits(p, grad, "grad", n)
+        if own != stride:
+            raise ValueError(f"grad: stride {own}, the policy's is {stride}")
+    _check(_lib.a2t_prefer_loss(p.ptr, len(rows) // 2, _p(rows, C.c_int32), ptr, stride, *ref,
+                                _flat(ref_logp, "ref_logp", torch.float32, n), _flat(target, "target", torch.int32, n),
+                                float(beta), float(smoothing), _flat(losses, "losses", torch.float32, 3),
+                                _flat(ratios, "ratios", torch.float32, len(rows)), g), "a2t_prefer_loss")

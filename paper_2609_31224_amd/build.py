@@ -17,7 +17,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 ROOT = os.path.dirname(HERE)
 LIB = os.path.join(HERE, "libA2T.so")
-SOURCES = ["kernels.hip", "attn_block.hip", "attn_f32.hip", "attn_mx4.hip", "attn_mx4_rows.hip", "mx4_rows.hip", "a2t.cpp", "distill.hip"]
+SOURCES = ["kernels.hip", "attn_block.hip", "attn_f32.hip", "attn_mx4.hip", "attn_mx4_rows.hip", "mx4_rows.hip", "a2t.cpp", "distill.hip",
+           "rope.hip", "prompt_attn.hip", "prompt_sort.hip", "prompt.cpp", "prefer.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"

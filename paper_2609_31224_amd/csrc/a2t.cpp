@@ -893,7 +893,8 @@ int a2t_cache_create(const a2t_config* cfg, void* hip_stream, a2t_cache** out) {
     d.unit_rows = k.unit_rows;
     d.kept_rows = k.kept_rows;
     d.max_step_rows = k.max_step_rows;
-    for (int i = 0; i < k.head_dim / 2; ++i) c->freq.f[i] = std::pow(c->cfg.rope_theta, (-2.0 * i) / k.head_dim);
+    const bool rotated = (k.flags & A2T_FLAG_ROTATED) != 0;   // angles of zero leave rows as they are
+    for (int i = 0; i < k.head_dim / 2; ++i) c->freq.f[i] = rotated ? 0.0 : std::pow(c->cfg.rope_theta, (-2.0 * i) / k.head_dim);
     d.scale_log2e = (float)(c->cfg.attn_scale * 1.4426950408889634);
     if (c->host_only) {
         *out = c;

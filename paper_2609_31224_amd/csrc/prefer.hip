@@ -1,0 +1,422 @@
+// The preference loss of paired answers on given logits, and the log probabilities of
+// target tokens (gfx950).  Public API: include/a2t.h (a2t_prefer_*).
+//
+//   prefer_rows_kernel  one workgroup per row (policy rows, then reference rows): (max, sum
+//                       of exponentials) of the row and log p(target) = x_t - max - ln sum.
+//   prefer_grad_kernel  one workgroup per policy row: the sums of the row's pair, the slope
+//                       of the loss, and the gradient slope (p_v - [v = target]); one more
+//                       workgroup writes the loss and every answer's ratio.
+// The slope of a row depends on all rows of its pair, so the policy's logits are read twice.
+// Every workgroup adds a pair's rows by itself, in the same order (deterministic, and one
+// launch less), in 64 bits: a ratio is a small difference of large sums.
+#include "../../include/a2t.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <new>
+#include <type_traits>
+
+namespace {
+
+constexpr int kChunk = 8;             // elements of a chunk (16 bytes of bf16, 32 of fp32)
+constexpr int kMaxPairs = A2T_PREFER_MAX_PAIRS;
+constexpr int kAnswers = 2 * kMaxPairs;
+constexpr float kLog2e = 1.44269504088896340736f;
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+struct bf16_t {
+    uint16_t bits;
+};
+// one chunk as stored
+template <typename T> struct Raw;
+template <> struct Raw<bf16_t> {
+    u32x4 a;
+};
+template <> struct Raw<float> {
+    u32x4 a, b;
+};
+__device__ __forceinline__ Raw<bf16_t> load_raw(const bf16_t* row, int c) {
+    return {reinterpret_cast<const u32x4*>(row)[c]};
+}
+__device__ __forceinline__ Raw<float> load_raw(const float* row, int c) {
+    const u32x4* p = reinterpret_cast<const u32x4*>(row) + 2 * c;
+    return {p[0], p[1]};
+}
+__device__ __forceinline__ void unpack(const Raw<bf16_t>& r, float (&x)[kChunk]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(r.a[e] << 16);
+        x[2 * e + 1] = __uint_as_float(r.a[e] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void unpack(const Raw<float>& r, float (&x)[kChunk]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = __uint_as_float(r.a[e]);
+        x[4 + e] = __uint_as_float(r.b[e]);
+    }
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    const bf16x2 v = {(__bf16)a, (__bf16)b};   // round to nearest even, once per output
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ void store_chunk(bf16_t* row, int c, const float (&x)[kChunk]) {
+    reinterpret_cast<u32x4*>(row)[c] = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+}
+__device__ __forceinline__ void store_chunk(float* row, int c, const float (&x)[kChunk]) {
+    u32x4 a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        a[e] = __float_as_uint(x[e]);
+        b[e] = __float_as_uint(x[4 + e]);
+    }
+    reinterpret_cast<u32x4*>(row)[2 * c] = a;
+    reinterpret_cast<u32x4*>(row)[2 * c + 1] = b;
+}
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ float value(const bf16_t* row, int i) { return __uint_as_float((uint32_t)row[i].bits << 16); }
+__device__ __forceinline__ float value(const float* row, int i) { return row[i]; }
+
+// (largest value m, sum of e^(x - m)) of parts of a row
+struct Sum {
+    float m, z;
+};
+__device__ __forceinline__ Sum join(Sum a, Sum b) {
+    const float m = fmaxf(a.m, b.m), ref = m == -INFINITY ? 0.f : m;
+    return {m, a.z * exp2_((a.m - ref) * kLog2e) + b.z * exp2_((b.m - ref) * kLog2e)};
+}
+
+// Statistics of a row: its largest logit and the logarithm of its sum, and log p(target).
+struct RowStat {
+    double logp;
+    float m, z;
+};
+
+template <typename T>
+struct RowsArgs {
+    const T* x[2];            // policy, reference (null: policy rows only)
+    int64_t stride[2];
+    const int32_t* target;
+    RowStat* stat;            // [2][n] out, or null
+    float* logp;              // [n] out, or null
+    int32_t n, vocab;
+};
+
+template <typename T, int TH>
+__global__ __launch_bounds__(TH) void prefer_rows_kernel(RowsArgs<T> a) {
+    const int tid = threadIdx.x, which = (int)blockIdx.x >= a.n, row = (int)blockIdx.x - which * a.n;
+    const int target = a.target[row];
+    RowStat* stat = a.stat ? a.stat + blockIdx.x : nullptr;
+    if (target < 0 || target >= a.vocab) {   // no loss at this row
+        if (tid == 0) {
+            if (stat) *stat = {0.0, 0.f, 0.f};
+            if (a.logp) a.logp[row] = 0.f;
+        }
+        return;
+    }
+    const T* x = a.x[which] + row * a.stride[which];
+    const int full = a.vocab / kChunk;
+    Sum s{-INFINITY, 0.f};
+    auto add = [&](const float (&v)[kChunk]) {
+        float m = s.m;
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) m = fmaxf(m, v[e]);
+        const float ref = m == -INFINITY ? 0.f : m;
+        float z = s.z * exp2_((s.m - ref) * kLog2e);
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) z += exp2_((v[e] - ref) * kLog2e);
+        s = {m, z};
+    };
+    constexpr int kAhead = 4;   // chunks requested at once
+    int c = tid;
+    for (; c + (kAhead - 1) * TH < full; c += kAhead * TH) {
+        Raw<T> r[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) r[k] = load_raw(x, c + k * TH);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            float v[kChunk];
+            unpack(r[k], v);
+            add(v);
+        }
+    }
+    for (; c < full; c += TH) {
+        float v[kChunk];
+        unpack(load_raw(x, c), v);
+        add(v);
+    }
+    if (tid < a.vocab - full * kChunk) s = join(s, {value(x, full * kChunk + tid), 1.f});
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) s = join(s, {__shfl_xor(s.m, d), __shfl_xor(s.z, d)});
+    __shared__ Sum part[TH / 64];
+    if (tid % 64 == 0) part[tid / 64] = s;
+    __syncthreads();
+    if (tid) return;
+    for (int w = 1; w < TH / 64; ++w) s = join(s, part[w]);
+    const double logp = (double)(value(x, target) - s.m) - log((double)s.z);
+    if (stat) *stat = {logp, s.m, s.z};
+    if (a.logp) a.logp[row] = (float)logp;
+}
+
+template <typename T>
+struct GradArgs {
+    const T* x;
+    T* grad;                  // null: no gradient
+    int64_t stride;
+    const RowStat* stat;      // [2][n]
+    const float* ref_logp;    // [n], or null: the reference's rows are in stat
+    const int32_t* target;
+    float* losses;            // [3]
+    float* ratios;            // [2 pairs], or null
+    int32_t n, vocab, pairs;
+    float beta, smoothing;
+    int32_t start[kAnswers + 1];   // first row of each answer
+};
+
+// sum over rows lo..hi of log p_policy - log p_reference: every lane of the wave gets it
+template <typename T>
+__device__ __forceinline__ double answer_ratio(const GradArgs<T>& a, int lo, int hi) {
+    double r = 0.0;
+    for (int i = lo + (threadIdx.x & 63); i < hi; i += 64) {
+        const int t = a.target[i];
+        if (t >= 0 && t < a.vocab) r += a.stat[i].logp - (a.ref_logp ? (double)a.ref_logp[i] : a.stat[a.n + i].logp);
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) r += __shfl_xor(r, d);
+    return r;
+}
+// ln(1 / (1 + e^-h))
+__device__ __forceinline__ double log_sigmoid(double h) { return fmin(h, 0.0) - log1p(exp(-fabs(h))); }
+__device__ __forceinline__ double sigmoid(double h) { return 1.0 / (1.0 + exp(-h)); }
+
+template <typename T, int TH>
+__global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (blockIdx.x == 0) {   // the loss
+        __shared__ double sums[TH / 64][3];
+        double loss = 0.0, margin = 0.0, won = 0.0;
+        for (int p = wave; p < a.pairs; p += TH / 64) {
+            const double good = answer_ratio(a, a.start[2 * p], a.start[2 * p + 1]);
+            const double poor = answer_ratio(a, a.start[2 * p + 1], a.start[2 * p + 2]);
+            const double h = a.beta * (good - poor);
+            loss -= (1.0 - a.smoothing) * log_sigmoid(h) + a.smoothing * log_sigmoid(-h);
+            margin += h;
+            won += h > 0.0 ? 1.0 : 0.0;
+            if (a.ratios && lane == 0) {
+                a.ratios[2 * p] = (float)good;
+                a.ratios[2 * p + 1] = (float)poor;
+            }
+        }
+        if (lane == 0) sums[wave][0] = loss, sums[wave][1] = margin, sums[wave][2] = won;
+        __syncthreads();
+        if (tid < 3) {
+            double t = 0.0;
+            for (int w = 0; w < TH / 64; ++w) t += sums[w][tid];
+            a.losses[tid] = (float)(t / a.pairs);
+        }
+        return;
+    }
+    const int row = a.n - (int)blockIdx.x;   // the rows read last come first: they may still be in a cache
+    const int target = a.target[row];
+    T* g = a.grad + row * a.stride;
+    const int chunks = (int)(a.stride / kChunk);
+    float slope = 0.f, m = 0.f, inv = 0.f;
+    if (target >= 0 && target < a.vocab) {
+        // the row's answer: as many answers start at or before it, less one
+        int before = 0;
+        for (int k = lane; k < 2 * a.pairs; k += 64) before += a.start[k] <= row;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
+        const int answer = before - 1, p = answer / 2;
+        const double good = answer_ratio(a, a.start[2 * p], a.start[2 * p + 1]);
+        const double poor = answer_ratio(a, a.start[2 * p + 1], a.start[2 * p + 2]);
+        const double h = a.beta * (good - poor);
+        // -dL/d(good): L falls as the chosen answer's ratio grows
+        const double c = a.beta * ((1.0 - a.smoothing) * sigmoid(-h) - a.smoothing * sigmoid(h)) / a.pairs;
+        slope = (float)(answer & 1 ? -c : c);
+        m = a.stat[row].m;
+        inv = slope / a.stat[row].z;
+    }
+    const T* x = a.x + row * a.stride;
+    const int used = (a.vocab + kChunk - 1) / kChunk;
+    auto write = [&](int c, const Raw<T>& r) {
+        float v[kChunk];
+        unpack(r, v);
+#pragma unroll
+        for (int e = 0; e < kChunk; ++e) {
+            const int i = c * kChunk + e;
+            v[e] = inv * exp2_((v[e] - m) * kLog2e);
+            if (i == target) v[e] -= slope;
+            if (slope == 0.f || i >= a.vocab) v[e] = 0.f;
+        }
+        store_chunk(g, c, v);
+    };
+    constexpr int kAhead = 4;
+    int c = tid;
+    for (; c + (kAhead - 1) * TH < used; c += kAhead * TH) {
+        Raw<T> r[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) r[k] = load_raw(x, c + k * TH);
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) write(c + k * TH, r[k]);
+    }
+    for (; c < used; c += TH) write(c, load_raw(x, c));
+    for (; c < chunks; c += TH) {
+        const float zero[kChunk] = {};
+        store_chunk(g, c, zero);
+    }
+}
+
+struct DevGuard {
+    int prev = -1;
+    explicit DevGuard(int dev) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        if (prev != dev) (void)hipSetDevice(dev);
+    }
+    ~DevGuard() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1u)) != 0; }
+
+}  // namespace
+
+struct a2t_prefer {
+    int32_t max_rows = 0, vocab = 0, dtype = 0, device = 0;
+    hipStream_t stream = nullptr;
+    RowStat* stat = nullptr;   // [2][max_rows]
+    int cus = 256;
+    bool poisoned = false;
+};
+
+namespace {
+
+// Row statistics of the policy's rows and, with `reference`, of the reference's behind them.
+template <typename T>
+hipError_t launch_rows(a2t_prefer* p, int n, const void* policy, int64_t ps, const void* reference, int64_t rs, const int32_t* target,
+                       RowStat* stat, float* logp) {
+    RowsArgs<T> a{{static_cast<const T*>(policy), static_cast<const T*>(reference)}, {ps, rs}, target, stat, logp, n, p->vocab};
+    const int64_t rows = reference ? 2 * (int64_t)n : n;
+    const int chunks = p->vocab / kChunk;
+    const dim3 grid((uint32_t)rows);
+    // more threads a row where the rows alone do not fill the CUs
+    if (rows < 4 * p->cus && chunks >= 1024) hipLaunchKernelGGL((prefer_rows_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
+    else hipLaunchKernelGGL((prefer_rows_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+extern "C" int a2t_prefer_create(int32_t max_rows, int32_t vocab, int32_t dtype, int32_t device, void* hip_stream, a2t_prefer** out) {
+    if (!out) return A2T_ERR_INVALID;
+    *out = nullptr;
+    if (max_rows < 1 || max_rows > (1 << 22) || vocab < 1 || vocab > (1 << 30) || (dtype != A2T_F32 && dtype != A2T_BF16)) return A2T_ERR_INVALID;
+    int n_dev = 0;
+    if (hipGetDeviceCount(&n_dev) != hipSuccess || device < 0 || device >= n_dev) return A2T_ERR_NODEV;
+    DevGuard g(device);
+    a2t_prefer* p = new (std::nothrow) a2t_prefer();
+    if (!p) return A2T_ERR_OOM;
+    p->max_rows = max_rows;
+    p->vocab = vocab;
+    p->dtype = dtype;
+    p->device = device;
+    p->stream = static_cast<hipStream_t>(hip_stream);
+    int cus = 0;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && cus > 0) p->cus = cus;
+    if (hipMalloc(&p->stat, sizeof(RowStat) * 2 * (size_t)max_rows) != hipSuccess) {
+        (void)hipGetLastError();
+        delete p;
+        return A2T_ERR_OOM;
+    }
+    *out = p;
+    return A2T_OK;
+}
+
+extern "C" int a2t_prefer_destroy(a2t_prefer* p) {
+    if (!p) return A2T_ERR_INVALID;
+    {
+        DevGuard g(p->device);
+        (void)hipStreamSynchronize(p->stream);
+        (void)hipFree(p->stat);
+    }
+    delete p;
+    return A2T_OK;
+}
+
+extern "C" int a2t_prefer_set_stream(a2t_prefer* p, void* hip_stream) {
+    if (!p) return A2T_ERR_INVALID;
+    p->stream = static_cast<hipStream_t>(hip_stream);
+    return A2T_OK;
+}
+
+extern "C" int a2t_prefer_logp(a2t_prefer* p, int32_t n_rows, const void* logits, int64_t stride, const int32_t* target, float* logp) {
+    if (!p) return A2T_ERR_INVALID;
+    if (p->poisoned) return A2T_ERR_HIP;
+    if (n_rows < 1 || n_rows > p->max_rows || !logits || !target || !logp || stride < p->vocab || stride % 8 || stride > (1ll << 40) ||
+        misaligned(logits, 16) || misaligned(target, 4) || misaligned(logp, 4))
+        return A2T_ERR_INVALID;
+    DevGuard g(p->device);
+    const hipError_t e = p->dtype == A2T_F32 ? launch_rows<float>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp)
+                                             : launch_rows<bf16_t>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp);
+    if (e != hipSuccess) {
+        p->poisoned = true;
+        return A2T_ERR_HIP;
+    }
+    return A2T_OK;
+}
+
+extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* answer_rows, const void* policy, int64_t policy_stride,
+                               const void* reference, int64_t reference_stride, const float* ref_logp, const int32_t* target,
+                               float beta, float smoothing, float* losses, float* ratios, void* grad) {
+    if (!p) return A2T_ERR_INVALID;
+    if (p->poisoned) return A2T_ERR_HIP;
+    if (n_pairs < 1 || n_pairs > kMaxPairs || !answer_rows || !policy || !target || !losses || (reference != nullptr) == (ref_logp != nullptr))
+        return A2T_ERR_INVALID;
+    if (!std::isfinite(beta) || beta <= 0.f || !(smoothing >= 0.f && smoothing <= 1.f)) return A2T_ERR_INVALID;
+    int64_t n = 0;
+    for (int i = 0; i < 2 * n_pairs; ++i) {
+        if (answer_rows[i] < 0) return A2T_ERR_INVALID;
+        n += answer_rows[i];
+    }
+    if (n < 1 || n > p->max_rows) return A2T_ERR_INVALID;
+    auto bad_stride = [&](int64_t s) { return s < p->vocab || s % 8 || s > (1ll << 33); };
+    if (bad_stride(policy_stride) || (reference && bad_stride(reference_stride)) || misaligned(policy, 16) || misaligned(reference, 16) ||
+        misaligned(grad, 16) || misaligned(ref_logp, 4) || misaligned(target, 4) || misaligned(losses, 4) || misaligned(ratios, 4))
+        return A2T_ERR_INVALID;
+    DevGuard g(p->device);
+    auto go = [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        hipError_t e = launch_rows<T>(p, (int)n, policy, policy_stride, reference, reference_stride, target, p->stat, nullptr);
+        if (e != hipSuccess) return e;
+        GradArgs<T> a{};
+        a.x = static_cast<const T*>(policy);
+        a.grad = static_cast<T*>(grad);
+        a.stride = policy_stride;
+        a.stat = p->stat;
+        a.ref_logp = ref_logp;
+        a.target = target;
+        a.losses = losses;
+        a.ratios = ratios;
+        a.n = (int32_t)n;
+        a.vocab = p->vocab;
+        a.pairs = n_pairs;
+        a.beta = beta;
+        a.smoothing = smoothing;
+        for (int i = 0; i < 2 * n_pairs; ++i) a.start[i + 1] = a.start[i] + answer_rows[i];
+        const dim3 grid(grad ? (uint32_t)n + 1 : 1);
+        const int chunks = p->vocab / kChunk;
+        if (n < 4 * p->cus && chunks >= 1024) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
+        else hipLaunchKernelGGL((prefer_grad_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
+        return hipGetLastError();
+    };
+    const hipError_t e = p->dtype == A2T_F32 ? go((float*)nullptr) : go((bf16_t*)nullptr);
+    if (e != hipSuccess) {
+        p->poisoned = true;
+        return A2T_ERR_HIP;
+    }
+    return A2T_OK;
+}

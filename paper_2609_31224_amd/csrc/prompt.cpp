@@ -1,0 +1,239 @@
+// Host side of the attention over packed sequences (a2t_prompt_* of include/a2t.h): argument
+// checks, the table of sequences that a launch carries, and the launches.
+#include "../../include/a2t.h"
+#include "prompt.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+using namespace a2t::prompt;
+
+struct a2t_prompt {
+    int32_t max_rows = 0, Hq = 0, Hkv = 0, D = 0, dtype = 0, device = 0;
+    double scale = 0.0;
+    hipStream_t stream = nullptr;
+    float* delta = nullptr;      // [Hq][rows of the call]
+    // handles for calls with `until`: sorted copies of K and V, and what the kernels know of them
+    void* k = nullptr;
+    void* v = nullptr;
+    int2* meta = nullptr;
+    int32_t* lasting = nullptr;
+    int32_t* first = nullptr;
+    int32_t* reach = nullptr;
+    bool until = false;
+    bool poisoned = false;
+};
+
+namespace {
+
+struct DevGuard {
+    int prev = -1;
+    explicit DevGuard(int dev) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        if (prev != dev) (void)hipSetDevice(dev);
+    }
+    ~DevGuard() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+void free_prompt(a2t_prompt* p) {
+    for (void* m : {(void*)p->delta, p->k, p->v, (void*)p->meta, (void*)p->lasting, (void*)p->first, (void*)p->reach})
+        if (m) (void)hipFree(m);
+    delete p;
+}
+
+bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1u)) != 0; }
+
+// A call's rows, checked: 0 where something is wrong with them.
+int64_t total_rows(const a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows) {
+    if (n_seqs < 1 || !seq_rows) return 0;
+    int64_t total = 0;
+    for (int32_t i = 0; i < n_seqs; ++i) {
+        if (seq_rows[i] < 0) return 0;
+        total += seq_rows[i];
+        if (total > p->max_rows) return 0;
+    }
+    return total;
+}
+
+bool bad_rows(const a2t_prompt* p, const void* x, int64_t stride, int heads) {
+    return !x || misaligned(x, 16) || stride < (int64_t)heads * p->D || stride % 8 || stride > (1ll << 31);
+}
+
+// Calls f with tables of at most kMaxSeqs sequences, longest first (the launch's last workgroups
+// are short ones); sequences without rows take no part.
+template <class F>
+hipError_t in_tables(int32_t n_seqs, const int32_t* seq_rows, F&& f) {
+    struct Seq {
+        int32_t row0, rows;
+    } s[kMaxSeqs];
+    int32_t row0 = 0;
+    for (int32_t i = 0; i < n_seqs;) {
+        int count = 0;
+        for (; i < n_seqs && count < kMaxSeqs; row0 += seq_rows[i++])
+            if (seq_rows[i]) s[count++] = {row0, seq_rows[i]};
+        if (!count) continue;
+        std::sort(s, s + count, [](const Seq& a, const Seq& b) { return a.rows != b.rows ? a.rows > b.rows : a.row0 < b.row0; });
+        SeqTable<kMaxSeqs> t;
+        t.count = count;
+        for (int k = 0; k < count; ++k) t.row0[k] = s[k].row0, t.rows[k] = s[k].rows, t.block0[k] = 0;
+        const hipError_t e = f(t);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
+}
+// The first block of every sequence of `rows_of(i)` rows; the number of blocks.
+template <class F>
+int place_blocks(SeqTable<kMaxSeqs>& t, F&& rows_of) {
+    int64_t blocks = 0;
+    for (int i = 0; i < t.count; ++i) {
+        t.block0[i] = (int32_t)blocks;
+        blocks += (rows_of(i) + kBlock - 1) / kBlock;
+    }
+    return (int)blocks;
+}
+
+Args base_args(const a2t_prompt* p, int64_t total, const void* q, int64_t qs, const void* k, int64_t ks, const void* v, int64_t vs,
+               bool until) {
+    Args a{};
+    const int64_t own = (int64_t)p->Hkv * p->D;
+    a.kv = until ? KeyRows{p->k, p->v, own, own, p->meta, p->lasting, p->first} : KeyRows{k, v, ks, vs, nullptr, nullptr, nullptr};
+    a.q = q;
+    a.q_stride = qs;
+    a.delta = p->delta;
+    a.k_out = ks;
+    a.v_out = vs;
+    a.Hq = p->Hq;
+    a.Hkv = p->Hkv;
+    a.G = p->Hq / p->Hkv;
+    a.total = (int32_t)total;
+    a.inv_g = (65536u + a.G - 1) / a.G;
+    a.scale = (float)p->scale;
+    a.scale_log2e = (float)(p->scale * 1.44269504088896340736);
+    return a;
+}
+hipError_t sort_keys(const a2t_prompt* p, const SeqTable<kMaxSeqs>& t, const int32_t* until, const void* k, int64_t ks, const void* v, int64_t vs) {
+    const int size = p->dtype == A2T_F32 ? 4 : 2;
+    const SortArgs s{until, k, v, ks * size, vs * size, p->k, p->v, p->Hkv * p->D * size, p->meta, p->lasting, p->first, p->reach};
+    return launch_sort(s, t, p->stream);
+}
+
+}  // namespace
+
+extern "C" int a2t_prompt_create(int32_t max_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                                 double attn_scale, uint32_t flags, int32_t device, void* hip_stream, a2t_prompt** out) {
+    if (!out) return A2T_ERR_INVALID;
+    *out = nullptr;
+    if (max_rows < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 128 ||
+        (int64_t)max_rows * n_q_heads > (1 << 30) || (head_dim != 64 && head_dim != 128) || (dtype != A2T_F32 && dtype != A2T_BF16) ||
+        (flags & ~A2T_PROMPT_UNTIL) || !std::isfinite(attn_scale) || attn_scale < 0.0 || attn_scale > 1e6 ||
+        (attn_scale != 0.0 && attn_scale < 1e-6))
+        return A2T_ERR_INVALID;
+    int n_dev = 0;
+    if (hipGetDeviceCount(&n_dev) != hipSuccess || device < 0 || device >= n_dev) return A2T_ERR_NODEV;
+    DevGuard g(device);
+    a2t_prompt* p = new (std::nothrow) a2t_prompt();
+    if (!p) return A2T_ERR_OOM;
+    p->max_rows = max_rows;
+    p->Hq = n_q_heads;
+    p->Hkv = n_kv_heads;
+    p->D = head_dim;
+    p->dtype = dtype;
+    p->device = device;
+    p->scale = attn_scale == 0.0 ? 1.0 / std::sqrt((double)head_dim) : attn_scale;
+    p->stream = static_cast<hipStream_t>(hip_stream);
+    p->until = flags & A2T_PROMPT_UNTIL;
+    const size_t rows = (size_t)max_rows, row = (size_t)n_kv_heads * head_dim * (dtype == A2T_F32 ? 4 : 2);
+    bool ok = hipMalloc(&p->delta, rows * n_q_heads * sizeof(float)) == hipSuccess;
+    if (p->until)
+        ok = ok && hipMalloc(&p->k, rows * row) == hipSuccess && hipMalloc(&p->v, rows * row) == hipSuccess &&
+             hipMalloc(&p->meta, rows * sizeof(int2)) == hipSuccess && hipMalloc(&p->lasting, rows * 4) == hipSuccess &&
+             hipMalloc(&p->first, rows * 4) == hipSuccess && hipMalloc(&p->reach, rows * 4) == hipSuccess;
+    if (!ok) {
+        (void)hipGetLastError();
+        free_prompt(p);
+        return A2T_ERR_OOM;
+    }
+    *out = p;
+    return A2T_OK;
+}
+
+extern "C" int a2t_prompt_destroy(a2t_prompt* p) {
+    if (!p) return A2T_ERR_INVALID;
+    DevGuard g(p->device);
+    (void)hipStreamSynchronize(p->stream);
+    free_prompt(p);
+    return A2T_OK;
+}
+
+extern "C" int a2t_prompt_set_stream(a2t_prompt* p, void* hip_stream) {
+    if (!p) return A2T_ERR_INVALID;
+    p->stream = static_cast<hipStream_t>(hip_stream);
+    return A2T_OK;
+}
+
+extern "C" int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows, const void* q, int64_t q_stride, const void* k,
+                               int64_t k_stride, const void* v, int64_t v_stride, const int32_t* until, void* o, float* lse) {
+    if (!p) return A2T_ERR_INVALID;
+    if (p->poisoned) return A2T_ERR_HIP;
+    const int64_t total = total_rows(p, n_seqs, seq_rows);
+    if (!total || bad_rows(p, q, q_stride, p->Hq) || bad_rows(p, k, k_stride, p->Hkv) || bad_rows(p, v, v_stride, p->Hkv) || !o ||
+        misaligned(o, 16) || misaligned(lse, 4) || misaligned(until, 4) || (until && !p->until))
+        return A2T_ERR_INVALID;
+    DevGuard g(p->device);
+    Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until != nullptr);
+    a.o = o;
+    a.lse = lse;
+    const Shape shape{p->dtype == A2T_F32, p->D};
+    const hipError_t e = in_tables(n_seqs, seq_rows, [&](SeqTable<kMaxSeqs>& t) {
+        hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
+        if (s != hipSuccess) return s;
+        const int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
+        return launch_forward(shape, a, t, blocks, p->stream);
+    });
+    if (e != hipSuccess) {
+        p->poisoned = true;
+        return A2T_ERR_HIP;
+    }
+    return A2T_OK;
+}
+
+extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows, const void* q, int64_t q_stride,
+                                    const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* until,
+                                    const void* o, const float* lse, const void* d_o, void* dq, void* dk, void* dv) {
+    if (!p) return A2T_ERR_INVALID;
+    if (p->poisoned) return A2T_ERR_HIP;
+    const int64_t total = total_rows(p, n_seqs, seq_rows);
+    if (!total || bad_rows(p, q, q_stride, p->Hq) || bad_rows(p, k, k_stride, p->Hkv) || bad_rows(p, v, v_stride, p->Hkv) || !o || !lse ||
+        !d_o || !dq || !dk || !dv || misaligned(o, 16) || misaligned(lse, 4) || misaligned(d_o, 16) || misaligned(dq, 16) ||
+        misaligned(dk, 16) || misaligned(dv, 16) || misaligned(until, 4) || (until && !p->until))
+        return A2T_ERR_INVALID;
+    DevGuard g(p->device);
+    Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until != nullptr);
+    a.o_in = o;
+    a.d_o = d_o;
+    a.lse = const_cast<float*>(lse);
+    a.dq = dq;
+    a.dk = dk;
+    a.dv = dv;
+    const Shape shape{p->dtype == A2T_F32, p->D};
+    const hipError_t e = in_tables(n_seqs, seq_rows, [&](SeqTable<kMaxSeqs>& t) {
+        hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
+        if (s != hipSuccess) return s;
+        int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
+        s = launch_dq(shape, a, t, blocks, p->stream);
+        if (s != hipSuccess) return s;
+        blocks = place_blocks(t, [&](int i) { return (int64_t)t.rows[i]; });
+        return launch_dkv(shape, a, t, blocks, p->stream);
+    });
+    if (e != hipSuccess) {
+        p->poisoned = true;
+        return A2T_ERR_HIP;
+    }
+    return A2T_OK;
+}

@@ -1,0 +1,498 @@
+// Causal attention over packed sequences, forward (gfx950): per query head and row i of a sequence
+//   O_i = sum_j softmax_j(scale q_i . k_j) v_j,  lse_i = ln sum_j exp(scale q_i . k_j),
+// over the rows j <= i < until_j of the same sequence.
+//
+// One workgroup = 128 packed query rows of a KV head (row m of a sequence is head m % G of the
+// group at place m / G, so that the G heads of a group share every key tile), four waves of 32
+// rows.  Key tiles of 64 rows go through registers into one of two LDS stages.  A wave's scores are
+// S^T = K Q^T on 32 x 32 matrix instructions: a lane has 16 of 32 keys of its own query, softmax
+// needs one exchange between two lanes, and the probabilities are the operand of O^T = V^T P^T as
+// they are.  The running maximum is raised lazily (when a tile exceeds it by 2^8), so that most
+// tiles rescale nothing.
+#include "prompt_device.h"
+
+namespace a2t {
+namespace prompt {
+namespace {
+
+// The key tiles of a block of queries at places first .. last: one or two runs of rows.
+struct Runs {
+    int start[2], end[2], tiles0, tiles;
+    __device__ __forceinline__ void at(int t, int* lo, int* hi) const {
+        const int second = t >= tiles0;
+        *lo = start[second] + (t - (second ? tiles0 : 0)) * kTile;
+        *hi = end[second];
+    }
+};
+template <bool UNTIL>
+__device__ __forceinline__ Runs key_runs(const KeyRows& kv, int row0, int n, int first, int last) {
+    Runs r;
+    r.start[0] = 0;
+    r.end[0] = last + 1;
+    r.start[1] = r.end[1] = 0;
+    if constexpr (UNTIL) {   // lasting keys, then the passing ones that some query may still see
+        const int all = uniform(kv.lasting[row0 + n - 1]), seen = uniform(kv.lasting[row0 + last]);
+        r.end[0] = seen;
+        r.start[1] = all + uniform(kv.first[row0 + first]);
+        r.end[1] = all + (last + 1 - seen);
+        if (r.end[1] < r.start[1]) r.end[1] = r.start[1];
+    }
+    r.tiles0 = (r.end[0] - r.start[0] + kTile - 1) / kTile;
+    r.tiles = r.tiles0 + (r.end[1] - r.start[1] + kTile - 1) / kTile;
+    return r;
+}
+
+// Which keys lo .. lo + 63 of a tile (up to hi) the rows at places first .. last of a wave see.
+enum class Sees { none, some, all };
+template <bool UNTIL>
+__device__ __forceinline__ Sees sees(const int2* meta, int lo, int hi, int first, int last) {
+    if constexpr (UNTIL) {
+        const int lane = threadIdx.x & 63;
+        const int2 m = meta[lane];
+        const bool in = lo + lane < hi;
+        if (!__any(in && m.x <= last && m.y > first)) return Sees::none;
+        return __all(in && m.x <= first && m.y > last) ? Sees::all : Sees::some;
+    } else {
+        if (lo > last) return Sees::none;
+        return lo + kTile - 1 <= first ? Sees::all : Sees::some;
+    }
+}
+// Whether the query at place i sees key k of a tile.
+template <bool UNTIL>
+__device__ __forceinline__ bool visible(const int2* meta, int lo, int hi, int k, int i) {
+    if constexpr (UNTIL) return lo + k < hi && meta[k].x <= i && i < meta[k].y;
+    return lo + k <= i;
+}
+
+template <typename T, int D, bool UNTIL, int N>
+__global__ __launch_bounds__(kThreads) void prompt_attn_kernel(Args a, SeqTable<N> t) {
+    using Tl = Tile<T, D>;
+    constexpr int DB = Tl::DB;
+    __shared__ __align__(1024) char s_k[2][Tl::BYTES];
+    __shared__ __align__(1024) char s_v[2][Tl::BYTES];
+    __shared__ int2 s_meta[2][UNTIL ? kTile : 1];
+
+    const int g = blockIdx.x % a.Hkv, G = a.G;
+    int place;
+    const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
+    const int n = t.rows[z], row0 = t.row0[z], M = G * n;
+    const int m0 = ((M + kBlock - 1) / kBlock - 1 - place) * kBlock;   // the rows that see most come first
+    const int base = uniform(m0 / G), rem = m0 - base * G;
+    auto place_of = [&](int r) { return base + (int)(((uint32_t)(rem + r) * a.inv_g) >> 16); };   // of row m0 + r
+    const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const int rows = min(kBlock, M - m0);
+    const bool busy = 32 * w < rows;
+    const int r = min(32 * w + l32, rows - 1);
+    const int i = place_of(r), hh = rem + r - (i - base) * G;
+    const int i_first = uniform(place_of(min(32 * w, rows - 1))), i_last = uniform(place_of(min(32 * w + 31, rows - 1)));
+    const Runs runs = key_runs<UNTIL>(a.kv, row0, n, base, uniform(place_of(rows - 1)));
+
+    const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
+    const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
+    Moving<T, D> mk, mv;
+    int2 mm = {0, 0};
+    auto load = [&](int tile) {
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        auto row = [&](int r) { return (int64_t)min(lo + r, n - 1); };
+        mk.load([&](int r) { return kp + row(r) * a.kv.k_stride * (int64_t)sizeof(T); });
+        mv.load([&](int r) { return vp + row(r) * a.kv.v_stride * (int64_t)sizeof(T); });
+        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + row(threadIdx.x)];
+    };
+    auto store = [&](int stage) {
+        mk.store(s_k[stage]);
+        mv.store(s_v[stage]);
+        if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
+    };
+    if (runs.tiles) load(0);
+
+    u32x4 qop[Tl::STEPS];
+    {
+        const char* qp = static_cast<const char*>(a.q) + ((row0 + i) * a.q_stride + (g * G + hh) * D) * (int64_t)sizeof(T) + 16 * h;
+#pragma unroll
+        for (int s = 0; s < Tl::STEPS; ++s) qop[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+    }
+    if (runs.tiles) store(0);
+
+    // base-2 logarithms throughout: mref is the reference of the lane's row (its scaled scores less mref
+    // are at most 8), sum of 2^(score - mref)
+    const float c = a.scale_log2e;
+    float mrun = -INFINITY, mref = 0.f, sum = 0.f;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+
+    for (int tile = 0; tile < runs.tiles; ++tile) {
+        const int stage = tile & 1;
+        __syncthreads();
+        if (tile + 1 < runs.tiles) load(tile + 1);
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        const Sees what = busy ? sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last) : Sees::none;
+        if (what != Sees::none) {
+            f32x16 s[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_k[stage], 32 * b + l32, k, h), qop[k], s[b]);
+            }
+            if (what == Sees::some) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!visible<UNTIL>(s_meta[stage], lo, hi, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3), i)) s[b][e] = -INFINITY;
+            }
+            float top = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+            for (int e = 1; e < 16; ++e) top = fmaxf(fmaxf(top, s[0][e]), s[1][e]);
+            top = swap_max(top) * c;
+            if (__any(top > mrun + 8.f)) {
+                const float up = fmaxf(mrun, top), ref = up == -INFINITY ? 0.f : up;
+                const float by = exp2_(mrun - ref);
+                sum *= by;
+#pragma unroll
+                for (int db = 0; db < DB; ++db) acc[db] *= by;
+                mrun = up;
+                mref = ref;
+            }
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    s[b][e] = exp2_(__builtin_fmaf(s[b][e], c, -mref));
+                    sum += s[b][e];
+                }
+                mma_rows<D, T>(s_v[stage], 32 * b, s[b], acc);
+            }
+        }
+        if (tile + 1 < runs.tiles) store(stage ^ 1);
+    }
+
+    if (32 * w + l32 >= rows) return;
+    const float total = swap_sum(sum);
+    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;   // a row without keys is zero
+    const int64_t row = row0 + i;
+    if (a.lse && h == 0) a.lse[(int64_t)(g * G + hh) * a.total + row] = (mref + __builtin_amdgcn_logf(total)) * kLn2;
+    T* o = static_cast<T*>(a.o) + (row * a.Hq + g * G + hh) * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            store4(o + 32 * db + 8 * e, acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv, acc[db][4 * e + 3] * inv);
+}
+
+// ---- gradient with respect to the queries
+//   delta_i = dO_i . O_i,  P_ij = exp(scale q_i . k_j - lse_i),  dS_ij = P_ij (dO_i . v_j - delta_i),
+//   dQ_i = scale sum_j dS_ij k_j
+// Workgroups as above; delta goes to memory for the gradient of the keys.
+template <typename T, int D, bool UNTIL, int N>
+__global__ __launch_bounds__(kThreads) void prompt_dq_kernel(Args a, SeqTable<N> t) {
+    using Tl = Tile<T, D>;
+    constexpr int DB = Tl::DB;
+    __shared__ __align__(1024) char s_k[2][Tl::BYTES];
+    __shared__ __align__(1024) char s_v[2][Tl::BYTES];
+    __shared__ int2 s_meta[2][UNTIL ? kTile : 1];
+
+    const int g = blockIdx.x % a.Hkv, G = a.G;
+    int place;
+    const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
+    const int n = t.rows[z], row0 = t.row0[z], M = G * n;
+    const int m0 = ((M + kBlock - 1) / kBlock - 1 - place) * kBlock;
+    const int base = uniform(m0 / G), rem = m0 - base * G;
+    auto place_of = [&](int r) { return base + (int)(((uint32_t)(rem + r) * a.inv_g) >> 16); };
+    const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const int rows = min(kBlock, M - m0);
+    const bool busy = 32 * w < rows;
+    const int r = min(32 * w + l32, rows - 1);
+    const int i = place_of(r), hh = rem + r - (i - base) * G;
+    const int i_first = uniform(place_of(min(32 * w, rows - 1))), i_last = uniform(place_of(min(32 * w + 31, rows - 1)));
+    const Runs runs = key_runs<UNTIL>(a.kv, row0, n, base, uniform(place_of(rows - 1)));
+
+    const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
+    const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
+    Moving<T, D> mk, mv;
+    int2 mm = {0, 0};
+    auto load = [&](int tile) {
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        auto row = [&](int r) { return (int64_t)min(lo + r, n - 1); };
+        mk.load([&](int r) { return kp + row(r) * a.kv.k_stride * (int64_t)sizeof(T); });
+        mv.load([&](int r) { return vp + row(r) * a.kv.v_stride * (int64_t)sizeof(T); });
+        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + row(threadIdx.x)];
+    };
+    auto store = [&](int stage) {
+        mk.store(s_k[stage]);
+        mv.store(s_v[stage]);
+        if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
+    };
+    if (runs.tiles) load(0);
+
+    u32x4 qop[Tl::STEPS], dop[Tl::STEPS];
+    const int64_t row = row0 + i, head = g * G + hh;
+    float delta = 0.f;
+    {
+        const char* qp = static_cast<const char*>(a.q) + (row * a.q_stride + head * D) * (int64_t)sizeof(T) + 16 * h;
+        const char* dp = static_cast<const char*>(a.d_o) + (row * a.Hq + head) * D * (int64_t)sizeof(T) + 16 * h;
+        const char* op = static_cast<const char*>(a.o_in) + (row * a.Hq + head) * D * (int64_t)sizeof(T) + 16 * h;
+#pragma unroll
+        for (int s = 0; s < Tl::STEPS; ++s) {
+            qop[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+            dop[s] = *reinterpret_cast<const u32x4*>(dp + 32 * s);
+            const u32x4 o = *reinterpret_cast<const u32x4*>(op + 32 * s);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (sizeof(T) == 2) {
+                    delta += __uint_as_float(o[e] << 16) * __uint_as_float(dop[s][e] << 16);
+                    delta += __uint_as_float(o[e] & 0xffff0000u) * __uint_as_float(dop[s][e] & 0xffff0000u);
+                } else {
+                    delta += __uint_as_float(o[e]) * __uint_as_float(dop[s][e]);
+                }
+            }
+        }
+    }
+    delta = swap_sum(delta);
+    float lse2 = a.lse[head * a.total + row] * kLog2e;
+    if (lse2 == -INFINITY) lse2 = 0.f;   // a row without keys: nothing is visible below
+    if (32 * w + l32 < rows && h == 0) a.delta[head * a.total + row] = delta;
+    if (runs.tiles) store(0);
+
+    const float c = a.scale_log2e;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+
+    for (int tile = 0; tile < runs.tiles; ++tile) {
+        const int stage = tile & 1;
+        __syncthreads();
+        if (tile + 1 < runs.tiles) load(tile + 1);
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        const Sees what = busy ? sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last) : Sees::none;
+        if (what != Sees::none) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x16 s, p;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = p[e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_k[stage], 32 * b + l32, k, h), qop[k], s);
+#pragma unroll
+                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_v[stage], 32 * b + l32, k, h), dop[k], p);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) p[e] = exp2_(__builtin_fmaf(s[e], c, -lse2)) * (p[e] - delta);
+                if (what == Sees::some) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (!visible<UNTIL>(s_meta[stage], lo, hi, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3), i)) p[e] = 0.f;
+                }
+                mma_rows<D, T>(s_k[stage], 32 * b, p, acc);
+            }
+        }
+        if (tile + 1 < runs.tiles) store(stage ^ 1);
+    }
+
+    if (32 * w + l32 >= rows) return;
+    T* o = static_cast<T*>(a.dq) + row * a.q_stride + head * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            store4(o + 32 * db + 8 * e, acc[db][4 * e] * a.scale, acc[db][4 * e + 1] * a.scale, acc[db][4 * e + 2] * a.scale,
+                   acc[db][4 * e + 3] * a.scale);
+}
+
+// ---- gradient with respect to keys and values
+//   dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij q_i, over all heads of the group
+// One workgroup = 128 keys of a KV head, four waves of 32, over tiles of 64 packed query rows: the
+// sums over the group's heads are sums over packed rows, in one fixed order.
+template <typename T, int D, bool UNTIL, int N>
+__global__ __launch_bounds__(kThreads) void prompt_dkv_kernel(Args a, SeqTable<N> t) {
+    using Tl = Tile<T, D>;
+    constexpr int DB = Tl::DB;
+    __shared__ __align__(1024) char s_q[2][Tl::BYTES];
+    __shared__ __align__(1024) char s_d[2][Tl::BYTES];
+    __shared__ __align__(16) float2 s_stat[2][kTile];   // lse (base 2) and delta of the tile's rows
+    __shared__ __align__(16) int s_place[2][kTile];
+    __shared__ int s_range[2][4];
+
+    const int g = blockIdx.x % a.Hkv, G = a.G;
+    int place;
+    const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
+    const int n = t.rows[z], row0 = t.row0[z];
+    const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const int k0 = place * kBlock + 32 * w, key = min(k0 + l32, n - 1);
+    const bool busy = k0 < n;
+    // the lane's key: its place, and the first place that does not see it
+    int2 me = {key, n};
+    if constexpr (UNTIL) {
+        me = a.kv.meta[row0 + key];
+        me.y = min(me.y, n);
+    }
+    int j_min = me.x, j_max = me.x, u_min = me.y, u_max = me.y;
+#pragma unroll
+    for (int d = 1; d < 32; d *= 2) {
+        j_min = min(j_min, __shfl_xor(j_min, d));
+        j_max = max(j_max, __shfl_xor(j_max, d));
+        u_min = min(u_min, __shfl_xor(u_min, d));
+        u_max = max(u_max, __shfl_xor(u_max, d));
+    }
+    j_min = uniform(j_min), j_max = uniform(j_max), u_min = uniform(u_min), u_max = uniform(u_max);
+    if (lane == 0) s_range[0][w] = j_min, s_range[1][w] = u_max;   // idle waves repeat the last key's
+    __syncthreads();
+    const int from = uniform(min(min(s_range[0][0], s_range[0][1]), min(s_range[0][2], s_range[0][3])));
+    const int to = uniform(max(max(s_range[1][0], s_range[1][1]), max(s_range[1][2], s_range[1][3])));
+    const int m_from = from * G, m_to = max(to, from) * G;   // packed rows that see some of the keys
+    const int tiles = (m_to - m_from + kTile - 1) / kTile;
+
+    const int64_t at_k = (row0 + key) * a.kv.k_stride + g * D, at_v = (row0 + key) * a.kv.v_stride + g * D;
+    u32x4 kop[Tl::STEPS], vop[Tl::STEPS];
+#pragma unroll
+    for (int s = 0; s < Tl::STEPS; ++s) {
+        kop[s] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.kv.k) + at_k * sizeof(T) + 16 * h + 32 * s);
+        vop[s] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.kv.v) + at_v * sizeof(T) + 16 * h + 32 * s);
+    }
+
+    const char* qp = static_cast<const char*>(a.q) + ((int64_t)row0 * a.q_stride + g * G * D) * sizeof(T);
+    const char* dp = static_cast<const char*>(a.d_o) + ((int64_t)row0 * a.Hq + g * G) * D * sizeof(T);
+    Moving<T, D> mq, md;
+    float2 stat = {0.f, 0.f};
+    int stat_place = 0;
+    auto load = [&](int tile) {
+        const int m = m_from + tile * kTile, base = uniform(m / G), rem = m - base * G, last = min(kTile, m_to - m) - 1;
+        auto split = [&](int r, int* hh) {
+            const uint32_t x = rem + min(r, last), q = (x * a.inv_g) >> 16;
+            *hh = x - q * G;
+            return base + (int)q;
+        };
+        mq.load([&](int r) {
+            int hh;
+            const int64_t i = split(r, &hh);
+            return qp + (i * a.q_stride + hh * D) * (int64_t)sizeof(T);
+        });
+        md.load([&](int r) {
+            int hh;
+            const int64_t i = split(r, &hh);
+            return dp + (i * a.Hq + hh) * D * (int64_t)sizeof(T);
+        });
+        if (threadIdx.x < kTile) {
+            int hh;
+            stat_place = split(threadIdx.x, &hh);
+            const int64_t at = (int64_t)(g * G + hh) * a.total + row0 + stat_place;
+            stat = make_float2(a.lse[at] * kLog2e, a.delta[at]);
+            if (stat.x == -INFINITY) stat.x = 0.f;
+            if ((int)threadIdx.x > last) stat_place = -1;   // sees no key
+        }
+    };
+    auto store = [&](int stage) {
+        mq.store(s_q[stage]);
+        md.store(s_d[stage]);
+        if (threadIdx.x < kTile) s_stat[stage][threadIdx.x] = stat, s_place[stage][threadIdx.x] = stat_place;
+    };
+    if (tiles) {
+        load(0);
+        store(0);
+    }
+
+    const float c = a.scale_log2e;
+    f32x16 ak[DB], av[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ak[db][e] = av[db][e] = 0.f;
+
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int stage = tile & 1;
+        __syncthreads();
+        if (tile + 1 < tiles) load(tile + 1);
+        const int m = m_from + tile * kTile;
+        const int i_first = uniform(m / G), i_last = uniform((min(m + kTile, m_to) - 1) / G);
+        if (busy && i_last >= j_min && i_first < u_max) {
+            const bool all = m + kTile <= m_to && i_first >= j_max && i_last < u_min;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+                f32x16 s, p;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[e] = p[e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_q[stage], 32 * b + l32, k, h), kop[k], s);
+#pragma unroll
+                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_d[stage], 32 * b + l32, k, h), vop[k], p);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float2 st = s_stat[stage][32 * b + 8 * (e >> 2) + 4 * h + (e & 3)];
+                    s[e] = exp2_(__builtin_fmaf(s[e], c, -st.x));
+                    p[e] = s[e] * (p[e] - st.y);
+                }
+                if (!all) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int i = s_place[stage][32 * b + 8 * (e >> 2) + 4 * h + (e & 3)];
+                        if (i < me.x || i >= me.y) s[e] = p[e] = 0.f;
+                    }
+                }
+                mma_rows<D, T>(s_d[stage], 32 * b, s, av);
+                mma_rows<D, T>(s_q[stage], 32 * b, p, ak);
+            }
+        }
+        if (tile + 1 < tiles) store(stage ^ 1);
+    }
+
+    if (k0 + l32 >= n) return;
+    // gradients lie as the caller's K and V do, whatever order the keys were read in
+    T* ok = static_cast<T*>(a.dk) + (row0 + me.x) * a.k_out + g * D + 4 * h;
+    T* ov = static_cast<T*>(a.dv) + (row0 + me.x) * a.v_out + g * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            store4(ok + 32 * db + 8 * e, ak[db][4 * e] * a.scale, ak[db][4 * e + 1] * a.scale, ak[db][4 * e + 2] * a.scale, ak[db][4 * e + 3] * a.scale);
+            store4(ov + 32 * db + 8 * e, av[db][4 * e], av[db][4 * e + 1], av[db][4 * e + 2], av[db][4 * e + 3]);
+        }
+}
+
+enum class Kernel { forward, dq, dkv };
+
+template <Kernel K, typename T, int D, bool UNTIL>
+hipError_t launch(const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
+    return by_count(t, [&](const auto& s) {
+        constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
+        const dim3 grid((uint32_t)(blocks * a.Hkv));
+        if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_attn_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
+        else if constexpr (K == Kernel::dq) hipLaunchKernelGGL((prompt_dq_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
+        else hipLaunchKernelGGL((prompt_dkv_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
+        return hipGetLastError();
+    });
+}
+template <Kernel K>
+hipError_t launch(const Shape& s, const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
+    auto typed = [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        const bool u = a.kv.meta != nullptr;
+        if (s.head_dim == 128) return u ? launch<K, T, 128, true>(a, t, blocks, stream) : launch<K, T, 128, false>(a, t, blocks, stream);
+        if (s.head_dim == 64) return u ? launch<K, T, 64, true>(a, t, blocks, stream) : launch<K, T, 64, false>(a, t, blocks, stream);
+        return hipErrorInvalidValue;
+    };
+    return s.f32 ? typed((float*)nullptr) : typed((bf16_t*)nullptr);
+}
+
+}  // namespace
+
+hipError_t launch_forward(const Shape& s, const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
+    return launch<Kernel::forward>(s, a, t, blocks, stream);
+}
+hipError_t launch_dq(const Shape& s, const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
+    return launch<Kernel::dq>(s, a, t, blocks, stream);
+}
+hipError_t launch_dkv(const Shape& s, const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
+    return launch<Kernel::dkv>(s, a, t, blocks, stream);
+}
+
+}  // namespace prompt
+}  // namespace a2t

@@ -1,0 +1,111 @@
+// Keys sorted for attention over packed sequences with keys that expire (a2t_prompt_* with
+// `until`).  Eviction keeps a few rows of every unit, so that a tile of 64 consecutive keys is
+// never quite dead: sorted into lasting and passing keys, what a block of queries sees is two
+// dense runs, and the kernels skip the rest (a ten-minute session with a budget of 4,096 rows: 52 %
+// of the pairs of a causal triangle).  The copies cost two passes over K and V.
+#include "prompt_device.h"
+
+namespace a2t {
+namespace prompt {
+namespace {
+
+constexpr int kScanThreads = 1024;
+constexpr int kCopyRows = 16;    // rows of a copying workgroup
+
+// One workgroup a sequence: counts of lasting keys and reach of the passing ones, by place.
+template <int N>
+__global__ __launch_bounds__(kScanThreads) void prompt_scan_kernel(SortArgs a, SeqTable<N> t) {
+    const int n = t.rows[blockIdx.x], row0 = t.row0[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    __shared__ int s_count[kScanThreads / 64], s_reach[kScanThreads / 64];
+    int count = 0, reach = -0x7fffffff;   // of the chunks before
+    for (int j0 = 0; j0 < n; j0 += kScanThreads) {
+        const int j = j0 + tid;
+        const int until = j < n ? a.until[row0 + j] : 0;
+        const bool lasts = j < n && until >= n;
+        const uint64_t mask = __ballot(lasts);
+        const int before = __builtin_popcountll(mask & ((2ull << lane) - 1));   // up to and with this key
+        int r = j < n && !lasts ? until : -0x7fffffff;
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int o = __shfl_up(r, d);
+            if (lane >= d) r = max(r, o);
+        }
+        if (lane == 63) s_count[w] = before, s_reach[w] = r;
+        __syncthreads();
+        int c = count, m = reach;
+        for (int k = 0; k < kScanThreads / 64; ++k) {
+            if (k < w) c += s_count[k], m = max(m, s_reach[k]);
+            count += s_count[k];
+            reach = max(reach, s_reach[k]);
+        }
+        if (j < n) {
+            const int seen = c + before;
+            a.lasting[row0 + j] = seen;
+            if (!lasts) a.reach[row0 + (j - seen)] = max(m, r);
+        }
+        __syncthreads();
+    }
+}
+
+template <int N>
+__global__ __launch_bounds__(kThreads) void prompt_copy_kernel(SortArgs a, SeqTable<N> t) {
+    int place;
+    const int z = sequence_of(t, (int)blockIdx.x, &place);
+    const int n = t.rows[z], row0 = t.row0[z], i0 = place * kCopyRows, rows = min(kCopyRows, n - i0);
+    const int all = a.lasting[row0 + n - 1];
+    auto sorted = [&](int j, bool* lasts) {
+        const int seen = a.lasting[row0 + j];
+        *lasts = seen > (j ? a.lasting[row0 + j - 1] : 0);
+        return *lasts ? seen - 1 : all + j - seen;
+    };
+    if ((int)threadIdx.x < rows) {
+        const int j = i0 + threadIdx.x;
+        bool lasts;
+        const int at = sorted(j, &lasts);
+        a.meta[row0 + at] = make_int2(j, lasts ? 0x7fffffff : a.until[row0 + j]);
+        // the first passing key that place j may still see: reach does not fall
+        int lo = 0, hi = n - all;
+        while (lo < hi) {
+            const int mid = (lo + hi) / 2;
+            if (a.reach[row0 + mid] > j) hi = mid;
+            else lo = mid + 1;
+        }
+        a.first[row0 + j] = lo;
+    }
+    const int chunks = a.row_bytes / 16;
+    for (int x = threadIdx.x; x < rows * chunks; x += kThreads) {
+        const int j = i0 + x / chunks, c = x % chunks;
+        bool lasts;
+        const int64_t to = (int64_t)(row0 + sorted(j, &lasts)) * a.row_bytes;
+        reinterpret_cast<u32x4*>(static_cast<char*>(a.k_out) + to)[c] =
+            reinterpret_cast<const u32x4*>(static_cast<const char*>(a.k) + (row0 + j) * a.k_stride)[c];
+        reinterpret_cast<u32x4*>(static_cast<char*>(a.v_out) + to)[c] =
+            reinterpret_cast<const u32x4*>(static_cast<const char*>(a.v) + (row0 + j) * a.v_stride)[c];
+    }
+}
+
+}  // namespace
+
+hipError_t launch_sort(const SortArgs& a, const SeqTable<kMaxSeqs>& t, hipStream_t stream) {
+    hipError_t e = by_count(t, [&](const auto& s) {
+        constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
+        hipLaunchKernelGGL((prompt_scan_kernel<N>), dim3(t.count), dim3(kScanThreads), 0, stream, a, s);
+        return hipGetLastError();
+    });
+    if (e != hipSuccess) return e;
+    SeqTable<kMaxSeqs> u = t;
+    int blocks = 0;
+    for (int i = 0; i < t.count; ++i) {
+        u.block0[i] = blocks;
+        blocks += (t.rows[i] + kCopyRows - 1) / kCopyRows;
+    }
+    return by_count(u, [&](const auto& s) {
+        constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
+        hipLaunchKernelGGL((prompt_copy_kernel<N>), dim3(blocks), dim3(kThreads), 0, stream, a, s);
+        return hipGetLastError();
+    });
+}
+
+}  // namespace prompt
+}  // namespace a2t

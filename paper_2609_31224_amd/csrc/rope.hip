@@ -1,0 +1,284 @@
+// Rotary encoding of packed rows of queries and keys and its gradient (gfx950).
+// Public API: include/a2t.h (a2t_rope_*).
+//
+// Row t turns channel pairs (x, y) of its first r channels by the angle a = pos_t f_i:
+//   x' = m (x cos a - y sin a),  y' = m (y cos a + x sin a)
+// (the gradient by -a); the other channels are copied.  Angles are products in 64 bits,
+// reduced to a fraction of a turn there; sine and cosine of the fraction are fp32.
+//
+// Bound: HBM, every element read and written once.  A workgroup takes a few rows: it
+// evaluates their r / 2 angles once, into LDS, and then every thread turns 8 pairs at a
+// time (two 16-byte chunks of bf16) of one head after the other, so that the 64-bit
+// arithmetic is shared by all heads of a row.
+#include "../../include/a2t.h"
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <new>
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kPairs = 8;         // pairs of a unit of work (16 elements)
+constexpr int kMaxRows = 8;       // most rows of a workgroup
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+struct bf16_t {
+    uint16_t bits;
+};
+
+struct RopeArgs {
+    double turns[64];     // f_i / (2 pi)
+    const int32_t* pos;
+    const void* in[2];    // queries, keys
+    void* out[2];
+    int64_t in_stride[2], out_stride[2];   // elements between rows
+    int32_t heads0, heads;                 // heads of the queries, of both
+    int32_t n, rows;                       // rows, rows of a workgroup
+    int32_t part2, half;                   // r / 2; pairs (i, i + r/2) or (2i, 2i + 1)
+    float m, sign;
+};
+
+// 8 elements
+__device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(w[e] << 16);
+        x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    const u32x4 a = reinterpret_cast<const u32x4*>(p)[0], b = reinterpret_cast<const u32x4*>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[e] = __uint_as_float(a[e]);
+        x[4 + e] = __uint_as_float(b[e]);
+    }
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
+    const bf16x2 v = {(__bf16)a, (__bf16)b};   // round to nearest even, once per output
+    return __builtin_bit_cast(uint32_t, v);
+}
+__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
+    *reinterpret_cast<u32x4*>(p) = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    u32x4 a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        a[e] = __float_as_uint(x[e]);
+        b[e] = __float_as_uint(x[4 + e]);
+    }
+    reinterpret_cast<u32x4*>(p)[0] = a;
+    reinterpret_cast<u32x4*>(p)[1] = b;
+}
+
+template <typename T, int D>
+__global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
+    __shared__ __align__(16) float2 s_cs[kMaxRows][D / 2];
+    const int tid = threadIdx.x, row0 = blockIdx.x * a.rows, rows = min(a.rows, a.n - row0);
+    for (int k = tid; k < rows * (D / 2); k += kThreads) {
+        const int r = k / (D / 2), i = k % (D / 2);
+        if (i >= a.part2) continue;
+        double t = (double)a.pos[row0 + r] * a.turns[i];
+        t -= rint(t);
+        float s, c;
+        sincospif(2.f * (float)t, &s, &c);
+        s_cs[r][i] = make_float2(a.m * c, a.sign * a.m * s);
+    }
+    __syncthreads();
+    constexpr int U = D / (2 * kPairs);   // units of a head
+    const int per_row = a.heads * U, rotated = a.part2 / kPairs;
+    for (int k = tid; k < rows * per_row; k += kThreads) {
+        const int r = k / per_row, h = k % per_row / U, u = k % U;
+        const int which = h >= a.heads0;
+        const int64_t row = row0 + r;
+        const int head = (h - (which ? a.heads0 : 0)) * D;
+        const T* in = static_cast<const T*>(a.in[which]) + row * a.in_stride[which] + head;
+        T* out = static_cast<T*>(a.out[which]) + row * a.out_stride[which] + head;
+        // where the unit's two chunks of 8 elements are
+        const bool turn = u < rotated;
+        const int c0 = turn && a.half ? kPairs * u : 2 * kPairs * u;
+        const int c1 = turn && a.half ? c0 + a.part2 : c0 + kPairs;
+        float x[8], y[8], p[8], q[8];
+        load8(in + c0, x);
+        load8(in + c1, y);
+        if (!turn) {
+            if (in != out) {
+                store8(out + c0, x);
+                store8(out + c1, y);
+            }
+            continue;
+        }
+        const float2* cs = &s_cs[r][kPairs * u];
+        if (a.half) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                p[e] = x[e] * cs[e].x - y[e] * cs[e].y;
+                q[e] = y[e] * cs[e].x + x[e] * cs[e].y;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float2 f = cs[e], g = cs[4 + e];
+                p[2 * e] = x[2 * e] * f.x - x[2 * e + 1] * f.y;
+                p[2 * e + 1] = x[2 * e + 1] * f.x + x[2 * e] * f.y;
+                q[2 * e] = y[2 * e] * g.x - y[2 * e + 1] * g.y;
+                q[2 * e + 1] = y[2 * e + 1] * g.x + y[2 * e] * g.y;
+            }
+        }
+        store8(out + c0, p);
+        store8(out + c1, q);
+    }
+}
+
+struct DevGuard {
+    int prev = -1;
+    explicit DevGuard(int dev) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        if (prev != dev) (void)hipSetDevice(dev);
+    }
+    ~DevGuard() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+}  // namespace
+
+struct a2t_rope {
+    a2t_rope_config cfg{};
+    int32_t part = 0;
+    double freq[64] = {};
+    double m = 1.0;
+    hipStream_t stream = nullptr;
+    int cus = 256;
+    bool poisoned = false;
+};
+
+extern "C" int a2t_rope_create(const a2t_rope_config* cfg, void* hip_stream, a2t_rope** out) {
+    if (!out) return A2T_ERR_INVALID;
+    *out = nullptr;
+    if (!cfg) return A2T_ERR_INVALID;
+    const int D = cfg->head_dim, part = cfg->rotary_dim ? cfg->rotary_dim : D;
+    const double theta = cfg->theta == 0.0 ? 1e6 : cfg->theta;
+    if ((D != 64 && D != 128) || part < 16 || part > D || part % 16 || (cfg->dtype != A2T_F32 && cfg->dtype != A2T_BF16) ||
+        (cfg->layout != A2T_ROPE_HALF && cfg->layout != A2T_ROPE_PAIRS) || !std::isfinite(theta) || theta <= 1.0)
+        return A2T_ERR_INVALID;
+    const double f = cfg->factor;
+    if (cfg->scaling < A2T_ROPE_PLAIN || cfg->scaling > A2T_ROPE_YARN) return A2T_ERR_INVALID;
+    if (cfg->scaling != A2T_ROPE_PLAIN && (!std::isfinite(f) || f < 1.0)) return A2T_ERR_INVALID;
+    if (cfg->scaling == A2T_ROPE_YARN &&
+        (cfg->trained_rows < 1 || !std::isfinite(cfg->turns_fast) || !std::isfinite(cfg->turns_slow) ||
+         cfg->turns_slow <= 0.0 || cfg->turns_fast < cfg->turns_slow))
+        return A2T_ERR_INVALID;
+    int n_dev = 0;
+    if (hipGetDeviceCount(&n_dev) != hipSuccess || cfg->device < 0 || cfg->device >= n_dev) return A2T_ERR_NODEV;
+    a2t_rope* r = new (std::nothrow) a2t_rope();
+    if (!r) return A2T_ERR_OOM;
+    r->cfg = *cfg;
+    r->part = part;
+    r->stream = static_cast<hipStream_t>(hip_stream);
+    int cus = 0;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, cfg->device) == hipSuccess && cus > 0) r->cus = cus;
+    const double pi = 3.14159265358979323846;
+    const double base = cfg->scaling == A2T_ROPE_NTK ? theta * std::pow(f, part / (part - 2.0)) : theta;
+    // channel pair whose wavelength fits `turns` times into the trained rows
+    auto pair_of = [&](double turns) { return part * std::log(cfg->trained_rows / (turns * 2 * pi)) / (2 * std::log(theta)); };
+    double low = 0, high = 1;
+    if (cfg->scaling == A2T_ROPE_YARN) {
+        low = std::fmax(std::floor(pair_of(cfg->turns_fast)), 0.0);
+        high = std::fmin(std::ceil(pair_of(cfg->turns_slow)), part - 1.0);
+        r->m = 0.1 * std::log(f) + 1.0;
+    }
+    for (int i = 0; i < part / 2; ++i) {
+        double w = std::pow(base, -2.0 * i / part);
+        if (cfg->scaling == A2T_ROPE_LINEAR) w /= f;
+        if (cfg->scaling == A2T_ROPE_YARN) {
+            const double ramp = std::fmin(1.0, std::fmax(0.0, (i - low) / std::fmax(high - low, 1e-3)));
+            w = w * (1.0 - ramp) + w / f * ramp;
+        }
+        r->freq[i] = w;
+    }
+    *out = r;
+    return A2T_OK;
+}
+
+extern "C" int a2t_rope_destroy(a2t_rope* r) {
+    if (!r) return A2T_ERR_INVALID;
+    delete r;
+    return A2T_OK;
+}
+
+extern "C" int a2t_rope_set_stream(a2t_rope* r, void* hip_stream) {
+    if (!r) return A2T_ERR_INVALID;
+    r->stream = static_cast<hipStream_t>(hip_stream);
+    return A2T_OK;
+}
+
+extern "C" int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, int32_t q_heads, const void* q, int64_t q_stride,
+                              void* q_out, int64_t q_out_stride, int32_t k_heads, const void* k, int64_t k_stride, void* k_out,
+                              int64_t k_out_stride, int32_t grad) {
+    if (!r) return A2T_ERR_INVALID;
+    if (r->poisoned) return A2T_ERR_HIP;
+    const int D = r->cfg.head_dim, size = r->cfg.dtype == A2T_F32 ? 4 : 2;
+    if (n_rows < 1 || n_rows > (1 << 26) || !pos || (reinterpret_cast<uintptr_t>(pos) & 3u)) return A2T_ERR_INVALID;
+    if (!q) q_heads = 0;
+    if (!k) k_heads = 0;
+    if (q_heads < 0 || k_heads < 0 || (q && q_heads < 1) || (k && k_heads < 1) || q_heads + (int64_t)k_heads < 1 ||
+        q_heads + (int64_t)k_heads > 4096)
+        return A2T_ERR_INVALID;
+    auto bad = [&](int heads, const void* in, int64_t is, const void* out, int64_t os) {
+        if (!heads) return false;
+        const uintptr_t a = reinterpret_cast<uintptr_t>(in), b = reinterpret_cast<uintptr_t>(out);
+        if (!out || ((a | b) & 15u) || is < (int64_t)heads * D || os < (int64_t)heads * D || is % 8 || os % 8 ||
+            is > (1ll << 40) || os > (1ll << 40))
+            return true;
+        // in place means the same rows; any other overlap would be a race
+        const uintptr_t na = (uintptr_t)((n_rows - 1) * is + (int64_t)heads * D) * size;
+        const uintptr_t nb = (uintptr_t)((n_rows - 1) * os + (int64_t)heads * D) * size;
+        if (a == b) return is != os;
+        if (is == os) {   // the same rows of one buffer, other channels: no row touches another
+            const uintptr_t gap = (a > b ? a - b : b - a) % (uintptr_t)(is * size), row = (uintptr_t)heads * D * size;
+            if (gap >= row && gap + row <= (uintptr_t)(is * size)) return false;
+        }
+        return a < b + nb && b < a + na;
+    };
+    if (bad(q_heads, q, q_stride, q_out, q_out_stride) || bad(k_heads, k, k_stride, k_out, k_out_stride)) return A2T_ERR_INVALID;
+    DevGuard g(r->cfg.device);
+    RopeArgs a{};
+    const double two_pi = 6.28318530717958647692;
+    for (int i = 0; i < r->part / 2; ++i) a.turns[i] = r->freq[i] / two_pi;
+    a.pos = pos;
+    a.in[0] = q, a.in[1] = k;
+    a.out[0] = q_out, a.out[1] = k_out;
+    a.in_stride[0] = q_stride, a.in_stride[1] = k_stride;
+    a.out_stride[0] = q_out_stride, a.out_stride[1] = k_out_stride;
+    a.heads0 = q_heads;
+    a.heads = q_heads + k_heads;
+    a.n = n_rows;
+    a.part2 = r->part / 2;
+    a.half = r->cfg.layout == A2T_ROPE_HALF;
+    a.m = (float)r->m;
+    a.sign = grad ? -1.f : 1.f;
+    // as many rows a workgroup as leave every CU a few workgroups
+    a.rows = 1;
+    while (a.rows < kMaxRows && (int64_t)n_rows >= (int64_t)a.rows * 2 * 4 * r->cus) a.rows *= 2;
+    const dim3 grid((n_rows + a.rows - 1) / a.rows);
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, r->stream, a); };
+    if (r->cfg.dtype == A2T_F32) {
+        if (D == 64) go(rope_kernel<float, 64>);
+        else go(rope_kernel<float, 128>);
+    } else {
+        if (D == 64) go(rope_kernel<bf16_t, 64>);
+        else go(rope_kernel<bf16_t, 128>);
+    }
+    if (hipGetLastError() != hipSuccess) {
+        r->poisoned = true;
+        return A2T_ERR_HIP;
+    }
+    return A2T_OK;
+}
