@@ -675,7 +675,7 @@ int a2t_prompt_set_stream(a2t_prompt* p, void* hip_stream);
 /* Forward pass.
  *   seq_rows  host [n_seqs], rows of each sequence (>= 0), at least one and at
  *             most max_rows in all
- *   q, k, v   device rows, strides in elements (at most 2^31)
+ *   q, k, v   device rows, strides in elements (at most 2^22)
  *   until     device int32 [rows] or NULL
  *   o         device [rows][Hq][D] out
  *   lse       device float [Hq][rows] out (natural logarithm), or NULL

@@ -62,7 +62,7 @@ int64_t total_rows(const a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows)
 }
 
 bool bad_rows(const a2t_prompt* p, const void* x, int64_t stride, int heads) {
-    return !x || misaligned(x, 16) || stride < (int64_t)heads * p->D || stride % 8 || stride > (1ll << 31);
+    return !x || misaligned(x, 16) || stride < (int64_t)heads * p->D || stride % 8 || stride > (1 << 22);
 }
 
 // Calls f with tables of at most kMaxSeqs sequences, longest first (the launch's last workgroups

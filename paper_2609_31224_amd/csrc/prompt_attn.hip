@@ -11,6 +11,8 @@
 // tiles rescale nothing.
 #include "prompt_device.h"
 
+#include <type_traits>
+
 namespace a2t {
 namespace prompt {
 namespace {
@@ -65,7 +67,7 @@ __device__ __forceinline__ bool visible(const int2* meta, int lo, int hi, int k,
 }
 
 template <typename T, int D, bool UNTIL, int N>
-__global__ __launch_bounds__(kThreads) void prompt_attn_kernel(Args a, SeqTable<N> t) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
     constexpr int DB = Tl::DB;
     __shared__ __align__(1024) char s_k[2][Tl::BYTES];
@@ -89,19 +91,16 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(Args a, SeqTable<
 
     const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
     const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
-    Moving<T, D> mk, mv;
     int2 mm = {0, 0};
     auto load = [&](int tile) {
         int lo, hi;
         runs.at(tile, &lo, &hi);
-        auto row = [&](int r) { return (int64_t)min(lo + r, n - 1); };
-        mk.load([&](int r) { return kp + row(r) * a.kv.k_stride * (int64_t)sizeof(T); });
-        mv.load([&](int r) { return vp + row(r) * a.kv.v_stride * (int64_t)sizeof(T); });
-        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + row(threadIdx.x)];
+        const int stage = tile & 1;
+        Coming<T, D>::rows(kp, a.kv.k_stride * sizeof(T), lo, n - 1, w, lds_address(s_k[stage]));
+        Coming<T, D>::rows(vp, a.kv.v_stride * sizeof(T), lo, n - 1, w, lds_address(s_v[stage]));
+        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + min(lo + (int)threadIdx.x, n - 1)];
     };
     auto store = [&](int stage) {
-        mk.store(s_k[stage]);
-        mv.store(s_v[stage]);
         if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
     };
     if (runs.tiles) load(0);
@@ -126,6 +125,7 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(Args a, SeqTable<
 
     for (int tile = 0; tile < runs.tiles; ++tile) {
         const int stage = tile & 1;
+        wait_tiles();
         __syncthreads();
         if (tile + 1 < runs.tiles) load(tile + 1);
         int lo, hi;
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(kThreads) void prompt_attn_kernel(Args a, SeqTable<
 //   dQ_i = scale sum_j dS_ij k_j
 // Workgroups as above; delta goes to memory for the gradient of the keys.
 template <typename T, int D, bool UNTIL, int N>
-__global__ __launch_bounds__(kThreads) void prompt_dq_kernel(Args a, SeqTable<N> t) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prompt_dq_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
     constexpr int DB = Tl::DB;
     __shared__ __align__(1024) char s_k[2][Tl::BYTES];
@@ -215,19 +215,16 @@ __global__ __launch_bounds__(kThreads) void prompt_dq_kernel(Args a, SeqTable<N>
 
     const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
     const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
-    Moving<T, D> mk, mv;
     int2 mm = {0, 0};
     auto load = [&](int tile) {
         int lo, hi;
         runs.at(tile, &lo, &hi);
-        auto row = [&](int r) { return (int64_t)min(lo + r, n - 1); };
-        mk.load([&](int r) { return kp + row(r) * a.kv.k_stride * (int64_t)sizeof(T); });
-        mv.load([&](int r) { return vp + row(r) * a.kv.v_stride * (int64_t)sizeof(T); });
-        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + row(threadIdx.x)];
+        const int stage = tile & 1;
+        Coming<T, D>::rows(kp, a.kv.k_stride * sizeof(T), lo, n - 1, w, lds_address(s_k[stage]));
+        Coming<T, D>::rows(vp, a.kv.v_stride * sizeof(T), lo, n - 1, w, lds_address(s_v[stage]));
+        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + min(lo + (int)threadIdx.x, n - 1)];
     };
     auto store = [&](int stage) {
-        mk.store(s_k[stage]);
-        mv.store(s_v[stage]);
         if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
     };
     if (runs.tiles) load(0);
@@ -270,6 +267,7 @@ __global__ __launch_bounds__(kThreads) void prompt_dq_kernel(Args a, SeqTable<N>
 
     for (int tile = 0; tile < runs.tiles; ++tile) {
         const int stage = tile & 1;
+        wait_tiles();
         __syncthreads();
         if (tile + 1 < runs.tiles) load(tile + 1);
         int lo, hi;
@@ -310,24 +308,39 @@ __global__ __launch_bounds__(kThreads) void prompt_dq_kernel(Args a, SeqTable<N>
 
 // ---- gradient with respect to keys and values
 //   dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij q_i, over all heads of the group
-// One workgroup = 128 keys of a KV head, four waves of 32, over tiles of 64 packed query rows: the
-// sums over the group's heads are sums over packed rows, in one fixed order.
+// One workgroup = 128 keys of a KV head, 32 a wave, over tiles of 64 query rows of one head of the
+// group after the other: one sum, in one fixed order.  A wave needs both gradients' sums (D registers
+// each) beside its operands, and two waves a SIMD, for one's matrix products to run beside the other's
+// exponentials: with K in registers, V in LDS and two waves sharing 32 keys (each takes half of a
+// tile's rows; their sums are added at the end) it has 256 registers' room.  (V in registers too:
+// spills, 4.9 instead of 3.3 ms; one wave a SIMD: 3.3.)  Rows of 512 bytes (fp32, 128 dimensions) do not
+// fit so: four waves, one a SIMD, everything in registers.
+template <typename T, int D>
+struct KeyShape {
+    static constexpr bool kWide = Tile<T, D>::RB <= 256;
+    static constexpr int kWaves = kWide ? 8 : 4;
+};
 template <typename T, int D, bool UNTIL, int N>
-__global__ __launch_bounds__(kThreads) void prompt_dkv_kernel(Args a, SeqTable<N> t) {
+__global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWide ? 2 : 1)) void prompt_dkv_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
-    constexpr int DB = Tl::DB;
-    __shared__ __align__(1024) char s_q[2][Tl::BYTES];
-    __shared__ __align__(1024) char s_d[2][Tl::BYTES];
-    __shared__ __align__(16) float2 s_stat[2][kTile];   // lse (base 2) and delta of the tile's rows
-    __shared__ __align__(16) int s_place[2][kTile];
+    constexpr int DB = Tl::DB, WAVES = KeyShape<T, D>::kWaves;
+    constexpr bool WIDE = KeyShape<T, D>::kWide;
+    using In = Coming<T, D, WAVES>;
+    __shared__ __align__(1024) char s_tile[4][Tl::BYTES];            // Q and dO, two stages of each
+    __shared__ __align__(1024) char s_v[WIDE ? 2 : 1][WIDE ? Tl::BYTES : 16];
+    constexpr bool HALF_K = sizeof(T) == 2 && D == 128;              // K's second half of dimensions is read from LDS
+    __shared__ __align__(1024) char s_k[HALF_K ? 2 : 1][HALF_K ? Tl::BYTES : 16];
+    __shared__ __align__(16) float s_lse[2][kTile], s_delta[2][kTile];   // -lse / scale (fp32: -lse log2 e) and -delta of the tile's rows
     __shared__ int s_range[2][4];
+    static_assert(!WIDE || 4 * Tl::BYTES >= 4 * DB * 16 * 256, "one gradient's sums of four waves fit the tiles");
 
     const int g = blockIdx.x % a.Hkv, G = a.G;
     int place;
     const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
     const int n = t.rows[z], row0 = t.row0[z];
     const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
-    const int k0 = place * kBlock + 32 * w, key = min(k0 + l32, n - 1);
+    const int kg = w & 3, rg = w >> 2;        // keys, rows of a tile that are the wave's
+    const int k0 = place * kBlock + 32 * kg, key = min(k0 + l32, n - 1);
     const bool busy = k0 < n;
     // the lane's key: its place, and the first place that does not see it
     int2 me = {key, n};
@@ -344,59 +357,50 @@ __global__ __launch_bounds__(kThreads) void prompt_dkv_kernel(Args a, SeqTable<N
         u_max = max(u_max, __shfl_xor(u_max, d));
     }
     j_min = uniform(j_min), j_max = uniform(j_max), u_min = uniform(u_min), u_max = uniform(u_max);
-    if (lane == 0) s_range[0][w] = j_min, s_range[1][w] = u_max;   // idle waves repeat the last key's
+    if (lane == 0) s_range[0][kg] = j_min, s_range[1][kg] = u_max;   // idle waves repeat the last key's
     __syncthreads();
     const int from = uniform(min(min(s_range[0][0], s_range[0][1]), min(s_range[0][2], s_range[0][3])));
     const int to = uniform(max(max(s_range[1][0], s_range[1][1]), max(s_range[1][2], s_range[1][3])));
-    const int m_from = from * G, m_to = max(to, from) * G;   // packed rows that see some of the keys
-    const int tiles = (m_to - m_from + kTile - 1) / kTile;
+    const int per_head = max(to - from + kTile - 1, 0) / kTile, tiles = G * per_head;   // places from .. to - 1, head by head
 
-    const int64_t at_k = (row0 + key) * a.kv.k_stride + g * D, at_v = (row0 + key) * a.kv.v_stride + g * D;
-    u32x4 kop[Tl::STEPS], vop[Tl::STEPS];
+    const char* kb = static_cast<const char*>(a.kv.k) + (row0 * a.kv.k_stride + g * D) * (int64_t)sizeof(T);
+    const char* kp = kb + key * a.kv.k_stride * (int64_t)sizeof(T) + 16 * h;
+    const char* vp = static_cast<const char*>(a.kv.v) + (row0 * a.kv.v_stride + g * D) * (int64_t)sizeof(T);
+    u32x4 kop[HALF_K ? 4 : Tl::STEPS], vop[WIDE ? 1 : Tl::STEPS];
 #pragma unroll
     for (int s = 0; s < Tl::STEPS; ++s) {
-        kop[s] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.kv.k) + at_k * sizeof(T) + 16 * h + 32 * s);
-        vop[s] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.kv.v) + at_v * sizeof(T) + 16 * h + 32 * s);
+        if (!HALF_K || s < 4) kop[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
+        if constexpr (!WIDE) vop[s] = *reinterpret_cast<const u32x4*>(vp + key * a.kv.v_stride * (int64_t)sizeof(T) + 16 * h + 32 * s);
     }
 
     const char* qp = static_cast<const char*>(a.q) + ((int64_t)row0 * a.q_stride + g * G * D) * sizeof(T);
     const char* dp = static_cast<const char*>(a.d_o) + ((int64_t)row0 * a.Hq + g * G) * D * sizeof(T);
-    Moving<T, D> mq, md;
     float2 stat = {0.f, 0.f};
-    int stat_place = 0;
-    auto load = [&](int tile) {
-        const int m = m_from + tile * kTile, base = uniform(m / G), rem = m - base * G, last = min(kTile, m_to - m) - 1;
-        auto split = [&](int r, int* hh) {
-            const uint32_t x = rem + min(r, last), q = (x * a.inv_g) >> 16;
-            *hh = x - q * G;
-            return base + (int)q;
-        };
-        mq.load([&](int r) {
-            int hh;
-            const int64_t i = split(r, &hh);
-            return qp + (i * a.q_stride + hh * D) * (int64_t)sizeof(T);
-        });
-        md.load([&](int r) {
-            int hh;
-            const int64_t i = split(r, &hh);
-            return dp + (i * a.Hq + hh) * D * (int64_t)sizeof(T);
-        });
+    const float lse_by = sizeof(T) == 2 ? -1.f / a.scale : -kLog2e;
+    auto load = [&](int hh, int lo, int stage) {
+        In::rows(qp + hh * D * sizeof(T), a.q_stride * sizeof(T), lo, n - 1, w, lds_address(s_tile[stage]));
+        In::rows(dp + hh * D * sizeof(T), (int64_t)a.Hq * D * sizeof(T), lo, n - 1, w, lds_address(s_tile[2 + stage]));
         if (threadIdx.x < kTile) {
-            int hh;
-            stat_place = split(threadIdx.x, &hh);
-            const int64_t at = (int64_t)(g * G + hh) * a.total + row0 + stat_place;
-            stat = make_float2(a.lse[at] * kLog2e, a.delta[at]);
-            if (stat.x == -INFINITY) stat.x = 0.f;
-            if ((int)threadIdx.x > last) stat_place = -1;   // sees no key
+            const int64_t at = (int64_t)(g * G + hh) * a.total + row0 + min(lo + (int)threadIdx.x, n - 1);
+            stat = make_float2(a.lse[at], a.delta[at]);
         }
     };
     auto store = [&](int stage) {
-        mq.store(s_q[stage]);
-        md.store(s_d[stage]);
-        if (threadIdx.x < kTile) s_stat[stage][threadIdx.x] = stat, s_place[stage][threadIdx.x] = stat_place;
+        if (threadIdx.x < kTile) {
+            s_lse[stage][threadIdx.x] = stat.x == -INFINITY ? 0.f : stat.x * lse_by;   // a row without keys sees none of these
+            s_delta[stage][threadIdx.x] = -stat.y;
+        }
     };
     if (tiles) {
-        load(0);
+        if constexpr (WIDE) {
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                const int first = min(place * kBlock + x * kTile, n - 1);
+                In::rows(vp, a.kv.v_stride * sizeof(T), first, n - 1, w, lds_address(s_v[x]));
+                if constexpr (HALF_K) In::rows(kb, a.kv.k_stride * sizeof(T), first, n - 1, w, lds_address(s_k[x]));
+            }
+        }
+        load(0, from, 0);
         store(0);
     }
 
@@ -407,44 +411,188 @@ __global__ __launch_bounds__(kThreads) void prompt_dkv_kernel(Args a, SeqTable<N
 #pragma unroll
         for (int e = 0; e < 16; ++e) ak[db][e] = av[db][e] = 0.f;
 
-    for (int tile = 0; tile < tiles; ++tile) {
-        const int stage = tile & 1;
-        __syncthreads();
-        if (tile + 1 < tiles) load(tile + 1);
-        const int m = m_from + tile * kTile;
-        const int i_first = uniform(m / G), i_last = uniform((min(m + kTile, m_to) - 1) / G);
-        if (busy && i_last >= j_min && i_first < u_max) {
-            const bool all = m + kTile <= m_to && i_first >= j_max && i_last < u_min;
+    // rows 32 b + 8 (e / 4) + 4 h + e % 4 of a tile, as the products' sums hold them
+    auto init = [&](f32x16& x, const float* of, int b) {
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                f32x16 s, p;
+        for (int q = 0; q < 4; ++q) {
+            const float4 y = *reinterpret_cast<const float4*>(of + 32 * b + 8 * q + 4 * h);
+            x[4 * q] = y.x, x[4 * q + 1] = y.y, x[4 * q + 2] = y.z, x[4 * q + 3] = y.w;
+        }
+    };
+    auto block = [&](const char* q, const char* d, const float* lse, const float* delta, int b, int first, bool all) {
+        // bf16 starts the products from -lse / scale and -delta of their rows, so that no subtraction
+        // comes after them; sums that start at -lse / scale would round to its size in fp32
+        f32x16 s, p;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = p[e] = 0.f;
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_q[stage], 32 * b + l32, k, h), kop[k], s);
+        for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(q, 32 * b + l32, k, h), kop[k], s);
+        init(p, delta, b);
 #pragma unroll
-                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_d[stage], 32 * b + l32, k, h), vop[k], p);
+        for (int k = 0; k < Tl::STEPS; ++k) {
+            u32x4 v;
+            if constexpr (WIDE) v = row_operand<T, D>(s_v[0], 32 * kg + l32, k, h);
+            else v = vop[k];
+            mma_step<T>(row_operand<T, D>(d, 32 * b + l32, k, h), v, p);
+        }
+        f32x16 l;
+        init(l, lse, b);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float2 st = s_stat[stage][32 * b + 8 * (e >> 2) + 4 * h + (e & 3)];
-                    s[e] = exp2_(__builtin_fmaf(s[e], c, -st.x));
-                    p[e] = s[e] * (p[e] - st.y);
-                }
-                if (!all) {
+        for (int e = 0; e < 16; ++e) s[e] = exp2_(__builtin_fmaf(s[e], c, l[e]));
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int i = s_place[stage][32 * b + 8 * (e >> 2) + 4 * h + (e & 3)];
-                        if (i < me.x || i >= me.y) s[e] = p[e] = 0.f;
-                    }
-                }
-                mma_rows<D, T>(s_d[stage], 32 * b, s, av);
-                mma_rows<D, T>(s_q[stage], 32 * b, p, ak);
+        for (int e = 0; e < 16; ++e) p[e] *= s[e];
+        if (!all) {   // a pair that is not visible has no gradient, whatever its products were
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = first + 32 * b + 8 * (e >> 2) + 4 * h + (e & 3);
+                if (i < me.x || i >= me.y) s[e] = p[e] = 0.f;
             }
         }
+        mma_rows<D, T>(d, 32 * b, s, av);
+        mma_rows<D, T>(q, 32 * b, p, ak);
+    };
+    // the same for bf16, with LDS reads issued two groups ahead of the products that use them
+    auto block16 = [&](uint32_t q, uint32_t d, const float* lse, const float* delta, int b, int first, bool all) {
+        f32x16 s, p;
+        const int r = 32 * b + l32;
+        const RowReads<D> qr(q, r, h), dr(d, r, h), vr(lds_address(s_v[0]), 32 * kg + l32, h);
+        const RowReads<D> kr(HALF_K ? lds_address(s_k[0]) : 0, 32 * kg + l32, h);
+        const TransReads<D> qt(q, 32 * b), dt(d, 32 * b);
+        u32x4 x[4], y[4];
+        uint2 tx[D / 16], ty[D / 16];
+        auto q_group = [&](u32x4 (&f)[4], auto k) {
+            constexpr int K = decltype(k)::value;
+            f[0] = qr.template step<K>(), f[1] = qr.template step<K + 1>(), f[2] = qr.template step<K + 2>(), f[3] = qr.template step<K + 3>();
+        };
+        auto qk_group = [&](u32x4 (&f)[4], auto k) {
+            constexpr int K = decltype(k)::value;
+            f[0] = qr.template step<K>(), f[1] = kr.template step<K>(), f[2] = qr.template step<K + 1>(), f[3] = kr.template step<K + 1>();
+        };
+        auto qk_mma = [&](const u32x4 (&f)[4]) {
+            mma_step<T>(f[0], f[1], s);
+            mma_step<T>(f[2], f[3], s);
+        };
+        auto dv_group = [&](u32x4 (&f)[4], auto k) {
+            constexpr int K = decltype(k)::value;
+            f[0] = dr.template step<K>(), f[1] = vr.template step<K>(), f[2] = dr.template step<K + 1>(), f[3] = vr.template step<K + 1>();
+        };
+        auto q_mma = [&](const u32x4 (&f)[4], int k) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) mma_step<T>(f[e], kop[k + e], s);
+        };
+        auto dv_mma = [&](const u32x4 (&f)[4]) {
+            mma_step<T>(f[0], f[1], p);
+            mma_step<T>(f[2], f[3], p);
+        };
+        using std::integral_constant;
+#define A2T_I(k) integral_constant<int, k>{}
+        init(s, lse, b);
+        init(p, delta, b);
+        q_group(x, A2T_I(0));
+        if constexpr (D == 128) {
+            qk_group(y, A2T_I(4));
+            lds_wait<4>(x);
+            q_mma(x, 0);
+            qk_group(x, A2T_I(6));
+            lds_wait<4>(y);
+            qk_mma(y);
+            dv_group(y, A2T_I(0));
+            lds_wait<4>(x);
+            qk_mma(x);
+            dv_group(x, A2T_I(2));
+            lds_wait<4>(y);
+            dv_mma(y);
+            dv_group(y, A2T_I(4));
+            lds_wait<4>(x);
+            dv_mma(x);
+            dv_group(x, A2T_I(6));
+        } else {
+            dv_group(y, A2T_I(0));
+            lds_wait<4>(x);
+            q_mma(x, 0);
+            dv_group(x, A2T_I(2));
+        }
+        auto last_two = [&](u32x4 (&f)[4], u32x4 (&g)[4]) {
+            lds_wait<4>(f);
+            dv_mma(f);
+            dt.template group<0>(tx);
+            lds_wait<D / 16>(g);
+            dv_mma(g);
+            dt.template group<1>(ty);
+        };
+        last_two(y, x);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            s[e] = exp2_(s[e] * c);
+            p[e] *= s[e];
+        }
+        if (!all) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int i = first + 32 * b + 8 * (e >> 2) + 4 * h + (e & 3);
+                if (i < me.x || i >= me.y) s[e] = p[e] = 0.f;
+            }
+        }
+        lds_wait<D / 16>(tx);
+        mma_group<D>(tx, pack8(s, 0), av);
+        qt.template group<0>(tx);
+        lds_wait<D / 16>(ty);
+        mma_group<D>(ty, pack8(s, 1), av);
+        qt.template group<1>(ty);
+        lds_wait<D / 16>(tx);
+        mma_group<D>(tx, pack8(p, 0), ak);
+        lds_wait<0>(ty);
+        mma_group<D>(ty, pack8(p, 1), ak);
+#undef A2T_I
+    };
+    int lo = from, hh = 0;
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int stage = tile & 1;
+        int next = lo + kTile, next_hh = hh;
+        if (next >= to) next = from, next_hh = hh + 1;
+        wait_tiles();
+        __syncthreads();
+        if (tile + 1 < tiles) load(next_hh, next, stage ^ 1);
+        auto visit = [&](int b) {
+            const int first = lo + 32 * b, last = min(first + 32, n) - 1;
+            if (!busy || last < j_min || first >= u_max) return;
+            const bool all = first >= j_max && first + 32 <= u_min;
+            if constexpr (sizeof(T) == 2) block16(lds_address(s_tile[stage]), lds_address(s_tile[2 + stage]), s_lse[stage], s_delta[stage], b, lo, all);
+            else block(s_tile[stage], s_tile[2 + stage], s_lse[stage], s_delta[stage], b, lo, all);
+        };
+        if constexpr (WIDE) {
+            visit(rg);
+        } else {
+            visit(0);
+            visit(1);
+        }
         if (tile + 1 < tiles) store(stage ^ 1);
+        lo = next;
+        hh = next_hh;
     }
 
-    if (k0 + l32 >= n) return;
+    if constexpr (WIDE) {   // the second half's sums to the first half's waves, one gradient after the other
+        float* part = reinterpret_cast<float*>(s_tile[0]) + kg * (DB * 16 * 64) + lane;
+        auto add = [&](f32x16 (&x)[DB]) {
+            __syncthreads();
+            if (rg == 1) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) part[(db * 16 + e) * 64] = x[db][e];
+            }
+            __syncthreads();
+            if (rg == 0) {
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[db][e] += part[(db * 16 + e) * 64];
+            }
+        };
+        add(ak);
+        add(av);
+    }
+    if (rg || k0 + l32 >= n) return;
     // gradients lie as the caller's K and V do, whatever order the keys were read in
     T* ok = static_cast<T*>(a.dk) + (row0 + me.x) * a.k_out + g * D + 4 * h;
     T* ov = static_cast<T*>(a.dv) + (row0 + me.x) * a.v_out + g * D + 4 * h;
@@ -466,7 +614,7 @@ hipError_t launch(const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStr
         const dim3 grid((uint32_t)(blocks * a.Hkv));
         if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_attn_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
         else if constexpr (K == Kernel::dq) hipLaunchKernelGGL((prompt_dq_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
-        else hipLaunchKernelGGL((prompt_dkv_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
+        else hipLaunchKernelGGL((prompt_dkv_kernel<T, D, UNTIL, N>), grid, dim3(64 * KeyShape<T, D>::kWaves), 0, stream, a, s);
         return hipGetLastError();
     });
 }

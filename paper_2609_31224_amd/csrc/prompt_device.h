@@ -62,22 +62,36 @@ __device__ __forceinline__ int sequence_of(const SeqTable<N>& t, int y, int* pla
     return z;
 }
 
-// A tile holds kTile rows of a head, RB bytes each, in 16-byte chunks.  Chunk c of row r is at
-// place c ^ swizzle(r) of its row, so that neither way of reading it has a bank conflict: the 16
-// rows of a quarter of a row read (one chunk of each) lie in 16 different places of 256 bytes, and
-// the four rows x 64 bytes that half of a transposed read touches do as well.
+// A tile holds kTile rows of a head, RB bytes each, in blocks of 1 KiB (RPB rows) that lie 1,040
+// bytes apart.  Within a block the 16-byte chunks of its rows are interleaved so that neither way of
+// reading has a bank conflict: 16 rows' chunk c lie in 16 different places of 256 bytes (row reads), and
+// so do four rows x 64 bytes (transposed reads); and so that a lane's addresses differ by
+// constants: one register for all steps of a product (an exclusive-or of row and chunk, without the 16
+// bytes, took one a step).
 template <typename T, int D>
 struct Tile {
     static constexpr int RB = D * (int)sizeof(T);
     static constexpr int CPR = RB / 16;          // chunks of a row
     static constexpr int STEPS = RB / 32;        // steps of a product over the head dimension
     static constexpr int DB = D / 32;            // blocks of 32 dimensions
-    static constexpr int BYTES = kTile * RB;
-    static constexpr int PER = kTile * CPR / kThreads;   // chunks of a tile that a thread moves
-    static __device__ __forceinline__ int swizzle(int r) {
-        return CPR == 8 ? (((r >> 1) & 1) << 2) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3);
+    static constexpr int RPB = 1024 / RB;        // rows of a block
+    static constexpr int BLOCK = 1040;
+    static constexpr int BYTES = kTile / RPB * BLOCK;
+    static_assert(RPB == 2 || RPB == 4 || RPB == 8, "rows of 128, 256 or 512 bytes");
+    // chunk c of row r
+    static __device__ __forceinline__ int at(int r, int c) {
+        const int block = r / RPB * BLOCK, q = r % RPB;
+        if (RPB == 4) return block + (c >> 2) * 256 + q * 64 + (c & 3) * 16;
+        if (RPB == 2) return block + (c >> 3) * 256 + q * 128 + (c & 7) * 16;
+        return block + (c >> 2) * 512 + (q >> 2) * 256 + (q & 3) * 64 + (((c & 3) ^ ((q >> 2) << 1)) * 16);
     }
-    static __device__ __forceinline__ int at(int r, int c) { return r * RB + ((c ^ swizzle(r)) << 4); }
+    // row of a block and chunk that place j of it holds
+    static __device__ __forceinline__ int row_of(int j) {
+        return RPB == 4 ? (j >> 2) & 3 : RPB == 2 ? (j >> 3) & 1 : ((j >> 4) & 1) * 4 + ((j >> 2) & 3);
+    }
+    static __device__ __forceinline__ int chunk_of(int j) {
+        return RPB == 4 ? (j >> 4) * 4 + (j & 3) : RPB == 2 ? (j >> 4) * 8 + (j & 7) : (j >> 5) * 4 + ((j & 3) ^ (((j >> 4) & 1) << 1));
+    }
 };
 
 // Operand of a row for a product over the head dimension, step s: 16 bytes, the lane's half of
@@ -111,8 +125,8 @@ __device__ __forceinline__ void mma_rows(const char* tile, int r0, const f32x16&
         typedef __attribute__((__vector_size__(4 * sizeof(short)))) short s16x4;
         const int l16 = lane & 15, lg = lane >> 4;
         const int row = 4 * h + (l16 >> 2), chunk = 2 * (lg & 1) + ((l16 & 3) >> 1);
-        const uint32_t base = (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)(tile + r0 * Tl::RB);
-        const uint32_t a0 = base + Tl::at(row, chunk) + 8 * (l16 & 1), a1 = base + Tl::at(row + 8, chunk) + 8 * (l16 & 1);
+        const char* const from = tile + Tl::at(row, chunk) + 8 * (l16 & 1);   // rows r0 + 16 c + row and 8 further, block db
+        const char* const from8 = tile + Tl::at(row + 8, chunk) + 8 * (l16 & 1);
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             const u32x4 pk = {pack_bf16x2(p[8 * c], p[8 * c + 1]), pack_bf16x2(p[8 * c + 2], p[8 * c + 3]),
@@ -120,11 +134,10 @@ __device__ __forceinline__ void mma_rows(const char* tile, int r0, const f32x16&
             const bf16x8 b = __builtin_bit_cast(bf16x8, pk);
 #pragma unroll
             for (int db = 0; db < D / 32; ++db) {
-                auto read = [&](uint32_t at) {
-                    return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                        (__attribute__((address_space(3))) s16x4*)(uintptr_t)((at ^ (64 * db)) + 16 * c * Tl::RB));
+                auto read = [&](const char* at) {
+                    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(at + Tl::at(r0 + 16 * c, 4 * db)));
                 };
-                const s16x4 x = read(a0), y = read(a1);
+                const s16x4 x = read(from), y = read(from8);
                 typedef __attribute__((__vector_size__(8 * sizeof(short)))) short s16x8;
                 const s16x8 xy = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
                 acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, xy), b, acc[db], 0, 0, 0);
@@ -143,28 +156,122 @@ __device__ __forceinline__ void mma_rows(const char* tile, int r0, const f32x16&
     }
 }
 
-// A tile on its way from memory to LDS through registers: chunk i of a thread is chunk
-// (tid % CPR) of row tid / CPR + i * (256 / CPR).
-template <typename T, int D>
-struct Moving {
-    using Tl = Tile<T, D>;
-    u32x4 x[Tl::PER];
-    template <class RowPtr>   // row of the tile -> its first byte in memory
-    __device__ __forceinline__ void load(RowPtr&& row) {
-#pragma unroll
-        for (int i = 0; i < Tl::PER; ++i) {
-            const int r = threadIdx.x / Tl::CPR + i * (kThreads / Tl::CPR), c = threadIdx.x % Tl::CPR;
-            x[i] = *reinterpret_cast<const u32x4*>(static_cast<const char*>(row(r)) + 16 * c);
-        }
+// ---- bf16: LDS reads issued ahead as assembly, in groups of at most 16 registers.  The compiler,
+// left to itself, requests all of a product's operands at once, which costs the 256 registers that a
+// wave of two on a SIMD has (spills to memory, whose reloads then wait for the next tile too), or waits
+// for each before the next.  A group's registers hold nothing until lds_wait() has named them; LDS
+// reads return in order, so that waiting for all but the N youngest is enough, and any read of the
+// compiler's between them makes the wait longer, never shorter.
+template <int OFF>
+__device__ __forceinline__ u32x4 read16(uint32_t at) {
+    u32x4 r;
+    asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(r) : "v"(at), "i"(OFF));
+    return r;
+}
+template <int OFF>
+__device__ __forceinline__ uint2 read8t(uint32_t at) {
+    uint2 r;
+    asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(r) : "v"(at), "i"(OFF));
+    return r;
+}
+template <int N>
+__device__ __forceinline__ void lds_wait(u32x4 (&a)[4]) {
+    asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]) : "i"(N));
+}
+template <int N>
+__device__ __forceinline__ void lds_wait(uint2 (&a)[8]) {
+    asm volatile("s_waitcnt lgkmcnt(%8)"
+                 : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(a[4]), "+v"(a[5]), "+v"(a[6]), "+v"(a[7])
+                 : "i"(N));
+}
+template <int N>
+__device__ __forceinline__ void lds_wait(uint2 (&a)[4]) {
+    asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]) : "i"(N));
+}
+
+// Row reads of a lane: its row of the tile at LDS address `tile` (row r of it), operand of step K.
+template <int D>
+struct RowReads {
+    using Tl = Tile<bf16_t, D>;
+    uint32_t even, odd;   // of even and odd steps (D 128: 32 bytes apart)
+    __device__ __forceinline__ RowReads(uint32_t tile, int r, int h) : even(tile + Tl::at(r, h)), odd(tile + Tl::at(r, 2 + h)) {}
+    template <int K>
+    __device__ __forceinline__ u32x4 step() const {
+        if constexpr (D == 128) return read16<(K >> 1) * 256 + (K & 1) * 32>(even);
+        else return read16<(K >> 1) * 512>(K & 1 ? odd : even);
     }
-    __device__ __forceinline__ void store(char* tile) const {
-#pragma unroll
-        for (int i = 0; i < Tl::PER; ++i) {
-            const int r = threadIdx.x / Tl::CPR + i * (kThreads / Tl::CPR), c = threadIdx.x % Tl::CPR;
-            *reinterpret_cast<u32x4*>(tile + Tl::at(r, c)) = x[i];
+};
+// Transposed reads: rows r0 + 16 C .. + 15 of the tile (r0 a multiple of 32), all blocks of 32
+// dimensions; group C of a 32-row block.
+template <int D>
+struct TransReads {
+    using Tl = Tile<bf16_t, D>;
+    uint32_t from;
+    __device__ __forceinline__ TransReads(uint32_t tile, int r0) {
+        const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
+        from = tile + Tl::at(r0 + 4 * (lane >> 5) + (l16 >> 2), 2 * (lg & 1) + ((l16 & 3) >> 1)) + 8 * (l16 & 1);
+    }
+    template <int C, int DB0 = 0>
+    __device__ __forceinline__ void group(uint2 (&x)[D / 16]) const {
+        if constexpr (DB0 < D / 32) {
+            constexpr int OFF = 16 * C / Tl::RPB * Tl::BLOCK + DB0 * (D == 128 ? 256 : 512);
+            x[2 * DB0] = read8t<OFF>(from);
+            x[2 * DB0 + 1] = read8t<OFF + 8 / Tl::RPB * Tl::BLOCK>(from);
+            group<C, DB0 + 1>(x);
         }
     }
 };
+__device__ __forceinline__ bf16x8 pack8(const f32x16& p, int c) {
+    const u32x4 pk = {pack_bf16x2(p[8 * c], p[8 * c + 1]), pack_bf16x2(p[8 * c + 2], p[8 * c + 3]),
+                      pack_bf16x2(p[8 * c + 4], p[8 * c + 5]), pack_bf16x2(p[8 * c + 6], p[8 * c + 7])};
+    return __builtin_bit_cast(bf16x8, pk);
+}
+// acc[db] += rows of a transposed group times the packed values of the same rows
+template <int D>
+__device__ __forceinline__ void mma_group(const uint2 (&x)[D / 16], const bf16x8& p, f32x16 (&acc)[D / 32]) {
+#pragma unroll
+    for (int db = 0; db < D / 32; ++db) {
+        const u32x4 a = {x[2 * db].x, x[2 * db].y, x[2 * db + 1].x, x[2 * db + 1].y};
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p, acc[db], 0, 0, 0);
+    }
+}
+
+// A tile's way from memory into LDS: 1 KiB blocks, PER of them a wave, 16 bytes a lane, without
+// registers between.  Lane j of a block fills place j % CPR of the block's row j / CPR; the address it
+// reads picks the chunk that belongs there.  Written as assembly: of the builtin's loads the compiler
+// waits for all before it reads any LDS, the next tile's with this one's.  What it counts itself
+// stays right (loads return in order, so that more of them outstanding than it knows make its waits
+// longer, never shorter); wait_tiles() is the wait for these.
+template <typename T, int D, int WAVES = 4>
+struct Coming {
+    using Tl = Tile<T, D>;
+    static constexpr int PER = kTile / Tl::RPB / WAVES;  // blocks of a wave
+    static_assert(PER >= 1, "a wave moves whole blocks");
+    static __device__ __forceinline__ void block(const char* base, uint32_t at, uint32_t lds) {
+        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(at), "s"(base) : "memory");
+    }
+    // rows lo .. lo + 63, those past `last` read row `last`
+    static __device__ __forceinline__ void rows(const char* base, int64_t stride, int lo, int last, int w, uint32_t lds) {
+        const int lane = threadIdx.x & 63, r0 = w * PER * Tl::RPB, row = Tl::row_of(lane);
+        const uint32_t byte = Tl::chunk_of(lane) * 16;
+        const char* first = base + (lo + r0) * stride;
+        lds += w * PER * Tl::BLOCK;
+        if (lo + kTile - 1 <= last) {
+            const uint32_t at = (uint32_t)row * (uint32_t)stride + byte;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) block(first + i * Tl::RPB * stride, at, lds + i * Tl::BLOCK);
+        } else {
+            first = base + lo * stride;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+                block(first, (uint32_t)min(r0 + i * Tl::RPB + row, last - lo) * (uint32_t)stride + byte, lds + i * Tl::BLOCK);
+        }
+    }
+};
+__device__ __forceinline__ uint32_t lds_address(const void* p) {
+    return (uint32_t)uniform((int)(uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)(p));
+}
+__device__ __forceinline__ void wait_tiles() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Four consecutive dimensions (registers 4 a .. 4 a + 3 of a block of acc) of the lane's column,
 // as stored: the lanes of a column, l and l ^ 32, hold every second four.

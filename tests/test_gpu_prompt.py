@@ -361,7 +361,7 @@ def test_refusals(gpu):
     try:
         assert call() == a2t.A2T_OK
         for bad in (dict(rows=()), dict(rows=(0, 0)), dict(rows=(20, -1)), dict(rows=(20, 5)), dict(rows=(2**31 - 1, 2**31 - 1)),
-                    dict(q=None), dict(q=q.data_ptr() + 8), dict(qs=248), dict(qs=260), dict(ks=120), dict(qs=2**31 + 8), dict(o=None),
+                    dict(q=None), dict(q=q.data_ptr() + 8), dict(qs=248), dict(qs=260), dict(ks=120), dict(qs=2**22 + 8), dict(o=None),
                     dict(o=o.data_ptr() + 2), dict(until=ut.data_ptr()), dict(lse=lse.data_ptr() + 2)):
             for grad in (False, True):
                 if grad and bad.get("o") is None and "o" in bad:
