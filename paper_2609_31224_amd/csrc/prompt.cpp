@@ -17,6 +17,9 @@ struct a2t_prompt {
     double scale = 0.0;
     hipStream_t stream = nullptr;
     float* delta = nullptr;      // [Hq][rows of the call]
+    float* part = nullptr;       // sums of split blocks
+    int64_t part_rows = 0;       // (row, head, split) triples that fit it
+    int cus = 256;
     // handles for calls with `until`: sorted copies of K and V, and what the kernels know of them
     void* k = nullptr;
     void* v = nullptr;
@@ -42,10 +45,14 @@ struct DevGuard {
 };
 
 void free_prompt(a2t_prompt* p) {
-    for (void* m : {(void*)p->delta, p->k, p->v, (void*)p->meta, (void*)p->lasting, (void*)p->first, (void*)p->reach})
+    for (void* m : {(void*)p->delta, p->k, p->v, (void*)p->meta, (void*)p->lasting, (void*)p->first, (void*)p->reach, (void*)p->part})
         if (m) (void)hipFree(m);
     delete p;
 }
+
+constexpr int kTileRows = 64;
+constexpr int kSplitSeqs = 64;                   // launches of more sequences are not split
+constexpr int64_t kPartRows = 1 << 18;           // most (row, head, split) triples of split sums (130 MiB of 128 dimensions)
 
 bool misaligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1u)) != 0; }
 
@@ -113,9 +120,18 @@ Args base_args(const a2t_prompt* p, int64_t total, const void* q, int64_t qs, co
     a.G = p->Hq / p->Hkv;
     a.total = (int32_t)total;
     a.inv_g = (65536u + a.G - 1) / a.G;
+    a.part = p->part;
+    a.splits = 1;
     a.scale = (float)p->scale;
     a.scale_log2e = (float)(p->scale * 1.44269504088896340736);
     return a;
+}
+// Workgroups that a block's tiles are split over: as many as give every CU `per_cu` of them, if a
+// split keeps `least` tiles of 64 rows of the longest block's `tiles` and the sums fit.
+int splits_for(const a2t_prompt* p, int64_t wgs, int64_t tiles, int per_cu, int least, int64_t rows) {
+    int64_t s = (int64_t)per_cu * p->cus / wgs;
+    s = std::min({s, tiles / least, p->part_rows / rows, (int64_t)16});
+    return s < 1 ? 1 : (int)s;
 }
 hipError_t sort_keys(const a2t_prompt* p, const SeqTable<kMaxSeqs>& t, const int32_t* until, const void* k, int64_t ks, const void* v, int64_t vs) {
     const int size = p->dtype == A2T_F32 ? 4 : 2;
@@ -148,8 +164,12 @@ extern "C" int a2t_prompt_create(int32_t max_rows, int32_t n_q_heads, int32_t n_
     p->scale = attn_scale == 0.0 ? 1.0 / std::sqrt((double)head_dim) : attn_scale;
     p->stream = static_cast<hipStream_t>(hip_stream);
     p->until = flags & A2T_PROMPT_UNTIL;
+    int cus = 0;
+    if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && cus > 0) p->cus = cus;
+    p->part_rows = std::min<int64_t>((int64_t)max_rows * n_q_heads * 16, kPartRows);
     const size_t rows = (size_t)max_rows, row = (size_t)n_kv_heads * head_dim * (dtype == A2T_F32 ? 4 : 2);
     bool ok = hipMalloc(&p->delta, rows * n_q_heads * sizeof(float)) == hipSuccess;
+    ok = ok && hipMalloc(&p->part, (size_t)p->part_rows * (head_dim + 2) * sizeof(float)) == hipSuccess;
     if (p->until)
         ok = ok && hipMalloc(&p->k, rows * row) == hipSuccess && hipMalloc(&p->v, rows * row) == hipSuccess &&
              hipMalloc(&p->meta, rows * sizeof(int2)) == hipSuccess && hipMalloc(&p->lasting, rows * 4) == hipSuccess &&
@@ -194,6 +214,7 @@ extern "C" int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq
         hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
         if (s != hipSuccess) return s;
         const int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
+        a.splits = t.count > kSplitSeqs ? 1 : splits_for(p, (int64_t)blocks * p->Hkv, (t.rows[0] + kTileRows - 1) / kTileRows, 2, 2, total * p->Hq);
         return launch_forward(shape, a, t, blocks, p->stream);
     });
     if (e != hipSuccess) {
@@ -226,9 +247,12 @@ extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t
         hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
         if (s != hipSuccess) return s;
         int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
+        const int64_t tiles = (t.rows[0] + kTileRows - 1) / kTileRows;
+        a.splits = t.count > kSplitSeqs ? 1 : splits_for(p, (int64_t)blocks * p->Hkv, tiles, 2, 2, total * p->Hq);
         s = launch_dq(shape, a, t, blocks, p->stream);
         if (s != hipSuccess) return s;
         blocks = place_blocks(t, [&](int i) { return (int64_t)t.rows[i]; });
+        a.splits = t.count > kSplitSeqs ? 1 : splits_for(p, (int64_t)blocks * p->Hkv, a.G * tiles, 2, 2, total * p->Hkv * 2);
         return launch_dkv(shape, a, t, blocks, p->stream);
     });
     if (e != hipSuccess) {

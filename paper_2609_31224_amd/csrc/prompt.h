@@ -55,6 +55,9 @@ struct Args {
     int32_t total;          // packed rows
     uint32_t inv_g;         // ceil(2^16 / G)
     float scale, scale_log2e;
+    // a block's tiles may be split over several workgroups: their fp32 sums go to `part`
+    int32_t splits;
+    float* part;
 };
 
 struct Shape {

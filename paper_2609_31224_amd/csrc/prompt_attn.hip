@@ -75,8 +75,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     __shared__ int2 s_meta[2][UNTIL ? kTile : 1];
 
     const int g = blockIdx.x % a.Hkv, G = a.G;
-    int place;
-    const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
+    int sp = (int)(blockIdx.x / a.Hkv), place;   // split of the block's tiles
+    const int y = sp / a.splits;
+    sp -= y * a.splits;
+    const int z = sequence_of(t, y, &place);
     const int n = t.rows[z], row0 = t.row0[z], M = G * n;
     const int m0 = ((M + kBlock - 1) / kBlock - 1 - place) * kBlock;   // the rows that see most come first
     const int base = uniform(m0 / G), rem = m0 - base * G;
@@ -88,6 +90,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     const int i = place_of(r), hh = rem + r - (i - base) * G;
     const int i_first = uniform(place_of(min(32 * w, rows - 1))), i_last = uniform(place_of(min(32 * w + 31, rows - 1)));
     const Runs runs = key_runs<UNTIL>(a.kv, row0, n, base, uniform(place_of(rows - 1)));
+    const int t0 = runs.tiles * sp / a.splits, t1 = runs.tiles * (sp + 1) / a.splits;
 
     const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
     const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
@@ -103,7 +106,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     auto store = [&](int stage) {
         if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
     };
-    if (runs.tiles) load(0);
+    if (t0 < t1) load(t0);
 
     u32x4 qop[Tl::STEPS];
     {
@@ -111,7 +114,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
 #pragma unroll
         for (int s = 0; s < Tl::STEPS; ++s) qop[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
     }
-    if (runs.tiles) store(0);
+    if (t0 < t1) store(t0 & 1);
 
     // base-2 logarithms throughout: mref is the reference of the lane's row (its scaled scores less mref
     // are at most 8), sum of 2^(score - mref)
@@ -123,11 +126,11 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
 
-    for (int tile = 0; tile < runs.tiles; ++tile) {
+    for (int tile = t0; tile < t1; ++tile) {
         const int stage = tile & 1;
         wait_tiles();
         __syncthreads();
-        if (tile + 1 < runs.tiles) load(tile + 1);
+        if (tile + 1 < t1) load(tile + 1);
         int lo, hi;
         runs.at(tile, &lo, &hi);
         const Sees what = busy ? sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last) : Sees::none;
@@ -170,11 +173,21 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
                 mma_rows<D, T>(s_v[stage], 32 * b, s[b], acc);
             }
         }
-        if (tile + 1 < runs.tiles) store(stage ^ 1);
+        if (tile + 1 < t1) store(stage ^ 1);
     }
 
     if (32 * w + l32 >= rows) return;
     const float total = swap_sum(sum);
+    if (a.splits > 1) {   // the split's own sums; prompt_join_kernel puts them together
+        const int64_t at = ((int64_t)sp * a.total + row0 + i) * a.Hq + g * G + hh;
+        if (h == 0) *reinterpret_cast<float2*>(a.part + (int64_t)a.splits * a.total * a.Hq * D + 2 * at) = make_float2(mrun, total);
+        float* o = a.part + at * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store4(o + 32 * db + 8 * e, acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
+        return;
+    }
     const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;   // a row without keys is zero
     const int64_t row = row0 + i;
     if (a.lse && h == 0) a.lse[(int64_t)(g * G + hh) * a.total + row] = (mref + __builtin_amdgcn_logf(total)) * kLn2;
@@ -199,8 +212,10 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     __shared__ int2 s_meta[2][UNTIL ? kTile : 1];
 
     const int g = blockIdx.x % a.Hkv, G = a.G;
-    int place;
-    const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
+    int sp = (int)(blockIdx.x / a.Hkv), place;   // split of the block's tiles
+    const int y = sp / a.splits;
+    sp -= y * a.splits;
+    const int z = sequence_of(t, y, &place);
     const int n = t.rows[z], row0 = t.row0[z], M = G * n;
     const int m0 = ((M + kBlock - 1) / kBlock - 1 - place) * kBlock;
     const int base = uniform(m0 / G), rem = m0 - base * G;
@@ -212,6 +227,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     const int i = place_of(r), hh = rem + r - (i - base) * G;
     const int i_first = uniform(place_of(min(32 * w, rows - 1))), i_last = uniform(place_of(min(32 * w + 31, rows - 1)));
     const Runs runs = key_runs<UNTIL>(a.kv, row0, n, base, uniform(place_of(rows - 1)));
+    const int t0 = runs.tiles * sp / a.splits, t1 = runs.tiles * (sp + 1) / a.splits;
 
     const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
     const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
@@ -227,7 +243,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     auto store = [&](int stage) {
         if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
     };
-    if (runs.tiles) load(0);
+    if (t0 < t1) load(t0);
 
     u32x4 qop[Tl::STEPS], dop[Tl::STEPS];
     const int64_t row = row0 + i, head = g * G + hh;
@@ -255,8 +271,8 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
     delta = swap_sum(delta);
     float lse2 = a.lse[head * a.total + row] * kLog2e;
     if (lse2 == -INFINITY) lse2 = 0.f;   // a row without keys: nothing is visible below
-    if (32 * w + l32 < rows && h == 0) a.delta[head * a.total + row] = delta;
-    if (runs.tiles) store(0);
+    if (sp == 0 && 32 * w + l32 < rows && h == 0) a.delta[head * a.total + row] = delta;
+    if (t0 < t1) store(t0 & 1);
 
     const float c = a.scale_log2e;
     f32x16 acc[DB];
@@ -265,11 +281,11 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
 
-    for (int tile = 0; tile < runs.tiles; ++tile) {
+    for (int tile = t0; tile < t1; ++tile) {
         const int stage = tile & 1;
         wait_tiles();
         __syncthreads();
-        if (tile + 1 < runs.tiles) load(tile + 1);
+        if (tile + 1 < t1) load(tile + 1);
         int lo, hi;
         runs.at(tile, &lo, &hi);
         const Sees what = busy ? sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last) : Sees::none;
@@ -293,10 +309,18 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
                 mma_rows<D, T>(s_k[stage], 32 * b, p, acc);
             }
         }
-        if (tile + 1 < runs.tiles) store(stage ^ 1);
+        if (tile + 1 < t1) store(stage ^ 1);
     }
 
     if (32 * w + l32 >= rows) return;
+    if (a.splits > 1) {
+        float* o = a.part + (((int64_t)sp * a.total + row) * a.Hq + head) * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store4(o + 32 * db + 8 * e, acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
+        return;
+    }
     T* o = static_cast<T*>(a.dq) + row * a.q_stride + head * D + 4 * h;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -335,8 +359,10 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     static_assert(!WIDE || 4 * Tl::BYTES >= 4 * DB * 16 * 256, "one gradient's sums of four waves fit the tiles");
 
     const int g = blockIdx.x % a.Hkv, G = a.G;
-    int place;
-    const int z = sequence_of(t, (int)(blockIdx.x / a.Hkv), &place);
+    int sp = (int)(blockIdx.x / a.Hkv), place;   // split of the block's tiles
+    const int y = sp / a.splits;
+    sp -= y * a.splits;
+    const int z = sequence_of(t, y, &place);
     const int n = t.rows[z], row0 = t.row0[z];
     const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
     const int kg = w & 3, rg = w >> 2;        // keys, rows of a tile that are the wave's
@@ -361,15 +387,17 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     __syncthreads();
     const int from = uniform(min(min(s_range[0][0], s_range[0][1]), min(s_range[0][2], s_range[0][3])));
     const int to = uniform(max(max(s_range[1][0], s_range[1][1]), max(s_range[1][2], s_range[1][3])));
-    const int per_head = max(to - from + kTile - 1, 0) / kTile, tiles = G * per_head;   // places from .. to - 1, head by head
+    // places from .. to - 1, head by head; the split's tiles
+    const int per_head = max(to - from + kTile - 1, 0) / kTile;
+    const int t0 = (int)((int64_t)G * per_head * sp / a.splits), t1 = (int)((int64_t)G * per_head * (sp + 1) / a.splits);
 
     const char* kb = static_cast<const char*>(a.kv.k) + (row0 * a.kv.k_stride + g * D) * (int64_t)sizeof(T);
     const char* kp = kb + key * a.kv.k_stride * (int64_t)sizeof(T) + 16 * h;
     const char* vp = static_cast<const char*>(a.kv.v) + (row0 * a.kv.v_stride + g * D) * (int64_t)sizeof(T);
-    u32x4 kop[HALF_K ? 4 : Tl::STEPS], vop[WIDE ? 1 : Tl::STEPS];
+    u32x4 kop[HALF_K ? 1 : Tl::STEPS], vop[WIDE ? 1 : Tl::STEPS];
 #pragma unroll
     for (int s = 0; s < Tl::STEPS; ++s) {
-        if (!HALF_K || s < 4) kop[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
+        if (!HALF_K) kop[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
         if constexpr (!WIDE) vop[s] = *reinterpret_cast<const u32x4*>(vp + key * a.kv.v_stride * (int64_t)sizeof(T) + 16 * h + 32 * s);
     }
 
@@ -391,7 +419,8 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
             s_delta[stage][threadIdx.x] = -stat.y;
         }
     };
-    if (tiles) {
+    int hh = per_head ? t0 / per_head : 0, lo = from + (t0 - hh * per_head) * kTile;
+    if (t0 < t1) {
         if constexpr (WIDE) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
@@ -400,8 +429,8 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
                 if constexpr (HALF_K) In::rows(kb, a.kv.k_stride * sizeof(T), first, n - 1, w, lds_address(s_k[x]));
             }
         }
-        load(0, from, 0);
-        store(0);
+        load(hh, lo, t0 & 1);
+        store(t0 & 1);
     }
 
     const float c = a.scale_log2e;
@@ -480,52 +509,62 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
 #pragma unroll
             for (int e = 0; e < 4; ++e) mma_step<T>(f[e], kop[k + e], s);
         };
-        auto dv_mma = [&](const u32x4 (&f)[4]) {
+        // two products beside which the exponentials of EXPS scores run
+        constexpr int EXPS = 32 / Tl::STEPS;
+        auto dv_mma = [&](const u32x4 (&f)[4], int part) {
             mma_step<T>(f[0], f[1], p);
+#pragma unroll
+            for (int e = EXPS * part; e < EXPS * part + EXPS / 2; ++e) s[e] = exp2_(s[e] * c);
+            __builtin_amdgcn_sched_barrier(0);
             mma_step<T>(f[2], f[3], p);
+#pragma unroll
+            for (int e = EXPS * part + EXPS / 2; e < EXPS * part + EXPS; ++e) s[e] = exp2_(s[e] * c);
+            __builtin_amdgcn_sched_barrier(0);
         };
         using std::integral_constant;
 #define A2T_I(k) integral_constant<int, k>{}
-        init(s, lse, b);
-        init(p, delta, b);
-        q_group(x, A2T_I(0));
-        if constexpr (D == 128) {
-            qk_group(y, A2T_I(4));
-            lds_wait<4>(x);
-            q_mma(x, 0);
-            qk_group(x, A2T_I(6));
-            lds_wait<4>(y);
-            qk_mma(y);
-            dv_group(y, A2T_I(0));
-            lds_wait<4>(x);
-            qk_mma(x);
-            dv_group(x, A2T_I(2));
-            lds_wait<4>(y);
-            dv_mma(y);
-            dv_group(y, A2T_I(4));
-            lds_wait<4>(x);
-            dv_mma(x);
-            dv_group(x, A2T_I(6));
-        } else {
-            dv_group(y, A2T_I(0));
-            lds_wait<4>(x);
-            q_mma(x, 0);
-            dv_group(x, A2T_I(2));
-        }
         auto last_two = [&](u32x4 (&f)[4], u32x4 (&g)[4]) {
             lds_wait<4>(f);
-            dv_mma(f);
+            dv_mma(f, Tl::STEPS / 2 - 2);
             dt.template group<0>(tx);
             lds_wait<D / 16>(g);
-            dv_mma(g);
+            dv_mma(g, Tl::STEPS / 2 - 1);
             dt.template group<1>(ty);
         };
-        last_two(y, x);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            s[e] = exp2_(s[e] * c);
-            p[e] *= s[e];
+        init(s, lse, b);
+        init(p, delta, b);
+        if constexpr (D == 128) {
+            qk_group(x, A2T_I(0));
+            qk_group(y, A2T_I(2));
+            lds_wait<4>(x);
+            qk_mma(x);
+            qk_group(x, A2T_I(4));
+            lds_wait<4>(y);
+            qk_mma(y);
+            qk_group(y, A2T_I(6));
+            lds_wait<4>(x);
+            qk_mma(x);
+            dv_group(x, A2T_I(0));
+            lds_wait<4>(y);
+            qk_mma(y);
+            dv_group(y, A2T_I(2));
+            lds_wait<4>(x);
+            dv_mma(x, 0);
+            dv_group(x, A2T_I(4));
+            lds_wait<4>(y);
+            dv_mma(y, 1);
+            dv_group(y, A2T_I(6));
+            last_two(x, y);
+        } else {
+            q_group(x, A2T_I(0));
+            dv_group(y, A2T_I(0));
+            lds_wait<4>(x);
+            q_mma(x, 0);
+            dv_group(x, A2T_I(2));
+            last_two(y, x);
         }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) p[e] *= s[e];
         if (!all) {
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
@@ -545,14 +584,13 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
         mma_group<D>(ty, pack8(p, 1), ak);
 #undef A2T_I
     };
-    int lo = from, hh = 0;
-    for (int tile = 0; tile < tiles; ++tile) {
+    for (int tile = t0; tile < t1; ++tile) {
         const int stage = tile & 1;
         int next = lo + kTile, next_hh = hh;
         if (next >= to) next = from, next_hh = hh + 1;
         wait_tiles();
         __syncthreads();
-        if (tile + 1 < tiles) load(next_hh, next, stage ^ 1);
+        if (tile + 1 < t1) load(next_hh, next, stage ^ 1);
         auto visit = [&](int b) {
             const int first = lo + 32 * b, last = min(first + 32, n) - 1;
             if (!busy || last < j_min || first >= u_max) return;
@@ -566,7 +604,7 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
             visit(0);
             visit(1);
         }
-        if (tile + 1 < tiles) store(stage ^ 1);
+        if (tile + 1 < t1) store(stage ^ 1);
         lo = next;
         hh = next_hh;
     }
@@ -593,6 +631,17 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
         add(av);
     }
     if (rg || k0 + l32 >= n) return;
+    if (a.splits > 1) {
+        float* o = a.part + (((int64_t)sp * a.total + row0 + me.x) * a.Hkv + g) * 2 * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                store4(o + 32 * db + 8 * e, ak[db][4 * e], ak[db][4 * e + 1], ak[db][4 * e + 2], ak[db][4 * e + 3]);
+                store4(o + D + 32 * db + 8 * e, av[db][4 * e], av[db][4 * e + 1], av[db][4 * e + 2], av[db][4 * e + 3]);
+            }
+        return;
+    }
     // gradients lie as the caller's K and V do, whatever order the keys were read in
     T* ok = static_cast<T*>(a.dk) + (row0 + me.x) * a.k_out + g * D + 4 * h;
     T* ov = static_cast<T*>(a.dv) + (row0 + me.x) * a.v_out + g * D + 4 * h;
@@ -605,17 +654,84 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
         }
 }
 
+// ---- blocks whose tiles were split: the splits' sums put together, in order
+// Four elements a thread; a row of the launch's sequences by its place among their rows.
+template <int N>
+__device__ __forceinline__ int64_t joined_row(const SeqTable<N>& t, int64_t r) {
+    for (int z = 0; z < t.count; ++z) {   // few: launches of many sequences are not split
+        if (r < t.rows[z]) return t.row0[z] + r;
+        r -= t.rows[z];
+    }
+    return -1;
+}
+template <typename T, int D, int N>
+__global__ __launch_bounds__(kThreads) void prompt_join_kernel(Args a, SeqTable<N> t) {
+    const int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x, rh = x / (D / 4);
+    const int c = (int)(x % (D / 4)) * 4, head = (int)(rh % a.Hq);
+    const int64_t row = joined_row(t, rh / a.Hq);
+    if (row < 0) return;
+    const float* ml = a.part + (int64_t)a.splits * a.total * a.Hq * D;
+    auto at = [&](int sp) { return ((int64_t)sp * a.total + row) * a.Hq + head; };
+    float m = -INFINITY;
+    for (int sp = 0; sp < a.splits; ++sp) m = fmaxf(m, ml[2 * at(sp)]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+    float sum = 0.f;
+    for (int sp = 0; sp < a.splits; ++sp) {
+        const float2 p = *reinterpret_cast<const float2*>(ml + 2 * at(sp));
+        const float by = exp2_(p.x - ref);
+        const float4 q = *reinterpret_cast<const float4*>(a.part + at(sp) * D + c);
+        sum += by * p.y;
+        o.x += by * q.x, o.y += by * q.y, o.z += by * q.z, o.w += by * q.w;
+    }
+    const float inv = sum > 0.f ? 1.f / sum : sum == 0.f ? 0.f : sum;
+    if (a.lse && c == 0) a.lse[(int64_t)head * a.total + row] = (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+    store4(static_cast<T*>(a.o) + (row * a.Hq + head) * D + c, o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+}
+// dQ, or dK and dV (WIDTH D or 2 D a head)
+template <typename T, int D, bool KEYS, int N>
+__global__ __launch_bounds__(kThreads) void prompt_add_kernel(Args a, SeqTable<N> t) {
+    constexpr int WIDTH = KEYS ? 2 * D : D;
+    const int heads = KEYS ? a.Hkv : a.Hq;
+    const int64_t x = (int64_t)blockIdx.x * kThreads + threadIdx.x, rh = x / (WIDTH / 4);
+    const int c = (int)(x % (WIDTH / 4)) * 4, head = (int)(rh % heads);
+    const int64_t row = joined_row(t, rh / heads);
+    if (row < 0) return;
+    float4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int sp = 0; sp < a.splits; ++sp) {
+        const float4 q = *reinterpret_cast<const float4*>(a.part + (((int64_t)sp * a.total + row) * heads + head) * WIDTH + c);
+        o.x += q.x, o.y += q.y, o.z += q.z, o.w += q.w;
+    }
+    const bool v = KEYS && c >= D;
+    const float by = v ? 1.f : a.scale;
+    T* to = KEYS ? v ? static_cast<T*>(a.dv) + row * a.v_out + head * D + c - D : static_cast<T*>(a.dk) + row * a.k_out + head * D + c
+                 : static_cast<T*>(a.dq) + row * a.q_stride + head * D + c;
+    store4(to, o.x * by, o.y * by, o.z * by, o.w * by);
+}
+
 enum class Kernel { forward, dq, dkv };
 
+template <Kernel K, typename T, int D, int N>
+hipError_t join(const Args& a, const SeqTable<N>& s, hipStream_t stream) {
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    int64_t rows = 0;
+    for (int i = 0; i < s.count; ++i) rows += s.rows[i];
+    const int64_t fours = rows * (K == Kernel::dkv ? (int64_t)a.Hkv * 2 : a.Hq) * (D / 4);
+    const dim3 grid((uint32_t)((fours + kThreads - 1) / kThreads));
+    if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_join_kernel<T, D, N>), grid, dim3(kThreads), 0, stream, a, s);
+    else hipLaunchKernelGGL((prompt_add_kernel<T, D, K == Kernel::dkv, N>), grid, dim3(kThreads), 0, stream, a, s);
+    return hipGetLastError();
+}
 template <Kernel K, typename T, int D, bool UNTIL>
 hipError_t launch(const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
     return by_count(t, [&](const auto& s) {
         constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
-        const dim3 grid((uint32_t)(blocks * a.Hkv));
+        const dim3 grid((uint32_t)(blocks * a.splits * a.Hkv));
         if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_attn_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
         else if constexpr (K == Kernel::dq) hipLaunchKernelGGL((prompt_dq_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
         else hipLaunchKernelGGL((prompt_dkv_kernel<T, D, UNTIL, N>), grid, dim3(64 * KeyShape<T, D>::kWaves), 0, stream, a, s);
-        return hipGetLastError();
+        return a.splits == 1 ? hipGetLastError() : join<K, T, D, N>(a, s, stream);
     });
 }
 template <Kernel K>
