@@ -126,12 +126,43 @@ Args base_args(const a2t_prompt* p, int64_t total, const void* q, int64_t qs, co
     a.scale_log2e = (float)(p->scale * 1.44269504088896340736);
     return a;
 }
-// Workgroups that a block's tiles are split over: as many as give every CU `per_cu` of them, if a
-// split keeps `least` tiles of 64 rows of the longest block's `tiles` and the sums fit.
-int splits_for(const a2t_prompt* p, int64_t wgs, int64_t tiles, int per_cu, int least, int64_t rows) {
-    int64_t s = (int64_t)per_cu * p->cus / wgs;
-    s = std::min({s, tiles / least, p->part_rows / rows, (int64_t)16});
-    return s < 1 ? 1 : (int)s;
+// What a launch's workgroups cost, us: a tile of 64 rows with `per_cu` workgroups on every CU, and a
+// workgroup's beginning and end.  (Measured on sequences of 8,192 and 1,500 rows.)
+struct Cost {
+    double tile, start;
+    int per_cu;
+};
+enum { kForward, kQueries, kKeys };
+Cost cost_of(const a2t_prompt* p, int kernel) {
+    static const Cost bf16[2][3] = {{{2.4, 3, 4}, {2.6, 3, 3}, {1.7, 4, 1}}, {{2.2, 3, 2}, {2.5, 3, 2}, {2.4, 5, 1}}};
+    static const Cost f32[2][3] = {{{7, 3, 2}, {10, 3, 2}, {8.5, 4, 1}}, {{9, 4, 1}, {13, 4, 1}, {17, 5, 1}}};
+    return (p->dtype == A2T_F32 ? f32 : bf16)[p->D == 128][kernel];
+}
+// Workgroups that each block's tiles are split over.  A launch takes about as long as its longest
+// workgroup, or as all of them spread over the CUs if that is more; splits cost their sums' way to
+// memory and a launch that adds them.
+int splits_for(const a2t_prompt* p, const SeqTable<kMaxSeqs>& t, int kernel, int64_t total) {
+    if (t.count > kSplitSeqs) return 1;
+    const Cost c = cost_of(p, kernel);
+    const int64_t G = p->Hq / p->Hkv, slots = (int64_t)p->cus * c.per_cu, heads = kernel == kKeys ? 2 * (int64_t)p->Hkv : p->Hq;
+    int64_t wgs = 0, work = 0, longest = 0;
+    for (int i = 0; i < t.count; ++i) {
+        const int64_t tiles = (t.rows[i] + kTileRows - 1) / kTileRows * (kernel == kKeys ? G : 1);
+        const int64_t blocks = ((kernel == kKeys ? 1 : G) * t.rows[i] + kBlock - 1) / kBlock * p->Hkv;
+        wgs += blocks;
+        work += blocks * (tiles + 1) / 2;
+        longest = std::max(longest, tiles);
+    }
+    int best = 1;
+    double least = 0.0;
+    for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
+        if (s > 1 && (s > longest || s * total * heads > p->part_rows)) break;
+        const double tiles = std::max((double)((longest + s - 1) / s), (double)work / slots);
+        const double join = s > 1 ? 4.0 + (double)(s * total * heads) * p->D * 8 / 3e6 : 0.0;
+        const double us = tiles * c.tile + c.start * ((wgs * s + slots - 1) / slots) + join;
+        if (s == 1 || us < least) best = s, least = us;
+    }
+    return best;
 }
 hipError_t sort_keys(const a2t_prompt* p, const SeqTable<kMaxSeqs>& t, const int32_t* until, const void* k, int64_t ks, const void* v, int64_t vs) {
     const int size = p->dtype == A2T_F32 ? 4 : 2;
@@ -214,7 +245,7 @@ extern "C" int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq
         hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
         if (s != hipSuccess) return s;
         const int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
-        a.splits = t.count > kSplitSeqs ? 1 : splits_for(p, (int64_t)blocks * p->Hkv, (t.rows[0] + kTileRows - 1) / kTileRows, 2, 2, total * p->Hq);
+        a.splits = splits_for(p, t, kForward, total);
         return launch_forward(shape, a, t, blocks, p->stream);
     });
     if (e != hipSuccess) {
@@ -247,12 +278,11 @@ extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t
         hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
         if (s != hipSuccess) return s;
         int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
-        const int64_t tiles = (t.rows[0] + kTileRows - 1) / kTileRows;
-        a.splits = t.count > kSplitSeqs ? 1 : splits_for(p, (int64_t)blocks * p->Hkv, tiles, 2, 2, total * p->Hq);
+        a.splits = splits_for(p, t, kQueries, total);
         s = launch_dq(shape, a, t, blocks, p->stream);
         if (s != hipSuccess) return s;
         blocks = place_blocks(t, [&](int i) { return (int64_t)t.rows[i]; });
-        a.splits = t.count > kSplitSeqs ? 1 : splits_for(p, (int64_t)blocks * p->Hkv, a.G * tiles, 2, 2, total * p->Hkv * 2);
+        a.splits = splits_for(p, t, kKeys, total);
         return launch_dkv(shape, a, t, blocks, p->stream);
     });
     if (e != hipSuccess) {
