@@ -80,7 +80,9 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 __device__ __forceinline__ float value(const bf16_t* row, int i) { return __uint_as_float((uint32_t)row[i].bits << 16); }
 __device__ __forceinline__ float value(const float* row, int i) { return row[i]; }
 
-// (largest value m, sum of e^(x - m)) of parts of a row
+// Part of a row's sum: z of e^(x - m).  m is a logit that no other passes by kSlack; it follows the
+// largest one lazily, which leaves most chunks without a rescaling.
+constexpr float kSlack = 16.f;
 struct Sum {
     float m, z;
 };
@@ -89,7 +91,7 @@ __device__ __forceinline__ Sum join(Sum a, Sum b) {
     return {m, a.z * exp2_((a.m - ref) * kLog2e) + b.z * exp2_((b.m - ref) * kLog2e)};
 }
 
-// Statistics of a row: its largest logit and the logarithm of its sum, and log p(target).
+// ln p(target) of a row, and what its probabilities are made from: p_v = e^(x_v - m) / z.
 struct RowStat {
     double logp;
     float m, z;
@@ -107,9 +109,10 @@ struct RowsArgs {
 
 template <typename T, int TH>
 __global__ __launch_bounds__(TH) void prefer_rows_kernel(RowsArgs<T> a) {
-    const int tid = threadIdx.x, which = (int)blockIdx.x >= a.n, row = (int)blockIdx.x - which * a.n;
+    // the reference's rows first: the gradient then finds the policy's last rows in the caches
+    const int tid = threadIdx.x, which = (int)gridDim.x > a.n && (int)blockIdx.x < a.n, row = (int)(blockIdx.x % (uint32_t)a.n);
     const int target = a.target[row];
-    RowStat* stat = a.stat ? a.stat + blockIdx.x : nullptr;
+    RowStat* stat = a.stat ? a.stat + which * a.n + row : nullptr;
     if (target < 0 || target >= a.vocab) {   // no loss at this row
         if (tid == 0) {
             if (stat) *stat = {0.0, 0.f, 0.f};
@@ -120,17 +123,20 @@ __global__ __launch_bounds__(TH) void prefer_rows_kernel(RowsArgs<T> a) {
     const T* x = a.x[which] + row * a.stride[which];
     const int full = a.vocab / kChunk;
     Sum s{-INFINITY, 0.f};
+    float ref = 0.f;   // m, or 0 before the first finite logit
     auto add = [&](const float (&v)[kChunk]) {
-        float m = s.m;
+        float m = v[0];
 #pragma unroll
-        for (int e = 0; e < kChunk; ++e) m = fmaxf(m, v[e]);
-        const float ref = m == -INFINITY ? 0.f : m;
-        float z = s.z * exp2_((s.m - ref) * kLog2e);
+        for (int e = 1; e < kChunk; ++e) m = fmaxf(m, v[e]);
+        if (__any(m > s.m + kSlack)) {
+            m = fmaxf(m, s.m);
+            ref = m == -INFINITY ? 0.f : m;
+            s = {m, s.z * exp2_((s.m - ref) * kLog2e)};
+        }
 #pragma unroll
-        for (int e = 0; e < kChunk; ++e) z += exp2_((v[e] - ref) * kLog2e);
-        s = {m, z};
+        for (int e = 0; e < kChunk; ++e) s.z += exp2_((v[e] - ref) * kLog2e);
     };
-    constexpr int kAhead = 4;   // chunks requested at once
+    constexpr int kAhead = sizeof(T) == 2 ? 8 : 4;   // chunks requested at once: 64 KiB and more of a CU's waves
     int c = tid;
     for (; c + (kAhead - 1) * TH < full; c += kAhead * TH) {
         Raw<T> r[kAhead];
@@ -176,16 +182,17 @@ struct GradArgs {
     int32_t start[kAnswers + 1];   // first row of each answer
 };
 
-// sum over rows lo..hi of log p_policy - log p_reference: every lane of the wave gets it
-template <typename T>
+// Sum over rows lo .. hi - 1 of ln p_policy - ln p_reference, by WIDTH lanes that all get it.
+template <int WIDTH, typename T>
 __device__ __forceinline__ double answer_ratio(const GradArgs<T>& a, int lo, int hi) {
     double r = 0.0;
-    for (int i = lo + (threadIdx.x & 63); i < hi; i += 64) {
+    for (int i = lo + (int)(threadIdx.x % WIDTH); i < hi; i += WIDTH) {
         const int t = a.target[i];
-        if (t >= 0 && t < a.vocab) r += a.stat[i].logp - (a.ref_logp ? (double)a.ref_logp[i] : a.stat[a.n + i].logp);
+        const double p = a.stat[i].logp, q = a.ref_logp ? (double)a.ref_logp[i] : a.stat[a.n + i].logp;
+        r += t >= 0 && t < a.vocab ? p - q : 0.0;
     }
 #pragma unroll
-    for (int d = 1; d < 64; d *= 2) r += __shfl_xor(r, d);
+    for (int d = 1; d < WIDTH; d *= 2) r += __shfl_xor(r, d);
     return r;
 }
 // ln(1 / (1 + e^-h))
@@ -194,27 +201,29 @@ __device__ __forceinline__ double sigmoid(double h) { return 1.0 / (1.0 + exp(-h
 
 template <typename T, int TH>
 __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (blockIdx.x == 0) {   // the loss
-        __shared__ double sums[TH / 64][3];
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (blockIdx.x == 0) {   // the loss: eight lanes a pair
+        constexpr int WIDTH = 8, GROUPS = TH / WIDTH;
+        __shared__ double sums[GROUPS][3];
+        const int group = tid / WIDTH;
         double loss = 0.0, margin = 0.0, won = 0.0;
-        for (int p = wave; p < a.pairs; p += TH / 64) {
-            const double good = answer_ratio(a, a.start[2 * p], a.start[2 * p + 1]);
-            const double poor = answer_ratio(a, a.start[2 * p + 1], a.start[2 * p + 2]);
+        for (int p = group; p < a.pairs; p += GROUPS) {
+            const double good = answer_ratio<WIDTH>(a, a.start[2 * p], a.start[2 * p + 1]);
+            const double poor = answer_ratio<WIDTH>(a, a.start[2 * p + 1], a.start[2 * p + 2]);
             const double h = a.beta * (good - poor);
             loss -= (1.0 - a.smoothing) * log_sigmoid(h) + a.smoothing * log_sigmoid(-h);
             margin += h;
             won += h > 0.0 ? 1.0 : 0.0;
-            if (a.ratios && lane == 0) {
+            if (a.ratios && tid % WIDTH == 0) {
                 a.ratios[2 * p] = (float)good;
                 a.ratios[2 * p + 1] = (float)poor;
             }
         }
-        if (lane == 0) sums[wave][0] = loss, sums[wave][1] = margin, sums[wave][2] = won;
+        if (tid % WIDTH == 0) sums[group][0] = loss, sums[group][1] = margin, sums[group][2] = won;
         __syncthreads();
         if (tid < 3) {
             double t = 0.0;
-            for (int w = 0; w < TH / 64; ++w) t += sums[w][tid];
+            for (int w = 0; w < GROUPS && w < a.pairs; ++w) t += sums[w][tid];
             a.losses[tid] = (float)(t / a.pairs);
         }
         return;
@@ -223,7 +232,7 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
     const int target = a.target[row];
     T* g = a.grad + row * a.stride;
     const int chunks = (int)(a.stride / kChunk);
-    float slope = 0.f, m = 0.f, inv = 0.f;
+    float slope = 0.f, ref = 0.f, inv = 0.f;
     if (target >= 0 && target < a.vocab) {
         // the row's answer: as many answers start at or before it, less one
         int before = 0;
@@ -231,13 +240,13 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
         const int answer = before - 1, p = answer / 2;
-        const double good = answer_ratio(a, a.start[2 * p], a.start[2 * p + 1]);
-        const double poor = answer_ratio(a, a.start[2 * p + 1], a.start[2 * p + 2]);
+        const double good = answer_ratio<64>(a, a.start[2 * p], a.start[2 * p + 1]);
+        const double poor = answer_ratio<64>(a, a.start[2 * p + 1], a.start[2 * p + 2]);
         const double h = a.beta * (good - poor);
         // -dL/d(good): L falls as the chosen answer's ratio grows
         const double c = a.beta * ((1.0 - a.smoothing) * sigmoid(-h) - a.smoothing * sigmoid(h)) / a.pairs;
         slope = (float)(answer & 1 ? -c : c);
-        m = a.stat[row].m;
+        ref = a.stat[row].m;
         inv = slope / a.stat[row].z;
     }
     const T* x = a.x + row * a.stride;
@@ -248,7 +257,7 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
 #pragma unroll
         for (int e = 0; e < kChunk; ++e) {
             const int i = c * kChunk + e;
-            v[e] = inv * exp2_((v[e] - m) * kLog2e);
+            v[e] = inv * exp2_((v[e] - ref) * kLog2e);
             if (i == target) v[e] -= slope;
             if (slope == 0.f || i >= a.vocab) v[e] = 0.f;
         }
@@ -409,7 +418,7 @@ extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* an
         for (int i = 0; i < 2 * n_pairs; ++i) a.start[i + 1] = a.start[i] + answer_rows[i];
         const dim3 grid(grad ? (uint32_t)n + 1 : 1);
         const int chunks = p->vocab / kChunk;
-        if (n < 4 * p->cus && chunks >= 1024) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
+        if (!grad || (n < 4 * p->cus && chunks >= 1024)) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
         else hipLaunchKernelGGL((prefer_grad_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
         return hipGetLastError();
     };

@@ -36,6 +36,7 @@ struct RopeArgs {
     void* out[2];
     int64_t in_stride[2], out_stride[2];   // elements between rows
     int32_t heads0, heads;                 // heads of the queries, of both
+    uint64_t inv_heads;                    // ceil(2^32 / heads)
     int32_t n, rows;                       // rows, rows of a workgroup
     int32_t part2, half;                   // r / 2; pairs (i, i + r/2) or (2i, 2i + 1)
     float m, sign;
@@ -92,29 +93,42 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     }
     __syncthreads();
     constexpr int U = D / (2 * kPairs);   // units of a head
-    const int per_row = a.heads * U, rotated = a.part2 / kPairs;
-    for (int k = tid; k < rows * per_row; k += kThreads) {
-        const int r = k / per_row, h = k % per_row / U, u = k % U;
-        const int which = h >= a.heads0;
-        const int64_t row = row0 + r;
+    const int rotated = a.part2 / kPairs, u = tid % U;
+    // the unit's two chunks of 8 elements
+    const bool turn = u < rotated;
+    const int c0 = turn && a.half ? kPairs * u : 2 * kPairs * u;
+    const int c1 = turn && a.half ? c0 + a.part2 : c0 + kPairs;
+    const int all = rows * a.heads;       // heads of all rows
+    constexpr int STEP = kThreads / U;
+    struct Unit {
+        float x[8], y[8];
+        T* out;
+        int row;
+        bool here;
+    };
+    auto load = [&](Unit& t, int k) {
+        t.here = k < all;
+        if (!t.here) return;
+        t.row = (int)((uint64_t)(uint32_t)k * a.inv_heads >> 32);
+        const int h = k - t.row * a.heads, which = h >= a.heads0;
+        const int64_t row = row0 + t.row;
         const int head = (h - (which ? a.heads0 : 0)) * D;
         const T* in = static_cast<const T*>(a.in[which]) + row * a.in_stride[which] + head;
-        T* out = static_cast<T*>(a.out[which]) + row * a.out_stride[which] + head;
-        // where the unit's two chunks of 8 elements are
-        const bool turn = u < rotated;
-        const int c0 = turn && a.half ? kPairs * u : 2 * kPairs * u;
-        const int c1 = turn && a.half ? c0 + a.part2 : c0 + kPairs;
-        float x[8], y[8], p[8], q[8];
-        load8(in + c0, x);
-        load8(in + c1, y);
+        t.out = static_cast<T*>(a.out[which]) + row * a.out_stride[which] + head;
+        if (!turn && in == t.out) t.here = false;
+        load8(in + c0, t.x);
+        load8(in + c1, t.y);
+    };
+    auto finish = [&](Unit& t) {
+        if (!t.here) return;
+        const float(&x)[8] = t.x, (&y)[8] = t.y;
         if (!turn) {
-            if (in != out) {
-                store8(out + c0, x);
-                store8(out + c1, y);
-            }
-            continue;
+            store8(t.out + c0, x);
+            store8(t.out + c1, y);
+            return;
         }
-        const float2* cs = &s_cs[r][kPairs * u];
+        float p[8], q[8];
+        const float2* cs = &s_cs[t.row][kPairs * u];
         if (a.half) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -131,8 +145,17 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 q[2 * e + 1] = y[2 * e + 1] * g.x + y[2 * e] * g.y;
             }
         }
-        store8(out + c0, p);
-        store8(out + c1, q);
+        store8(t.out + c0, p);
+        store8(t.out + c1, q);
+    };
+    // a unit's loads are under way while another is finished (in place, a unit's elements are its own)
+    Unit a0, a1;
+    load(a0, tid / U);
+    for (int k = tid / U; k < all; k += 2 * STEP) {
+        load(a1, k + STEP);
+        finish(a0);
+        load(a0, k + 2 * STEP);
+        finish(a1);
     }
 }
 
@@ -259,6 +282,7 @@ extern "C" int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, i
     a.out_stride[0] = q_out_stride, a.out_stride[1] = k_out_stride;
     a.heads0 = q_heads;
     a.heads = q_heads + k_heads;
+    a.inv_heads = ((1ull << 32) + a.heads - 1) / a.heads;
     a.n = n_rows;
     a.part2 = r->part / 2;
     a.half = r->cfg.layout == A2T_ROPE_HALF;
