@@ -23,6 +23,9 @@ namespace {
 constexpr int kChunk = 8;             // elements of a chunk (16 bytes of bf16, 32 of fp32)
 constexpr int kMaxPairs = A2T_PREFER_MAX_PAIRS;
 constexpr int kAnswers = 2 * kMaxPairs;
+// Policy logits that the gradient still finds in the caches when it comes back to them, last rows
+// first (the memory-side cache holds 256 MiB).
+constexpr int64_t kKeepBytes = 160ll << 20;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -37,12 +40,19 @@ template <> struct Raw<bf16_t> {
 template <> struct Raw<float> {
     u32x4 a, b;
 };
-__device__ __forceinline__ Raw<bf16_t> load_raw(const bf16_t* row, int c) {
-    return {reinterpret_cast<const u32x4*>(row)[c]};
+// STREAM: past the caches (what will not be read again before it would be pushed out)
+template <bool STREAM>
+__device__ __forceinline__ u32x4 load16(const u32x4* p) {
+    return STREAM ? __builtin_nontemporal_load(p) : *p;
 }
+template <bool STREAM>
+__device__ __forceinline__ Raw<bf16_t> load_raw(const bf16_t* row, int c) {
+    return {load16<STREAM>(reinterpret_cast<const u32x4*>(row) + c)};
+}
+template <bool STREAM>
 __device__ __forceinline__ Raw<float> load_raw(const float* row, int c) {
     const u32x4* p = reinterpret_cast<const u32x4*>(row) + 2 * c;
-    return {p[0], p[1]};
+    return {load16<STREAM>(p), load16<STREAM>(p + 1)};
 }
 __device__ __forceinline__ void unpack(const Raw<bf16_t>& r, float (&x)[kChunk]) {
 #pragma unroll
@@ -63,8 +73,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const bf16x2 v = {(__bf16)a, (__bf16)b};   // round to nearest even, once per output
     return __builtin_bit_cast(uint32_t, v);
 }
+// (The gradient is stored past the caches: written through them, 389 MB of it in a step of 1,440 rows
+// x 151,938 logits cost that pass and the next step's first reads 55 of 335 us.)
 __device__ __forceinline__ void store_chunk(bf16_t* row, int c, const float (&x)[kChunk]) {
-    reinterpret_cast<u32x4*>(row)[c] = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+    __builtin_nontemporal_store((u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}),
+                                reinterpret_cast<u32x4*>(row) + c);
 }
 __device__ __forceinline__ void store_chunk(float* row, int c, const float (&x)[kChunk]) {
     u32x4 a, b;
@@ -73,7 +86,7 @@ __device__ __forceinline__ void store_chunk(float* row, int c, const float (&x)[
         a[e] = __float_as_uint(x[e]);
         b[e] = __float_as_uint(x[4 + e]);
     }
-    reinterpret_cast<u32x4*>(row)[2 * c] = a;
+    reinterpret_cast<u32x4*>(row)[2 * c] = a;   // half of a lane's 32 bytes each: through the caches
     reinterpret_cast<u32x4*>(row)[2 * c + 1] = b;
 }
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -105,6 +118,7 @@ struct RowsArgs {
     RowStat* stat;            // [2][n] out, or null
     float* logp;              // [n] out, or null
     int32_t n, vocab;
+    int32_t stream;           // policy rows before this one are streamed, and all of the reference's
 };
 
 template <typename T, int TH>
@@ -137,23 +151,28 @@ __global__ __launch_bounds__(TH) void prefer_rows_kernel(RowsArgs<T> a) {
         for (int e = 0; e < kChunk; ++e) s.z += exp2_((v[e] - ref) * kLog2e);
     };
     constexpr int kAhead = sizeof(T) == 2 ? 8 : 4;   // chunks requested at once: 64 KiB and more of a CU's waves
-    int c = tid;
-    for (; c + (kAhead - 1) * TH < full; c += kAhead * TH) {
-        Raw<T> r[kAhead];
+    auto sweep = [&](auto stream) {
+        constexpr bool STREAM = decltype(stream)::value;
+        int c = tid;
+        for (; c + (kAhead - 1) * TH < full; c += kAhead * TH) {
+            Raw<T> r[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) r[k] = load_raw(x, c + k * TH);
+            for (int k = 0; k < kAhead; ++k) r[k] = load_raw<STREAM>(x, c + k * TH);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
+            for (int k = 0; k < kAhead; ++k) {
+                float v[kChunk];
+                unpack(r[k], v);
+                add(v);
+            }
+        }
+        for (; c < full; c += TH) {
             float v[kChunk];
-            unpack(r[k], v);
+            unpack(load_raw<STREAM>(x, c), v);
             add(v);
         }
-    }
-    for (; c < full; c += TH) {
-        float v[kChunk];
-        unpack(load_raw(x, c), v);
-        add(v);
-    }
+    };
+    if (which || row < a.stream) sweep(std::true_type{});
+    else sweep(std::false_type{});
     if (tid < a.vocab - full * kChunk) s = join(s, {value(x, full * kChunk + tid), 1.f});
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) s = join(s, {__shfl_xor(s.m, d), __shfl_xor(s.z, d)});
@@ -178,6 +197,7 @@ struct GradArgs {
     float* losses;            // [3]
     float* ratios;            // [2 pairs], or null
     int32_t n, vocab, pairs;
+    int32_t stream;           // rows before this one are streamed
     float beta, smoothing;
     int32_t start[kAnswers + 1];   // first row of each answer
 };
@@ -264,15 +284,20 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
         store_chunk(g, c, v);
     };
     constexpr int kAhead = 4;
-    int c = tid;
-    for (; c + (kAhead - 1) * TH < used; c += kAhead * TH) {
-        Raw<T> r[kAhead];
+    auto sweep = [&](auto stream) {
+        constexpr bool STREAM = decltype(stream)::value;
+        int c = tid;
+        for (; c + (kAhead - 1) * TH < used; c += kAhead * TH) {
+            Raw<T> r[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) r[k] = load_raw(x, c + k * TH);
+            for (int k = 0; k < kAhead; ++k) r[k] = load_raw<STREAM>(x, c + k * TH);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) write(c + k * TH, r[k]);
-    }
-    for (; c < used; c += TH) write(c, load_raw(x, c));
+            for (int k = 0; k < kAhead; ++k) write(c + k * TH, r[k]);
+        }
+        for (; c < used; c += TH) write(c, load_raw<STREAM>(x, c));
+        return c;
+    };
+    int c = row < a.stream ? sweep(std::true_type{}) : sweep(std::false_type{});
     for (; c < chunks; c += TH) {
         const float zero[kChunk] = {};
         store_chunk(g, c, zero);
@@ -304,16 +329,20 @@ struct a2t_prefer {
 
 namespace {
 
+// 1,024 threads a row instead of 256: where rows are long (1,440 gradient rows of 151,938 bf16 logits:
+// 147 against 156 us), or where they alone do not fill the CUs.
+bool wide_rows(const a2t_prefer* p, int64_t rows) {
+    const int chunks = p->vocab / kChunk;
+    return chunks >= 8192 || (rows < 4 * p->cus && chunks >= 1024);
+}
 // Row statistics of the policy's rows and, with `reference`, of the reference's behind them.
 template <typename T>
 hipError_t launch_rows(a2t_prefer* p, int n, const void* policy, int64_t ps, const void* reference, int64_t rs, const int32_t* target,
-                       RowStat* stat, float* logp) {
-    RowsArgs<T> a{{static_cast<const T*>(policy), static_cast<const T*>(reference)}, {ps, rs}, target, stat, logp, n, p->vocab};
+                       RowStat* stat, float* logp, int stream) {
+    RowsArgs<T> a{{static_cast<const T*>(policy), static_cast<const T*>(reference)}, {ps, rs}, target, stat, logp, n, p->vocab, stream};
     const int64_t rows = reference ? 2 * (int64_t)n : n;
-    const int chunks = p->vocab / kChunk;
     const dim3 grid((uint32_t)rows);
-    // more threads a row where the rows alone do not fill the CUs
-    if (rows < 4 * p->cus && chunks >= 1024) hipLaunchKernelGGL((prefer_rows_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
+    if (wide_rows(p, rows)) hipLaunchKernelGGL((prefer_rows_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
     else hipLaunchKernelGGL((prefer_rows_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
     return hipGetLastError();
 }
@@ -369,8 +398,8 @@ extern "C" int a2t_prefer_logp(a2t_prefer* p, int32_t n_rows, const void* logits
         misaligned(logits, 16) || misaligned(target, 4) || misaligned(logp, 4))
         return A2T_ERR_INVALID;
     DevGuard g(p->device);
-    const hipError_t e = p->dtype == A2T_F32 ? launch_rows<float>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp)
-                                             : launch_rows<bf16_t>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp);
+    const hipError_t e = p->dtype == A2T_F32 ? launch_rows<float>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp, 0)
+                                             : launch_rows<bf16_t>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp, 0);
     if (e != hipSuccess) {
         p->poisoned = true;
         return A2T_ERR_HIP;
@@ -399,7 +428,9 @@ extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* an
     DevGuard g(p->device);
     auto go = [&](auto* type) {
         using T = std::remove_pointer_t<decltype(type)>;
-        hipError_t e = launch_rows<T>(p, (int)n, policy, policy_stride, reference, reference_stride, target, p->stat, nullptr);
+        const int64_t keep = kKeepBytes / (policy_stride * (int64_t)sizeof(T));
+        const int stream = n > keep ? (int)(n - keep) : 0;
+        hipError_t e = launch_rows<T>(p, (int)n, policy, policy_stride, reference, reference_stride, target, p->stat, nullptr, stream);
         if (e != hipSuccess) return e;
         GradArgs<T> a{};
         a.x = static_cast<const T*>(policy);
@@ -411,14 +442,14 @@ extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* an
         a.losses = losses;
         a.ratios = ratios;
         a.n = (int32_t)n;
+        a.stream = stream;
         a.vocab = p->vocab;
         a.pairs = n_pairs;
         a.beta = beta;
         a.smoothing = smoothing;
         for (int i = 0; i < 2 * n_pairs; ++i) a.start[i + 1] = a.start[i] + answer_rows[i];
         const dim3 grid(grad ? (uint32_t)n + 1 : 1);
-        const int chunks = p->vocab / kChunk;
-        if (!grad || (n < 4 * p->cus && chunks >= 1024)) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
+        if (!grad || wide_rows(p, n)) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
         else hipLaunchKernelGGL((prefer_grad_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
         return hipGetLastError();
     };

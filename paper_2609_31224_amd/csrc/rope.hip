@@ -17,12 +17,15 @@
 #include <cmath>
 #include <cstdint>
 #include <new>
+#include <type_traits>
 
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kPairs = 8;         // pairs of a unit of work (16 elements)
 constexpr int kMaxRows = 8;       // most rows of a workgroup
+// Outputs larger than the L2 caches (32 MiB together) are stored past them (16,384 rows of 40 bf16
+// heads: 70 us; 52 so, and 59 where loads go past them instead).
+constexpr int64_t kStreamBytes = 32 << 20;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 struct bf16_t {
@@ -42,8 +45,8 @@ struct RopeArgs {
     float m, sign;
 };
 
-// 8 elements
-__device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
+// the elements of 16 bytes
+__device__ __forceinline__ void load(const bf16_t* p, float (&x)[8]) {
     const u32x4 w = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -51,34 +54,31 @@ __device__ __forceinline__ void load8(const bf16_t* p, float (&x)[8]) {
         x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
 }
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-    const u32x4 a = reinterpret_cast<const u32x4*>(p)[0], b = reinterpret_cast<const u32x4*>(p)[1];
+__device__ __forceinline__ void load(const float* p, float (&x)[4]) {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(p);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        x[e] = __uint_as_float(a[e]);
-        x[4 + e] = __uint_as_float(b[e]);
-    }
+    for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(w[e]);
 }
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
     typedef __attribute__((__vector_size__(2 * sizeof(__bf16)))) __bf16 bf16x2;
     const bf16x2 v = {(__bf16)a, (__bf16)b};   // round to nearest even, once per output
     return __builtin_bit_cast(uint32_t, v);
 }
-__device__ __forceinline__ void store8(bf16_t* p, const float (&x)[8]) {
-    *reinterpret_cast<u32x4*>(p) = u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])};
+template <bool STREAM>
+__device__ __forceinline__ void store16(void* p, const u32x4& x) {
+    if (STREAM) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(p));
+    else *reinterpret_cast<u32x4*>(p) = x;
 }
-__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
-    u32x4 a, b;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        a[e] = __float_as_uint(x[e]);
-        b[e] = __float_as_uint(x[4 + e]);
-    }
-    reinterpret_cast<u32x4*>(p)[0] = a;
-    reinterpret_cast<u32x4*>(p)[1] = b;
+template <bool STREAM>
+__device__ __forceinline__ void store(bf16_t* p, const float (&x)[8]) {
+    store16<STREAM>(p, u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])});
+}
+template <bool STREAM>
+__device__ __forceinline__ void store(float* p, const float (&x)[4]) {
+    store16<STREAM>(p, u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])});
 }
 
-template <typename T, int D>
+template <typename T, int D, bool STREAM>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     __shared__ __align__(16) float2 s_cs[kMaxRows][D / 2];
     const int tid = threadIdx.x, row0 = blockIdx.x * a.rows, rows = min(a.rows, a.n - row0);
@@ -92,21 +92,24 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         s_cs[r][i] = make_float2(a.m * c, a.sign * a.m * s);
     }
     __syncthreads();
-    constexpr int U = D / (2 * kPairs);   // units of a head
-    const int rotated = a.part2 / kPairs, u = tid % U;
-    // the unit's two chunks of 8 elements
-    const bool turn = u < rotated;
-    const int c0 = turn && a.half ? kPairs * u : 2 * kPairs * u;
-    const int c1 = turn && a.half ? c0 + a.part2 : c0 + kPairs;
+    // A unit is two chunks of 16 bytes, P elements each.  Lanes next to each other take chunks next to
+    // each other, so that every access is whole lines.
+    constexpr int P = 16 / (int)sizeof(T), U = D / (2 * P);   // units of a head
+    const int u = tid % U, part = 2 * a.part2, rest = (D - part) / 2;
+    const bool both = a.half && u < a.part2 / P;              // half layout: the chunks are each other's partners
+    const int c0 = !a.half || both ? P * u : part + P * u - a.part2;
+    const int c1 = c0 + (!a.half ? D / 2 : both ? a.part2 : rest);
+    // pairs layout: each chunk has its own pairs, or none
+    const bool turn0 = !a.half && c0 < part, turn1 = !a.half && c1 < part, moves = both || turn0 || turn1;
     const int all = rows * a.heads;       // heads of all rows
     constexpr int STEP = kThreads / U;
     struct Unit {
-        float x[8], y[8];
+        float x[P], y[P];
         T* out;
         int row;
         bool here;
     };
-    auto load = [&](Unit& t, int k) {
+    auto fetch = [&](Unit& t, int k) {
         t.here = k < all;
         if (!t.here) return;
         t.row = (int)((uint64_t)(uint32_t)k * a.inv_heads >> 32);
@@ -115,46 +118,44 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
         const int head = (h - (which ? a.heads0 : 0)) * D;
         const T* in = static_cast<const T*>(a.in[which]) + row * a.in_stride[which] + head;
         t.out = static_cast<T*>(a.out[which]) + row * a.out_stride[which] + head;
-        if (!turn && in == t.out) t.here = false;
-        load8(in + c0, t.x);
-        load8(in + c1, t.y);
+        if (!moves && in == t.out) t.here = false;
+        load(in + c0, t.x);
+        load(in + c1, t.y);
     };
     auto finish = [&](Unit& t) {
         if (!t.here) return;
-        const float(&x)[8] = t.x, (&y)[8] = t.y;
-        if (!turn) {
-            store8(t.out + c0, x);
-            store8(t.out + c1, y);
+        if (both) {
+            float p[P], q[P];
+            const float2* cs = &s_cs[t.row][P * u];
+#pragma unroll
+            for (int e = 0; e < P; ++e) {
+                p[e] = t.x[e] * cs[e].x - t.y[e] * cs[e].y;
+                q[e] = t.y[e] * cs[e].x + t.x[e] * cs[e].y;
+            }
+            store<STREAM>(t.out + c0, p);
+            store<STREAM>(t.out + c1, q);
             return;
         }
-        float p[8], q[8];
-        const float2* cs = &s_cs[t.row][kPairs * u];
-        if (a.half) {
+        auto pairs = [&](float (&x)[P], const float2* cs) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                p[e] = x[e] * cs[e].x - y[e] * cs[e].y;
-                q[e] = y[e] * cs[e].x + x[e] * cs[e].y;
+            for (int e = 0; e < P / 2; ++e) {
+                const float a = x[2 * e], b = x[2 * e + 1];
+                x[2 * e] = a * cs[e].x - b * cs[e].y;
+                x[2 * e + 1] = b * cs[e].x + a * cs[e].y;
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 f = cs[e], g = cs[4 + e];
-                p[2 * e] = x[2 * e] * f.x - x[2 * e + 1] * f.y;
-                p[2 * e + 1] = x[2 * e + 1] * f.x + x[2 * e] * f.y;
-                q[2 * e] = y[2 * e] * g.x - y[2 * e + 1] * g.y;
-                q[2 * e + 1] = y[2 * e + 1] * g.x + y[2 * e] * g.y;
-            }
-        }
-        store8(t.out + c0, p);
-        store8(t.out + c1, q);
+        };
+        if (turn0) pairs(t.x, &s_cs[t.row][c0 / 2]);
+        if (turn1) pairs(t.y, &s_cs[t.row][c1 / 2]);
+        store<STREAM>(t.out + c0, t.x);
+        store<STREAM>(t.out + c1, t.y);
     };
     // a unit's loads are under way while another is finished (in place, a unit's elements are its own)
     Unit a0, a1;
-    load(a0, tid / U);
+    fetch(a0, tid / U);
     for (int k = tid / U; k < all; k += 2 * STEP) {
-        load(a1, k + STEP);
+        fetch(a1, k + STEP);
         finish(a0);
-        load(a0, k + 2 * STEP);
+        fetch(a0, k + 2 * STEP);
         finish(a1);
     }
 }
@@ -293,13 +294,14 @@ extern "C" int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, i
     while (a.rows < kMaxRows && (int64_t)n_rows >= (int64_t)a.rows * 2 * 4 * r->cus) a.rows *= 2;
     const dim3 grid((n_rows + a.rows - 1) / a.rows);
     auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, r->stream, a); };
-    if (r->cfg.dtype == A2T_F32) {
-        if (D == 64) go(rope_kernel<float, 64>);
-        else go(rope_kernel<float, 128>);
-    } else {
-        if (D == 64) go(rope_kernel<bf16_t, 64>);
-        else go(rope_kernel<bf16_t, 128>);
-    }
+    const bool stream = (int64_t)n_rows * a.heads * D * size > kStreamBytes;
+    auto typed = [&](auto* type) {
+        using T = std::remove_pointer_t<decltype(type)>;
+        if (D == 64) stream ? go(rope_kernel<T, 64, true>) : go(rope_kernel<T, 64, false>);
+        else stream ? go(rope_kernel<T, 128, true>) : go(rope_kernel<T, 128, false>);
+    };
+    if (r->cfg.dtype == A2T_F32) typed((float*)nullptr);
+    else typed((bf16_t*)nullptr);
     if (hipGetLastError() != hipSuccess) {
         r->poisoned = true;
         return A2T_ERR_HIP;
