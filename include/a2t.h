@@ -665,7 +665,14 @@ typedef struct a2t_prompt a2t_prompt;
  * n_q_heads a multiple of n_kv_heads, at most 128 times as many; head_dim 64 or
  * 128; dtype A2T_F32 or A2T_BF16; attn_scale 0 selects 1/sqrt(head_dim),
  * otherwise within [1e-6, 1e6].  Allocates 4 n_q_heads bytes a row and, with
- * A2T_PROMPT_UNTIL, K's and V's bytes and 20 more.  Errors: INVALID, OOM, NODEV. */
+ * A2T_PROMPT_UNTIL, K's and V's bytes and 20 more, and at most 130 MiB for sums of
+ * split blocks.  Tuning read from the environment at creation (for tests and
+ * measurements; results stay within their tolerances whatever they are):
+ *   A2T_PROMPT_SORT    rows of the longest sequence from which keys that expire are
+ *                      sorted before attention (default 512)
+ *   A2T_PROMPT_SPLITS  1..16: workgroups that the keys (or queries) of a block are
+ *                      split over (0 = planned)
+ * Errors: INVALID, OOM, NODEV. */
 int a2t_prompt_create(int32_t max_rows, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                       double attn_scale, uint32_t flags, int32_t device, void* hip_stream, a2t_prompt** out);
 /* Waits for the stream, then frees the handle. */

@@ -8,9 +8,15 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <cstdlib>
 #include <new>
 
 using namespace a2t::prompt;
+
+namespace {
+constexpr int kTileRows = 64;
+constexpr int kSortRows = 512;                  // rows of the longest sequence from which keys that expire are sorted
+}  // namespace
 
 struct a2t_prompt {
     int32_t max_rows = 0, Hq = 0, Hkv = 0, D = 0, dtype = 0, device = 0;
@@ -28,6 +34,8 @@ struct a2t_prompt {
     int32_t* first = nullptr;
     int32_t* reach = nullptr;
     bool until = false;
+    int sort_rows = kSortRows;   // A2T_PROMPT_SORT
+    int force_splits = 0;        // A2T_PROMPT_SPLITS
     bool poisoned = false;
 };
 
@@ -44,13 +52,17 @@ struct DevGuard {
     }
 };
 
+int env_int(const char* name, int dflt) {
+    const char* v = std::getenv(name);
+    return (v && *v) ? std::atoi(v) : dflt;
+}
+
 void free_prompt(a2t_prompt* p) {
     for (void* m : {(void*)p->delta, p->k, p->v, (void*)p->meta, (void*)p->lasting, (void*)p->first, (void*)p->reach, (void*)p->part})
         if (m) (void)hipFree(m);
     delete p;
 }
 
-constexpr int kTileRows = 64;
 constexpr int kSplitSeqs = 64;                   // launches of more sequences are not split
 constexpr int64_t kPartRows = 1 << 18;           // most (row, head, split) triples of split sums (130 MiB of 128 dimensions)
 
@@ -105,11 +117,18 @@ int place_blocks(SeqTable<kMaxSeqs>& t, F&& rows_of) {
     return (int)blocks;
 }
 
+// Whether keys that expire are sorted first: two launches and a copy of K and V against the pairs
+// that nobody sees.
+bool sort_pays(const a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows) {
+    return *std::max_element(seq_rows, seq_rows + n_seqs) >= p->sort_rows;
+}
+
 Args base_args(const a2t_prompt* p, int64_t total, const void* q, int64_t qs, const void* k, int64_t ks, const void* v, int64_t vs,
-               bool until) {
+               const int32_t* until, bool sorted) {
     Args a{};
     const int64_t own = (int64_t)p->Hkv * p->D;
-    a.kv = until ? KeyRows{p->k, p->v, own, own, p->meta, p->lasting, p->first} : KeyRows{k, v, ks, vs, nullptr, nullptr, nullptr};
+    a.kv = KeyRows{k, v, ks, vs, until, nullptr, nullptr, nullptr};
+    if (sorted) a.kv = KeyRows{p->k, p->v, own, own, until, p->meta, p->lasting, p->first};
     a.q = q;
     a.q_stride = qs;
     a.delta = p->delta;
@@ -153,12 +172,13 @@ int splits_for(const a2t_prompt* p, const SeqTable<kMaxSeqs>& t, int kernel, int
         work += blocks * (tiles + 1) / 2;
         longest = std::max(longest, tiles);
     }
+    if (p->force_splits) return (int)std::max<int64_t>(1, std::min<int64_t>(p->force_splits, p->part_rows / (total * heads)));
     int best = 1;
     double least = 0.0;
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
         if (s > 1 && (s > longest || s * total * heads > p->part_rows)) break;
         const double tiles = std::max((double)((longest + s - 1) / s), (double)work / slots);
-        const double join = s > 1 ? 4.0 + (double)(s * total * heads) * p->D * 8 / 3e6 : 0.0;
+        const double join = s > 1 ? 4.0 + (double)(s * total * heads) * p->D * 8 / 8e6 : 0.0;
         const double us = tiles * c.tile + c.start * ((wgs * s + slots - 1) / slots) + join;
         if (s == 1 || us < least) best = s, least = us;
     }
@@ -197,6 +217,8 @@ extern "C" int a2t_prompt_create(int32_t max_rows, int32_t n_q_heads, int32_t n_
     p->until = flags & A2T_PROMPT_UNTIL;
     int cus = 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && cus > 0) p->cus = cus;
+    p->sort_rows = env_int("A2T_PROMPT_SORT", kSortRows);
+    p->force_splits = std::min(16, std::max(0, env_int("A2T_PROMPT_SPLITS", 0)));
     p->part_rows = std::min<int64_t>((int64_t)max_rows * n_q_heads * 16, kPartRows);
     const size_t rows = (size_t)max_rows, row = (size_t)n_kv_heads * head_dim * (dtype == A2T_F32 ? 4 : 2);
     bool ok = hipMalloc(&p->delta, rows * n_q_heads * sizeof(float)) == hipSuccess;
@@ -237,12 +259,13 @@ extern "C" int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq
         misaligned(o, 16) || misaligned(lse, 4) || misaligned(until, 4) || (until && !p->until))
         return A2T_ERR_INVALID;
     DevGuard g(p->device);
-    Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until != nullptr);
+    const bool sorted = until && sort_pays(p, n_seqs, seq_rows);
+    Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until, sorted);
     a.o = o;
     a.lse = lse;
     const Shape shape{p->dtype == A2T_F32, p->D};
     const hipError_t e = in_tables(n_seqs, seq_rows, [&](SeqTable<kMaxSeqs>& t) {
-        hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
+        hipError_t s = sorted ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
         if (s != hipSuccess) return s;
         const int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
         a.splits = splits_for(p, t, kForward, total);
@@ -266,7 +289,8 @@ extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t
         misaligned(dk, 16) || misaligned(dv, 16) || misaligned(until, 4) || (until && !p->until))
         return A2T_ERR_INVALID;
     DevGuard g(p->device);
-    Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until != nullptr);
+    const bool sorted = until && sort_pays(p, n_seqs, seq_rows);
+    Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until, sorted);
     a.o_in = o;
     a.d_o = d_o;
     a.lse = const_cast<float*>(lse);
@@ -275,7 +299,7 @@ extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t
     a.dv = dv;
     const Shape shape{p->dtype == A2T_F32, p->D};
     const hipError_t e = in_tables(n_seqs, seq_rows, [&](SeqTable<kMaxSeqs>& t) {
-        hipError_t s = until ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
+        hipError_t s = sorted ? sort_keys(p, t, until, k, k_stride, v, v_stride) : hipSuccess;
         if (s != hipSuccess) return s;
         int blocks = place_blocks(t, [&](int i) { return (int64_t)a.G * t.rows[i]; });
         a.splits = splits_for(p, t, kQueries, total);

@@ -26,13 +26,14 @@ struct SeqTable {
     int32_t rows[N];
 };
 
-// Keys and values as the kernels read them.  Without `meta`, row r of a sequence is its key r.
-// With it the rows are sorted (lasting keys first) and meta tells each one's place and the
-// first place that does not see it.
+// Keys and values as the kernels read them.  Row r of a sequence is its key r, expiring at `until`
+// if that is given, unless `meta` is: then the rows are sorted (lasting keys first) and meta tells
+// each one's place and the first place that does not see it.
 struct KeyRows {
     const void* k;
     const void* v;
     int64_t k_stride, v_stride;   // elements between rows
+    const int32_t* until;         // [rows] or null
     const int2* meta;             // [rows] (place, until) or null
     const int32_t* lasting;       // [rows] lasting keys at or before the place
     const int32_t* first;         // [rows] first passing key (in sorted order) that the place may still see

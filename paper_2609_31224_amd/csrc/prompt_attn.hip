@@ -26,13 +26,17 @@ struct Runs {
         *hi = end[second];
     }
 };
+// Place and `until` of row r of a sequence's keys as the kernels read them.
+__device__ __forceinline__ int2 key_place(const KeyRows& kv, int row0, int r) {
+    return kv.meta ? kv.meta[row0 + r] : make_int2(r, kv.until[row0 + r]);
+}
 template <bool UNTIL>
 __device__ __forceinline__ Runs key_runs(const KeyRows& kv, int row0, int n, int first, int last) {
     Runs r;
     r.start[0] = 0;
     r.end[0] = last + 1;
     r.start[1] = r.end[1] = 0;
-    if constexpr (UNTIL) {   // lasting keys, then the passing ones that some query may still see
+    if (UNTIL && kv.meta) {   // lasting keys, then the passing ones that some query may still see
         const int all = uniform(kv.lasting[row0 + n - 1]), seen = uniform(kv.lasting[row0 + last]);
         r.end[0] = seen;
         r.start[1] = all + uniform(kv.first[row0 + first]);
@@ -44,19 +48,21 @@ __device__ __forceinline__ Runs key_runs(const KeyRows& kv, int row0, int n, int
     return r;
 }
 
-// Which keys lo .. lo + 63 of a tile (up to hi) the rows at places first .. last of a wave see.
-enum class Sees { none, some, all };
+// Which of keys lo .. lo + 63 of a tile (up to hi) some row of a wave's at places first .. last sees,
+// by blocks of 32, and whether all rows see all of them.
+struct Sees {
+    bool block[2], all;
+};
 template <bool UNTIL>
 __device__ __forceinline__ Sees sees(const int2* meta, int lo, int hi, int first, int last) {
     if constexpr (UNTIL) {
         const int lane = threadIdx.x & 63;
         const int2 m = meta[lane];
         const bool in = lo + lane < hi;
-        if (!__any(in && m.x <= last && m.y > first)) return Sees::none;
-        return __all(in && m.x <= first && m.y > last) ? Sees::all : Sees::some;
+        const uint64_t some = __ballot(in && m.x <= last && m.y > first);
+        return {(uint32_t)some != 0, (some >> 32) != 0, (bool)__all(in && m.x <= first && m.y > last)};
     } else {
-        if (lo > last) return Sees::none;
-        return lo + kTile - 1 <= first ? Sees::all : Sees::some;
+        return {lo <= last, lo + 32 <= last, lo + kTile - 1 <= first};
     }
 }
 // Whether the query at place i sees key k of a tile.
@@ -67,7 +73,7 @@ __device__ __forceinline__ bool visible(const int2* meta, int lo, int hi, int k,
 }
 
 template <typename T, int D, bool UNTIL, int N>
-__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 128 ? 4 : sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
     constexpr int DB = Tl::DB;
     __shared__ __align__(1024) char s_k[2][Tl::BYTES];
@@ -101,7 +107,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
         const int stage = tile & 1;
         Coming<T, D>::rows(kp, a.kv.k_stride * sizeof(T), lo, n - 1, w, lds_address(s_k[stage]));
         Coming<T, D>::rows(vp, a.kv.v_stride * sizeof(T), lo, n - 1, w, lds_address(s_v[stage]));
-        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + min(lo + (int)threadIdx.x, n - 1)];
+        if (UNTIL && threadIdx.x < kTile) mm = key_place(a.kv, row0, min(lo + (int)threadIdx.x, n - 1));
     };
     auto store = [&](int stage) {
         if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
@@ -133,17 +139,19 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
         if (tile + 1 < t1) load(tile + 1);
         int lo, hi;
         runs.at(tile, &lo, &hi);
-        const Sees what = busy ? sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last) : Sees::none;
-        if (what != Sees::none) {
+        const Sees what = sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last);
+        if (busy && (what.block[0] || what.block[1])) {
             f32x16 s[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[b][e] = 0.f;
+                if (what.block[b]) {
 #pragma unroll
-                for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_k[stage], 32 * b + l32, k, h), qop[k], s[b]);
+                    for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_k[stage], 32 * b + l32, k, h), qop[k], s[b]);
+                }
             }
-            if (what == Sees::some) {
+            if (!what.all) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -170,7 +178,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
                     s[b][e] = exp2_(__builtin_fmaf(s[b][e], c, -mref));
                     sum += s[b][e];
                 }
-                mma_rows<D, T>(s_v[stage], 32 * b, s[b], acc);
+                if (what.block[b]) mma_rows<D, T>(s_v[stage], 32 * b, s[b], acc);
             }
         }
         if (tile + 1 < t1) store(stage ^ 1);
@@ -238,7 +246,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
         const int stage = tile & 1;
         Coming<T, D>::rows(kp, a.kv.k_stride * sizeof(T), lo, n - 1, w, lds_address(s_k[stage]));
         Coming<T, D>::rows(vp, a.kv.v_stride * sizeof(T), lo, n - 1, w, lds_address(s_v[stage]));
-        if (UNTIL && threadIdx.x < kTile) mm = a.kv.meta[row0 + min(lo + (int)threadIdx.x, n - 1)];
+        if (UNTIL && threadIdx.x < kTile) mm = key_place(a.kv, row0, min(lo + (int)threadIdx.x, n - 1));
     };
     auto store = [&](int stage) {
         if (UNTIL && threadIdx.x < kTile) s_meta[stage][threadIdx.x] = mm;
@@ -288,10 +296,11 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
         if (tile + 1 < t1) load(tile + 1);
         int lo, hi;
         runs.at(tile, &lo, &hi);
-        const Sees what = busy ? sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last) : Sees::none;
-        if (what != Sees::none) {
+        const Sees what = sees<UNTIL>(s_meta[stage], lo, hi, i_first, i_last);
+        if (busy) {
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
+                if (!what.block[b]) continue;
                 f32x16 s, p;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = p[e] = 0.f;
@@ -301,7 +310,7 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
                 for (int k = 0; k < Tl::STEPS; ++k) mma_step<T>(row_operand<T, D>(s_v[stage], 32 * b + l32, k, h), dop[k], p);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) p[e] = exp2_(__builtin_fmaf(s[e], c, -lse2)) * (p[e] - delta);
-                if (what == Sees::some) {
+                if (!what.all) {
 #pragma unroll
                     for (int e = 0; e < 16; ++e)
                         if (!visible<UNTIL>(s_meta[stage], lo, hi, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3), i)) p[e] = 0.f;
@@ -371,7 +380,7 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     // the lane's key: its place, and the first place that does not see it
     int2 me = {key, n};
     if constexpr (UNTIL) {
-        me = a.kv.meta[row0 + key];
+        me = key_place(a.kv, row0, key);
         me.y = min(me.y, n);
     }
     int j_min = me.x, j_max = me.x, u_min = me.y, u_max = me.y;
@@ -738,7 +747,7 @@ template <Kernel K>
 hipError_t launch(const Shape& s, const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
     auto typed = [&](auto* type) {
         using T = std::remove_pointer_t<decltype(type)>;
-        const bool u = a.kv.meta != nullptr;
+        const bool u = a.kv.until != nullptr;
         if (s.head_dim == 128) return u ? launch<K, T, 128, true>(a, t, blocks, stream) : launch<K, T, 128, false>(a, t, blocks, stream);
         if (s.head_dim == 64) return u ? launch<K, T, 64, true>(a, t, blocks, stream) : launch<K, T, 64, false>(a, t, blocks, stream);
         return hipErrorInvalidValue;

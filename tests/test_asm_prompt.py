@@ -112,7 +112,7 @@ def test_lds_reads_are_waited_for(kernels):
                 assert after is not None, (name, l)
                 queue = after
             todo += [(s, queue) for s in blocks[i][1]]
-        assert reads, name
+        assert reads or "prompt_join" in name or "prompt_add" in name, name
 
 
 def test_a_missing_wait_is_found():

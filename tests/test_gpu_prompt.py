@@ -104,10 +104,13 @@ SHAPES = [
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("until", [None, "evicted", "random"])
+@pytest.mark.parametrize("until", [None, "evicted", "random", "evicted sorted", "random sorted"])
 @pytest.mark.parametrize("lengths,hq,hkv,d", SHAPES)
-def test_against_oracle(gpu, lengths, hq, hkv, d, until, dtype):
+def test_against_oracle(gpu, monkeypatch, lengths, hq, hkv, d, until, dtype):
     import paper_2609_31224_amd as a2t
+    if until and until.endswith("sorted"):
+        monkeypatch.setenv("A2T_PROMPT_SORT", "1")
+        until = until.split()[0]
     q, k, v, do, ut = _case(lengths, hq, hkv, d, dtype, until, seed=len(lengths) + hq)
     h = a2t.a2t_prompt_create(sum(lengths), hq, hkv, d, a2t.A2T_F32 if dtype == "f32" else a2t.A2T_BF16,
                               flags=0 if until is None else a2t.A2T_PROMPT_UNTIL)
@@ -119,9 +122,12 @@ def test_against_oracle(gpu, lengths, hq, hkv, d, until, dtype):
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 @pytest.mark.parametrize("until", ["window", "nothing"])
-def test_other_masks(gpu, until, dtype, d):
-    """A sliding window, and rows that see nothing at all."""
+@pytest.mark.parametrize("sort,splits", [(512, 0), (1, 0), (1, 3), (512, 16)])
+def test_other_masks(gpu, monkeypatch, sort, splits, until, dtype, d):
+    """A sliding window, and rows that see nothing at all, with keys sorted or as they are and blocks split or not."""
     import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_PROMPT_SORT", str(sort))
+    monkeypatch.setenv("A2T_PROMPT_SPLITS", str(splits))
     lengths = [150, 1, 66]
     q, k, v, do, ut = _case(lengths, 4, 2, d, dtype, until)
     h = a2t.a2t_prompt_create(500, 4, 2, d, a2t.A2T_F32 if dtype == "f32" else a2t.A2T_BF16, flags=a2t.A2T_PROMPT_UNTIL)
@@ -143,6 +149,22 @@ def test_wide_groups_and_scales(gpu, groups, scale):
     h = a2t.a2t_prompt_create(64, groups, 1, 64, a2t.A2T_BF16, attn_scale=scale, flags=a2t.A2T_PROMPT_UNTIL)
     try:
         _check(_run(h, lengths, q, k, v, do, ut), lengths, q, k, v, do, ut, "bf16", scale or None)
+    finally:
+        a2t.a2t_prompt_destroy(h)
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("splits", [1, 2, 5, 16])
+def test_splits(gpu, monkeypatch, splits, dtype, d):
+    """Every number of splits, more than a block's tiles too: some have nothing to add."""
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_PROMPT_SPLITS", str(splits))
+    lengths = [230, 3, 64, 0, 129]
+    q, k, v, do, ut = _case(lengths, 6, 2, d, dtype, "evicted")
+    h = a2t.a2t_prompt_create(500, 6, 2, d, a2t.A2T_F32 if dtype == "f32" else a2t.A2T_BF16, flags=a2t.A2T_PROMPT_UNTIL)
+    try:
+        for until in (None, ut):
+            _check(_run(h, lengths, q, k, v, do, until), lengths, q, k, v, do, until, dtype)
     finally:
         a2t.a2t_prompt_destroy(h)
 
