@@ -177,9 +177,12 @@ int splits_for(const a2t_prompt* p, const SeqTable<kMaxSeqs>& t, int kernel, int
     double least = 0.0;
     for (int s : {1, 2, 3, 4, 6, 8, 12, 16}) {
         if (s > 1 && (s > longest || s * total * heads > p->part_rows)) break;
-        const double tiles = std::max((double)((longest + s - 1) / s), (double)work / slots);
+        const double most = (double)((longest + s - 1) / s);
+        const double tiles = std::max(most, (double)work / slots + 0.35 * most);   // the last ones end unevenly
+        // a CU's workgroups slow each other down: alone, one takes 0.55 of a tile's time
+        const double full = c.per_cu == 1 ? 1.0 : std::min(1.0, std::max(0.0, ((double)(wgs * s) / p->cus - 1.0) / (c.per_cu - 1)));
         const double join = s > 1 ? 4.0 + (double)(s * total * heads) * p->D * 8 / 8e6 : 0.0;
-        const double us = tiles * c.tile + c.start * ((wgs * s + slots - 1) / slots) + join;
+        const double us = tiles * c.tile * (0.55 + 0.45 * full) + c.start * ((wgs * s + slots - 1) / slots) + join;
         if (s == 1 || us < least) best = s, least = us;
     }
     return best;

@@ -73,7 +73,7 @@ __device__ __forceinline__ bool visible(const int2* meta, int lo, int hi, int k,
 }
 
 template <typename T, int D, bool UNTIL, int N>
-__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 128 ? 4 : sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 128 ? 3 : sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
     constexpr int DB = Tl::DB;
     __shared__ __align__(1024) char s_k[2][Tl::BYTES];
