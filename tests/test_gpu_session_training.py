@@ -1,0 +1,269 @@
+"""The operators for training on whole sessions as they are used: one after the other, and against the
+streaming cache that serves the same session.
+
+* A session served step by step under eviction and the same session attended at once with the `until`
+  that its evictions give agree within the cache's attention tolerance (2e-2 for bf16, 1e-4 for fp32,
+  as everywhere in these tests) and the oracle's bounds for the other side.
+* A cache created with A2T_FLAG_ROTATED holds rows as they come and attends to them as they are.
+* A training step (rotary encoding, attention, a projection to logits, a loss, and all gradients back) in
+  fp32 against torch's float64 autograd on the CPU.  Each stage is off by at most (terms of a sum) x 2^-24
+  of its norm, about 2e-5 for 300 terms; six stages follow each other: 2e-4 of each gradient's norm.
+"""
+import numpy as np
+import pytest
+
+from oracle.attention import attend
+from oracle.distill import distill_losses
+from oracle.prompt import prompt_attention
+from oracle.rope_forms import frequencies
+
+pytestmark = pytest.mark.gpu
+
+SEG_ACOUSTIC, SEG_DELIM, SEG_TEXT = 1, 2, 3
+
+
+def _units(rng, n):
+    """Classes of the rows of n listening units."""
+    return [[SEG_ACOUSTIC] * 17 + [SEG_DELIM] + [SEG_TEXT] * int(rng.poisson(3)) + [SEG_DELIM] for _ in range(n)]
+
+
+def _f64(x):
+    return x.detach().cpu().double().numpy()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("sort", [1, 100000])
+def test_session_as_served(gpu, monkeypatch, dtype, sort):
+    import torch
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_PROMPT_SORT", str(sort))
+    rng = np.random.default_rng(4)
+    hq, hkv, d, budget, window = 4, 2, 64, 150, 3
+    units = _units(rng, 25)
+    n = sum(map(len, units))
+    dt, code = (torch.float32, a2t.A2T_F32) if dtype == "f32" else (torch.bfloat16, a2t.A2T_BF16)
+    both = torch.from_numpy(rng.standard_normal((n, hq + 2 * hkv, d)).astype(np.float32)).to("cuda").to(dt)
+    pos = np.arange(n, dtype=np.int32) + 70000
+    # long contexts: positions that the caches' own encoding does not scale
+    rope = a2t.a2t_rope_create(d, code, rotary_dim=32, layout=a2t.A2T_ROPE_PAIRS, scaling=a2t.A2T_ROPE_YARN, factor=8.0, trained_rows=8192)
+    a2t.a2t_rope_apply(rope, torch.from_numpy(pos).to("cuda"), both[:, :hq], both[:, hq:hq + hkv], both[:, :hq], both[:, hq:hq + hkv])
+    q, k, v = both[:, :hq], both[:, hq:hq + hkv], both[:, hq + hkv:]
+    cache = a2t.a2t_cache_create(1, 1, hq, hkv, d, code, n, n, 128, flags=a2t.A2T_FLAG_ROTATED)
+    served = torch.empty((n, hq, d), dtype=dt, device="cuda")
+    until, resident, at, evictions = np.full(n, 2**31 - 1, np.int64), [], 0, 0
+    for u, seg in enumerate(units):
+        m = len(seg)
+        w = slice(at, at + m)
+        o = torch.empty((m, hq, d), dtype=dt, device="cuda")
+        a2t.a2t_append_attn(cache, 0, [0], [m], k[w].contiguous(), v[w].contiguous(), seg, pos[w], [u], [m], q[w].contiguous(), o)
+        served[w] = o
+        resident += [at + i for i in range(m) if seg[i] != SEG_TEXT]
+        at += m
+        gone = int(a2t.a2t_evict(cache, [0], budget, window)[0][0])
+        until[resident[:gone]] = at                # the oldest rows of the evictable classes
+        resident = resident[gone:]
+        evictions += gone > 0
+    assert evictions > 10
+    layout, _, _ = a2t.a2t_read_layout(cache, 0)
+    assert np.array_equal(np.sort(layout) - 70000, np.flatnonzero(until > n))
+    h = a2t.a2t_prompt_create(n, hq, hkv, d, code, flags=a2t.A2T_PROMPT_UNTIL)
+    o = torch.empty_like(served)
+    a2t.a2t_prompt_attn(h, [n], q, k, v, o, until=torch.from_numpy(until.astype(np.int32)).to("cuda"))
+    torch.cuda.synchronize()
+    u = 2.0 ** -8 if dtype == "bf16" else 2.0 ** -24
+    ref = prompt_attention([n], _f64(q), _f64(k), _f64(v), until, u_store=u, u_mul=u if dtype == "bf16" else 0.0)
+    tol = 2e-2 if dtype == "bf16" else 1e-4
+    assert (np.abs(_f64(o) - ref.o) <= ref.bounds["o"]).all()
+    assert (np.abs(_f64(served) - _f64(o)) <= tol + ref.bounds["o"]).all()
+    a2t.a2t_prompt_destroy(h)
+    a2t.a2t_cache_destroy(cache)
+    a2t.a2t_rope_destroy(rope)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "mx4", "device"])
+def test_rows_that_come_rotated(gpu, dtype):
+    """A2T_FLAG_ROTATED for every type of cache and for device-planned steps: the rows held are the rows given,
+    whatever their positions."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    rng = np.random.default_rng(5)
+    hq, hkv, d, n = 4, 2, 128, 70
+    code = {"f32": a2t.A2T_F32, "mx4": a2t.A2T_MX4}.get(dtype, a2t.A2T_BF16)
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    q, k, v = (torch.from_numpy(rng.standard_normal((n, h, d)).astype(np.float32)).to("cuda").to(dt) for h in (hq, hkv, hkv))
+    pos = np.cumsum(rng.integers(1, 9000, n)).astype(np.int32)
+    o = torch.empty_like(q)
+    got = {}
+    for flags in (a2t.A2T_FLAG_ROTATED, 0):
+        cache = a2t.a2t_cache_create(1, 1, hq, hkv, d, code, 100, 4, 80, flags=flags)
+        p = pos if flags else np.arange(n, dtype=np.int32)
+        if dtype == "device":
+            a2t.a2t_dev_begin(cache)
+            pad = lambda x: torch.cat([x, x.new_zeros((80 - n,) + x.shape[1:])])  # noqa: E731
+            buf = [pad(x).contiguous() for x in (k, v, q)]
+            out = torch.empty_like(buf[2])
+            i32 = lambda x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+            dpos = torch.zeros((1, 80), dtype=torch.int32, device="cuda")
+            dpos[0, :n] = torch.from_numpy(p).to("cuda")
+            a2t.a2t_dev_open(cache, [0], i32([n]), i32([0]), torch.full((1, 80), SEG_TEXT, dtype=torch.uint8, device="cuda"), dpos)
+            a2t.a2t_dev_append_attn(cache, 0, buf[0], buf[1], buf[2], out)
+            a2t.a2t_dev_evict(cache, i32([1000]), 1)
+            a2t.a2t_dev_end(cache)
+            o.copy_(out[:n])
+        else:
+            a2t.a2t_append_attn(cache, 0, [0], [n], k, v, [SEG_TEXT] * n, p, [0], [n], q, o)
+        held, held_v = a2t.a2t_read_kv(cache, 0, 0)
+        got[flags] = held
+        a2t.a2t_cache_destroy(cache)
+        if not flags:
+            break
+        if dtype != "mx4":
+            assert np.array_equal(held, k.cpu().numpy() if dtype == "f32" else k.cpu().view(torch.int16).numpy().view(np.uint16))
+        as64 = lambda y: y.astype(np.float64) if dtype == "f32" else torch.from_numpy(y.view(np.int16).copy()).view(torch.bfloat16).double().numpy()  # noqa: E731
+        ref = attend(_f64(q), as64(held), as64(held_v), np.arange(n), np.arange(n), d ** -0.5)
+        assert np.abs(_f64(o) - ref).max() <= (1e-4 if dtype == "f32" else 2e-2)
+    # the row at position 0 is not turned by the caches' own encoding either: the same bits
+    assert np.array_equal(got[0][0], got[a2t.A2T_FLAG_ROTATED][0])
+
+
+def _training_step(a2t, torch, handles, x, w, pos, until, lengths, loss):
+    """x [rows][heads][D] -> rotated q, k -> attention -> logits -> loss; gradients of x and w."""
+    rope, prompt = handles
+    hq, hkv = prompt.n_q_heads, prompt.n_kv_heads
+    rot = x.clone()
+    a2t.a2t_rope_apply(rope, pos, x[:, :hq], x[:, hq:hq + hkv], rot[:, :hq], rot[:, hq:hq + hkv])
+    q, k, v = rot[:, :hq], rot[:, hq:hq + hkv], rot[:, hq + hkv:]
+    n = len(x)
+    o, lse = torch.empty_like(x[:, :hq], memory_format=torch.contiguous_format), torch.empty((hq, n), device="cuda")
+    a2t.a2t_prompt_attn(prompt, lengths, q, k, v, o, lse, until)
+    logits = o.flatten(1) @ w
+    glogits = torch.empty_like(logits)
+    out = loss(logits, glogits)
+    gw = o.flatten(1).T @ glogits
+    do = (glogits @ w.T).view_as(o).contiguous()
+    gx = torch.empty_like(x)
+    a2t.a2t_prompt_attn_grad(prompt, lengths, q, k, v, o, lse, do, gx[:, :hq], gx[:, hq:hq + hkv], gx[:, hq + hkv:], until)
+    a2t.a2t_rope_apply(rope, pos, gx[:, :hq], gx[:, hq:hq + hkv], gx[:, :hq], gx[:, hq:hq + hkv], grad=True)
+    return out, gx, gw
+
+
+def _step_in_64(torch, x, w, pos, until, lengths, hq, hkv, d, freq):
+    """The same in float64 on the CPU, to the logits."""
+    x, w = x.detach().cpu().double().requires_grad_(), w.detach().cpu().double().requires_grad_()
+    a = pos.cpu().double()[:, None, None] * torch.from_numpy(freq)
+    half = d // 2
+
+    def turn(y):
+        lo, hi = y[..., :half], y[..., half:]
+        return torch.cat([lo * a.cos() - hi * a.sin(), hi * a.cos() + lo * a.sin()], -1)
+    q, k, v = turn(x[:, :hq]), turn(x[:, hq:hq + hkv]), x[:, hq + hkv:]
+    at, outs = 0, []
+    for m in lengths:
+        s = slice(at, at + m)
+        at += m
+        i = torch.arange(m)
+        see = i[None, :] <= i[:, None]
+        if until is not None:
+            see &= i[:, None] < until.cpu()[s][None, :]
+        score = torch.einsum("ihd,jhd->hij", q[s], k[s].repeat_interleave(hq // hkv, 1)) * d ** -0.5
+        p = torch.softmax(score.masked_fill(~see, -np.inf), -1)
+        outs.append(torch.einsum("hij,jhd->ihd", p, v[s].repeat_interleave(hq // hkv, 1)))
+    return x, w, torch.cat(outs).flatten(1) @ w
+
+
+def _near(got, want, what):
+    got, want = _f64(got), want.detach().numpy()
+    assert np.linalg.norm(got - want) <= 2e-4 * np.linalg.norm(want), what
+
+
+@pytest.mark.parametrize("kind", ["preference", "adaptation"])
+def test_training_step(gpu, kind):
+    import torch
+    import paper_2609_31224_amd as a2t
+    rng = np.random.default_rng(6)
+    hq, hkv, d, vocab = 4, 2, 64, 203
+    lengths = [31, 40, 26, 55]
+    n = sum(lengths)
+    f32 = lambda *s: torch.from_numpy(rng.standard_normal(s).astype(np.float32)).to("cuda")  # noqa: E731
+    x, w = f32(n, hq + 2 * hkv, d), 0.3 * f32(hq * d, 208)
+    pos = torch.cat([torch.arange(m, dtype=torch.int32) for m in lengths]).to("cuda") + 1000
+    place = np.concatenate([np.arange(m) for m in lengths])
+    until = torch.from_numpy(np.where(place % 3 == 0, place + 20, 1000).astype(np.int32)).to("cuda")
+    target = torch.from_numpy(rng.integers(0, vocab, n).astype(np.int32)).to("cuda")
+    rope = a2t.a2t_rope_create(d, a2t.A2T_F32)
+    prompt = a2t.a2t_prompt_create(n, hq, hkv, d, a2t.A2T_F32, flags=a2t.A2T_PROMPT_UNTIL)
+    freq, _ = frequencies(d, 1e6)
+    x64, w64, logits64 = _step_in_64(torch, x, w, pos, until, lengths, hq, hkv, d, freq)
+    if kind == "preference":
+        ref_logp = 0.1 * f32(n) - 5.0
+        h = a2t.a2t_prefer_create(n, vocab, a2t.A2T_F32)
+        losses = torch.empty(3, device="cuda")
+
+        def loss(logits, g):
+            a2t.a2t_prefer_loss(h, lengths, logits, target, losses, ref_logp=ref_logp, beta=0.3, grad=g)
+            return losses
+        lp = torch.log_softmax(logits64[:, :vocab], -1)[torch.arange(n), target.cpu().long()] - ref_logp.cpu().double()
+        a = [y.sum() for y in lp.split(lengths)]
+        want = -torch.nn.functional.logsigmoid(0.3 * torch.stack([a[0] - a[1], a[2] - a[3]])).mean()
+    else:
+        teacher = f32(n, 208)
+        row = np.where(np.arange(n) % 3 == 0, 1, 2).astype(np.int8)
+        dec, turn = (np.arange(n) % 3 - 1).astype(np.int8), np.full(n, -1, np.int8)
+        h = a2t.a2t_distill_create(n, 200, 3, a2t.A2T_F32)
+        losses = torch.empty(5, device="cuda")
+
+        def loss(logits, g):
+            a2t.a2t_distill_loss(h, logits, teacher, row, target.cpu().numpy(), dec, turn, 1.0, losses, g)
+            return losses
+        ref = distill_losses(logits64.detach().numpy()[:, :203], _f64(teacher)[:, :200], row, target.cpu().numpy(), dec, turn)
+        full = np.zeros(logits64.shape)
+        full[:, :203] = ref.grad
+        want = (logits64 * torch.from_numpy(full)).sum()
+    out, gx, gw = _training_step(a2t, torch, (rope, prompt), x, w, pos, until, lengths, loss)
+    torch.cuda.synchronize()
+    g64 = torch.autograd.grad(want, (x64, w64))
+    value = want.item() if kind == "preference" else ref.losses["total"]
+    assert abs(out[0 if kind == "preference" else 4].item() - value) <= 2e-4 * abs(value)
+    _near(gx, g64[0], "gx")
+    _near(gw[:, :vocab], g64[1][:, :vocab], "gw")
+    a2t.a2t_prompt_destroy(prompt)
+    a2t.a2t_rope_destroy(rope)
+    (a2t.a2t_prefer_destroy if kind == "preference" else a2t.a2t_distill_destroy)(h)
+
+
+def test_two_sessions_at_once(gpu):
+    """Handles of their own on streams of their own: what each computes alone, bit by bit."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    rng = np.random.default_rng(7)
+    hq, hkv, d, n = 8, 2, 128, 900
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    jobs = []
+    for s in streams:
+        x = torch.from_numpy(rng.standard_normal((n, hq + 2 * hkv, d)).astype(np.float32)).to("cuda").bfloat16()
+        do = torch.from_numpy(rng.standard_normal((n, hq, d)).astype(np.float32)).to("cuda").bfloat16()
+        jobs.append(dict(h=a2t.a2t_prompt_create(n, hq, hkv, d, a2t.A2T_BF16, stream=s), x=x, do=do, g=torch.zeros_like(x),
+                         o=torch.zeros_like(do), lse=torch.zeros((hq, n), device="cuda")))
+
+    def run(j):
+        parts = lambda y: (y[:, :hq], y[:, hq:hq + hkv], y[:, hq + hkv:])  # noqa: E731
+        a2t.a2t_prompt_attn(j["h"], [n], *parts(j["x"]), j["o"], j["lse"])
+        a2t.a2t_prompt_attn_grad(j["h"], [n], *parts(j["x"]), j["o"], j["lse"], j["do"], *parts(j["g"]))
+    torch.cuda.synchronize()
+    want = []
+    for j in jobs:
+        run(j)
+        torch.cuda.synchronize()
+        want.append([j[c].clone() for c in ("o", "lse", "g")])
+    for turn in range(3):
+        for j in jobs:
+            for c in ("o", "lse", "g"):
+                j[c].zero_()
+        torch.cuda.synchronize()
+        for j in jobs:
+            run(j)
+        torch.cuda.synchronize()
+        for j, w in zip(jobs, want):
+            assert all(torch.equal(j[c], y) for c, y in zip(("o", "lse", "g"), w)), turn
+    for j in jobs:
+        a2t.a2t_prompt_destroy(j["h"])
