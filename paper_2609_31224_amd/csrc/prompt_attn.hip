@@ -207,6 +207,220 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 128 ? 3 : sizeof(T) * D
             store4(o + 32 * db + 8 * e, acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv, acc[db][4 * e + 3] * inv);
 }
 
+// The same for bf16, a tile ahead: the scores of the next tile run on the matrix units beside the
+// exponentials of this one, and this one's products with V after them.  LDS reads are issued two
+// groups ahead.
+template <int D, bool UNTIL, int N>
+__global__ __launch_bounds__(kThreads, 2) void prompt_attn16_kernel(Args a, SeqTable<N> t) {
+    using T = bf16_t;
+    using Tl = Tile<T, D>;
+    constexpr int DB = Tl::DB, STEPS = Tl::STEPS;
+    __shared__ __align__(1024) char s_k[2][Tl::BYTES];
+    __shared__ __align__(1024) char s_v[2][Tl::BYTES];
+    __shared__ int2 s_meta[2][UNTIL ? kTile : 1];
+
+    const int g = blockIdx.x % a.Hkv, G = a.G;
+    int sp = (int)(blockIdx.x / a.Hkv), place;   // split of the block's tiles
+    const int y = sp / a.splits;
+    sp -= y * a.splits;
+    const int z = sequence_of(t, y, &place);
+    const int n = t.rows[z], row0 = t.row0[z], M = G * n;
+    const int m0 = ((M + kBlock - 1) / kBlock - 1 - place) * kBlock;   // the rows that see most come first
+    const int base = uniform(m0 / G), rem = m0 - base * G;
+    auto place_of = [&](int r) { return base + (int)(((uint32_t)(rem + r) * a.inv_g) >> 16); };   // of row m0 + r
+    const int w = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, l32 = lane & 31, h = lane >> 5;
+    const int rows = min(kBlock, M - m0);
+    const int r = min(32 * w + l32, rows - 1);
+    const int i = place_of(r), hh = rem + r - (i - base) * G;
+    const int i_first = uniform(place_of(min(32 * w, rows - 1))), i_last = uniform(place_of(min(32 * w + 31, rows - 1)));
+    const Runs runs = key_runs<UNTIL>(a.kv, row0, n, base, uniform(place_of(rows - 1)));
+    const int t0 = runs.tiles * sp / a.splits, t1 = runs.tiles * (sp + 1) / a.splits;
+
+    const char* kp = static_cast<const char*>(a.kv.k) + ((int64_t)row0 * a.kv.k_stride + g * D) * sizeof(T);
+    const char* vp = static_cast<const char*>(a.kv.v) + ((int64_t)row0 * a.kv.v_stride + g * D) * sizeof(T);
+    int2 mm = {0, 0};
+    auto load_k = [&](int tile) {
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        Coming<T, D>::rows(kp, a.kv.k_stride * sizeof(T), lo, n - 1, w, lds_address(s_k[tile & 1]));
+        if (UNTIL && threadIdx.x < kTile) mm = key_place(a.kv, row0, min(lo + (int)threadIdx.x, n - 1));
+    };
+    auto load_v = [&](int tile) {
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        Coming<T, D>::rows(vp, a.kv.v_stride * sizeof(T), lo, n - 1, w, lds_address(s_v[tile & 1]));
+    };
+    auto store_meta = [&](int tile) {
+        if (UNTIL && threadIdx.x < kTile) s_meta[tile & 1][threadIdx.x] = mm;
+    };
+    if (t0 < t1) {
+        load_k(t0);
+        store_meta(t0);
+        load_v(t0);
+    }
+    u32x4 qop[STEPS];
+    {
+        const char* qp = static_cast<const char*>(a.q) + ((row0 + i) * a.q_stride + (g * G + hh) * D) * (int64_t)sizeof(T) + 16 * h;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) qop[s] = *reinterpret_cast<const u32x4*>(qp + 32 * s);
+    }
+
+    // base-2 logarithms throughout: mref is the reference of the lane's row (its scaled scores less mref
+    // are at most 8), sum of 2^(score - mref)
+    const float c = a.scale_log2e;
+    float mrun = -INFINITY, mref = 0.f, sum = 0.f, sum1 = 0.f, top = -INFINITY;
+    f32x16 acc[DB], s[2], next[2];
+    uint32_t pk[16];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[db][e] = 0.f;
+
+    auto probability = [&](int e) {   // of the scores' pair e
+        const float p = exp2_(__builtin_fmaf(s[e >> 3][(2 * e) & 15], c, -mref)), q = exp2_(__builtin_fmaf(s[e >> 3][(2 * e + 1) & 15], c, -mref));
+        sum += p;
+        sum1 += q;
+        pk[e] = pack_bf16x2(p, q);
+    };
+    // scores of the tile in stage `st` into `next`; BESIDE: the probabilities of `s` with them
+    auto scores = [&](int st, auto beside) {
+        constexpr bool BESIDE = decltype(beside)::value;
+        const RowReads<D> kr(lds_address(s_k[st]), l32, h);
+        u32x4 x[4], y[4];
+        auto group = [&](u32x4 (&f)[4], auto k) {   // two steps of both blocks of 32 keys
+            constexpr int K = decltype(k)::value;
+            f[0] = kr.template step<K>(), f[1] = kr.template step<K, 32>(), f[2] = kr.template step<K + 1>(), f[3] = kr.template step<K + 1, 32>();
+        };
+        auto products = [&](const u32x4 (&f)[4], int k) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                mma_step<T>(f[e], qop[k + e / 2], next[e & 1]);
+                if constexpr (BESIDE) {
+#pragma unroll
+                    for (int x = 0; x < 8 / STEPS; ++x) probability(8 / STEPS * (2 * k + e) + x);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+        };
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) next[b][e] = 0.f;
+        using std::integral_constant;
+#define A2T_I(k) integral_constant<int, k>{}
+        group(x, A2T_I(0));
+        group(y, A2T_I(2));
+        lds_wait<4>(x);
+        products(x, 0);
+        if constexpr (D == 128) {
+            group(x, A2T_I(4));
+            lds_wait<4>(y);
+            products(y, 2);
+            group(y, A2T_I(6));
+            lds_wait<4>(x);
+            products(x, 4);
+            lds_wait<0>(y);
+            products(y, 6);
+        } else {
+            lds_wait<0>(y);
+            products(y, 2);
+        }
+#undef A2T_I
+    };
+    // the tile's scores that a row does not see, and the largest of the rest
+    auto finish = [&](int tile) {
+        int lo, hi;
+        runs.at(tile, &lo, &hi);
+        const int2* meta = s_meta[tile & 1];
+        if (!sees<UNTIL>(meta, lo, hi, i_first, i_last).all) {
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    if (!visible<UNTIL>(meta, lo, hi, 32 * b + 8 * (e >> 2) + 4 * h + (e & 3), i)) next[b][e] = -INFINITY;
+        }
+        float m = fmaxf(next[0][0], next[1][0]);
+#pragma unroll
+        for (int e = 1; e < 16; ++e) m = fmaxf(fmaxf(m, next[0][e]), next[1][e]);
+        top = swap_max(m) * c;
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = next[b];
+    };
+
+    if (t0 < t1) {
+        wait_tiles();
+        __syncthreads();
+        if (t0 + 1 < t1) load_k(t0 + 1);
+        scores(t0 & 1, std::false_type{});
+        finish(t0);
+        if (t0 + 1 < t1) store_meta(t0 + 1);
+    }
+    for (int tile = t0; tile < t1; ++tile) {
+        // here: s and top are the tile's; its V and the next K are there once everybody has come
+        wait_tiles();
+        __syncthreads();
+        if (tile + 2 < t1) load_k(tile + 2);
+        if (tile + 1 < t1) load_v(tile + 1);
+        if (__any(top > mrun + 8.f)) {
+            const float up = fmaxf(mrun, top), ref = up == -INFINITY ? 0.f : up;
+            const float by = exp2_(mrun - ref);
+            sum *= by;
+            sum1 *= by;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) acc[db] *= by;
+            mrun = up;
+            mref = ref;
+        }
+        const TransReads<D> vt(lds_address(s_v[tile & 1]), 0);
+        if (tile + 1 < t1) {
+            scores((tile + 1) & 1, std::true_type{});
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) probability(e);
+        }
+        uint2 x[D / 16], y[D / 16];
+        auto products = [&](const uint2 (&f)[D / 16], int k) {
+            mma_group<D>(f, __builtin_bit_cast(bf16x8, (u32x4{pk[4 * k], pk[4 * k + 1], pk[4 * k + 2], pk[4 * k + 3]})), acc);
+        };
+        vt.template group<0>(x);
+        vt.template group<1>(y);
+        lds_wait<D / 16>(x);
+        products(x, 0);
+        vt.template group<2>(x);
+        lds_wait<D / 16>(y);
+        products(y, 1);
+        vt.template group<3>(y);
+        lds_wait<D / 16>(x);
+        products(x, 2);
+        lds_wait<0>(y);
+        products(y, 3);
+        if (tile + 1 < t1) finish(tile + 1);
+        if (tile + 2 < t1) store_meta(tile + 2);
+    }
+
+    if (32 * w + l32 >= rows) return;
+    const float total = swap_sum(sum + sum1);
+    if (a.splits > 1) {   // the split's own sums; prompt_join_kernel puts them together
+        const int64_t at = ((int64_t)sp * a.total + row0 + i) * a.Hq + g * G + hh;
+        if (h == 0) *reinterpret_cast<float2*>(a.part + (int64_t)a.splits * a.total * a.Hq * D + 2 * at) = make_float2(mrun, total);
+        float* o = a.part + at * D + 4 * h;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) store4(o + 32 * db + 8 * e, acc[db][4 * e], acc[db][4 * e + 1], acc[db][4 * e + 2], acc[db][4 * e + 3]);
+        return;
+    }
+    const float inv = total > 0.f ? 1.f / total : total == 0.f ? 0.f : total;   // a row without keys is zero
+    const int64_t row = row0 + i;
+    if (a.lse && h == 0) a.lse[(int64_t)(g * G + hh) * a.total + row] = (mref + __builtin_amdgcn_logf(total)) * kLn2;
+    T* o = static_cast<T*>(a.o) + (row * a.Hq + g * G + hh) * D + 4 * h;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            store4(o + 32 * db + 8 * e, acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv, acc[db][4 * e + 3] * inv);
+}
+
 // ---- gradient with respect to the queries
 //   delta_i = dO_i . O_i,  P_ij = exp(scale q_i . k_j - lse_i),  dS_ij = P_ij (dO_i . v_j - delta_i),
 //   dQ_i = scale sum_j dS_ij k_j
@@ -737,7 +951,8 @@ hipError_t launch(const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStr
     return by_count(t, [&](const auto& s) {
         constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
         const dim3 grid((uint32_t)(blocks * a.splits * a.Hkv));
-        if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_attn_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
+        if constexpr (K == Kernel::forward && sizeof(T) == 2) hipLaunchKernelGGL((prompt_attn16_kernel<D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
+        else if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_attn_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
         else if constexpr (K == Kernel::dq) hipLaunchKernelGGL((prompt_dq_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
         else hipLaunchKernelGGL((prompt_dkv_kernel<T, D, UNTIL, N>), grid, dim3(64 * KeyShape<T, D>::kWaves), 0, stream, a, s);
         return a.splits == 1 ? hipGetLastError() : join<K, T, D, N>(a, s, stream);

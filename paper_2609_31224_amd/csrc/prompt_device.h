@@ -195,10 +195,11 @@ struct RowReads {
     using Tl = Tile<bf16_t, D>;
     uint32_t even, odd;   // of even and odd steps (D 128: 32 bytes apart)
     __device__ __forceinline__ RowReads(uint32_t tile, int r, int h) : even(tile + Tl::at(r, h)), odd(tile + Tl::at(r, 2 + h)) {}
-    template <int K>
+    template <int K, int ROWS = 0>   // of the row ROWS further (a multiple of 32)
     __device__ __forceinline__ u32x4 step() const {
-        if constexpr (D == 128) return read16<(K >> 1) * 256 + (K & 1) * 32>(even);
-        else return read16<(K >> 1) * 512>(K & 1 ? odd : even);
+        constexpr int OFF = ROWS / Tl::RPB * Tl::BLOCK;
+        if constexpr (D == 128) return read16<OFF + (K >> 1) * 256 + (K & 1) * 32>(even);
+        else return read16<OFF + (K >> 1) * 512>(K & 1 ? odd : even);
     }
 };
 // Transposed reads: rows r0 + 16 C .. + 15 of the tile (r0 a multiple of 32), all blocks of 32
