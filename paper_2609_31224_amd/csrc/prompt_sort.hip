@@ -12,40 +12,56 @@ namespace {
 constexpr int kScanThreads = 1024;
 constexpr int kCopyRows = 16;    // rows of a copying workgroup
 
-// One workgroup a sequence: counts of lasting keys and reach of the passing ones, by place.
+// One workgroup a sequence: counts of lasting keys and reach of the passing ones, by place.  A thread
+// takes neighbouring places, so that the threads meet once (13,200 rows: 20 us with a meeting every 1,024).
 template <int N>
 __global__ __launch_bounds__(kScanThreads) void prompt_scan_kernel(SortArgs a, SeqTable<N> t) {
+    constexpr int kWaves = kScanThreads / 64;
+    constexpr int kNone = -0x7fffffff;
     const int n = t.rows[blockIdx.x], row0 = t.row0[blockIdx.x];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    __shared__ int s_count[kScanThreads / 64], s_reach[kScanThreads / 64];
-    int count = 0, reach = -0x7fffffff;   // of the chunks before
-    for (int j0 = 0; j0 < n; j0 += kScanThreads) {
-        const int j = j0 + tid;
-        const int until = j < n ? a.until[row0 + j] : 0;
-        const bool lasts = j < n && until >= n;
-        const uint64_t mask = __ballot(lasts);
-        const int before = __builtin_popcountll(mask & ((2ull << lane) - 1));   // up to and with this key
-        int r = j < n && !lasts ? until : -0x7fffffff;
+    const int per = (n + kScanThreads - 1) / kScanThreads;
+    const int j0 = (int)min((int64_t)tid * per, (int64_t)n), j1 = min(j0 + per, n);
+    __shared__ int s_count[kWaves], s_reach[kWaves];
+    // eight places' values at a time
+    auto each = [&](auto f) {
+        for (int j = j0; j < j1; j += 8) {
+            int until[8];
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int o = __shfl_up(r, d);
-            if (lane >= d) r = max(r, o);
+            for (int e = 0; e < 8; ++e) until[e] = a.until[row0 + min(j + e, j1 - 1)];
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (j + e < j1) f(j + e, until[e]);
         }
-        if (lane == 63) s_count[w] = before, s_reach[w] = r;
-        __syncthreads();
-        int c = count, m = reach;
-        for (int k = 0; k < kScanThreads / 64; ++k) {
-            if (k < w) c += s_count[k], m = max(m, s_reach[k]);
-            count += s_count[k];
-            reach = max(reach, s_reach[k]);
-        }
-        if (j < n) {
-            const int seen = c + before;
-            a.lasting[row0 + j] = seen;
-            if (!lasts) a.reach[row0 + (j - seen)] = max(m, r);
-        }
-        __syncthreads();
+    };
+    int count = 0, reach = kNone;
+    each([&](int, int until) {
+        if (until >= n) ++count;
+        else reach = max(reach, until);
+    });
+    // of the threads before and this one
+    int c = count, m = reach;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int oc = __shfl_up(c, d), om = __shfl_up(m, d);
+        if (lane >= d) c += oc, m = max(m, om);
     }
+    if (lane == 63) s_count[w] = c, s_reach[w] = m;
+    // of the threads before alone
+    c -= count;
+    m = __shfl_up(m, 1);
+    if (lane == 0) m = kNone;
+    __syncthreads();
+    for (int k = 0; k < w; ++k) c += s_count[k], m = max(m, s_reach[k]);
+    each([&](int j, int until) {
+        if (until >= n) {
+            ++c;
+        } else {
+            m = max(m, until);
+            a.reach[row0 + (j - c)] = m;
+        }
+        a.lasting[row0 + j] = c;
+    });
 }
 
 template <int N>
