@@ -574,9 +574,10 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     constexpr bool WIDE = KeyShape<T, D>::kWide;
     using In = Coming<T, D, WAVES>;
     __shared__ __align__(1024) char s_tile[4][Tl::BYTES];            // Q and dO, two stages of each
-    __shared__ __align__(1024) char s_v[WIDE ? 2 : 1][WIDE ? Tl::BYTES : 16];
-    constexpr bool HALF_K = sizeof(T) == 2 && D == 128;              // K's second half of dimensions is read from LDS
-    __shared__ __align__(1024) char s_k[HALF_K ? 2 : 1][HALF_K ? Tl::BYTES : 16];
+    // where the operands of the wave's keys are
+    constexpr bool KV_LDS = sizeof(T) == 2 && D == 128, V_LDS = KV_LDS || (sizeof(T) == 4 && WIDE);
+    __shared__ __align__(1024) char s_v[V_LDS ? 2 : 1][V_LDS ? Tl::BYTES : 16];
+    __shared__ __align__(1024) char s_k[KV_LDS ? 2 : 1][KV_LDS ? Tl::BYTES : 16];
     __shared__ __align__(16) float s_lse[2][kTile], s_delta[2][kTile];   // -lse / scale (fp32: -lse log2 e) and -delta of the tile's rows
     __shared__ int s_range[2][4];
     static_assert(!WIDE || 4 * Tl::BYTES >= 4 * DB * 16 * 256, "one gradient's sums of four waves fit the tiles");
@@ -617,11 +618,11 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     const char* kb = static_cast<const char*>(a.kv.k) + (row0 * a.kv.k_stride + g * D) * (int64_t)sizeof(T);
     const char* kp = kb + key * a.kv.k_stride * (int64_t)sizeof(T) + 16 * h;
     const char* vp = static_cast<const char*>(a.kv.v) + (row0 * a.kv.v_stride + g * D) * (int64_t)sizeof(T);
-    u32x4 kop[HALF_K ? 1 : Tl::STEPS], vop[WIDE ? 1 : Tl::STEPS];
+    u32x4 kop[KV_LDS ? 1 : Tl::STEPS], vop[V_LDS ? 1 : Tl::STEPS];
 #pragma unroll
     for (int s = 0; s < Tl::STEPS; ++s) {
-        if (!HALF_K) kop[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
-        if constexpr (!WIDE) vop[s] = *reinterpret_cast<const u32x4*>(vp + key * a.kv.v_stride * (int64_t)sizeof(T) + 16 * h + 32 * s);
+        if constexpr (!KV_LDS) kop[s] = *reinterpret_cast<const u32x4*>(kp + 32 * s);
+        if constexpr (!V_LDS) vop[s] = *reinterpret_cast<const u32x4*>(vp + key * a.kv.v_stride * (int64_t)sizeof(T) + 16 * h + 32 * s);
     }
 
     const char* qp = static_cast<const char*>(a.q) + ((int64_t)row0 * a.q_stride + g * G * D) * sizeof(T);
@@ -644,12 +645,12 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     };
     int hh = per_head ? t0 / per_head : 0, lo = from + (t0 - hh * per_head) * kTile;
     if (t0 < t1) {
-        if constexpr (WIDE) {
+        if constexpr (V_LDS) {
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 const int first = min(place * kBlock + x * kTile, n - 1);
                 In::rows(vp, a.kv.v_stride * sizeof(T), first, n - 1, w, lds_address(s_v[x]));
-                if constexpr (HALF_K) In::rows(kb, a.kv.k_stride * sizeof(T), first, n - 1, w, lds_address(s_k[x]));
+                if constexpr (KV_LDS) In::rows(kb, a.kv.k_stride * sizeof(T), first, n - 1, w, lds_address(s_k[x]));
             }
         }
         load(hh, lo, t0 & 1);
@@ -683,7 +684,7 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
 #pragma unroll
         for (int k = 0; k < Tl::STEPS; ++k) {
             u32x4 v;
-            if constexpr (WIDE) v = row_operand<T, D>(s_v[0], 32 * kg + l32, k, h);
+            if constexpr (V_LDS) v = row_operand<T, D>(s_v[0], 32 * kg + l32, k, h);
             else v = vop[k];
             mma_step<T>(row_operand<T, D>(d, 32 * b + l32, k, h), v, p);
         }
@@ -703,109 +704,98 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
         mma_rows<D, T>(d, 32 * b, s, av);
         mma_rows<D, T>(q, 32 * b, p, ak);
     };
-    // the same for bf16, with LDS reads issued two groups ahead of the products that use them
+    // The same for bf16, with LDS reads in groups of eight registers, three of them under way: rows of Q,
+    // rows of dO (with K's and V's where those are in LDS), then both transposed.
     auto block16 = [&](uint32_t q, uint32_t d, const float* lse, const float* delta, int b, int first, bool all) {
         f32x16 s, p;
         const int r = 32 * b + l32;
-        const RowReads<D> qr(q, r, h), dr(d, r, h), vr(lds_address(s_v[0]), 32 * kg + l32, h);
-        const RowReads<D> kr(HALF_K ? lds_address(s_k[0]) : 0, 32 * kg + l32, h);
+        const RowReads<D> qr(q, r, h), dr(d, r, h);
+        const RowReads<D> kr(KV_LDS ? lds_address(s_k[0]) : 0, 32 * kg + l32, h), vr(KV_LDS ? lds_address(s_v[0]) : 0, 32 * kg + l32, h);
         const TransReads<D> qt(q, 32 * b), dt(d, 32 * b);
-        u32x4 x[4], y[4];
-        uint2 tx[D / 16], ty[D / 16];
-        auto q_group = [&](u32x4 (&f)[4], auto k) {
-            constexpr int K = decltype(k)::value;
-            f[0] = qr.template step<K>(), f[1] = qr.template step<K + 1>(), f[2] = qr.template step<K + 2>(), f[3] = qr.template step<K + 3>();
-        };
-        auto qk_group = [&](u32x4 (&f)[4], auto k) {
-            constexpr int K = decltype(k)::value;
-            f[0] = qr.template step<K>(), f[1] = kr.template step<K>(), f[2] = qr.template step<K + 1>(), f[3] = kr.template step<K + 1>();
-        };
-        auto qk_mma = [&](const u32x4 (&f)[4]) {
-            mma_step<T>(f[0], f[1], s);
-            mma_step<T>(f[2], f[3], s);
-        };
-        auto dv_group = [&](u32x4 (&f)[4], auto k) {
-            constexpr int K = decltype(k)::value;
-            f[0] = dr.template step<K>(), f[1] = vr.template step<K>(), f[2] = dr.template step<K + 1>(), f[3] = vr.template step<K + 1>();
-        };
-        auto q_mma = [&](const u32x4 (&f)[4], int k) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) mma_step<T>(f[e], kop[k + e], s);
-        };
-        // two products beside which the exponentials of EXPS scores run
-        constexpr int EXPS = 32 / Tl::STEPS;
-        auto dv_mma = [&](const u32x4 (&f)[4], int part) {
-            mma_step<T>(f[0], f[1], p);
-#pragma unroll
-            for (int e = EXPS * part; e < EXPS * part + EXPS / 2; ++e) s[e] = exp2_(s[e] * c);
-            __builtin_amdgcn_sched_barrier(0);
-            mma_step<T>(f[2], f[3], p);
-#pragma unroll
-            for (int e = EXPS * part + EXPS / 2; e < EXPS * part + EXPS; ++e) s[e] = exp2_(s[e] * c);
-            __builtin_amdgcn_sched_barrier(0);
-        };
+        constexpr int NQ = KV_LDS ? Tl::STEPS : Tl::STEPS / 2, ND = NQ, NT = DB / 2 * 2, ALL = NQ + ND + 2 * NT;
+        constexpr int EXPS = 16 / Tl::STEPS;   // beside a product
+        u32x4 f[3][2];
+        uint2 tr[3][4];
+        bf16x8 packed[2];
         using std::integral_constant;
-#define A2T_I(k) integral_constant<int, k>{}
-        auto last_two = [&](u32x4 (&f)[4], u32x4 (&g)[4]) {
-            lds_wait<4>(f);
-            dv_mma(f, Tl::STEPS / 2 - 2);
-            dt.template group<0>(tx);
-            lds_wait<D / 16>(g);
-            dv_mma(g, Tl::STEPS / 2 - 1);
-            dt.template group<1>(ty);
+        auto issue = [&](auto at) {
+            constexpr int G = decltype(at)::value;
+            if constexpr (G < NQ) {
+                if constexpr (KV_LDS) f[G % 3][0] = qr.template step<G>(), f[G % 3][1] = kr.template step<G>();
+                else f[G % 3][0] = qr.template step<2 * G>(), f[G % 3][1] = qr.template step<2 * G + 1>();
+            } else if constexpr (G < NQ + ND) {
+                constexpr int X = G - NQ;
+                if constexpr (KV_LDS) f[G % 3][0] = dr.template step<X>(), f[G % 3][1] = vr.template step<X>();
+                else f[G % 3][0] = dr.template step<2 * X>(), f[G % 3][1] = dr.template step<2 * X + 1>();
+            } else if constexpr (G < ALL) {
+                constexpr int X = (G - NQ - ND) % NT;   // half of the rows, pair of blocks of 32 dimensions
+                if constexpr (G < NQ + ND + NT) dt.template pair<X / (NT / 2), 2 * (X % (NT / 2))>(tr[G % 3]);
+                else qt.template pair<X / (NT / 2), 2 * (X % (NT / 2))>(tr[G % 3]);
+            }
+        };
+        auto use = [&](auto at) {
+            constexpr int G = decltype(at)::value;
+            // reads of the two groups behind this one
+            constexpr int R1 = G + 1 >= ALL ? 0 : G + 1 < NQ + ND ? 2 : 4, R2 = G + 2 >= ALL ? 0 : G + 2 < NQ + ND ? 2 : 4;
+            if constexpr (G < NQ + ND) lds_wait<R1 + R2>(f[G % 3]);
+            else lds_wait<R1 + R2>(tr[G % 3]);
+            if constexpr (G < NQ) {
+                if constexpr (KV_LDS) mma_step<T>(f[G % 3][0], f[G % 3][1], s);
+                else mma_step<T>(f[G % 3][0], kop[2 * G], s), mma_step<T>(f[G % 3][1], kop[2 * G + 1], s);
+            } else if constexpr (G < NQ + ND) {
+                constexpr int X = G - NQ;
+#pragma unroll
+                for (int e = 0; e < (KV_LDS ? 1 : 2); ++e) {
+                    const int at = KV_LDS ? X : 2 * X + e;
+                    if constexpr (KV_LDS) mma_step<T>(f[G % 3][0], f[G % 3][1], p);
+                    else mma_step<T>(f[G % 3][e], vop[at], p);
+#pragma unroll
+                    for (int i = 0; i < EXPS; ++i) s[EXPS * at + i] = exp2_(s[EXPS * at + i] * c);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            } else {
+                constexpr int X = (G - NQ - ND) % NT, HALF = X / (NT / 2), DB0 = 2 * (X % (NT / 2));
+                constexpr bool OF_Q = G >= NQ + ND + NT;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const u32x4 o = {tr[G % 3][2 * e].x, tr[G % 3][2 * e].y, tr[G % 3][2 * e + 1].x, tr[G % 3][2 * e + 1].y};
+                    f32x16& acc = (OF_Q ? ak : av)[DB0 + e];
+                    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o), packed[HALF], acc, 0, 0, 0);
+                }
+            }
+        };
+        auto weights = [&] {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) p[e] *= s[e];
+            if (!all) {   // a pair that is not visible has no gradient, whatever its products were
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int i = first + 32 * b + 8 * (e >> 2) + 4 * h + (e & 3);
+                    if (i < me.x || i >= me.y) s[e] = p[e] = 0.f;
+                }
+            }
+            packed[0] = pack8(s, 0), packed[1] = pack8(s, 1);
+        };
+        auto step = [&](auto at) {
+            constexpr int G = decltype(at)::value;
+            if constexpr (G < ALL) {
+                if constexpr (G == NQ + ND) weights();
+                if constexpr (G == NQ + ND + NT) packed[0] = pack8(p, 0), packed[1] = pack8(p, 1);
+                use(at);
+                issue(integral_constant<int, G + 3>{});
+            }
         };
         init(s, lse, b);
         init(p, delta, b);
-        if constexpr (D == 128) {
-            qk_group(x, A2T_I(0));
-            qk_group(y, A2T_I(2));
-            lds_wait<4>(x);
-            qk_mma(x);
-            qk_group(x, A2T_I(4));
-            lds_wait<4>(y);
-            qk_mma(y);
-            qk_group(y, A2T_I(6));
-            lds_wait<4>(x);
-            qk_mma(x);
-            dv_group(x, A2T_I(0));
-            lds_wait<4>(y);
-            qk_mma(y);
-            dv_group(y, A2T_I(2));
-            lds_wait<4>(x);
-            dv_mma(x, 0);
-            dv_group(x, A2T_I(4));
-            lds_wait<4>(y);
-            dv_mma(y, 1);
-            dv_group(y, A2T_I(6));
-            last_two(x, y);
-        } else {
-            q_group(x, A2T_I(0));
-            dv_group(y, A2T_I(0));
-            lds_wait<4>(x);
-            q_mma(x, 0);
-            dv_group(x, A2T_I(2));
-            last_two(y, x);
-        }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) p[e] *= s[e];
-        if (!all) {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int i = first + 32 * b + 8 * (e >> 2) + 4 * h + (e & 3);
-                if (i < me.x || i >= me.y) s[e] = p[e] = 0.f;
-            }
-        }
-        lds_wait<D / 16>(tx);
-        mma_group<D>(tx, pack8(s, 0), av);
-        qt.template group<0>(tx);
-        lds_wait<D / 16>(ty);
-        mma_group<D>(ty, pack8(s, 1), av);
-        qt.template group<1>(ty);
-        lds_wait<D / 16>(tx);
-        mma_group<D>(tx, pack8(p, 0), ak);
-        lds_wait<0>(ty);
-        mma_group<D>(ty, pack8(p, 1), ak);
-#undef A2T_I
+        issue(integral_constant<int, 0>{});
+        issue(integral_constant<int, 1>{});
+        issue(integral_constant<int, 2>{});
+        static_assert(sizeof(T) == 4 || ALL <= 24, "steps of a block");
+#define A2T_G(k) step(integral_constant<int, k>{});
+        A2T_G(0) A2T_G(1) A2T_G(2) A2T_G(3) A2T_G(4) A2T_G(5) A2T_G(6) A2T_G(7) A2T_G(8)
+        A2T_G(9) A2T_G(10) A2T_G(11) A2T_G(12) A2T_G(13) A2T_G(14) A2T_G(15) A2T_G(16) A2T_G(17)
+        A2T_G(18) A2T_G(19) A2T_G(20) A2T_G(21) A2T_G(22) A2T_G(23)
+#undef A2T_G
     };
     for (int tile = t0; tile < t1; ++tile) {
         const int stage = tile & 1;

@@ -179,6 +179,10 @@ __device__ __forceinline__ void lds_wait(u32x4 (&a)[4]) {
     asm volatile("s_waitcnt lgkmcnt(%4)" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]) : "i"(N));
 }
 template <int N>
+__device__ __forceinline__ void lds_wait(u32x4 (&a)[2]) {
+    asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a[0]), "+v"(a[1]) : "i"(N));
+}
+template <int N>
 __device__ __forceinline__ void lds_wait(uint2 (&a)[8]) {
     asm volatile("s_waitcnt lgkmcnt(%8)"
                  : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(a[4]), "+v"(a[5]), "+v"(a[6]), "+v"(a[7])
@@ -211,6 +215,12 @@ struct TransReads {
     __device__ __forceinline__ TransReads(uint32_t tile, int r0) {
         const int lane = threadIdx.x & 63, l16 = lane & 15, lg = lane >> 4;
         from = tile + Tl::at(r0 + 4 * (lane >> 5) + (l16 >> 2), 2 * (lg & 1) + ((l16 & 3) >> 1)) + 8 * (l16 & 1);
+    }
+    template <int C, int DB0>   // blocks DB0 and DB0 + 1 alone
+    __device__ __forceinline__ void pair(uint2 (&x)[4]) const {
+        constexpr int BLOCK = D == 128 ? 256 : 512, OFF = 16 * C / Tl::RPB * Tl::BLOCK + DB0 * BLOCK, FAR = 8 / Tl::RPB * Tl::BLOCK;
+        x[0] = read8t<OFF>(from), x[1] = read8t<OFF + FAR>(from);
+        x[2] = read8t<OFF + BLOCK>(from), x[3] = read8t<OFF + BLOCK + FAR>(from);
     }
     template <int C, int DB0 = 0>
     __device__ __forceinline__ void group(uint2 (&x)[D / 16]) const {
