@@ -661,15 +661,15 @@ typedef struct a2t_prompt a2t_prompt;
 
 #define A2T_PROMPT_UNTIL 1u   /* calls may pass `until`: the handle holds copies of K and V */
 
-/* A handle for calls of up to max_rows packed rows (max_rows * n_q_heads <= 2^30).
- * n_q_heads a multiple of n_kv_heads, at most 128 times as many; head_dim 64 or
- * 128; dtype A2T_F32 or A2T_BF16; attn_scale 0 selects 1/sqrt(head_dim),
- * otherwise within [1e-6, 1e6].  Allocates 4 n_q_heads bytes a row and, with
- * A2T_PROMPT_UNTIL, K's and V's bytes and 20 more, and at most 130 MiB for sums of
- * split blocks.  Tuning read from the environment at creation (for tests and
+/* A handle for calls of up to max_rows packed rows (<= 2^26, and max_rows *
+ * n_q_heads <= 2^29).  n_q_heads a multiple of n_kv_heads, at most 128 times as
+ * many and at most 4,096; head_dim 64 or 128; dtype A2T_F32 or A2T_BF16;
+ * attn_scale 0 selects 1/sqrt(head_dim), otherwise within [1e-6, 1e6].  Allocates
+ * 4 n_q_heads bytes a row, with A2T_PROMPT_UNTIL K's and V's bytes and 20 more, and
+ * at most 130 MiB for the sums of split blocks.  Tuning read from the environment at creation (for tests and
  * measurements; results stay within their tolerances whatever they are):
- *   A2T_PROMPT_SORT    rows of the longest sequence from which keys that expire are
- *                      sorted before attention (default 512)
+ *   A2T_PROMPT_SORT    query rows (rows x heads) of the longest sequence from which
+ *                      keys that expire are sorted before attention (default 10240)
  *   A2T_PROMPT_SPLITS  1..16: workgroups that the keys (or queries) of a block are
  *                      split over (0 = planned)
  * Errors: INVALID, OOM, NODEV. */

@@ -1,14 +1,32 @@
-// Causal attention over packed sequences, forward (gfx950): per query head and row i of a sequence
-//   O_i = sum_j softmax_j(scale q_i . k_j) v_j,  lse_i = ln sum_j exp(scale q_i . k_j),
-// over the rows j <= i < until_j of the same sequence.
+// Causal attention over packed sequences, forward and gradients (gfx950).  Per query head and row i of
+// a sequence, over the rows j <= i < until_j of the same sequence:
+//   O_i = sum_j P_ij v_j,  P_ij = exp(scale q_i . k_j - lse_i),  lse_i = ln sum_j exp(scale q_i . k_j)
+//   delta_i = dO_i . O_i,  dS_ij = P_ij (dO_i . v_j - delta_i)
+//   dQ_i = scale sum_j dS_ij k_j,  dK_j = scale sum_i dS_ij q_i,  dV_j = sum_i P_ij dO_i
 //
-// One workgroup = 128 packed query rows of a KV head (row m of a sequence is head m % G of the
-// group at place m / G, so that the G heads of a group share every key tile), four waves of 32
-// rows.  Key tiles of 64 rows go through registers into one of two LDS stages.  A wave's scores are
-// S^T = K Q^T on 32 x 32 matrix instructions: a lane has 16 of 32 keys of its own query, softmax
-// needs one exchange between two lanes, and the probabilities are the operand of O^T = V^T P^T as
-// they are.  The running maximum is raised lazily (when a tile exceeds it by 2^8), so that most
-// tiles rescale nothing.
+//   prompt_attn16, prompt_attn   forward (bf16, fp32): 128 packed query rows of a KV head a workgroup
+//   prompt_dq                    dQ and delta, the same rows
+//   prompt_dkv                   dK and dV: 128 keys a workgroup, every query row that sees them
+//   prompt_join, prompt_add      sums of blocks that were split over workgroups
+// The scores are computed again for each gradient (seven products where five would do): dQ summed over
+// the key blocks would need sums in memory whose order changes from run to run, or a pass over as many
+// partial sums as there are key blocks.
+//
+// Row m of a sequence is head m % G of a KV head's group at place m / G, so that the G heads share
+// every key tile and a block's triangle at the diagonal is G times smaller.  Scores are S^T = K Q^T on 32 x
+// 32 matrix instructions: a lane has 16 of 32 keys of its own query, a row's maximum needs one
+// exchange between two lanes, and probabilities are the operand of O^T = V^T P^T as they lie in registers.
+//
+// Bound: the matrix units under the card's power (clock 1.9 to 2.0 GHz of 2.4; a library's product of
+// 8,192^3 reaches 1.23 PFLOP/s) and, beside them, LDS reads and exponentials.  Measured, head dim 128,
+// 32 heads on 8: forward of 16,384 rows 2.0 ms, 1.10 PFLOP/s; a ten-minute session of 13,200 rows under
+// eviction 0.80 ms forward (0.94 PFLOP/s of visible pairs), dQ 1.05 ms (1.07), dK and dV 1.75 ms (0.85); fp32
+// kernels run at 0.7 to 0.8 of the fp32 matrix rate where the blocks fill the CUs.
+// Of the forms tried: tiles through registers instead of straight into LDS, 3.4 instead of 2.3 ms
+// (the compiler took 296 registers, one wave a SIMD); scores a tile ahead of the exponentials, 2.3 ->
+// 2.1; waves of 64 keys for dK and dV, one a SIMD, 1.25 ms instead of 0.86 at head dim 64 (at 128
+// their sums alone are 256 registers and spill); priorities among a SIMD's waves, no change; without
+// barriers between tiles dK and dV would take 1.63 of 1.95 ms, without tile loads 1.80.
 #include "prompt_device.h"
 
 #include <type_traits>
@@ -421,10 +439,9 @@ __global__ __launch_bounds__(kThreads, 2) void prompt_attn16_kernel(Args a, SeqT
             store4(o + 32 * db + 8 * e, acc[db][4 * e] * inv, acc[db][4 * e + 1] * inv, acc[db][4 * e + 2] * inv, acc[db][4 * e + 3] * inv);
 }
 
-// ---- gradient with respect to the queries
-//   delta_i = dO_i . O_i,  P_ij = exp(scale q_i . k_j - lse_i),  dS_ij = P_ij (dO_i . v_j - delta_i),
-//   dQ_i = scale sum_j dS_ij k_j
-// Workgroups as above; delta goes to memory for the gradient of the keys.
+// ---- gradient with respect to the queries; delta goes to memory for the gradient of the keys.  bf16:
+// P (dO . v - delta) is rounded to bf16 for its product with K, half a step of 2^-8 of each term, and
+// delta comes from the O that was stored.
 template <typename T, int D, bool UNTIL, int N>
 __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prompt_dq_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
@@ -553,15 +570,15 @@ __global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prom
                    acc[db][4 * e + 3] * a.scale);
 }
 
-// ---- gradient with respect to keys and values
-//   dV_j = sum_i P_ij dO_i,  dK_j = scale sum_i dS_ij q_i, over all heads of the group
+// ---- gradient with respect to keys and values, over all heads of the group.
 // One workgroup = 128 keys of a KV head, 32 a wave, over tiles of 64 query rows of one head of the
-// group after the other: one sum, in one fixed order.  A wave needs both gradients' sums (D registers
-// each) beside its operands, and two waves a SIMD, for one's matrix products to run beside the other's
-// exponentials: with K in registers, V in LDS and two waves sharing 32 keys (each takes half of a
-// tile's rows; their sums are added at the end) it has 256 registers' room.  (V in registers too:
-// spills, 4.9 instead of 3.3 ms; one wave a SIMD: 3.3.)  Rows of 512 bytes (fp32, 128 dimensions) do not
-// fit so: four waves, one a SIMD, everything in registers.
+// group after the other: one sum, in one fixed order.  Two waves share 32 keys (each takes half of a
+// tile's rows; their sums are added at the end), two a SIMD, for one's products to run beside the
+// other's exponentials.  That leaves 256 registers a wave: at head dim 128 both gradients' sums take
+// 128 of them, and the keys' own rows of K and V are read from LDS with every tile (V in registers spills, and
+// its reloads wait for the next tile as well: 2.6 instead of 1.8 ms; K's half makes no difference);
+// at head dim 64 they stay in registers (0.76 instead of 0.85 ms for 8,192 rows of 32 heads).  fp32 rows of 512
+// bytes do not fit either way: four waves, one a SIMD, everything in registers.
 template <typename T, int D>
 struct KeyShape {
     static constexpr bool kWide = Tile<T, D>::RB <= 256;

@@ -2,7 +2,8 @@
 // `until`).  Eviction keeps a few rows of every unit, so that a tile of 64 consecutive keys is
 // never quite dead: sorted into lasting and passing keys, what a block of queries sees is two
 // dense runs, and the kernels skip the rest (a ten-minute session with a budget of 4,096 rows: 52 %
-// of the pairs of a causal triangle).  The copies cost two passes over K and V.
+// of the pairs of a causal triangle).  That costs a launch of one workgroup a sequence (17 us there, 5 for
+// 3,000 rows) and one that copies K and V (28 us there).
 #include "prompt_device.h"
 
 namespace a2t {
@@ -13,7 +14,7 @@ constexpr int kScanThreads = 1024;
 constexpr int kCopyRows = 16;    // rows of a copying workgroup
 
 // One workgroup a sequence: counts of lasting keys and reach of the passing ones, by place.  A thread
-// takes neighbouring places, so that the threads meet once (13,200 rows: 20 us with a meeting every 1,024).
+// takes neighbouring places, so that the threads meet once.
 template <int N>
 __global__ __launch_bounds__(kScanThreads) void prompt_scan_kernel(SortArgs a, SeqTable<N> t) {
     constexpr int kWaves = kScanThreads / 64;

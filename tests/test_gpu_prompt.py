@@ -122,7 +122,7 @@ def test_against_oracle(gpu, monkeypatch, lengths, hq, hkv, d, until, dtype):
 
 @pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 64)])
 @pytest.mark.parametrize("until", ["window", "nothing"])
-@pytest.mark.parametrize("sort,splits", [(512, 0), (1, 0), (1, 3), (512, 16)])
+@pytest.mark.parametrize("sort,splits", [(1 << 20, 0), (1, 0), (1, 3), (1 << 20, 16)])
 def test_other_masks(gpu, monkeypatch, sort, splits, until, dtype, d):
     """A sliding window, and rows that see nothing at all, with keys sorted or as they are and blocks split or not."""
     import paper_2609_31224_amd as a2t

@@ -31,7 +31,7 @@ def test_rope_create(kw):
 
 @pytest.mark.parametrize("args,kw", [((0, 4, 2, 64, 1), {}), ((8, 4, 0, 64, 1), {}), ((8, 6, 4, 64, 1), {}), ((8, 4, 2, 80, 1), {}), ((8, 4, 2, 64, 3), {}),
                                      ((8, 4, 2, 64, 1), dict(flags=4)), ((8, 4, 2, 64, 1), dict(attn_scale=1e-9)), ((8, 4, 2, 64, 1), dict(attn_scale=float("inf"))),
-                                     ((2**30 + 1, 1, 1, 64, 1), {}), ((2**31 - 1, 2**31 - 1, 1, 64, 1), {}), ((8, 258, 2, 64, 1), {})])
+                                     ((2**26 + 1, 1, 1, 64, 1), {}), ((2**26, 16, 1, 64, 1), {}), ((8, 4097, 4097, 64, 1), {}), ((2**31 - 1, 2**31 - 1, 1, 64, 1), {}), ((8, 258, 2, 64, 1), {})])
 def test_prompt_create(args, kw):
     assert _status(a2t.a2t_prompt_create, *args, **kw) == INVALID
 
