@@ -613,7 +613,7 @@ __global__ __launch_bounds__((64 * KeyShape<T, D>::kWaves), (KeyShape<T, D>::kWi
     int2 me = {key, n};
     if constexpr (UNTIL) {
         me = key_place(a.kv, row0, key);
-        me.y = min(me.y, n);
+        me.y = max(min(me.y, n), 0);   // any number is allowed: differences of places stay within 32 bits
     }
     int j_min = me.x, j_max = me.x, u_min = me.y, u_max = me.y;
 #pragma unroll

@@ -140,6 +140,29 @@ def test_other_masks(gpu, monkeypatch, sort, splits, until, dtype, d):
         a2t.a2t_prompt_destroy(h)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("sort,splits", [(1 << 20, 0), (1, 0), (1, 4), (1 << 20, 3)])
+def test_until_of_any_value(gpu, monkeypatch, sort, splits, dtype, d):
+    """The least and the largest 32-bit places: whole blocks of keys that were gone long before the first row (the
+    difference to a later place passes 32 bits), and both among others."""
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_PROMPT_SORT", str(sort))
+    monkeypatch.setenv("A2T_PROMPT_SPLITS", str(splits))
+    lengths = [300, 1, 266]
+    q, k, v, do, _ = _case(lengths, 4, 2, d, dtype, None, seed=3)
+    low, high = -2 ** 31, 2 ** 31 - 1
+    last = np.resize(np.array([low, high, -1, 150, low + 1, 267, low + 130], np.int64), 266)
+    last[:140] = low
+    ut = np.concatenate([np.full(300, low), [low], last]).astype(np.int32)
+    h = a2t.a2t_prompt_create(600, 4, 2, d, a2t.A2T_F32 if dtype == "f32" else a2t.A2T_BF16, flags=a2t.A2T_PROMPT_UNTIL)
+    try:
+        got = _run(h, lengths, q, k, v, do, ut)
+        _check(got, lengths, q, k, v, do, ut, dtype)
+        assert not any(got[c][:301].any() for c in ("o", "dq", "dk", "dv")) and (got["lse"][:, :301] == -np.inf).all()
+    finally:
+        a2t.a2t_prompt_destroy(h)
+
+
 @pytest.mark.parametrize("groups,scale", [(128, 0.0), (16, 0.02), (5, 1.0)])
 def test_wide_groups_and_scales(gpu, groups, scale):
     """Many query heads on one KV head (a row of keys has 128 packed queries), scales other than the default."""
