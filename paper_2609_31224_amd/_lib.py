@@ -529,14 +529,20 @@ def _torch_dtype(dtype: int):
     return torch.float32 if dtype == A2T_F32 else torch.bfloat16
 
 
-def _rows(x, what: str, dtype, heads: Optional[int], dim: int, n: Optional[int] = None):
+def _on(x, what: str, device: int) -> None:
+    """x lives on the handle's GPU: another's memory may be out of its reach."""
+    if x.get_device() != device:
+        where = f" of its handle ({device}), not {x.get_device()}" if x.is_cuda else ""
+        raise ValueError(f"{what}: tensor must live on the GPU{where}")
+
+
+def _rows(x, what: str, dtype, device: int, heads: Optional[int], dim: int, n: Optional[int] = None):
     """(address, row stride) of a GPU tensor [rows][heads][dim] whose rows are dense; the rows may
     be parts of wider ones.  Sizes that do not fit are a ValueError."""
     import torch
     if not isinstance(x, torch.Tensor):
         raise TypeError(f"{what}: expected a GPU torch tensor")
-    if not x.is_cuda:
-        raise ValueError(f"{what}: tensor must live on the GPU")
+    _on(x, what, device)
     if x.dtype != dtype:
         raise ValueError(f"{what}: dtype {x.dtype}, the handle uses {dtype}")
     if x.dim() != 3 or x.shape[2] != dim or (heads is not None and x.shape[1] != heads) or (n is not None and x.shape[0] != n):
@@ -548,13 +554,14 @@ def _rows(x, what: str, dtype, heads: Optional[int], dim: int, n: Optional[int] 
     return x.data_ptr(), int(stride)
 
 
-def _flat(x, what: str, dtype, numel: int):
+def _flat(x, what: str, dtype, device: int, numel: int):
     """Address of a contiguous GPU tensor with `numel` elements."""
     if x is None:
         return None
     if isinstance(x, int):
         raise TypeError(f"{what}: expected a GPU torch tensor")
     ptr = _dev(x, what, dtype)
+    _on(x, what, device)
     if x.numel() != numel:
         raise ValueError(f"{what}: {x.numel()} elements, expected {numel}")
     return ptr
@@ -566,6 +573,7 @@ class Rope:
     ptr: C.c_void_p
     head_dim: int
     dtype: int
+    device: int = 0
 
 
 def a2t_rope_create(head_dim: int, dtype: int, rotary_dim: int = 0, layout: int = A2T_ROPE_HALF, theta: float = 0.0,
@@ -575,7 +583,7 @@ def a2t_rope_create(head_dim: int, dtype: int, rotary_dim: int = 0, layout: int 
                           turns_slow, device, 0)
     out = C.c_void_p()
     _check(_lib.a2t_rope_create(C.byref(cfg), _stream_handle(stream), C.byref(out)), "a2t_rope_create")
-    return Rope(out, head_dim, dtype)
+    return Rope(out, head_dim, dtype, device)
 
 
 def a2t_rope_destroy(r: Rope) -> None:
@@ -601,8 +609,10 @@ def a2t_rope_apply(r: Rope, pos, q=None, k=None, q_out=None, k_out=None, grad: b
             args += [0, None, 0, None, 0]
             continue
         heads = int(x.shape[1]) if x.dim() == 3 else None
-        args += [heads or 0, *_rows(x, what, dt, None, r.head_dim, n), *_rows(out, what + "_out", dt, heads, r.head_dim, n)]
-    _check(_lib.a2t_rope_apply(r.ptr, n, _flat(pos, "pos", torch.int32, n), *args, int(bool(grad))), "a2t_rope_apply")
+        args += [heads or 0, *_rows(x, what, dt, r.device, None, r.head_dim, n),
+                 *_rows(out, what + "_out", dt, r.device, heads, r.head_dim, n)]
+    _check(_lib.a2t_rope_apply(r.ptr, n, _flat(pos, "pos", torch.int32, r.device, n), *args, int(bool(grad))),
+           "a2t_rope_apply")
 
 
 @dataclass
@@ -614,6 +624,7 @@ class Prompt:
     n_kv_heads: int
     head_dim: int
     dtype: int
+    device: int = 0
 
 
 def a2t_prompt_create(max_rows: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: int, attn_scale: float = 0.0,
@@ -621,7 +632,7 @@ def a2t_prompt_create(max_rows: int, n_q_heads: int, n_kv_heads: int, head_dim: 
     out = C.c_void_p()
     _check(_lib.a2t_prompt_create(max_rows, n_q_heads, n_kv_heads, head_dim, dtype, attn_scale, flags, device,
                                   _stream_handle(stream), C.byref(out)), "a2t_prompt_create")
-    return Prompt(out, max_rows, n_q_heads, n_kv_heads, head_dim, dtype)
+    return Prompt(out, max_rows, n_q_heads, n_kv_heads, head_dim, dtype, device)
 
 
 def a2t_prompt_destroy(p: Prompt) -> None:
@@ -641,11 +652,16 @@ def _prompt_rows(p: Prompt, seq_rows, q, k, v, until):
     dt = _torch_dtype(p.dtype)
     given = []
     for what, x, heads in (("q", q, p.n_q_heads), ("k", k, p.n_kv_heads), ("v", v, p.n_kv_heads)):
-        given.append(_rows(x, what, dt, heads, p.head_dim))
+        given.append(_rows(x, what, dt, p.device, heads, p.head_dim))
         if x.shape[0] < n:
             raise ValueError(f"{what}: {x.shape[0]} rows, the sequences have {n}")
-    if until is not None and _dev(until, "until", torch.int32) is not None and until.numel() < n:
-        raise ValueError(f"until: {until.numel()} entries, the sequences have {n} rows")
+    if until is not None:
+        if not isinstance(until, torch.Tensor):
+            raise TypeError("until: expected a GPU torch tensor")
+        _dev(until, "until", torch.int32)
+        _on(until, "until", p.device)
+        if until.numel() < n:
+            raise ValueError(f"until: {until.numel()} entries, the sequences have {n} rows")
     return rows, n, dt, given, None if until is None else until.data_ptr()
 
 
@@ -653,6 +669,7 @@ def _packed(x, what: str, dt, p: Prompt, n: int):
     ptr = _dev(x, what, dt)
     if ptr is None or isinstance(x, int):
         raise TypeError(f"{what}: expected a GPU torch tensor")
+    _on(x, what, p.device)
     if x.dim() != 3 or x.shape[0] < n or tuple(x.shape[1:]) != (p.n_q_heads, p.head_dim):
         raise ValueError(f"{what}: shape {tuple(x.shape)}, expected [{n}][{p.n_q_heads}][{p.head_dim}]")
     return ptr
@@ -664,7 +681,7 @@ def a2t_prompt_attn(p: Prompt, seq_rows: Sequence[int], q, k, v, o, lse=None, un
     import torch
     rows, n, dt, given, ut = _prompt_rows(p, seq_rows, q, k, v, until)
     _check(_lib.a2t_prompt_attn(p.ptr, len(rows), _p(rows, C.c_int32), *given[0], *given[1], *given[2], ut,
-                                _packed(o, "o", dt, p, n), _flat(lse, "lse", torch.float32, n * p.n_q_heads)),
+                                _packed(o, "o", dt, p, n), _flat(lse, "lse", torch.float32, p.device, n * p.n_q_heads)),
            "a2t_prompt_attn")
 
 
@@ -675,14 +692,14 @@ def a2t_prompt_attn_grad(p: Prompt, seq_rows: Sequence[int], q, k, v, o, lse, d_
     outs = []
     for what, x, like, (_, stride), heads in (("dq", dq, q, given[0], p.n_q_heads), ("dk", dk, k, given[1], p.n_kv_heads),
                                               ("dv", dv, v, given[2], p.n_kv_heads)):
-        ptr, own = _rows(x, what, dt, heads, p.head_dim)
+        ptr, own = _rows(x, what, dt, p.device, heads, p.head_dim)
         if x.shape[0] < n or (own != stride and n > 1):
             raise ValueError(f"{what}: {x.shape[0]} rows with stride {own}, expected {n} with stride {stride}")
         outs.append(ptr)
     if lse is None:
         raise ValueError("lse: the forward pass's")
     _check(_lib.a2t_prompt_attn_grad(p.ptr, len(rows), _p(rows, C.c_int32), *given[0], *given[1], *given[2], ut,
-                                     _packed(o, "o", dt, p, n), _flat(lse, "lse", torch.float32, n * p.n_q_heads),
+                                     _packed(o, "o", dt, p, n), _flat(lse, "lse", torch.float32, p.device, n * p.n_q_heads),
                                      _packed(d_o, "d_o", dt, p, n), *outs), "a2t_prompt_attn_grad")
 
 
@@ -693,12 +710,13 @@ class Prefer:
     max_rows: int
     vocab: int
     dtype: int
+    device: int = 0
 
 
 def a2t_prefer_create(max_rows: int, vocab: int, dtype: int, device: int = 0, stream=None) -> Prefer:
     out = C.c_void_p()
     _check(_lib.a2t_prefer_create(max_rows, vocab, dtype, device, _stream_handle(stream), C.byref(out)), "a2t_prefer_create")
-    return Prefer(out, max_rows, vocab, dtype)
+    return Prefer(out, max_rows, vocab, dtype, device)
 
 
 def a2t_prefer_destroy(p: Prefer) -> None:
@@ -716,6 +734,7 @@ def _logits(p: Prefer, x, what: str, n: int):
     import torch
     if not isinstance(x, torch.Tensor) or not x.is_cuda:
         raise ValueError(f"{what}: expected a GPU torch tensor")
+    _on(x, what, p.device)
     if x.dtype != _torch_dtype(p.dtype):
         raise ValueError(f"{what}: dtype {x.dtype}, the handle uses {_torch_dtype(p.dtype)}")
     if x.dim() != 2 or x.shape[0] < n or x.shape[1] < p.vocab or x.stride(1) != 1:
@@ -733,8 +752,8 @@ def a2t_prefer_logp(p: Prefer, logits, target, logp) -> None:
     """logits: GPU [rows][stride]; target: GPU int32 [rows]; logp: GPU float32 [rows] out."""
     import torch
     n = int(target.shape[0])
-    _check(_lib.a2t_prefer_logp(p.ptr, n, *_logits(p, logits, "logits", n), _flat(target, "target", torch.int32, n),
-                                _flat(logp, "logp", torch.float32, n)), "a2t_prefer_logp")
+    _check(_lib.a2t_prefer_logp(p.ptr, n, *_logits(p, logits, "logits", n), _flat(target, "target", torch.int32, p.device, n),
+                                _flat(logp, "logp", torch.float32, p.device, n)), "a2t_prefer_logp")
 
 
 def a2t_prefer_loss(p: Prefer, answer_rows: Sequence[int], policy, target, losses, reference=None, ref_logp=None,
@@ -755,6 +774,7 @@ def a2t_prefer_loss(p: Prefer, answer_rows: Sequence[int], policy, target, losse
         if own != stride:
             raise ValueError(f"grad: stride {own}, the policy's is {stride}")
     _check(_lib.a2t_prefer_loss(p.ptr, len(rows) // 2, _p(rows, C.c_int32), ptr, stride, *ref,
-                                _flat(ref_logp, "ref_logp", torch.float32, n), _flat(target, "target", torch.int32, n),
-                                float(beta), float(smoothing), _flat(losses, "losses", torch.float32, 3),
-                                _flat(ratios, "ratios", torch.float32, len(rows)), g), "a2t_prefer_loss")
+                                _flat(ref_logp, "ref_logp", torch.float32, p.device, n),
+                                _flat(target, "target", torch.int32, p.device, n),
+                                float(beta), float(smoothing), _flat(losses, "losses", torch.float32, p.device, 3),
+                                _flat(ratios, "ratios", torch.float32, p.device, len(rows)), g), "a2t_prefer_loss")

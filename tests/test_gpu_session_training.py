@@ -267,3 +267,25 @@ def test_two_sessions_at_once(gpu):
             assert all(torch.equal(j[c], y) for c, y in zip(("o", "lse", "g"), w)), turn
     for j in jobs:
         a2t.a2t_prompt_destroy(j["h"])
+
+
+def test_tensors_of_another_device_than_the_handle(gpu):
+    """Every tensor of a call lies on its handle's GPU (a handle that says it is another's refuses them all)."""
+    import dataclasses
+    import torch
+    import paper_2609_31224_amd as a2t
+    x, i = torch.zeros(4, 2, 64, device="cuda"), torch.zeros(4, dtype=torch.int32, device="cuda")
+    f = torch.zeros(8, device="cuda")
+    rope, prompt, prefer = a2t.a2t_rope_create(64, a2t.A2T_F32), a2t.a2t_prompt_create(4, 2, 2, 64, a2t.A2T_F32), a2t.a2t_prefer_create(4, 64, a2t.A2T_F32)
+    try:
+        other = [dataclasses.replace(h, device=h.device + 1) for h in (rope, prompt, prefer)]
+        for call in (lambda: a2t.a2t_rope_apply(other[0], i, x, None, x), lambda: a2t.a2t_prompt_attn(other[1], [4], x, x, x, x, f),
+                     lambda: a2t.a2t_prompt_attn_grad(other[1], [4], x, x, x, x, f, x, x, x, x),
+                     lambda: a2t.a2t_prefer_logp(other[2], x[:, 0], i, f[:4]),
+                     lambda: a2t.a2t_prefer_loss(other[2], [2, 2], x[:, 0], i, f[:3], ref_logp=f[:4])):
+            with pytest.raises(ValueError, match="of its handle"):
+                call()
+    finally:
+        a2t.a2t_rope_destroy(rope)
+        a2t.a2t_prompt_destroy(prompt)
+        a2t.a2t_prefer_destroy(prefer)

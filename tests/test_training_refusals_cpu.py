@@ -61,3 +61,15 @@ def test_without_a_device_or_a_handle():
     for name in ("rope", "prompt", "prefer"):
         assert getattr(lib, f"a2t_{name}_destroy")(None) == INVALID
         assert getattr(lib, f"a2t_{name}_set_stream")(None, None) == INVALID
+
+
+def test_tensors_in_host_memory():
+    import torch
+    x, i = torch.zeros(4, 2, 64), torch.zeros(4, dtype=torch.int32)
+    f = torch.zeros(8)
+    rope, prompt, prefer = a2t.Rope(C.c_void_p(), 64, a2t.A2T_F32), a2t.Prompt(C.c_void_p(), 4, 2, 2, 64, a2t.A2T_F32), a2t.Prefer(C.c_void_p(), 4, 64, a2t.A2T_F32)
+    for call in (lambda: a2t.a2t_rope_apply(rope, i, x, None, x), lambda: a2t.a2t_prompt_attn(prompt, [4], x, x, x, x, f),
+                 lambda: a2t.a2t_prompt_attn_grad(prompt, [4], x, x, x, x, f, x, x, x, x),
+                 lambda: a2t.a2t_prefer_logp(prefer, x[:, 0], i, f[:4]), lambda: a2t.a2t_prefer_loss(prefer, [2, 2], x[:, 0], i, f[:3], ref_logp=f[:4])):
+        with pytest.raises(ValueError, match="GPU"):
+            call()
