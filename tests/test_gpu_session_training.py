@@ -289,3 +289,50 @@ def test_tensors_of_another_device_than_the_handle(gpu):
         a2t.a2t_rope_destroy(rope)
         a2t.a2t_prompt_destroy(prompt)
         a2t.a2t_prefer_destroy(prefer)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rows_far_apart(gpu, monkeypatch, dtype):
+    """Rows 2^22 elements apart, whose offsets pass 32 bits: what the same rows give side by side, bit for bit."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    monkeypatch.setenv("A2T_PROMPT_SORT", "1")
+    dt = torch.float32 if dtype == "f32" else torch.bfloat16
+    code, n, d, apart = a2t.A2T_F32 if dtype == "f32" else a2t.A2T_BF16, 600, 64, 2 ** 22
+    gen = torch.Generator("cuda").manual_seed(5)
+    wide = torch.empty((n, apart // d, d), dtype=dt, device="cuda")      # 5 GB, 10 in fp32
+    dense = torch.randn((n, 8, d), device="cuda", generator=gen).to(dt)
+    wide[:, :8] = dense
+    until = (torch.arange(n, device="cuda") + 130 + 900 * (torch.arange(n, device="cuda") % 3 == 0)).to(torch.int32)
+    pos = torch.arange(n, dtype=torch.int32, device="cuda")
+    do = torch.randn((n, 4, d), device="cuda", generator=gen).to(dt)
+    rope = a2t.a2t_rope_create(d, code)
+    prompt = a2t.a2t_prompt_create(n, 4, 2, d, code, flags=a2t.A2T_PROMPT_UNTIL)
+    prefer = a2t.a2t_prefer_create(n, 8 * d, code)
+    try:
+        results = []
+        for x in (dense, wide):
+            q, k, v = x[:, :4], x[:, 4:6], x[:, 6:8]
+            a2t.a2t_rope_apply(rope, pos, q, k, q, k)
+            if x is dense:   # gradients have the strides of q, k and v
+                grads = [torch.empty_like(x)[:, :heads] for heads in (4, 2, 2)]
+            else:
+                grads = wide[:, 16:20], wide[:, 20:22], wide[:, 22:24]
+            got = [x[:, :8]]
+            for ut in (None, until):
+                for g in grads:
+                    g.fill_(7.0)
+                o, lse = torch.empty((n, 4, d), dtype=dt, device="cuda"), torch.empty((4, n), device="cuda")
+                a2t.a2t_prompt_attn(prompt, [17, n - 17], q, k, v, o, lse, ut)
+                a2t.a2t_prompt_attn_grad(prompt, [17, n - 17], q, k, v, o, lse, do, *grads, ut)
+                got += [o, lse] + [g.clone() for g in grads]
+            logp = torch.empty(n, device="cuda")
+            a2t.a2t_prefer_logp(prefer, x.view(n, -1), pos % (8 * d), logp)
+            torch.cuda.synchronize()
+            results.append(got + [logp])
+        for a, b in zip(*results):
+            assert torch.isfinite(a).all() and torch.equal(a, b)
+    finally:
+        a2t.a2t_rope_destroy(rope)
+        a2t.a2t_prompt_destroy(prompt)
+        a2t.a2t_prefer_destroy(prefer)
