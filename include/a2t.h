@@ -705,7 +705,10 @@ int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows,
  *   ratio_a = sum over the answer's rows of ln p_policy(target) - ln p_reference(target),
  *   h_p = beta (ratio_2p - ratio_2p+1),
  *   L = mean_p -(1 - smoothing) ln sigma(h_p) - smoothing ln sigma(-h_p).
- * A row whose target is outside [0, vocab) takes no part: ratio 0, zero gradient. */
+ * A row whose target is outside [0, vocab) takes no part: ratio 0, zero gradient.
+ * Logits may be -infinity; a target of such a logit makes its answer's ratio and h
+ * infinite, and a term of L whose weight is 0 is left out whatever h is (pairs with such
+ * targets in both answers, or in the policy and the reference, have no value: NaN). */
 #define A2T_PREFER_MAX_PAIRS 256
 
 typedef struct a2t_prefer a2t_prefer;

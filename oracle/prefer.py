@@ -43,7 +43,8 @@ def prefer_loss(answer_rows, policy, target, reference=None, ref_logp: Optional[
     answer = np.repeat(np.arange(len(rows)), rows)
     ratios = np.bincount(answer, diff, minlength=len(rows))
     h = beta * (ratios[0::2] - ratios[1::2])
-    loss = ((1 - smoothing) * np.logaddexp(0, -h) + smoothing * np.logaddexp(0, h)).mean()
+    # a term without weight is left out, also where h is infinite (a target whose logit is -infinity)
+    loss = sum((w * np.logaddexp(0, x) if w > 0 else np.zeros(len(h))) for w, x in ((1 - smoothing, -h), (smoothing, h))).mean()
     # d ln sigma(h) / dh = sigma(-h)
     with np.errstate(over="ignore"):
         up, down = 1 / (1 + np.exp(h)), 1 / (1 + np.exp(-h))

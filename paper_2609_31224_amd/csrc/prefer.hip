@@ -218,6 +218,9 @@ __device__ __forceinline__ double answer_ratio(const GradArgs<T>& a, int lo, int
 // ln(1 / (1 + e^-h))
 __device__ __forceinline__ double log_sigmoid(double h) { return fmin(h, 0.0) - log1p(exp(-fabs(h))); }
 __device__ __forceinline__ double sigmoid(double h) { return 1.0 / (1.0 + exp(-h)); }
+// weight times term; a term without weight is left out, also where it is infinite (a target whose logit
+// is -infinity makes h infinite)
+__device__ __forceinline__ double weigh(double weight, double term) { return weight > 0.0 ? weight * term : 0.0; }
 
 template <typename T, int TH>
 __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
@@ -231,7 +234,7 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
             const double good = answer_ratio<WIDTH>(a, a.start[2 * p], a.start[2 * p + 1]);
             const double poor = answer_ratio<WIDTH>(a, a.start[2 * p + 1], a.start[2 * p + 2]);
             const double h = a.beta * (good - poor);
-            loss -= (1.0 - a.smoothing) * log_sigmoid(h) + a.smoothing * log_sigmoid(-h);
+            loss -= weigh(1.0 - a.smoothing, log_sigmoid(h)) + weigh(a.smoothing, log_sigmoid(-h));
             margin += h;
             won += h > 0.0 ? 1.0 : 0.0;
             if (a.ratios && tid % WIDTH == 0) {
