@@ -6,13 +6,16 @@
 //   prefer_grad_kernel  one workgroup per policy row: the sums of the row's pair, the slope
 //                       of the loss, and the gradient slope (p_v - [v = target]); one more
 //                       workgroup writes the loss and every answer's ratio.
+//   prefer_ratio_kernel one workgroup per answer between the two, where answers are long.
 // The slope of a row depends on all rows of its pair, so the policy's logits are read twice.
-// Every workgroup adds a pair's rows by itself, in the same order (deterministic, and one
-// launch less), in 64 bits: a ratio is a small difference of large sums.
+// Sums of short answers are formed by every workgroup for its own pair, in the same order
+// (deterministic, and one launch less), in 64 bits: a ratio is a small difference of large sums.
+// That is work that grows with the square of an answer's rows: those of long ones are formed once.
 #include "../../include/a2t.h"
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -26,6 +29,12 @@ constexpr int kAnswers = 2 * kMaxPairs;
 // Policy logits that the gradient still finds in the caches when it comes back to them, last rows
 // first (the memory-side cache holds 256 MiB).
 constexpr int64_t kKeepBytes = 160ll << 20;
+constexpr int kRatioThreads = 1024;
+// Rows of a call's longest answer from which ratios are formed in a launch of their own.  (That against
+// every workgroup for itself, one pair: with gradient, 64 rows of 32,000 bf16 logits 15.8 against 15.4 us,
+// 128 rows 16.6 against 20.0, 1,024 rows 70 against 121; without, 64 rows 9.6 against 11.9 and 16 rows 9.4
+// against 9.0.)
+constexpr int kLongRows = 96;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
@@ -193,6 +202,7 @@ struct GradArgs {
     int64_t stride;
     const RowStat* stat;      // [2][n]
     const float* ref_logp;    // [n], or null: the reference's rows are in stat
+    double* sums;             // [2 pairs] ratios that prefer_ratio_kernel has formed, or null
     const int32_t* target;
     float* losses;            // [3]
     float* ratios;            // [2 pairs], or null
@@ -202,18 +212,40 @@ struct GradArgs {
     int32_t start[kAnswers + 1];   // first row of each answer
 };
 
-// Sum over rows lo .. hi - 1 of ln p_policy - ln p_reference, by WIDTH lanes that all get it.
-template <int WIDTH, typename T>
-__device__ __forceinline__ double answer_ratio(const GradArgs<T>& a, int lo, int hi) {
+// ln p_policy - ln p_reference of a row's target, summed over rows first, first + step, .. < end.
+template <typename T>
+__device__ __forceinline__ double rows_ratio(const GradArgs<T>& a, int first, int end, int step) {
     double r = 0.0;
-    for (int i = lo + (int)(threadIdx.x % WIDTH); i < hi; i += WIDTH) {
+    for (int i = first; i < end; i += step) {
         const int t = a.target[i];
         const double p = a.stat[i].logp, q = a.ref_logp ? (double)a.ref_logp[i] : a.stat[a.n + i].logp;
         r += t >= 0 && t < a.vocab ? p - q : 0.0;
     }
+    return r;
+}
+// The ratio of answer k, by WIDTH lanes that all get it.
+template <int WIDTH, typename T>
+__device__ __forceinline__ double answer_ratio(const GradArgs<T>& a, int k) {
+    if (a.sums) return a.sums[k];
+    double r = rows_ratio(a, a.start[k] + (int)(threadIdx.x % WIDTH), a.start[k + 1], WIDTH);
 #pragma unroll
     for (int d = 1; d < WIDTH; d *= 2) r += __shfl_xor(r, d);
     return r;
+}
+// The ratio of a long answer, once: every workgroup of the gradient would walk all of its pair's rows
+// (a pair of 4,096 rows an answer, 151,938 bf16 logits: 1,917 us, 1,373 so; 997 logits: 238 us, 36 so).
+template <typename T>
+__global__ __launch_bounds__(kRatioThreads) void prefer_ratio_kernel(GradArgs<T> a) {
+    const int tid = threadIdx.x, k = blockIdx.x;
+    __shared__ double part[kRatioThreads / 64];
+    double r = rows_ratio(a, a.start[k] + tid, a.start[k + 1], kRatioThreads);
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) r += __shfl_xor(r, d);
+    if (tid % 64 == 0) part[tid / 64] = r;
+    __syncthreads();
+    if (tid) return;
+    for (int w = 1; w < kRatioThreads / 64; ++w) r += part[w];
+    a.sums[k] = r;
 }
 // ln(1 / (1 + e^-h))
 __device__ __forceinline__ double log_sigmoid(double h) { return fmin(h, 0.0) - log1p(exp(-fabs(h))); }
@@ -231,8 +263,7 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
         const int group = tid / WIDTH;
         double loss = 0.0, margin = 0.0, won = 0.0;
         for (int p = group; p < a.pairs; p += GROUPS) {
-            const double good = answer_ratio<WIDTH>(a, a.start[2 * p], a.start[2 * p + 1]);
-            const double poor = answer_ratio<WIDTH>(a, a.start[2 * p + 1], a.start[2 * p + 2]);
+            const double good = answer_ratio<WIDTH>(a, 2 * p), poor = answer_ratio<WIDTH>(a, 2 * p + 1);
             const double h = a.beta * (good - poor);
             loss -= weigh(1.0 - a.smoothing, log_sigmoid(h)) + weigh(a.smoothing, log_sigmoid(-h));
             margin += h;
@@ -263,8 +294,7 @@ __global__ __launch_bounds__(TH) void prefer_grad_kernel(GradArgs<T> a) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) before += __shfl_xor(before, d);
         const int answer = before - 1, p = answer / 2;
-        const double good = answer_ratio<64>(a, a.start[2 * p], a.start[2 * p + 1]);
-        const double poor = answer_ratio<64>(a, a.start[2 * p + 1], a.start[2 * p + 2]);
+        const double good = answer_ratio<64>(a, 2 * p), poor = answer_ratio<64>(a, 2 * p + 1);
         const double h = a.beta * (good - poor);
         // -dL/d(good): L falls as the chosen answer's ratio grows
         const double c = a.beta * ((1.0 - a.smoothing) * sigmoid(-h) - a.smoothing * sigmoid(h)) / a.pairs;
@@ -326,6 +356,7 @@ struct a2t_prefer {
     int32_t max_rows = 0, vocab = 0, dtype = 0, device = 0;
     hipStream_t stream = nullptr;
     RowStat* stat = nullptr;   // [2][max_rows]
+    double* sums = nullptr;    // [kAnswers] ratios of a call with long answers
     int cus = 256;
     bool poisoned = false;
 };
@@ -368,8 +399,9 @@ extern "C" int a2t_prefer_create(int32_t max_rows, int32_t vocab, int32_t dtype,
     p->stream = static_cast<hipStream_t>(hip_stream);
     int cus = 0;
     if (hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device) == hipSuccess && cus > 0) p->cus = cus;
-    if (hipMalloc(&p->stat, sizeof(RowStat) * 2 * (size_t)max_rows) != hipSuccess) {
+    if (hipMalloc(&p->stat, sizeof(RowStat) * 2 * (size_t)max_rows) != hipSuccess || hipMalloc(&p->sums, sizeof(double) * kAnswers) != hipSuccess) {
         (void)hipGetLastError();
+        (void)hipFree(p->stat);
         delete p;
         return A2T_ERR_OOM;
     }
@@ -383,6 +415,7 @@ extern "C" int a2t_prefer_destroy(a2t_prefer* p) {
         DevGuard g(p->device);
         (void)hipStreamSynchronize(p->stream);
         (void)hipFree(p->stat);
+        (void)hipFree(p->sums);
     }
     delete p;
     return A2T_OK;
@@ -451,6 +484,12 @@ extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* an
         a.beta = beta;
         a.smoothing = smoothing;
         for (int i = 0; i < 2 * n_pairs; ++i) a.start[i + 1] = a.start[i] + answer_rows[i];
+        if (*std::max_element(answer_rows, answer_rows + 2 * n_pairs) >= kLongRows) {
+            a.sums = p->sums;
+            hipLaunchKernelGGL((prefer_ratio_kernel<T>), dim3(2 * n_pairs), dim3(kRatioThreads), 0, p->stream, a);
+            e = hipGetLastError();
+            if (e != hipSuccess) return e;
+        }
         const dim3 grid(grad ? (uint32_t)n + 1 : 1);
         if (!grad || wide_rows(p, n)) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
         else hipLaunchKernelGGL((prefer_grad_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
