@@ -741,6 +741,8 @@ def _logits(p: Prefer, x, what: str, n: int):
         raise ValueError(f"{what}: shape {tuple(x.shape)}, expected [{n}][{p.vocab} or more] with dense rows")
     if x.stride(0) < x.shape[1] and x.shape[0] > 1:
         raise ValueError(f"{what}: rows overlap")
+    if what == "grad" and x.stride(0) > (x.shape[1] + 7) // 8 * 8:
+        raise ValueError(f"grad: columns {x.shape[1]} to {x.stride(0)} of its rows would be zeroed: pass them, or a tensor of its own")
     # the last row is read (and the gradient's written) in whole chunks of 8 elements up to its stride
     room = x.untyped_storage().nbytes() // x.element_size() - x.storage_offset()
     if room < (n - 1) * x.stride(0) + (x.stride(0) if what == "grad" else (p.vocab + 7) // 8 * 8):
@@ -760,7 +762,8 @@ def a2t_prefer_loss(p: Prefer, answer_rows: Sequence[int], policy, target, losse
                     beta: float = 0.1, smoothing: float = 0.0, ratios=None, grad=None) -> None:
     """answer_rows: host, rows of the chosen and the rejected answer of each pair in turn; policy,
     reference: GPU [rows][stride] logits; losses: GPU float32 [3]; ratios: GPU float32, one per answer;
-    grad: GPU tensor like policy (or policy itself)."""
+    grad: GPU tensor like policy (or policy itself), zeroed from the vocabulary up to its rows' stride: a
+    view of some columns of wider rows is a ValueError."""
     import torch
     rows = _i32(answer_rows)
     if rows.ndim != 1 or len(rows) % 2:

@@ -1,4 +1,5 @@
-"""The preference loss at the ends of its range: targets of logits that are -infinity."""
+"""The preference loss at the ends of its range: targets of logits that are -infinity, gradients that are
+part of wider rows."""
 import numpy as np
 import pytest
 
@@ -39,5 +40,36 @@ def test_targets_without_weight(gpu, row, smoothing):
         else:
             assert abs(got[0] - want.loss) <= 2.0 ** -17 + 2.0 ** -23 * want.loss
         assert (np.abs(grad.cpu().double().numpy() - want.grad) <= 2.0 ** -18).all()
+    finally:
+        a2t.a2t_prefer_destroy(h)
+
+
+def test_a_part_of_wider_rows_takes_no_gradient(gpu):
+    """Columns beside the gradient's tensor would be zeroed: such a view is refused and nothing is written, while the
+    rows with all their columns, a tensor of the vocabulary's columns, and views as inputs are taken."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    vocab, rows = 60, [3, 2]
+    h = a2t.a2t_prefer_create(5, vocab, a2t.A2T_F32)
+    wide = torch.full((5, 128), 7.0, device="cuda")
+    target, lp = torch.zeros(5, dtype=torch.int32, device="cuda"), torch.full((5,), -4.0, device="cuda")
+    losses = torch.full((3,), 7.0, device="cuda")
+    view = wide[:, :vocab]
+    try:
+        for policy, grad in ((torch.zeros((5, 128), device="cuda"), view), (view, view), (torch.zeros((5, 128), device="cuda"), wide[:, :119]),
+                             (torch.zeros((1, 128), device="cuda"), wide[:1, :vocab])):
+            with pytest.raises(ValueError, match="zeroed"):
+                a2t.a2t_prefer_loss(h, rows if len(policy) == 5 else [1, 0], policy, target[:len(policy)], losses, ref_logp=lp[:len(policy)], grad=grad)
+        torch.cuda.synchronize()
+        assert (wide == 7).all() and (losses == 7).all()
+        a2t.a2t_prefer_loss(h, rows, view, target, losses, ref_logp=lp)
+        a2t.a2t_prefer_loss(h, rows, view, target, losses, ref_logp=lp, grad=torch.empty((5, 128), device="cuda"))
+        torch.cuda.synchronize()
+        assert (wide == 7).all() and torch.isfinite(losses).all()
+        close = torch.full((5, 64), 7.0, device="cuda")
+        a2t.a2t_prefer_loss(h, rows, close, target, losses, ref_logp=lp, grad=close[:, :vocab])
+        a2t.a2t_prefer_loss(h, rows, wide, target, losses, ref_logp=lp, grad=wide)
+        torch.cuda.synchronize()
+        assert not wide[:, vocab:].any() and not close[:, vocab:].any() and torch.equal(wide[:, :vocab], close[:, :vocab])
     finally:
         a2t.a2t_prefer_destroy(h)
