@@ -686,15 +686,18 @@ int a2t_prompt_set_stream(a2t_prompt* p, void* hip_stream);
  *   until     device int32 [rows] or NULL
  *   o         device [rows][Hq][D] out
  *   lse       device float [Hq][rows] out (natural logarithm), or NULL
- * Errors: INVALID (sizes, strides, alignment, `until` without A2T_PROMPT_UNTIL), HIP. */
+ * o and lse overlap neither each other nor an input, but o may be q itself (of stride Hq * D).
+ * Errors: INVALID (sizes, strides, alignment, `until` without A2T_PROMPT_UNTIL, outputs that
+ * overlap), HIP. */
 int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows, const void* q, int64_t q_stride,
                     const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* until,
                     void* o, float* lse);
 
 /* Gradients from that of o.  Inputs as in the forward pass, o and lse as it
  * left them, d_o device [rows][Hq][D]; dq, dk, dv device out, rows at the
- * strides of q, k and v (they may be parts of one tensor; they overlap no
- * input).  Errors: as above. */
+ * strides of q, k and v.  They may be parts of one tensor; they overlap neither
+ * each other nor an input, but dk may be k itself, dv v, and dq o (where q's stride
+ * is Hq * D).  Errors: as above. */
 int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows, const void* q, int64_t q_stride,
                          const void* k, int64_t k_stride, const void* v, int64_t v_stride, const int32_t* until,
                          const void* o, const float* lse, const void* d_o, void* dq, void* dk, void* dv);

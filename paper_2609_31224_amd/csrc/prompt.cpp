@@ -1,6 +1,7 @@
 // Host side of the attention over packed sequences (a2t_prompt_* of include/a2t.h): argument
 // checks, the table of sequences that a launch carries, and the launches.
 #include "../../include/a2t.h"
+#include "overlap.h"
 #include "prompt.h"
 
 #include <hip/hip_runtime.h>
@@ -83,6 +84,33 @@ int64_t total_rows(const a2t_prompt* p, int32_t n_seqs, const int32_t* seq_rows)
 bool bad_rows(const a2t_prompt* p, const void* x, int64_t stride, int heads) {
     return !x || misaligned(x, 16) || stride < (int64_t)heads * p->D || stride % 8 || stride > (1 << 22);
 }
+
+// A call's outputs and inputs in memory.  Every output is written while other workgroups, or a later
+// launch of the call, still read the inputs: they must not touch each other, but for an output that is
+// `in_place` of an input, row for row, where whoever reads a row is who writes it (or was a launch before).
+struct Memory {
+    const a2t_prompt* p;
+    int64_t total;
+    a2t::Rows out[3], in[7];
+    int outs = 0, ins = 0;
+    a2t::Rows rows(const void* x, int64_t stride, int heads) const {
+        const int64_t size = p->dtype == A2T_F32 ? 4 : 2;
+        return {x, total, (int64_t)heads * p->D * size, stride * size};
+    }
+    a2t::Rows packed(const void* x) const { return rows(x, (int64_t)p->Hq * p->D, p->Hq); }
+    a2t::Rows floats(const void* x, int64_t n) const { return a2t::run_of(x, n * 4); }
+    bool clash(const void* const (&in_place)[3]) const {
+        for (int i = 0; i < outs; ++i) {
+            for (int j = 0; j < i; ++j)
+                if (a2t::overlap(out[i], out[j])) return true;
+            for (int j = 0; j < ins; ++j) {
+                if (in[j].p == in_place[i] && in[j].p == out[i].p && in[j].stride == out[i].stride) continue;
+                if (a2t::overlap(out[i], in[j])) return true;
+            }
+        }
+        return false;
+    }
+};
 
 // Calls f with tables of at most kMaxSeqs sequences, longest first (the launch's last workgroups
 // are short ones); sequences without rows take no part.
@@ -263,6 +291,11 @@ extern "C" int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq
     if (!total || bad_rows(p, q, q_stride, p->Hq) || bad_rows(p, k, k_stride, p->Hkv) || bad_rows(p, v, v_stride, p->Hkv) || !o ||
         misaligned(o, 16) || misaligned(lse, 4) || misaligned(until, 4) || (until && !p->until))
         return A2T_ERR_INVALID;
+    Memory m{p, total};
+    for (const a2t::Rows& x : {m.rows(q, q_stride, p->Hq), m.rows(k, k_stride, p->Hkv), m.rows(v, v_stride, p->Hkv), m.floats(until, total)})
+        m.in[m.ins++] = x;
+    for (const a2t::Rows& x : {m.packed(o), m.floats(lse, total * p->Hq)}) m.out[m.outs++] = x;
+    if (m.clash({q, nullptr, nullptr})) return A2T_ERR_INVALID;   // a block reads its queries before its first tile
     DevGuard g(p->device);
     const bool sorted = until && sort_pays(p, n_seqs, seq_rows);
     Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until, sorted);
@@ -293,6 +326,14 @@ extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t
         !d_o || !dq || !dk || !dv || misaligned(o, 16) || misaligned(lse, 4) || misaligned(d_o, 16) || misaligned(dq, 16) ||
         misaligned(dk, 16) || misaligned(dv, 16) || misaligned(until, 4) || (until && !p->until))
         return A2T_ERR_INVALID;
+    Memory m{p, total};
+    for (const a2t::Rows& x : {m.rows(q, q_stride, p->Hq), m.rows(k, k_stride, p->Hkv), m.rows(v, v_stride, p->Hkv), m.floats(until, total),
+                               m.packed(o), m.floats(lse, total * p->Hq), m.packed(d_o)})
+        m.in[m.ins++] = x;
+    for (const a2t::Rows& x : {m.rows(dq, q_stride, p->Hq), m.rows(dk, k_stride, p->Hkv), m.rows(dv, v_stride, p->Hkv)}) m.out[m.outs++] = x;
+    // O is read by the rows' own blocks before their first tile; K and V by all blocks of the launch for dQ,
+    // then by the keys' own alone
+    if (m.clash({o, k, v})) return A2T_ERR_INVALID;
     DevGuard g(p->device);
     const bool sorted = until && sort_pays(p, n_seqs, seq_rows);
     Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until, sorted);
