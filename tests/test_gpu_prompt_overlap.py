@@ -50,12 +50,15 @@ def test_refusals(gpu):
     import paper_2609_31224_amd as a2t
     lib, n = a2t.raw_lib(), 24
     h = a2t.a2t_prompt_create(n, 4, 2, 64, a2t.A2T_BF16, flags=a2t.A2T_PROMPT_UNTIL)
-    wide = torch.randn((n, 32, 64), device="cuda").to(torch.bfloat16)      # operands side by side, 2,048 elements a row
+    # operands side by side, 2,048 elements a row, and others far from each other: every call below stays within the room
+    room = torch.zeros((16 * n, 32, 64), dtype=torch.bfloat16, device="cuda")
+    wide, S = room[4 * n:5 * n], 2048
+    wide.copy_(torch.randn(wide.shape, device="cuda"))
     keep = wide.clone()
-    S = 2048
     part = lambda head: wide.data_ptr() + head * 64 * 2  # noqa: E731
-    o, do, dq = (torch.zeros((n, 4, 64), dtype=torch.bfloat16, device="cuda") for _ in range(3))
-    lse, ut = torch.zeros((4, n), device="cuda"), torch.full((n,), n, dtype=torch.int32, device="cuda")
+    o, do, dq = (room[i * n:(i + 1) * n].view(-1)[:n * 256].view(n, 4, 64) for i in (8, 9, 10))
+    lse, ut = (room[i * n:(i + 1) * n].view(-1).view(t)[:size].view(shape) for i, t, size, shape in ((11, torch.float32, 4 * n, (4, n)), (12, torch.int32, n, (n,))))
+    ut.fill_(n)
     rows = (C.c_int32 * 2)(20, 4)
     base = dict(q=part(0), qs=S, k=part(4), v=part(6), until=ut.data_ptr(), o=o.data_ptr(), lse=lse.data_ptr())
 
