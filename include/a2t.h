@@ -628,12 +628,12 @@ int a2t_rope_set_stream(a2t_rope* r, void* hip_stream);
 /* Rotates n_rows rows (1 .. 2^26) of queries and keys in one launch; either may be NULL.
  *   pos          device int32 [n_rows]
  *   q, k         rows of q_heads, k_heads heads (4,096 together at most)
- *   q_out, k_out outputs: the input itself (in place, at the same stride), or memory
- *                that overlaps no input
+ *   q_out, k_out outputs: q, k itself (in place, at the same stride), or memory
+ *                that overlaps neither an input nor the other output
  *   grad         nonzero: the gradient of the inputs from that of the outputs
  *                (angles -a)
- * Errors: INVALID (sizes, strides, alignment, an output that partly overlaps
- * its input), HIP. */
+ * Errors: INVALID (sizes, strides, alignment, an output that overlaps an input
+ * otherwise, or the other output), HIP. */
 int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, int32_t q_heads, const void* q,
                    int64_t q_stride, void* q_out, int64_t q_out_stride, int32_t k_heads, const void* k,
                    int64_t k_stride, void* k_out, int64_t k_out_stride, int32_t grad);

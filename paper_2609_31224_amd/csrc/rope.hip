@@ -11,9 +11,11 @@
 // time (two 16-byte chunks of bf16) of one head after the other, so that the 64-bit
 // arithmetic is shared by all heads of a row.
 #include "../../include/a2t.h"
+#include "overlap.h"
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <new>
@@ -257,21 +259,19 @@ extern "C" int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, i
         return A2T_ERR_INVALID;
     auto bad = [&](int heads, const void* in, int64_t is, const void* out, int64_t os) {
         if (!heads) return false;
-        const uintptr_t a = reinterpret_cast<uintptr_t>(in), b = reinterpret_cast<uintptr_t>(out);
-        if (!out || ((a | b) & 15u) || is < (int64_t)heads * D || os < (int64_t)heads * D || is % 8 || os % 8 ||
-            is > (1ll << 40) || os > (1ll << 40))
-            return true;
-        // in place means the same rows; any other overlap would be a race
-        const uintptr_t na = (uintptr_t)((n_rows - 1) * is + (int64_t)heads * D) * size;
-        const uintptr_t nb = (uintptr_t)((n_rows - 1) * os + (int64_t)heads * D) * size;
-        if (a == b) return is != os;
-        if (is == os) {   // the same rows of one buffer, other channels: no row touches another
-            const uintptr_t gap = (a > b ? a - b : b - a) % (uintptr_t)(is * size), row = (uintptr_t)heads * D * size;
-            if (gap >= row && gap + row <= (uintptr_t)(is * size)) return false;
-        }
-        return a < b + nb && b < a + na;
+        return !out || (((uintptr_t)in | (uintptr_t)out) & 15u) || is < (int64_t)heads * D || os < (int64_t)heads * D || is % 8 || os % 8 ||
+               std::max(is, os) > (1ll << 56) / n_rows;
     };
     if (bad(q_heads, q, q_stride, q_out, q_out_stride) || bad(k_heads, k, k_stride, k_out, k_out_stride)) return A2T_ERR_INVALID;
+    // an output is in place of its own input, row for row, or apart from everything: workgroups read theirs
+    // at different times
+    auto rows = [&](const void* p, int heads, int64_t stride) { return a2t::Rows{p, n_rows, (int64_t)heads * D * size, stride * size}; };
+    const a2t::Rows in[] = {rows(q, q_heads, q_stride), rows(k, k_heads, k_stride), a2t::run_of(pos, (int64_t)n_rows * 4)};
+    const a2t::Rows to[] = {rows(q ? q_out : nullptr, q_heads, q_out_stride), rows(k ? k_out : nullptr, k_heads, k_out_stride)};
+    if (a2t::overlap(to[0], to[1])) return A2T_ERR_INVALID;
+    for (int x = 0; x < 2; ++x)
+        for (int y = 0; y < 3; ++y)
+            if (!(x == y && to[x].p == in[x].p && to[x].stride == in[x].stride) && a2t::overlap(to[x], in[y])) return A2T_ERR_INVALID;
     DevGuard g(r->cfg.device);
     RopeArgs a{};
     const double two_pi = 6.28318530717958647692;
