@@ -728,7 +728,7 @@ int a2t_prefer_set_stream(a2t_prefer* p, void* hip_stream);
  * reference model is kept by.
  *   logits  device [n_rows][stride], stride in elements, a multiple of 8
  *   target  device int32 [n_rows]
- *   logp    device float [n_rows] out.  Errors: INVALID, HIP. */
+ *   logp    device float [n_rows] out, apart from both.  Errors: INVALID, HIP. */
 int a2t_prefer_logp(a2t_prefer* p, int32_t n_rows, const void* logits, int64_t stride, const int32_t* target,
                     float* logp);
 
@@ -743,7 +743,8 @@ int a2t_prefer_logp(a2t_prefer* p, int32_t n_rows, const void* logits, int64_t s
  *   losses       device float[3] out: L, the mean of h, the share of pairs with h > 0
  *   ratios       device float [2 n_pairs] out, or NULL
  *   grad         device [rows][policy_stride] out, dL / d policy logits (zero in the
- *                stride's padding), or NULL; may be `policy` itself
+ *                stride's padding), or NULL; may be `policy` itself, or lie over `reference`
+ * The outputs overlap neither each other nor, otherwise, an input.
  * Errors: INVALID, HIP. */
 int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* answer_rows, const void* policy,
                     int64_t policy_stride, const void* reference, int64_t reference_stride,

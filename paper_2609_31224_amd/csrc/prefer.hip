@@ -12,6 +12,7 @@
 // (deterministic, and one launch less), in 64 bits: a ratio is a small difference of large sums.
 // That is work that grows with the square of an answer's rows: those of long ones are formed once.
 #include "../../include/a2t.h"
+#include "overlap.h"
 
 #include <hip/hip_runtime.h>
 
@@ -363,6 +364,11 @@ struct a2t_prefer {
 
 namespace {
 
+// n rows of logits, as far as they are read, or (`whole`) written.
+a2t::Rows logit_rows(const a2t_prefer* p, const void* x, int64_t stride, int64_t n, bool whole = false) {
+    const int64_t size = p->dtype == A2T_F32 ? 4 : 2;
+    return {x, n, (whole ? stride : ((int64_t)p->vocab + kChunk - 1) / kChunk * kChunk) * size, stride * size};
+}
 // 1,024 threads a row instead of 256: where rows are long (1,440 gradient rows of 151,938 bf16 logits:
 // 147 against 156 us), or where they alone do not fill the CUs.
 bool wide_rows(const a2t_prefer* p, int64_t rows) {
@@ -433,6 +439,8 @@ extern "C" int a2t_prefer_logp(a2t_prefer* p, int32_t n_rows, const void* logits
     if (n_rows < 1 || n_rows > p->max_rows || !logits || !target || !logp || stride < p->vocab || stride % 8 || stride > (1ll << 40) ||
         misaligned(logits, 16) || misaligned(target, 4) || misaligned(logp, 4))
         return A2T_ERR_INVALID;
+    const a2t::Rows to = a2t::run_of(logp, (int64_t)n_rows * 4);
+    if (a2t::overlap(to, logit_rows(p, logits, stride, n_rows)) || a2t::overlap(to, a2t::run_of(target, (int64_t)n_rows * 4))) return A2T_ERR_INVALID;
     DevGuard g(p->device);
     const hipError_t e = p->dtype == A2T_F32 ? launch_rows<float>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp, 0)
                                              : launch_rows<bf16_t>(p, n_rows, logits, stride, nullptr, 0, target, nullptr, logp, 0);
@@ -461,6 +469,19 @@ extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* an
     if (bad_stride(policy_stride) || (reference && bad_stride(reference_stride)) || misaligned(policy, 16) || misaligned(reference, 16) ||
         misaligned(grad, 16) || misaligned(ref_logp, 4) || misaligned(target, 4) || misaligned(losses, 4) || misaligned(ratios, 4))
         return A2T_ERR_INVALID;
+    // The gradient's workgroups write a row that they alone read, and read targets and log probabilities of all
+    // rows; the reference's logits are read by an earlier launch, so that the gradient may lie over them.
+    const a2t::Rows in[] = {logit_rows(p, policy, policy_stride, n), a2t::run_of(target, n * 4), a2t::run_of(ref_logp, n * 4),
+                            logit_rows(p, reference, reference_stride, n)};
+    const a2t::Rows to[] = {a2t::run_of(losses, 12), a2t::run_of(ratios, 8 * (int64_t)n_pairs), logit_rows(p, grad, policy_stride, n, true)};
+    for (int x = 0; x < 3; ++x) {
+        for (int y = 0; y < x; ++y)
+            if (a2t::overlap(to[x], to[y])) return A2T_ERR_INVALID;
+        for (int y = 0; y < 4; ++y) {
+            if (x == 2 && (y == 3 || (y == 0 && grad == policy))) continue;
+            if (a2t::overlap(to[x], in[y])) return A2T_ERR_INVALID;
+        }
+    }
     DevGuard g(p->device);
     auto go = [&](auto* type) {
         using T = std::remove_pointer_t<decltype(type)>;
