@@ -12,6 +12,7 @@
 // (deterministic, and one launch less), in 64 bits: a ratio is a small difference of large sums.
 // That is work that grows with the square of an answer's rows: those of long ones are formed once.
 #include "../../include/a2t.h"
+#include "launch.h"
 #include "overlap.h"
 
 #include <hip/hip_runtime.h>
@@ -382,9 +383,8 @@ hipError_t launch_rows(a2t_prefer* p, int n, const void* policy, int64_t ps, con
     RowsArgs<T> a{{static_cast<const T*>(policy), static_cast<const T*>(reference)}, {ps, rs}, target, stat, logp, n, p->vocab, stream};
     const int64_t rows = reference ? 2 * (int64_t)n : n;
     const dim3 grid((uint32_t)rows);
-    if (wide_rows(p, rows)) hipLaunchKernelGGL((prefer_rows_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
-    else hipLaunchKernelGGL((prefer_rows_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
-    return hipGetLastError();
+    if (wide_rows(p, rows)) return a2t::launch_kernel(prefer_rows_kernel<T, 1024>, grid, dim3(1024), p->stream, a);
+    return a2t::launch_kernel(prefer_rows_kernel<T, 256>, grid, dim3(256), p->stream, a);
 }
 
 }  // namespace
@@ -507,14 +507,12 @@ extern "C" int a2t_prefer_loss(a2t_prefer* p, int32_t n_pairs, const int32_t* an
         for (int i = 0; i < 2 * n_pairs; ++i) a.start[i + 1] = a.start[i] + answer_rows[i];
         if (*std::max_element(answer_rows, answer_rows + 2 * n_pairs) >= kLongRows) {
             a.sums = p->sums;
-            hipLaunchKernelGGL((prefer_ratio_kernel<T>), dim3(2 * n_pairs), dim3(kRatioThreads), 0, p->stream, a);
-            e = hipGetLastError();
+            e = a2t::launch_kernel(prefer_ratio_kernel<T>, dim3(2 * n_pairs), dim3(kRatioThreads), p->stream, a);
             if (e != hipSuccess) return e;
         }
         const dim3 grid(grad ? (uint32_t)n + 1 : 1);
-        if (!grad || wide_rows(p, n)) hipLaunchKernelGGL((prefer_grad_kernel<T, 1024>), grid, dim3(1024), 0, p->stream, a);
-        else hipLaunchKernelGGL((prefer_grad_kernel<T, 256>), grid, dim3(256), 0, p->stream, a);
-        return hipGetLastError();
+        if (!grad || wide_rows(p, n)) return a2t::launch_kernel(prefer_grad_kernel<T, 1024>, grid, dim3(1024), p->stream, a);
+        return a2t::launch_kernel(prefer_grad_kernel<T, 256>, grid, dim3(256), p->stream, a);
     };
     const hipError_t e = p->dtype == A2T_F32 ? go((float*)nullptr) : go((bf16_t*)nullptr);
     if (e != hipSuccess) {

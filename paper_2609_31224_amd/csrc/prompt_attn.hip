@@ -27,6 +27,7 @@
 // 2.1; waves of 64 keys for dK and dV, one a SIMD, 1.25 ms instead of 0.86 at head dim 64 (at 128
 // their sums alone are 256 registers and spill); priorities among a SIMD's waves, no change; without
 // barriers between tiles dK and dV would take 1.63 of 1.95 ms, without tile loads 1.80.
+#include "launch.h"
 #include "prompt_device.h"
 
 #include <type_traits>
@@ -943,26 +944,24 @@ enum class Kernel { forward, dq, dkv };
 
 template <Kernel K, typename T, int D, int N>
 hipError_t join(const Args& a, const SeqTable<N>& s, hipStream_t stream) {
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
     int64_t rows = 0;
     for (int i = 0; i < s.count; ++i) rows += s.rows[i];
     const int64_t fours = rows * (K == Kernel::dkv ? (int64_t)a.Hkv * 2 : a.Hq) * (D / 4);
     const dim3 grid((uint32_t)((fours + kThreads - 1) / kThreads));
-    if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_join_kernel<T, D, N>), grid, dim3(kThreads), 0, stream, a, s);
-    else hipLaunchKernelGGL((prompt_add_kernel<T, D, K == Kernel::dkv, N>), grid, dim3(kThreads), 0, stream, a, s);
-    return hipGetLastError();
+    if constexpr (K == Kernel::forward) return launch_kernel(prompt_join_kernel<T, D, N>, grid, dim3(kThreads), stream, a, s);
+    else return launch_kernel(prompt_add_kernel<T, D, K == Kernel::dkv, N>, grid, dim3(kThreads), stream, a, s);
 }
 template <Kernel K, typename T, int D, bool UNTIL>
 hipError_t launch(const Args& a, const SeqTable<kMaxSeqs>& t, int blocks, hipStream_t stream) {
     return by_count(t, [&](const auto& s) {
         constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
         const dim3 grid((uint32_t)(blocks * a.splits * a.Hkv));
-        if constexpr (K == Kernel::forward && sizeof(T) == 2) hipLaunchKernelGGL((prompt_attn16_kernel<D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
-        else if constexpr (K == Kernel::forward) hipLaunchKernelGGL((prompt_attn_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
-        else if constexpr (K == Kernel::dq) hipLaunchKernelGGL((prompt_dq_kernel<T, D, UNTIL, N>), grid, dim3(kThreads), 0, stream, a, s);
-        else hipLaunchKernelGGL((prompt_dkv_kernel<T, D, UNTIL, N>), grid, dim3(64 * KeyShape<T, D>::kWaves), 0, stream, a, s);
-        return a.splits == 1 ? hipGetLastError() : join<K, T, D, N>(a, s, stream);
+        hipError_t e;
+        if constexpr (K == Kernel::forward && sizeof(T) == 2) e = launch_kernel(prompt_attn16_kernel<D, UNTIL, N>, grid, dim3(kThreads), stream, a, s);
+        else if constexpr (K == Kernel::forward) e = launch_kernel(prompt_attn_kernel<T, D, UNTIL, N>, grid, dim3(kThreads), stream, a, s);
+        else if constexpr (K == Kernel::dq) e = launch_kernel(prompt_dq_kernel<T, D, UNTIL, N>, grid, dim3(kThreads), stream, a, s);
+        else e = launch_kernel(prompt_dkv_kernel<T, D, UNTIL, N>, grid, dim3(64 * KeyShape<T, D>::kWaves), stream, a, s);
+        return e != hipSuccess || a.splits == 1 ? e : join<K, T, D, N>(a, s, stream);
     });
 }
 template <Kernel K>

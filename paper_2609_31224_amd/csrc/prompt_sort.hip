@@ -4,6 +4,7 @@
 // dense runs, and the kernels skip the rest (a ten-minute session with a budget of 4,096 rows: 52 %
 // of the pairs of a causal triangle).  That costs a launch of one workgroup a sequence (17 us there, 5 for
 // 3,000 rows) and one that copies K and V (28 us there).
+#include "launch.h"
 #include "prompt_device.h"
 
 namespace a2t {
@@ -107,8 +108,7 @@ __global__ __launch_bounds__(kThreads) void prompt_copy_kernel(SortArgs a, SeqTa
 hipError_t launch_sort(const SortArgs& a, const SeqTable<kMaxSeqs>& t, hipStream_t stream) {
     hipError_t e = by_count(t, [&](const auto& s) {
         constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
-        hipLaunchKernelGGL((prompt_scan_kernel<N>), dim3(t.count), dim3(kScanThreads), 0, stream, a, s);
-        return hipGetLastError();
+        return launch_kernel(prompt_scan_kernel<N>, dim3(t.count), dim3(kScanThreads), stream, a, s);
     });
     if (e != hipSuccess) return e;
     SeqTable<kMaxSeqs> u = t;
@@ -119,8 +119,7 @@ hipError_t launch_sort(const SortArgs& a, const SeqTable<kMaxSeqs>& t, hipStream
     }
     return by_count(u, [&](const auto& s) {
         constexpr int N = sizeof(s.rows) / sizeof(s.rows[0]);
-        hipLaunchKernelGGL((prompt_copy_kernel<N>), dim3(blocks), dim3(kThreads), 0, stream, a, s);
-        return hipGetLastError();
+        return launch_kernel(prompt_copy_kernel<N>, dim3(blocks), dim3(kThreads), stream, a, s);
     });
 }
 

@@ -11,6 +11,7 @@
 // time (two 16-byte chunks of bf16) of one head after the other, so that the 64-bit
 // arithmetic is shared by all heads of a row.
 #include "../../include/a2t.h"
+#include "launch.h"
 #include "overlap.h"
 
 #include <hip/hip_runtime.h>
@@ -293,16 +294,14 @@ extern "C" int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, i
     a.rows = 1;
     while (a.rows < kMaxRows && (int64_t)n_rows >= (int64_t)a.rows * 2 * 4 * r->cus) a.rows *= 2;
     const dim3 grid((n_rows + a.rows - 1) / a.rows);
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(kThreads), 0, r->stream, a); };
+    auto go = [&](auto kernel) { return a2t::launch_kernel(kernel, grid, dim3(kThreads), r->stream, a); };
     const bool stream = (int64_t)n_rows * a.heads * D * size > kStreamBytes;
     auto typed = [&](auto* type) {
         using T = std::remove_pointer_t<decltype(type)>;
-        if (D == 64) stream ? go(rope_kernel<T, 64, true>) : go(rope_kernel<T, 64, false>);
-        else stream ? go(rope_kernel<T, 128, true>) : go(rope_kernel<T, 128, false>);
+        if (D == 64) return stream ? go(rope_kernel<T, 64, true>) : go(rope_kernel<T, 64, false>);
+        return stream ? go(rope_kernel<T, 128, true>) : go(rope_kernel<T, 128, false>);
     };
-    if (r->cfg.dtype == A2T_F32) typed((float*)nullptr);
-    else typed((bf16_t*)nullptr);
-    if (hipGetLastError() != hipSuccess) {
+    if ((r->cfg.dtype == A2T_F32 ? typed((float*)nullptr) : typed((bf16_t*)nullptr)) != hipSuccess) {
         r->poisoned = true;
         return A2T_ERR_HIP;
     }
