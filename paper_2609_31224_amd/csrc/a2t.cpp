@@ -1512,9 +1512,7 @@ int a2t_sync(a2t_cache* c) {
     if (c->host_only) return A2T_OK;
     if (c->poisoned) return A2T_ERR_HIP;
     DeviceGuard dg(c->cfg.device);
-    if (hipStreamSynchronize(c->stream) != hipSuccess) return hip_fail(c);
-    if (hipGetLastError() != hipSuccess) return hip_fail(c);
-    return A2T_OK;
+    return hipStreamSynchronize(c->stream) == hipSuccess ? A2T_OK : hip_fail(c);
 }
 
 int a2t_read_layout(a2t_cache* c, int32_t stream, int32_t* pos, uint8_t* seg, int32_t* unit) {

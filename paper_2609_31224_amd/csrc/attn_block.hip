@@ -21,8 +21,8 @@
 // phases by barriers 83 (and 18 instead of 15.5 us on a 777-row prompt at head dim 64).
 #include "a2t_internal.h"
 #include "device_common.h"
+#include "launch.h"
 
-#include <hip/hip_ext.h>
 
 #include <type_traits>
 
@@ -439,11 +439,7 @@ hipError_t launch_attn_block(const DevState& st, const AttnBatch& b, const void*
             return (st.G * b.d[i].n_q + kBlockRows - 1) / kBlockRows * b.d[i].splits * st.Hkv;
         });
         auto go = [&](auto kernel) {
-            if (kt.start)
-                hipExtLaunchKernelGGL(kernel, grid, dim3(kBlockThreads), 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo);
-            else
-                hipLaunchKernelGGL(kernel, grid, dim3(kBlockThreads), 0, stream, st, bb, start, qq, oo);
-            return hipGetLastError();
+            return launch_kernel(kernel, grid, dim3(kBlockThreads), {stream, kt.start, kt.stop}, st, bb, start, qq, oo);
         };
         if (st.D == 128) return go(attn_block_kernel<128, N>);
         if (st.D == 64) return go(attn_block_kernel<64, N>);

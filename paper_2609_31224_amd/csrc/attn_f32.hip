@@ -31,8 +31,8 @@
 // 6 % less time.
 #include "a2t_internal.h"
 #include "device_common.h"
+#include "launch.h"
 
-#include <hip/hip_ext.h>
 #include <math.h>
 
 #include <type_traits>
@@ -456,11 +456,7 @@ hipError_t launch_attn_f32(const DevState& st, const AttnBatch& b, int query_blo
             return f32_groups(st.G * b.d[i].n_q, query_blocks) * b.d[i].splits * st.Hkv;
         });
         auto go = [&](auto kernel) {
-            if (kt.start)
-                hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo, ki, vi);
-            else
-                hipLaunchKernelGGL(kernel, grid, block, 0, stream, st, bb, start, qq, oo, ki, vi);
-            return hipGetLastError();
+            return launch_kernel(kernel, grid, block, {stream, kt.start, kt.stop}, st, bb, start, qq, oo, ki, vi);
         };
         if (st.D == 128) return query_blocks == 1 ? go(attn_f32_kernel<128, 1, N>) : go(attn_f32_kernel<128, 2, N>);
         if (st.D == 64) return query_blocks == 1 ? go(attn_f32_kernel<64, 1, N>) : go(attn_f32_kernel<64, 2, N>);

@@ -31,9 +31,9 @@
 // together, which overlap little (a product takes the vector units' time, attn_mx4_rows.hip): 16 sessions of 22 rows
 // onto 8,192 keys 65 to 71 us, of which products are busy 33 %, vector operations 56 %.
 #include "a2t_internal.h"
+#include "launch.h"
 #include "mx4_device.h"
 
-#include <hip/hip_ext.h>
 #include <math.h>
 
 #include <type_traits>
@@ -638,11 +638,7 @@ hipError_t launch_attn_mx4(const DevState& st, const AttnBatch& b, int query_blo
         });
         auto go = [&](auto kernel) {
             const dim3 block(64 * kWaves);
-            if (kt.start)
-                hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo);
-            else
-                hipLaunchKernelGGL(kernel, grid, block, 0, stream, st, bb, start, qq, oo);
-            return hipGetLastError();
+            return launch_kernel(kernel, grid, block, {stream, kt.start, kt.stop}, st, bb, start, qq, oo);
         };
         auto sized = [&](auto dim) {
             constexpr int D = decltype(dim)::value;

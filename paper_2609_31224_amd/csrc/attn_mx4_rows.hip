@@ -14,9 +14,9 @@
 // power holds at 1.85 to 2.0 GHz.  That launch takes 274 to 317 us, card by card, attn_mx4's waves of 48 rows 338 where it
 // takes 274 (with two parts a query 251 to 283).
 #include "a2t_internal.h"
+#include "launch.h"
 #include "mx4_device.h"
 
-#include <hip/hip_ext.h>
 #include <math.h>
 
 #include <type_traits>
@@ -449,11 +449,7 @@ hipError_t launch_attn_mx4_rows(const DevState& st, const AttnBatch& b, int row_
         });
         auto go = [&](auto kernel) {
             const dim3 block(64 * row_waves * kGroups);
-            if (kt.start)
-                hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, kt.start, kt.stop, 0, st, bb, start, qq, oo);
-            else
-                hipLaunchKernelGGL(kernel, grid, block, 0, stream, st, bb, start, qq, oo);
-            return hipGetLastError();
+            return launch_kernel(kernel, grid, block, {stream, kt.start, kt.stop}, st, bb, start, qq, oo);
         };
         auto sized = [&](auto dim) {
             constexpr int D = decltype(dim)::value;

@@ -19,8 +19,8 @@
 // The weights of the four means are per-row coefficients computed on the host
 // from the row metadata.
 #include "../../include/a2t.h"
+#include "launch.h"
 
-#include <hip/hip_ext.h>
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -738,10 +738,9 @@ extern "C" int a2t_distill_loss(a2t_distill* d, int32_t n_rows, const void* stud
         const int chunks = (vs + kChunk - 1) / kChunk;
         auto go = [&](auto kernel, auto* logits, int th) {
             using T = std::remove_const_t<std::remove_pointer_t<decltype(logits)>>;
-            hipExtLaunchKernelGGL(kernel, dim3(n_rows), dim3(th), grad ? th * 128 : 0, d->stream, ev.first, ev.second, 0,
-                                  static_cast<const T*>(student), student_stride, static_cast<const T*>(teacher),
-                                  teacher_stride, d->vocab, vs, (const DistillRow*)d->rows_dev, inv_t, d->rowval_dev,
-                                  static_cast<T*>(grad));
+            e = a2t::launch_kernel(kernel, dim3(n_rows), dim3(th), {d->stream, ev.first, ev.second, grad ? th * 128u : 0u},
+                                   static_cast<const T*>(student), student_stride, static_cast<const T*>(teacher), teacher_stride,
+                                   d->vocab, vs, d->rows_dev, inv_t, d->rowval_dev, static_cast<T*>(grad));
         };
         // the kernel whose threads have few rounds more than the row asks for, because every
         // round is loaded and cut, used or not (row kernel alone, with gradient, 22 rows of 1,715
@@ -762,14 +761,10 @@ extern "C" int a2t_distill_loss(a2t_distill* d, int32_t n_rows, const void* stud
         };
         if (d->dtype == A2T_F32) sized((const float*)nullptr);
         else sized((const bf16_t*)nullptr);
-        e = hipGetLastError();
         if (ev.first) d->prof_pending.push_back(ev);
     }
-    if (e == hipSuccess) {
-        hipLaunchKernelGGL(distill_reduce_kernel, dim3(1), dim3(kReduceThreads), 0, d->stream,
-                           d->rows_dev, d->rowval_dev, n_rows, losses);
-        e = hipGetLastError();
-    }
+    if (e == hipSuccess)
+        e = a2t::launch_kernel(distill_reduce_kernel, dim3(1), dim3(kReduceThreads), d->stream, d->rows_dev, d->rowval_dev, n_rows, losses);
     if (e != hipSuccess) {
         d->poisoned = true;
         return A2T_ERR_HIP;

@@ -25,8 +25,8 @@
 #include "a2t_internal.h"
 #include "a2t.h"
 #include "device_common.h"
+#include "launch.h"
 
-#include <hip/hip_ext.h>
 #include <math.h>
 
 #include <mutex>
@@ -1492,24 +1492,18 @@ hipError_t static_scratch(int device, float** ptr, int64_t* floats) {
 }
 
 // ------------------------------------------------------------------ launchers
-// One dispatch, through hipExtLaunchKernelGGL when the caller asks for timestamps.
-#define A2T_DISPATCH(kernel, grid, block, stream, kt, ...)                                        \
-    do {                                                                                          \
-        if ((kt).start)                                                                           \
-            hipExtLaunchKernelGGL(kernel, grid, block, 0, stream, (kt).start, (kt).stop, 0,       \
-                                  __VA_ARGS__);                                                   \
-        else                                                                                      \
-            hipLaunchKernelGGL(kernel, grid, block, 0, stream, __VA_ARGS__);                      \
-    } while (0)
+// One dispatch, with timestamps when the caller asks for them.
+template <class K, class... A>
+hipError_t dispatch(K kernel, dim3 grid, dim3 block, hipStream_t stream, const KTimer& kt, const A&... args) {
+    return launch_kernel(kernel, grid, block, {stream, kt.start, kt.stop}, args...);
+}
 
 hipError_t launch_step_meta(const DevState& st, const RopeFreq& freq, const StepBatch& b, const uint8_t* seg,
                             const int32_t* pos, const int32_t* uid, hipStream_t stream,
                             const KTimer& kt) {
     return by_size<StepBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
-        A2T_DISPATCH((step_meta_kernel<RopeFreq, B>), dim3(b.max_n, b.count), dim3(64), stream, kt, st, freq, bb,
-                           seg, pos, uid);
-        return hipGetLastError();
+        return dispatch(step_meta_kernel<RopeFreq, B>, dim3(b.max_n, b.count), dim3(64), stream, kt, st, freq, bb, seg, pos, uid);
     });
 }
 
@@ -1520,12 +1514,10 @@ hipError_t launch_append(const DevState& st, const AppendBatch& b, int n_layers,
     return by_size<AppendBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         if (st.dtype == 0)
-            A2T_DISPATCH((append_kernel<float, B>), grid, dim3(256), stream, kt, st, bb,
-                               static_cast<const float*>(k), static_cast<const float*>(v));
+            return dispatch(append_kernel<float, B>, grid, dim3(256), stream, kt, st, bb, static_cast<const float*>(k), static_cast<const float*>(v));
         else
-            A2T_DISPATCH((append_kernel<bf16_t, B>), grid, dim3(256), stream, kt, st, bb,
-                               static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v));
-        return hipGetLastError();
+            return dispatch(append_kernel<bf16_t, B>, grid, dim3(256), stream, kt, st, bb,
+                            static_cast<const bf16_t*>(k), static_cast<const bf16_t*>(v));
     });
 }
 
@@ -1544,15 +1536,12 @@ hipError_t launch_attn_tile(const DevState& st, const AttnBatch& b, const void* 
     return by_size<AttnBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         if (st.D == 128) {
-            A2T_DISPATCH((attn_tile_kernel<128, B>), grid, dim3(kMfmaThreads), stream, kt, st, bb,
-                         qq, oo, ki, vi);
+            return dispatch(attn_tile_kernel<128, B>, grid, dim3(kMfmaThreads), stream, kt, st, bb, qq, oo, ki, vi);
         } else if (st.D == 64) {
-            A2T_DISPATCH((attn_tile_kernel<64, B>), grid, dim3(kMfmaThreads), stream, kt, st, bb,
-                         qq, oo, ki, vi);
+            return dispatch(attn_tile_kernel<64, B>, grid, dim3(kMfmaThreads), stream, kt, st, bb, qq, oo, ki, vi);
         } else {
             return hipErrorInvalidValue;
         }
-        return hipGetLastError();
     });
 }
 
@@ -1563,13 +1552,12 @@ static hipError_t valu_dispatch_g(const DevState& st, const B& b, const void* q,
     const T* qq = static_cast<const T*>(q);
     T* oo = static_cast<T*>(o);
     switch (st.Hq / st.Hkv) {
-        case 1: A2T_DISPATCH((attn_valu_kernel<T, D, 1, B>), grid, dim3(256), stream, kt, st, b, qq, oo); break;
-        case 2: A2T_DISPATCH((attn_valu_kernel<T, D, 2, B>), grid, dim3(256), stream, kt, st, b, qq, oo); break;
-        case 4: A2T_DISPATCH((attn_valu_kernel<T, D, 4, B>), grid, dim3(256), stream, kt, st, b, qq, oo); break;
-        case 8: A2T_DISPATCH((attn_valu_kernel<T, D, 8, B>), grid, dim3(256), stream, kt, st, b, qq, oo); break;
+        case 1: return dispatch(attn_valu_kernel<T, D, 1, B>, grid, dim3(256), stream, kt, st, b, qq, oo);
+        case 2: return dispatch(attn_valu_kernel<T, D, 2, B>, grid, dim3(256), stream, kt, st, b, qq, oo);
+        case 4: return dispatch(attn_valu_kernel<T, D, 4, B>, grid, dim3(256), stream, kt, st, b, qq, oo);
+        case 8: return dispatch(attn_valu_kernel<T, D, 8, B>, grid, dim3(256), stream, kt, st, b, qq, oo);
         default: return hipErrorInvalidValue;
     }
-    return hipGetLastError();
 }
 
 hipError_t launch_attn_valu(const DevState& st, const AttnBatch& b, const void* q, void* o,
@@ -1581,9 +1569,8 @@ hipError_t launch_attn_valu(const DevState& st, const AttnBatch& b, const void* 
             const float* qq = static_cast<const float*>(q);
             float* oo = static_cast<float*>(o);
             if (st.Hq != st.Hkv || (st.D != 64 && st.D != 128)) return hipErrorInvalidValue;
-            if (st.D == 128) A2T_DISPATCH((attn_valu_kernel<float, 128, 1, B>), grid, dim3(256), stream, kt, st, bb, qq, oo);
-            else A2T_DISPATCH((attn_valu_kernel<float, 64, 1, B>), grid, dim3(256), stream, kt, st, bb, qq, oo);
-            return hipGetLastError();
+            if (st.D == 128) return dispatch(attn_valu_kernel<float, 128, 1, B>, grid, dim3(256), stream, kt, st, bb, qq, oo);
+            return dispatch(attn_valu_kernel<float, 64, 1, B>, grid, dim3(256), stream, kt, st, bb, qq, oo);
         }
         if (st.D == 128) return valu_dispatch_g<bf16_t, 128>(st, bb, q, o, stream, kt);
         if (st.D == 64) return valu_dispatch_g<bf16_t, 64>(st, bb, q, o, stream, kt);
@@ -1605,27 +1592,18 @@ hipError_t launch_attn_merge(const DevState& st, const AttnBatch& b, void* o, hi
     return by_size<AttnBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         if (few)
-            A2T_DISPATCH((attn_merge_few_kernel<B>), few_grid, dim3(256), stream, kt, st, bb,
-                         static_cast<bf16_t*>(o));
-        else if (h16 && wide)
-            A2T_DISPATCH((attn_merge_kernel<bf16_t, 12, B, true>), grid, dim3(256), stream, kt, st, bb,
-                         static_cast<bf16_t*>(o));
-        else if (h16)
-            A2T_DISPATCH((attn_merge_kernel<bf16_t, 8, B, true>), grid, dim3(256), stream, kt, st, bb,
-                         static_cast<bf16_t*>(o));
-        else if (st.dtype == 0 && wide)
-            A2T_DISPATCH((attn_merge_kernel<float, 12, B>), grid, dim3(256), stream, kt, st, bb,
-                         static_cast<float*>(o));
-        else if (st.dtype == 0)
-            A2T_DISPATCH((attn_merge_kernel<float, 8, B>), grid, dim3(256), stream, kt, st, bb,
-                         static_cast<float*>(o));
-        else if (wide)
-            A2T_DISPATCH((attn_merge_kernel<bf16_t, 12, B>), grid, dim3(256), stream, kt, st, bb,
-                         static_cast<bf16_t*>(o));
-        else
-            A2T_DISPATCH((attn_merge_kernel<bf16_t, 8, B>), grid, dim3(256), stream, kt, st, bb,
-                         static_cast<bf16_t*>(o));
-        return hipGetLastError();
+            return dispatch(attn_merge_few_kernel<B>, few_grid, dim3(256), stream, kt, st, bb, static_cast<bf16_t*>(o));
+        if (h16 && wide)
+            return dispatch(attn_merge_kernel<bf16_t, 12, B, true>, grid, dim3(256), stream, kt, st, bb, static_cast<bf16_t*>(o));
+        if (h16)
+            return dispatch(attn_merge_kernel<bf16_t, 8, B, true>, grid, dim3(256), stream, kt, st, bb, static_cast<bf16_t*>(o));
+        if (st.dtype == 0 && wide)
+            return dispatch(attn_merge_kernel<float, 12, B>, grid, dim3(256), stream, kt, st, bb, static_cast<float*>(o));
+        if (st.dtype == 0)
+            return dispatch(attn_merge_kernel<float, 8, B>, grid, dim3(256), stream, kt, st, bb, static_cast<float*>(o));
+        if (wide)
+            return dispatch(attn_merge_kernel<bf16_t, 12, B>, grid, dim3(256), stream, kt, st, bb, static_cast<bf16_t*>(o));
+        return dispatch(attn_merge_kernel<bf16_t, 8, B>, grid, dim3(256), stream, kt, st, bb, static_cast<bf16_t*>(o));
     });
 }
 
@@ -1633,9 +1611,8 @@ hipError_t launch_attn_merge(const DevState& st, const AttnBatch& b, void* o, hi
 hipError_t launch_dev_open(const DevState& st, const DevStepArgs& a, const int32_t* n_rows,
                            const int32_t* unit, const uint8_t* seg, const int32_t* pos,
                            DevPlan* plan, hipStream_t stream) {
-    hipLaunchKernelGGL(dev_open_kernel, dim3(1), dim3(64 * kDevOpenWaves), 0, stream, st, a, n_rows, unit, seg,
-                       pos, plan);
-    return hipGetLastError();
+    return launch_kernel(dev_open_kernel, dim3(1), dim3(64 * kDevOpenWaves), stream, st, a, n_rows, unit, seg,
+                         pos, plan);
 }
 
 hipError_t launch_step_meta_dev(const DevState& st, const DevPlan* plan, int count,
@@ -1643,9 +1620,8 @@ hipError_t launch_step_meta_dev(const DevState& st, const DevPlan* plan, int cou
                                 hipStream_t stream) {
     const DevBatch<StepDesc> b{{plan->step}, 0, 0};
     const RopeFreqPtr freq{plan->freq.f};
-    hipLaunchKernelGGL((step_meta_kernel<RopeFreqPtr, DevBatch<StepDesc>>), dim3(st.max_step_rows, count),
-                       dim3(64), 0, stream, st, freq, b, seg, pos, unit);
-    return hipGetLastError();
+    return launch_kernel(step_meta_kernel<RopeFreqPtr, DevBatch<StepDesc>>, dim3(st.max_step_rows, count), dim3(64),
+                         stream, st, freq, b, seg, pos, unit);
 }
 
 hipError_t launch_attn_tile_dev(const DevState& st, const DevPlan* plan, int count,
@@ -1658,14 +1634,11 @@ hipError_t launch_attn_tile_dev(const DevState& st, const DevPlan* plan, int cou
     const uint16_t* ki = static_cast<const uint16_t*>(k_in);
     const uint16_t* vi = static_cast<const uint16_t*>(v_in);
     if (st.D == 128)
-        hipLaunchKernelGGL((attn_tile_kernel<128, DevBatch<AttnDesc>>), grid, dim3(kMfmaThreads), 0,
-                           stream, st, b, qq, oo, ki, vi);
+        return launch_kernel(attn_tile_kernel<128, DevBatch<AttnDesc>>, grid, dim3(kMfmaThreads), stream, st, b, qq, oo, ki, vi);
     else if (st.D == 64)
-        hipLaunchKernelGGL((attn_tile_kernel<64, DevBatch<AttnDesc>>), grid, dim3(kMfmaThreads), 0,
-                           stream, st, b, qq, oo, ki, vi);
+        return launch_kernel(attn_tile_kernel<64, DevBatch<AttnDesc>>, grid, dim3(kMfmaThreads), stream, st, b, qq, oo, ki, vi);
     else
         return hipErrorInvalidValue;
-    return hipGetLastError();
 }
 
 hipError_t launch_attn_merge_dev(const DevState& st, const DevPlan* plan, int count,
@@ -1678,29 +1651,22 @@ hipError_t launch_attn_merge_dev(const DevState& st, const DevPlan* plan, int co
     const dim3 grid(groups * st.Hkv, 1, count);
     const int nsg = 256 / (kMergeRows * st.D / 8);   // fp16 partials of the MFMA kernel
     if ((max_splits + nsg - 1) / nsg > 8)
-        hipLaunchKernelGGL((attn_merge_kernel<bf16_t, 12, DevBatch<AttnDesc>, true>), grid, dim3(256), 0,
-                           stream, st, b, static_cast<bf16_t*>(o));
+        return launch_kernel(attn_merge_kernel<bf16_t, 12, DevBatch<AttnDesc>, true>, grid, dim3(256), stream, st, b, static_cast<bf16_t*>(o));
     else
-        hipLaunchKernelGGL((attn_merge_kernel<bf16_t, 8, DevBatch<AttnDesc>, true>), grid, dim3(256), 0,
-                           stream, st, b, static_cast<bf16_t*>(o));
-    return hipGetLastError();
+        return launch_kernel(attn_merge_kernel<bf16_t, 8, DevBatch<AttnDesc>, true>, grid, dim3(256), stream, st, b, static_cast<bf16_t*>(o));
 }
 
 hipError_t launch_dev_evict(const DevState& st, const DevStepArgs& a, const int32_t* budget,
                             int32_t* n_evicted, uint8_t* budget_unmet, DevPlan* plan,
                             hipStream_t stream) {
-    hipLaunchKernelGGL(dev_evict_plan_kernel, dim3(a.count), dim3(256), 0, stream, st, a, budget,
-                       n_evicted, budget_unmet, plan);
-    hipError_t e = hipGetLastError();
+    const hipError_t e = launch_kernel(dev_evict_plan_kernel, dim3(a.count), dim3(256), stream, st, a, budget, n_evicted,
+                                       budget_unmet, plan);
     if (e != hipSuccess) return e;
     const DevBatch<EvictDesc> b{{plan->evict}, 0, 0};
     if (st.dtype == 0)
-        hipLaunchKernelGGL((evict_kernel<4, DevBatch<EvictDesc>>), dim3(st.L + 1, a.count), dim3(256),
-                           0, stream, st, b);
+        return launch_kernel(evict_kernel<4, DevBatch<EvictDesc>>, dim3(st.L + 1, a.count), dim3(256), stream, st, b);
     else
-        hipLaunchKernelGGL((evict_kernel<2, DevBatch<EvictDesc>>), dim3(st.L + 1, a.count), dim3(256),
-                           0, stream, st, b);
-    return hipGetLastError();
+        return launch_kernel(evict_kernel<2, DevBatch<EvictDesc>>, dim3(st.L + 1, a.count), dim3(256), stream, st, b);
 }
 
 hipError_t launch_evict(const DevState& st, const EvictBatch& b, hipStream_t stream,
@@ -1709,10 +1675,9 @@ hipError_t launch_evict(const DevState& st, const EvictBatch& b, hipStream_t str
     return by_size<EvictBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         if (st.dtype == 0)
-            A2T_DISPATCH((evict_kernel<4, B>), grid, dim3(256), stream, kt, st, bb);
+            return dispatch(evict_kernel<4, B>, grid, dim3(256), stream, kt, st, bb);
         else
-            A2T_DISPATCH((evict_kernel<2, B>), grid, dim3(256), stream, kt, st, bb);
-        return hipGetLastError();
+            return dispatch(evict_kernel<2, B>, grid, dim3(256), stream, kt, st, bb);
     });
 }
 

@@ -6,9 +6,9 @@
 //   read_rows   resident rows in cache order: decoded (A2T_MX4) or copied.
 #include "a2t_internal.h"
 #include "a2t.h"
+#include "launch.h"
 #include "mx4_device.h"
 
-#include <hip/hip_ext.h>
 
 #include <type_traits>
 
@@ -202,11 +202,7 @@ hipError_t launch_append_mx4(const DevState& st, const AppendBatch& b, int n_lay
     const uint16_t *kk = static_cast<const uint16_t*>(k), *vv = static_cast<const uint16_t*>(v);
     return by_size<AppendBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
-        if (kt.start)
-            hipExtLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb, kk, vv, heads);
-        else
-            hipLaunchKernelGGL((append_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, st, bb, kk, vv, heads);
-        return hipGetLastError();
+        return launch_kernel(append_mx4_kernel<B>, grid, dim3(kRowThreads), {stream, kt.start, kt.stop}, st, bb, kk, vv, heads);
     });
 }
 
@@ -216,11 +212,7 @@ hipError_t launch_move_mx4(const DevState& st, const EvictBatch& b, hipStream_t 
     const dim3 grid(st.L, b.count, span < 256 ? (span + 3) / 4 : 64);
     return by_size<EvictBatchT>(b, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
-        if (kt.start)
-            hipExtLaunchKernelGGL((move_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb);
-        else
-            hipLaunchKernelGGL((move_mx4_kernel<B>), grid, dim3(kRowThreads), 0, stream, st, bb);
-        return hipGetLastError();
+        return launch_kernel(move_mx4_kernel<B>, grid, dim3(kRowThreads), {stream, kt.start, kt.stop}, st, bb);
     });
 }
 
@@ -235,11 +227,7 @@ hipError_t launch_read_rows(const DevState& st, const ReadBatch& b, int n_layers
     return by_size<ReadBatchT>(rb, [&](const auto& bb) {
         using B = std::decay_t<decltype(bb)>;
         auto go = [&](auto kernel) {
-            if (kt.start)
-                hipExtLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, stream, kt.start, kt.stop, 0, st, bb, kk, vv);
-            else
-                hipLaunchKernelGGL(kernel, grid, dim3(kRowThreads), 0, stream, st, bb, kk, vv);
-            return hipGetLastError();
+            return launch_kernel(kernel, grid, dim3(kRowThreads), {stream, kt.start, kt.stop}, st, bb, kk, vv);
         };
         if (st.dtype == A2T_F32) return go(read_rows_kernel<A2T_F32, B>);
         if (st.dtype == A2T_BF16) return go(read_rows_kernel<A2T_BF16, B>);
