@@ -653,7 +653,9 @@ int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, int32_t q_he
  * came (as every eviction rule's do) cost what is visible; others are correct,
  * but may cost more.
  * Scores, softmax and sums are fp32; bf16 probabilities and score gradients
- * are rounded to bf16 for the products that they enter.  Results do not depend
+ * are rounded to bf16 for the products that they enter, and the gradient takes
+ * dO . O from the O that was stored, but for rows with at most two tiles of 64 keys
+ * in sight, where it is summed from the scores.  Results do not depend
  * on the order in which workgroups run.  Inputs are finite: a non-finite value
  * of a row of v or of a gradient may reach every row of its sequence, and none
  * of another's. */

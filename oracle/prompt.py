@@ -38,10 +38,12 @@ class PromptResult:
     bounds: Dict[str, np.ndarray] = field(default_factory=dict)   # how far each output may be off
 
 
-def prompt_attention(seq_rows, q, k, v, until=None, d_o=None, scale=None, u_store: float = 0.0, u_mul: float = 0.0) -> PromptResult:
+def prompt_attention(seq_rows, q, k, v, until=None, d_o=None, scale=None, u_store: float = 0.0, u_mul: float = 0.0,
+                     delta_rows: int = 0) -> PromptResult:
     """``u_store``: half a step of the type that outputs (and O, before the gradient reads it) are
     rounded to; ``u_mul``: of the type that probabilities and score gradients are rounded to before
-    their products.  fp32 is assumed elsewhere."""
+    their products.  fp32 is assumed elsewhere.  Sequences of up to ``delta_rows`` rows have their
+    delta as a sum of p_ij dO_i . v_j in fp32 instead of from the stored O."""
     q, k, v = (np.asarray(x, np.float64) for x in (q, k, v))
     rows, hq, d = q.shape
     G = hq // k.shape[1]
@@ -90,6 +92,8 @@ def prompt_attention(seq_rows, q, k, v, until=None, d_o=None, scale=None, u_stor
             # delta comes from the O that was stored; dO . v and delta are fp32 sums
             t = (np.abs(dO) * (to + u_store * to)).sum(1, keepdims=True)
             adp, adl = np.abs(dO) @ np.abs(V).T, (np.abs(dO) * np.abs(O)).sum(1, keepdims=True)
+            if n <= delta_rows:
+                t = (rho + e * (n + d + 16)) * (p * adp).sum(1, keepdims=True)
             off = p * (t + e * (d + 8) * (adp + adl)) + np.abs(ds) * (rho + u_mul + 2 * e)
             off_p = p * (rho + u_mul)
             abs_ds = p * (adp + adl)
