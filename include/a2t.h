@@ -648,7 +648,9 @@ int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, int32_t q_he
  * until that a2t_evict's decisions give (a row evicted after the step that
  * ends before place e has until = e; a row that stays, any number that is not
  * below the sequence's rows), a session sees what it will see when it is
- * served.  Any values are allowed; a row that sees nothing has O = 0,
+ * served.  Which rows an eviction removed is a2t_read_last_evict's mask, over the
+ * rows resident before it in cache order: survivors, in order, are those of the
+ * next, followed by the rows appended since.  Any values are allowed; a row that sees nothing has O = 0,
  * lse = -infinity and no gradient.  Rows of keys that leave in the order they
  * came (as every eviction rule's do) cost what is visible; others are correct,
  * but may cost more.
