@@ -84,8 +84,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
     const bf16x2 v = {(__bf16)a, (__bf16)b};   // round to nearest even, once per output
     return __builtin_bit_cast(uint32_t, v);
 }
-// (The gradient is stored past the caches: written through them, 389 MB of it in a step of 1,440 rows
-// x 151,938 logits cost that pass and the next step's first reads 55 of 335 us.)
+// (The gradient is stored past the caches.  Through them, 389 MB of it in a step of 1,280 rows x 151,938
+// logits make the next step's rows 157 us instead of 124, its own pass 139 instead of 151: the step 292, 271 so.)
 __device__ __forceinline__ void store_chunk(bf16_t* row, int c, const float (&x)[kChunk]) {
     __builtin_nontemporal_store((u32x4{pack2(x[0], x[1]), pack2(x[2], x[3]), pack2(x[4], x[5]), pack2(x[6], x[7])}),
                                 reinterpret_cast<u32x4*>(row) + c);
@@ -370,8 +370,8 @@ a2t::Rows logit_rows(const a2t_prefer* p, const void* x, int64_t stride, int64_t
     const int64_t size = p->dtype == A2T_F32 ? 4 : 2;
     return {x, n, (whole ? stride : ((int64_t)p->vocab + kChunk - 1) / kChunk * kChunk) * size, stride * size};
 }
-// 1,024 threads a row instead of 256: where rows are long (1,440 gradient rows of 151,938 bf16 logits:
-// 147 against 156 us), or where they alone do not fill the CUs.
+// 1,024 threads a row instead of 256: where rows are long (1,280 gradient rows of 151,938 bf16 logits:
+// 151 against 164 us), or where they alone do not fill the CUs.
 bool wide_rows(const a2t_prefer* p, int64_t rows) {
     const int chunks = p->vocab / kChunk;
     return chunks >= 8192 || (rows < 4 * p->cus && chunks >= 1024);

@@ -20,13 +20,13 @@
 // Bound: the matrix units under the card's power (clock 1.9 to 2.0 GHz of 2.4; a library's product of
 // 8,192^3 reaches 1.23 PFLOP/s) and, beside them, LDS reads and exponentials.  Measured, head dim 128,
 // 32 heads on 8: forward of 16,384 rows 2.0 ms, 1.10 PFLOP/s; a ten-minute session of 13,200 rows under
-// eviction 0.80 ms forward (0.94 PFLOP/s of visible pairs), dQ 1.05 ms (1.07), dK and dV 1.75 ms (0.85); fp32
-// kernels run at 0.7 to 0.8 of the fp32 matrix rate where the blocks fill the CUs.
+// eviction 0.80 ms forward (0.94 PFLOP/s of visible pairs), dQ 1.05 ms (1.07), dK and dV 1.75 ms (0.85).  fp32,
+// where the blocks fill the CUs (4,096 rows, the same heads): forward 0.74 of a library product's 154 TFLOP/s
+// (1.20 ms at head dim 128, 0.60 at 64), dQ 0.80 and 0.79, dK and dV 0.78 and 0.80.
 // Of the forms tried: tiles through registers instead of straight into LDS, 3.4 instead of 2.3 ms
 // (the compiler took 296 registers, one wave a SIMD); scores a tile ahead of the exponentials, 2.3 ->
 // 2.1; waves of 64 keys for dK and dV, one a SIMD, 1.25 ms instead of 0.86 at head dim 64 (at 128
-// their sums alone are 256 registers and spill); priorities among a SIMD's waves, no change; without
-// barriers between tiles dK and dV would take 1.63 of 1.95 ms, without tile loads 1.80.
+// their sums alone are 256 registers and spill); priorities among a SIMD's waves, no change.
 #include "launch.h"
 #include "prompt_device.h"
 
@@ -92,7 +92,7 @@ __device__ __forceinline__ bool visible(const int2* meta, int lo, int hi, int k,
 }
 
 template <typename T, int D, bool UNTIL, int N>
-__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 128 ? 3 : sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
+__global__ __launch_bounds__(kThreads, (sizeof(T) * D <= 256 ? 2 : 1)) void prompt_attn_kernel(Args a, SeqTable<N> t) {
     using Tl = Tile<T, D>;
     constexpr int DB = Tl::DB;
     __shared__ __align__(1024) char s_k[2][Tl::BYTES];

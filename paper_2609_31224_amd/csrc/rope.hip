@@ -26,8 +26,8 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxRows = 8;       // most rows of a workgroup
-// Outputs larger than the L2 caches (32 MiB together) are stored past them (16,384 rows of 40 bf16
-// heads: 70 us; 52 so, and 59 where loads go past them instead).
+// Outputs larger than the L2 caches (32 MiB together) are stored past them (three sets of inputs in turn,
+// 40 bf16 heads of 128: 5,000 rows 17.2 us against 21.2, 16,384 rows 67.8 against 71.7, 32,768 rows 132 against 136).
 constexpr int64_t kStreamBytes = 32 << 20;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
