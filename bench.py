@@ -317,7 +317,7 @@ class Runner:
 TRAFFIC_PROFILE = os.path.join(ROOT, "profiles", "attn_traffic.md")
 KERNEL_SOURCE = os.path.join(ROOT, "paper_2609_31224_amd", "csrc", "kernels.hip")
 # what the profiled kernels compile in besides
-KERNEL_HEADERS = [os.path.join(ROOT, "paper_2609_31224_amd", "csrc", f) for f in ("device_common.h", "a2t_internal.h")]
+KERNEL_HEADERS = [os.path.join(ROOT, "paper_2609_31224_amd", "csrc", f) for f in ("device_common.h", "a2t_internal.h", "launch.h")]
 
 
 def kernel_sha256():
