@@ -87,7 +87,8 @@ bool bad_rows(const a2t_prompt* p, const void* x, int64_t stride, int heads) {
 
 // A call's outputs and inputs in memory.  Every output is written while other workgroups, or a later
 // launch of the call, still read the inputs: they must not touch each other, but for an output that is
-// `in_place` of an input, row for row, where whoever reads a row is who writes it (or was a launch before).
+// `in_place` of one operand, row for row, where whoever reads a row is who writes it (or was a launch
+// before).  That holds for the operand, not for its memory: another one may be there too.
 struct Memory {
     const a2t_prompt* p;
     int64_t total;
@@ -99,12 +100,13 @@ struct Memory {
     }
     a2t::Rows packed(const void* x) const { return rows(x, (int64_t)p->Hq * p->D, p->Hq); }
     a2t::Rows floats(const void* x, int64_t n) const { return a2t::run_of(x, n * 4); }
-    bool clash(const void* const (&in_place)[3]) const {
+    // in_place[i]: the input that output i may be, or -1
+    bool clash(const int (&in_place)[3]) const {
         for (int i = 0; i < outs; ++i) {
             for (int j = 0; j < i; ++j)
                 if (a2t::overlap(out[i], out[j])) return true;
             for (int j = 0; j < ins; ++j) {
-                if (in[j].p == in_place[i] && in[j].p == out[i].p && in[j].stride == out[i].stride) continue;
+                if (j == in_place[i] && in[j].p == out[i].p && in[j].stride == out[i].stride) continue;
                 if (a2t::overlap(out[i], in[j])) return true;
             }
         }
@@ -295,7 +297,7 @@ extern "C" int a2t_prompt_attn(a2t_prompt* p, int32_t n_seqs, const int32_t* seq
     for (const a2t::Rows& x : {m.rows(q, q_stride, p->Hq), m.rows(k, k_stride, p->Hkv), m.rows(v, v_stride, p->Hkv), m.floats(until, total)})
         m.in[m.ins++] = x;
     for (const a2t::Rows& x : {m.packed(o), m.floats(lse, total * p->Hq)}) m.out[m.outs++] = x;
-    if (m.clash({q, nullptr, nullptr})) return A2T_ERR_INVALID;   // a block reads its queries before its first tile
+    if (m.clash({0, -1, -1})) return A2T_ERR_INVALID;   // o over q: a block reads its queries before its first tile
     DevGuard g(p->device);
     const bool sorted = until && sort_pays(p, n_seqs, seq_rows);
     Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until, sorted);
@@ -331,9 +333,9 @@ extern "C" int a2t_prompt_attn_grad(a2t_prompt* p, int32_t n_seqs, const int32_t
                                m.packed(o), m.floats(lse, total * p->Hq), m.packed(d_o)})
         m.in[m.ins++] = x;
     for (const a2t::Rows& x : {m.rows(dq, q_stride, p->Hq), m.rows(dk, k_stride, p->Hkv), m.rows(dv, v_stride, p->Hkv)}) m.out[m.outs++] = x;
-    // O is read by the rows' own blocks before their first tile; K and V by all blocks of the launch for dQ,
-    // then by the keys' own alone
-    if (m.clash({o, k, v})) return A2T_ERR_INVALID;
+    // dq over o: O is read by the rows' own blocks before their first tile; dk over k, dv over v: K and V are
+    // read by all blocks of the launch for dQ, then by the keys' own alone
+    if (m.clash({4, 1, 2})) return A2T_ERR_INVALID;
     DevGuard g(p->device);
     const bool sorted = until && sort_pays(p, n_seqs, seq_rows);
     Args a = base_args(p, total, q, q_stride, k, k_stride, v, v_stride, until, sorted);

@@ -94,3 +94,36 @@ def test_refusals(gpu):
         torch.cuda.synchronize()
     finally:
         a2t.a2t_prompt_destroy(h)
+
+
+def test_operands_that_share_memory(gpu):
+    """An output in place of one operand whose memory is another operand's too (keys that are the queries, a gradient of o that
+    is o): refused; inputs may share memory as they like."""
+    import torch
+    import paper_2609_31224_amd as a2t
+    n, lengths = 40, [30, 10]
+    h = a2t.a2t_prompt_create(n, 2, 2, 64, a2t.A2T_F32)
+    x, y, o, other = (torch.randn((n, 2, 64), device="cuda") for _ in range(4))
+    lse, grads = torch.zeros((2, n), device="cuda"), [torch.zeros((n, 2, 64), device="cuda") for _ in range(3)]
+    keep = [t.clone() for t in (x, y, o)]
+    try:
+        def refused(call, *args):
+            with pytest.raises(a2t.A2TError) as e:
+                call(h, lengths, *args)
+            assert e.value.status == a2t.A2T_ERR_INVALID
+        refused(a2t.a2t_prompt_attn, x, x, y, x)                # o over q, which is k
+        refused(a2t.a2t_prompt_attn, x, y, x, x)                # and v
+        for q, k, v, dq, dk, dv, d_o in ((x, x, y, grads[0], x, grads[2], other), (x, y, x, grads[0], grads[1], x, other), (x, y, y, grads[0], y, grads[2], other),
+                                         (x, y, other, o, grads[1], grads[2], o), (o, x, y, o, grads[1], grads[2], other)):
+            refused(a2t.a2t_prompt_attn_grad, q, k, v, o, lse, d_o, dq, dk, dv)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((x, y, o), keep)) and not any(g.any() for g in grads)
+        got = []
+        for q, k, v in ((x, x, x), (x.clone(), x.clone(), x.clone())):
+            a2t.a2t_prompt_attn(h, lengths, q, k, v, o, lse)
+            a2t.a2t_prompt_attn_grad(h, lengths, q, k, v, o, lse, o, *grads)
+            torch.cuda.synchronize()
+            got.append([t.clone() for t in (o, lse, *grads)])
+        assert all(torch.equal(a, b) for a, b in zip(*got))
+    finally:
+        a2t.a2t_prompt_destroy(h)
