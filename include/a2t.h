@@ -650,17 +650,16 @@ int a2t_rope_apply(a2t_rope* r, int32_t n_rows, const int32_t* pos, int32_t q_he
  * below the sequence's rows), a session sees what it will see when it is
  * served.  Which rows an eviction removed is a2t_read_last_evict's mask, over the
  * rows resident before it in cache order: survivors, in order, are those of the
- * next, followed by the rows appended since.  Any values are allowed; a row that sees nothing has O = 0,
- * lse = -infinity and no gradient.  Rows of keys that leave in the order they
- * came (as every eviction rule's do) cost what is visible; others are correct,
- * but may cost more.
+ * next, followed by the rows appended since.  Any values are allowed; a row that
+ * sees nothing has O = 0, lse = -infinity and no gradient.  Rows of keys that leave
+ * in the order they came (as every eviction rule's do) cost what is visible; others
+ * are correct, but may cost more.
  * Scores, softmax and sums are fp32; bf16 probabilities and score gradients
  * are rounded to bf16 for the products that they enter, and the gradient takes
  * dO . O from the O that was stored, but for rows with at most two tiles of 64 keys
- * in sight, where it is summed from the scores.  Results do not depend
- * on the order in which workgroups run.  Inputs are finite: a non-finite value
- * of a row of v or of a gradient may reach every row of its sequence, and none
- * of another's. */
+ * in sight, where it is summed from the scores.  Results do not depend on the order
+ * in which workgroups run.  Inputs are finite: a non-finite value of a row of v or
+ * of a gradient may reach every row of its sequence, and none of another's. */
 typedef struct a2t_prompt a2t_prompt;
 
 #define A2T_PROMPT_UNTIL 1u   /* calls may pass `until`: the handle holds copies of K and V */
